@@ -229,9 +229,13 @@ typedef struct {
   float *db2;
 } moe_expert_bias;
 
-/* Workspace bytes for moe_fwd (which = 1), moe_bwd (which = 2) and
- * moe_fwd_aggregation_ablation (which = 3). */
-enum { MOE_WS_FWD = 1, MOE_WS_BWD = 2, MOE_WS_FWD_AGG_ABLATION = 3 };
+/* Workspace bytes for moe_fwd (which = 1), moe_bwd (which = 2),
+ * moe_fwd_aggregation_ablation (which = 3), moe_fwd_quant (which = 4),
+ * moe_fwd_ckpt (which = 5) and moe_bwd_ckpt (which = 6). */
+enum {
+  MOE_WS_FWD = 1, MOE_WS_BWD = 2, MOE_WS_FWD_AGG_ABLATION = 3,
+  MOE_WS_FWD_QUANT = 4, MOE_WS_FWD_CKPT = 5, MOE_WS_BWD_CKPT = 6
+};
 size_t moe_workspace_bytes(moe_dims dims, int32_t capacity, int which);
 
 /*
@@ -315,6 +319,131 @@ int moe_fwd_aggregation_ablation(moe_dims dims, const moe_bf16 *X, const moe_bf1
                                  const moe_routing *r, moe_bf16 *H, moe_bf16 *O, int strategy, void *ws,
                                  size_t ws_bytes, void *stream);
 
+/*
+ * 8-bit block format.  A block of up to 128 values is held as e4m3 codes (OCP
+ * 8-bit floating point: no infinities, largest value 448) and one scale byte b,
+ * which stands for 2^(b - 127):
+ *   amax  = the largest finite |x| of the block
+ *   e     = the least integer >= -126 with amax <= 448 * 2^e;  b = e + 127
+ *   code  = e4m3(x * 2^-e), rounded to nearest even; infinities and NaN become
+ *           the NaN code (and stay visible: they do not move the others' scale)
+ *   value = code * 2^e; at most 2^-4 |x| off where |value| >= 2^(e - 6)
+ * Blocks are 128 consecutive columns of a row (the last one of a row may be
+ * shorter) and, for expert weights, 128 x 128 (W1: within the gate and within
+ * the up half; H likewise).
+ */
+typedef uint8_t moe_fp8;
+
+/* Bytes from one row's scales to the next: a row of `cols` columns has
+ * ceil(cols / 128) scale bytes, padded to a multiple of 4.  0 for cols < 1. */
+int32_t moe_scale_stride(int32_t cols);
+
+/*
+ * Rows of activations into the 8-bit block format and back (values of a block
+ * whose scale is the smallest may be rounded to bf16's own smallest, 2^-133).
+ *   rows   >= 0 (0: nothing is enqueued); cols a multiple of 8, >= 8;
+ *          rows * ceil(cols / 128) below 2^31
+ *   X      [rows,cols] bf16, 16-byte aligned
+ *   q      [rows,cols] codes, 8-byte aligned
+ *   scale  [rows][moe_scale_stride(cols)] bytes, 4-byte aligned; the bytes past a
+ *          row's last block are written as 127
+ * Inputs and outputs must not overlap.
+ */
+int moe_quantize_rows(int64_t rows, int32_t cols, const moe_bf16 *X, moe_fp8 *q, uint8_t *scale, void *stream);
+int moe_dequantize_rows(int64_t rows, int32_t cols, const moe_fp8 *q, const uint8_t *scale, moe_bf16 *X,
+                        void *stream);
+
+/* moe_qexperts.state and moe_ckpt.state */
+enum {
+  MOE_HELD_EMPTY = 0,  /* laid out; nothing written                            */
+  MOE_HELD_WRITTEN = 1 /* a call that writes it has been enqueued              */
+};
+
+/*
+ * The expert weights in the 8-bit block format, in the layout that the products
+ * of moe_fwd_quant read (k contiguous, n padded with zeros to a multiple of
+ * 128): written by moe_quantize_experts, read back by moe_dequantize_experts.
+ * One caller-allocated device buffer, laid out by moe_qexperts_init.
+ */
+typedef struct {
+  int32_t d, n, E; /* of the layer                                             */
+  int32_t state;   /* host-side, MOE_HELD_*                                    */
+  moe_fp8 *W1;
+  uint8_t *W1s;
+  moe_fp8 *W2;
+  uint8_t *W2s;
+} moe_qexperts;
+
+/* (T and K of the dims only have to be valid) */
+size_t moe_qexperts_bytes(moe_dims dims);
+int moe_qexperts_init(moe_dims dims, void *buf, size_t bytes, moe_qexperts *q);
+/* W1 [E,d,2n], W2 [E,n,d] bf16; q->state becomes MOE_HELD_WRITTEN */
+int moe_quantize_experts(moe_dims dims, const moe_bf16 *W1, const moe_bf16 *W2, moe_qexperts *q, void *stream);
+/* the values that q stands for, as bf16 (exact, but for values below 2^-133) */
+int moe_dequantize_experts(moe_dims dims, const moe_qexperts *q, moe_bf16 *W1, moe_bf16 *W2, void *stream);
+
+/*
+ * The activations a forward keeps for the backward, in the 8-bit block format:
+ * H (blocks of 128 columns within the gate and the up half: a row's scales are
+ * its ceil(n/128) gate blocks, then its up blocks) and, with MOE_CKPT_X, X.  2 P n (+ T d)
+ * bytes instead of 4 P n (+ 2 T d).  One caller-allocated device buffer, laid out
+ * by moe_ckpt_init, written by moe_fwd_ckpt or moe_fwd_quant, read by
+ * moe_bwd_ckpt.
+ */
+typedef struct {
+  int32_t T, d, n, capacity;
+  int32_t state;   /* host-side, MOE_HELD_*                                    */
+  int32_t reserved;
+  moe_fp8 *H;      /* [capacity,2n]                                            */
+  uint8_t *Hs;     /* [capacity][moe_scale_stride(256 * ceil(n/128))]          */
+  moe_fp8 *X;      /* [T,d], null without MOE_CKPT_X                           */
+  uint8_t *Xs;     /* [T][moe_scale_stride(d)]                                 */
+} moe_ckpt;
+
+enum { MOE_CKPT_X = 1 /* X is kept too, so that the backward needs no bf16 X */ };
+/* capacity: of the routing that the calls use */
+size_t moe_ckpt_bytes(moe_dims dims, int32_t capacity, int flags);
+int moe_ckpt_init(moe_dims dims, int32_t capacity, int flags, void *buf, size_t bytes, moe_ckpt *c);
+
+/*
+ * Forward with 8-bit expert products: with q() the block format,
+ *   H = gather(q(X)) q(W1_e) (+ b1_e);  A = SiLU(H_gate) * H_up
+ *   Y = q(A) q(W2_e) (+ b2_e);          O_t = sum_{rows of t} s * Y
+ * Products accumulate in fp32; A is quantised from fp32 (blocks of 128 columns of a row), Y
+ * is held in bf16 as in moe_fwd.
+ *   w    weights in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of the
+ *        same d, n and E
+ *   c    nullable: then nothing is kept for a backward.  Otherwise q(H) (and
+ *        q(X)) are written and c->state becomes MOE_HELD_WRITTEN: moe_bwd_ckpt
+ *        with the 16-bit weights is the backward of this forward, its
+ *        roundings taken to carry no gradient
+ *   ws   moe_workspace_bytes(dims, r->capacity, MOE_WS_FWD_QUANT) bytes
+ * Other arguments as moe_fwd.
+ */
+int moe_fwd_quant(moe_dims dims, const moe_bf16 *X, const moe_qexperts *w, const moe_expert_bias *eb,
+                  const moe_routing *r, moe_ckpt *c, moe_bf16 *O, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * moe_fwd that keeps its activations in 8 bits: the same O; in the place of H,
+ * c receives q(H) (from the fp32 H) and, with MOE_CKPT_X, q(X).
+ *   ws   moe_workspace_bytes(dims, r->capacity, MOE_WS_FWD_CKPT) bytes
+ */
+int moe_fwd_ckpt(moe_dims dims, const moe_bf16 *X, const moe_bf16 *W1, const moe_bf16 *W2, const moe_expert_bias *eb,
+                 const moe_routing *r, moe_ckpt *c, moe_bf16 *O, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * moe_bwd from an 8-bit checkpoint: the gradients of moe_bwd with the kept
+ * values in the place of H and, where X is null, of X.
+ *   c    checkpoint in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of
+ *        the same T, d, n and capacity
+ *   X    [T,d] bf16, or null to use the kept one (then c needs MOE_CKPT_X)
+ *   ws   moe_workspace_bytes(dims, r->capacity, MOE_WS_BWD_CKPT) bytes
+ */
+int moe_bwd_ckpt(moe_dims dims, const moe_bf16 *dO, const moe_bf16 *X, const moe_ckpt *c, const moe_bf16 *W1,
+                 const moe_bf16 *W2, const moe_expert_bias *eb, const moe_bf16 *Wr, const moe_routing *r, moe_bf16 *dX,
+                 moe_bf16 *dW1, moe_bf16 *dW2, float *dWr, float *dbias, float *dS, void *ws, size_t ws_bytes,
+                 void *stream);
+
 /* Static description of an error code. */
 const char *moe_strerror(int code);
 /* Thread-local description of the last error returned on this thread. */
@@ -332,6 +461,8 @@ enum {
   MOE_KC_DH, MOE_KC_DW2, MOE_KC_DXT, MOE_KC_DW1, MOE_KC_AGG_DX, MOE_KC_DWR,
   MOE_KC_ROUTER_TOPK, /* the router GEMM with fused softmax/top-K; for few tokens
                          (see moe_route) two launches, counted as one */
+  MOE_KC_QUANTIZE, /* activations into or out of the 8-bit block format */
+  MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT,
   MOE_KC_COUNT
 };
 int moe_prof_select(int kernel_class);

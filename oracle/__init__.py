@@ -18,10 +18,11 @@ from .routing import (router_logits, softmax_scores, topk_select, tc_membership,
                       routing_from_membership, round_tokens, route)
 from .layer import (swiglu, dswiglu, forward, backward, forward_tokens, backward_tokens,
                     weight_grad_columns, cached_bytes)
+from . import block8
 
 __all__ = [
     "router_logits", "softmax_scores", "topk_select", "tc_membership",
     "routing_from_membership", "round_tokens", "route",
     "swiglu", "dswiglu", "forward", "backward", "forward_tokens", "backward_tokens",
-    "weight_grad_columns", "cached_bytes",
+    "weight_grad_columns", "cached_bytes", "block8",
 ]

@@ -39,16 +39,26 @@ ROUND_MODES = {"nearest": 0, "up": 1, "down": 2, "balance": 3, "stochastic": 4}
 MOE_WS_FWD = 1
 MOE_WS_BWD = 2
 MOE_WS_FWD_AGG_ABLATION = 3
+MOE_WS_FWD_QUANT = 4
+MOE_WS_FWD_CKPT = 5
+MOE_WS_BWD_CKPT = 6
+
+MOE_HELD_EMPTY = 0
+MOE_HELD_WRITTEN = 1
+MOE_CKPT_X = 1
 
 AGG_STRATEGIES = {"gather_sum": 0, "scatter_sum": 1, "atomic_f32": 2}
 
 KERNEL_CLASSES = ["router_gemm", "topk", "routing_meta", "token_round", "up_proj", "down_proj", "aggregate_O",
-                  "dH", "dW2", "dXtilde", "dW1", "aggregate_dX", "dWr", "router_topk"]
+                  "dH", "dW2", "dXtilde", "dW1", "aggregate_dX", "dWr", "router_topk", "quantize", "up_proj_quant",
+                  "down_proj_quant"]
 
 EXPORTS = ["moe_routing_bytes", "moe_routing_init", "moe_round_capacity", "moe_route", "moe_round_tokens",
            "moe_workspace_bytes", "moe_fwd", "moe_bwd", "moe_strerror", "moe_last_error", "moe_prof_select",
            "moe_prof_read", "moe_kernel_class_name", "moe_fwd_aggregation_ablation", "moe_fwd_static",
-           "moe_fwd_static_max_bytes"]
+           "moe_fwd_static_max_bytes", "moe_scale_stride", "moe_quantize_rows", "moe_dequantize_rows",
+           "moe_qexperts_bytes", "moe_qexperts_init", "moe_quantize_experts", "moe_dequantize_experts",
+           "moe_ckpt_bytes", "moe_ckpt_init", "moe_fwd_quant", "moe_fwd_ckpt", "moe_bwd_ckpt"]
 
 
 class MoeDims(ctypes.Structure):
@@ -76,6 +86,16 @@ class MoeExpertBias(ctypes.Structure):
     _fields_ = [("b1", _P), ("b2", _P), ("db1", _P), ("db2", _P)]
 
 
+class MoeQExperts(ctypes.Structure):
+    _fields_ = [("d", ctypes.c_int32), ("n", ctypes.c_int32), ("E", ctypes.c_int32), ("state", ctypes.c_int32),
+                ("W1", _P), ("W1s", _P), ("W2", _P), ("W2s", _P)]
+
+
+class MoeCkpt(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("n", ctypes.c_int32), ("capacity", ctypes.c_int32),
+                ("state", ctypes.c_int32), ("reserved", ctypes.c_int32), ("H", _P), ("Hs", _P), ("X", _P), ("Xs", _P)]
+
+
 class MoEError(RuntimeError):
     def __init__(self, fn, code, detail):
         super().__init__(f"{fn} failed with {code}: {detail}")
@@ -95,6 +115,7 @@ def lib():
     L = ctypes.CDLL(LIB_PATH)
     sz, i32, vp = ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p
     D, R, EB = MoeDims, ctypes.POINTER(MoeRouting), ctypes.POINTER(MoeExpertBias)
+    Q, C = ctypes.POINTER(MoeQExperts), ctypes.POINTER(MoeCkpt)
     sig = {
         "moe_routing_bytes": (sz, [D, i32, ctypes.c_int]),
         "moe_routing_init": (ctypes.c_int, [D, i32, ctypes.c_int, vp, sz, R]),
@@ -107,6 +128,18 @@ def lib():
         "moe_fwd_aggregation_ablation": (ctypes.c_int, [D, vp, vp, vp, R, vp, vp, ctypes.c_int, vp, sz, vp]),
         "moe_fwd_static": (ctypes.c_int, [D, vp, vp, vp, EB, R, vp, vp, vp]),
         "moe_fwd_static_max_bytes": (sz, []),
+        "moe_scale_stride": (i32, [i32]),
+        "moe_quantize_rows": (ctypes.c_int, [ctypes.c_int64, i32, vp, vp, vp, vp]),
+        "moe_dequantize_rows": (ctypes.c_int, [ctypes.c_int64, i32, vp, vp, vp, vp]),
+        "moe_qexperts_bytes": (sz, [D]),
+        "moe_qexperts_init": (ctypes.c_int, [D, vp, sz, Q]),
+        "moe_quantize_experts": (ctypes.c_int, [D, vp, vp, Q, vp]),
+        "moe_dequantize_experts": (ctypes.c_int, [D, Q, vp, vp, vp]),
+        "moe_ckpt_bytes": (sz, [D, i32, ctypes.c_int]),
+        "moe_ckpt_init": (ctypes.c_int, [D, i32, ctypes.c_int, vp, sz, C]),
+        "moe_fwd_quant": (ctypes.c_int, [D, vp, Q, EB, R, C, vp, vp, sz, vp]),
+        "moe_fwd_ckpt": (ctypes.c_int, [D, vp, vp, vp, EB, R, C, vp, vp, sz, vp]),
+        "moe_bwd_ckpt": (ctypes.c_int, [D, vp, vp, C, vp, vp, EB, vp, R, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "moe_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         "moe_last_error": (ctypes.c_char_p, []),
         "moe_prof_select": (ctypes.c_int, [ctypes.c_int]),
@@ -256,6 +289,102 @@ def moe_fwd_aggregation_ablation(D, X, W1, W2, r: Routing, H, O, strategy, ws, s
     _check("moe_fwd_aggregation_ablation",
            lib().moe_fwd_aggregation_ablation(D, _ptr(X), _ptr(W1), _ptr(W2), ctypes.byref(r.struct), _ptr(H),
                                               _ptr(O), strategy, _ptr(ws), ws.numel() * ws.element_size(),
+                                              _stream(stream)))
+
+
+# ------------------------------------------------------------------ 8-bit block format
+def scale_stride(cols) -> int:
+    """Bytes from one row's scales to the next (moe_scale_stride)."""
+    return lib().moe_scale_stride(cols)
+
+
+def _aligned_buffer(nbytes, device):
+    """(uint8 tensor, offset of its first 256-byte aligned address)."""
+    import torch
+    buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+    return buf, (-buf.data_ptr()) % 256
+
+
+class QExperts:
+    """A device buffer for the 8-bit expert weights and its moe_qexperts struct."""
+
+    def __init__(self, D: MoeDims, device="cuda"):
+        nbytes = lib().moe_qexperts_bytes(D)
+        if nbytes == 0:
+            _check("moe_qexperts_bytes", MOE_ERR_INVALID_ARG)
+        self.buf, off = _aligned_buffer(nbytes, device)
+        self.struct = MoeQExperts()
+        _check("moe_qexperts_init", lib().moe_qexperts_init(D, ctypes.c_void_p(self.buf.data_ptr() + off), nbytes,
+                                                            ctypes.byref(self.struct)))
+
+
+class Checkpoint:
+    """A device buffer for the kept activations of one forward in 8 bits and its moe_ckpt struct."""
+
+    def __init__(self, D: MoeDims, capacity: int, keep_x: bool = False, device="cuda"):
+        flags = MOE_CKPT_X if keep_x else 0
+        nbytes = lib().moe_ckpt_bytes(D, capacity, flags)
+        if nbytes == 0:
+            _check("moe_ckpt_bytes", MOE_ERR_INVALID_ARG)
+        self.D = D
+        self.buf, off = _aligned_buffer(nbytes, device)
+        self.struct = MoeCkpt()
+        _check("moe_ckpt_init", lib().moe_ckpt_init(D, capacity, flags, ctypes.c_void_p(self.buf.data_ptr() + off),
+                                                    nbytes, ctypes.byref(self.struct)))
+
+    def arrays(self):
+        """uint8 views of the codes and scales: H, Hs and, where it is kept, X, Xs."""
+        s, D = self.struct, self.D
+        shapes = {"H": (s.capacity, 2 * D.n), "Hs": (s.capacity, scale_stride(256 * -(-D.n // 128))),
+                  "X": (D.T, D.d), "Xs": (D.T, scale_stride(D.d))}
+        out = {}
+        for name, (rows, cols) in shapes.items():
+            ptr = getattr(s, name)
+            if ptr:
+                start = ptr - self.buf.data_ptr()
+                out[name] = self.buf[start:start + rows * cols].view(rows, cols)
+        return out
+
+
+def _held(x):
+    return None if x is None else ctypes.byref(x.struct)
+
+
+def moe_quantize_rows(rows, cols, X, q, scale, stream=None):
+    _check("moe_quantize_rows", lib().moe_quantize_rows(rows, cols, _ptr(X), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def moe_dequantize_rows(rows, cols, q, scale, X, stream=None):
+    _check("moe_dequantize_rows", lib().moe_dequantize_rows(rows, cols, _ptr(q), _ptr(scale), _ptr(X),
+                                                            _stream(stream)))
+
+
+def moe_quantize_experts(D, W1, W2, q: QExperts, stream=None):
+    _check("moe_quantize_experts", lib().moe_quantize_experts(D, _ptr(W1), _ptr(W2), _held(q), _stream(stream)))
+
+
+def moe_dequantize_experts(D, q: QExperts, W1, W2, stream=None):
+    _check("moe_dequantize_experts", lib().moe_dequantize_experts(D, _held(q), _ptr(W1), _ptr(W2), _stream(stream)))
+
+
+def moe_fwd_quant(D, X, q: QExperts, r: Routing, ckpt, O, ws, stream=None, eb=None):
+    """ckpt: a Checkpoint, or None for a forward without a backward."""
+    _check("moe_fwd_quant", lib().moe_fwd_quant(D, _ptr(X), _held(q), _eb(eb), ctypes.byref(r.struct), _held(ckpt),
+                                                _ptr(O), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def moe_fwd_ckpt(D, X, W1, W2, r: Routing, ckpt: Checkpoint, O, ws, stream=None, eb=None):
+    _check("moe_fwd_ckpt", lib().moe_fwd_ckpt(D, _ptr(X), _ptr(W1), _ptr(W2), _eb(eb), ctypes.byref(r.struct),
+                                              _held(ckpt), _ptr(O), _ptr(ws), ws.numel() * ws.element_size(),
+                                              _stream(stream)))
+
+
+def moe_bwd_ckpt(D, dO, X, ckpt: Checkpoint, W1, W2, Wr, r: Routing, dX, dW1, dW2, dWr, dbias, dS, ws, stream=None,
+                 eb=None):
+    """X None: the checkpoint's own (keep_x)."""
+    _check("moe_bwd_ckpt", lib().moe_bwd_ckpt(D, _ptr(dO), _ptr(X), _held(ckpt), _ptr(W1), _ptr(W2), _eb(eb), _ptr(Wr),
+                                              ctypes.byref(r.struct), _ptr(dX), _ptr(dW1), _ptr(dW2), _ptr(dWr),
+                                              _ptr(dbias), _ptr(dS), _ptr(ws), ws.numel() * ws.element_size(),
                                               _stream(stream)))
 
 

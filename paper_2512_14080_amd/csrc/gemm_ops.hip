@@ -11,6 +11,7 @@
 // offsets, so no host synchronisation is needed for the ragged row counts.
 #include <algorithm>
 
+#include "fp8_block.h"
 #include "gemm_core.h"
 #include "launch.h"
 #include "topk_net.h"
@@ -45,6 +46,24 @@ __device__ __forceinline__ void load_block_bf16(const uint16_t* row_block, u32x2
     v[g] = u32x2{a[0], b[0]};
     v[g + 1] = u32x2{a[1], b[1]};
   }
+}
+
+// The same for a block of 8-bit codes: v[g] holds the codes of columns 8g + 4 *
+// (lane / 32) + [0, 4); two swaps leave a lane with 16 consecutive ones, lane < 32
+// with columns 0 .. 15 and lane >= 32 with 16 .. 31.
+__device__ __forceinline__ u32x4 swap_block_fp8(uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v0, v2, false, false);
+  const auto b = __builtin_amdgcn_permlane32_swap(v1, v3, false, false);
+  return u32x4{a[0], a[1], b[0], b[1]};
+}
+// and back
+__device__ __forceinline__ void unswap_block_fp8(const u32x4& x, uint32_t (&v)[4]) {
+  const auto a = __builtin_amdgcn_permlane32_swap(x[0], x[1], false, false);
+  const auto b = __builtin_amdgcn_permlane32_swap(x[2], x[3], false, false);
+  v[0] = a[0];
+  v[2] = a[1];
+  v[1] = b[0];
+  v[3] = b[1];
 }
 
 // ---------------------------------------------------------------- scheduling
@@ -1085,6 +1104,108 @@ struct OpUp {
   }
 };
 
+// The largest finite |x| of N values per lane
+template <int N>
+__device__ __forceinline__ float finite_amax(const float (&x)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]));  // (passes over NaN)
+  if (__builtin_expect(__any(m == INFINITY), 0)) {
+    m = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, finite_abs(x[i]));
+  }
+  return m;
+}
+
+// Up-projection whose H is kept in 8-bit blocks: A leaves as in OpUp, H as codes and
+// scale bytes, both from the fp32 accumulators.  The 128 gate (or up) columns of a
+// tile are one block: each of the two waves of a row group holds 64 of them, so the
+// two halves of a row's largest |x| meet in LDS, once per tile.
+template <class Cfg_, bool PLAIN = false>
+struct OpUpCkpt : OpUp<Cfg_, PLAIN> {
+  using Base = OpUp<Cfg_, PLAIN>;
+  using Cfg = Cfg_;
+  using typename Base::ColMap;
+  using typename Base::Params;
+  static constexpr int Wn = Base::Wn;
+  static_assert(Cfg::BM == 256 && Cfg::BN == 256 && Cfg::WN == 2 && Cfg::RN == 4 && Cfg::STAGE_BYTES >= Cfg::NW * 4096,
+                "two waves share a block of 128 columns");
+  // [gate, up][column group][row]; the A tile goes through the idle last stage
+  static constexpr int EPI_LDS = 2 * 2 * Cfg::BM * 4;
+  // full tile, per row block: A in four stores, H in two for each half
+  static constexpr int EPI_STORES = Cfg::RM * 8;
+  static __device__ void epilogue(const Params& p, const TileInfo& ti, Acc<Cfg>& t, char* epi) {
+    const UpArgs& a = p.a;
+    const int n = a.n, j0 = (ti.n0 / Cfg::BN) * (Cfg::BN / 2);
+    const int lane = epilogue_lane(), wn = t.wave_n(), h = lane >> 5;
+    const int wm0 = Cfg::wave_m(threadIdx.x >> 6) * (Cfg::BM / Cfg::WM);
+    if (a.b1) add_col_bias<Cfg, PLAIN>(t, a.b1 + (size_t)ti.e * (2 * n), ColMap{j0, n}, 2 * n);
+    const int col = j0 + wn * (Wn / 2);  // this wave's first gate column
+    const bool live = PLAIN || col < n;
+    float* amax = (float*)epi;
+#pragma unroll
+    for (int i = 0; i < Cfg::RM; ++i)
+#pragma unroll
+      for (int up = 0; up < 2; ++up) {
+        float x[32];
+#pragma unroll
+        for (int q = 0; q < 32; ++q) x[q] = t.acc[i][2 * up + q / 16][q % 16];
+        float m = finite_amax(x);
+        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        if (h == 0) amax[(up * 2 + wn) * Cfg::BM + wm0 + 32 * i + lane] = live ? m : 0.f;
+      }
+    barrier_lds();
+    char* st = epi - Cfg::STAGE_BYTES + (threadIdx.x >> 6) * 4096;
+    const int nb = q_blocks(n), hs = h8_stride(n);
+#pragma unroll
+    for (int i = 0; i < Cfg::RM; ++i) {
+      const int m0 = wm0 + 32 * i, m = m0 + (lane & 31);
+      if (m0 >= ti.mrows || !live) continue;
+      const size_t r0 = (size_t)(ti.row_base + m0);
+      int sb[2];
+#pragma unroll
+      for (int up = 0; up < 2; ++up)
+        sb[up] = scale_byte(__float_as_uint(fmaxf(amax[up * 2 * Cfg::BM + m], amax[(up * 2 + 1) * Cfg::BM + m])));
+      const float ig = scale_inverse(sb[0]), iu = scale_inverse(sb[1]);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x2 ha[4];
+        uint32_t cg[4], cu[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          float gv[4], uv[4], av[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            gv[r] = t.acc[i][q][4 * g + r];
+            uv[r] = t.acc[i][2 + q][4 * g + r];
+            float sg;
+            av[r] = silu_sig(gv[r], &sg) * uv[r];
+          }
+          ha[g] = pack_bf16x4(av[0], av[1], av[2], av[3]);
+          cg[g] = pack_fp8x4(gv[0] * ig, gv[1] * ig, gv[2] * ig, gv[3] * ig);
+          cu[g] = pack_fp8x4(uv[0] * iu, uv[1] * iu, uv[2] * iu, uv[3] * iu);
+        }
+        stage_block32(st, q, ha);
+        const u32x4 xg = swap_block_fp8(cg[0], cg[1], cg[2], cg[3]), xu = swap_block_fp8(cu[0], cu[1], cu[2], cu[3]);
+        if (m < ti.mrows) {
+          uint8_t* h8 = a.H8 + (r0 + (lane & 31)) * (2 * n) + col + 32 * q + 16 * h;
+          *(u32x4*)h8 = xg;
+          *(u32x4*)(h8 + n) = xu;
+        }
+      }
+      store_staged32(st, a.A + r0 * n + col, n, ti.mrows - m0);
+      // the first column group writes the gate's scales, the second the up half's
+      // (alone, the first writes both)
+      if (h == 0 && m < ti.mrows) {
+        uint8_t* s8 = a.Hs + (r0 + lane) * hs + j0 / kQBlock;
+        if (wn == 0) s8[0] = sb[0];
+        if (wn == 1 || j0 + Wn / 2 >= n) s8[nb] = sb[1];
+      }
+    }
+  }
+};
+
 // As store_rows_bf16, for ops whose last stage buffer is idle during the
 // epilogue (no DMA writes it before the next tile's first barrier): each 32 x
 // 64 block pair goes through the wave's 4 KB share of it in one round
@@ -1216,7 +1337,8 @@ struct OpDown {
 // Epilogue (down-proj backward): with A recomputed from the cached H,
 // dS = <dA', A> (reduced over this tile's n columns), dA = s dA',
 // dH = dSwiGLU(dA, H), A' = s A.
-template <class Cfg_, bool PLAIN = false>
+// Q8: H comes in 8-bit blocks of 128 columns (a wave's columns lie in one).
+template <class Cfg_, bool PLAIN = false, bool Q8 = false>
 struct OpDH {
   using Cfg = Cfg_;
   static constexpr int M_MODE = ROWS, N_MODE = ROWS;
@@ -1267,14 +1389,57 @@ struct OpDH {
       swr[i] = m < ti.mrows ? p.a.row_w[(size_t)(ti.row_base + m)] : 0.f;
     }
     u32x2 hg[2][4], hu[2][4];
+    u32x4 qg[2], qu[2];  // (Q8)
+    float qs[RM][2];
+    if constexpr (Q8) {
+      static_assert(Cfg::BN / Cfg::WN <= kQBlock, "a wave's columns lie in one block");
+      const int nb = q_blocks(n), hs = h8_stride(n), qb = min(col_of(0), n - 32) / kQBlock;
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        const int m = m_of(i);
+        const uint8_t* s8 = p.a.Hs + (size_t)(ti.row_base + (m < ti.mrows ? m : 0)) * hs + qb;
+        qs[i][0] = scale_value(s8[0]);
+        qs[i][1] = scale_value(s8[nb]);
+      }
+    }
     auto load_block = [&](int blk, int b) {
       const int i = blk / RN, j = blk % RN;
       const int m = m_of(i);
       const size_t row = (size_t)(ti.row_base + (m < ti.mrows ? m : 0));
-      const uint16_t* h = p.a.H + row * (2 * n);
       const int col = PLAIN ? col_of(j) : min(col_of(j), n - 32);  // (columns past n are not used)
-      load_block_bf16(h + col, hg[b]);
-      load_block_bf16(h + n + col, hu[b]);
+      if constexpr (Q8) {
+        const uint8_t* h = p.a.H8 + row * (2 * n) + col + 16 * (lane >> 5);
+        qg[b] = *(const u32x4*)h;
+        qu[b] = *(const u32x4*)(h + n);
+      } else {
+        const uint16_t* h = p.a.H + row * (2 * n);
+        load_block_bf16(h + col, hg[b]);
+        load_block_bf16(h + n + col, hu[b]);
+      }
+    };
+    // gate and up values of block blk: four runs of four columns
+    auto values = [&](int blk, int b, f32x4 (&gv)[4], f32x4 (&uv)[4]) {
+      if constexpr (Q8) {
+        uint32_t g8[4], u8[4];
+        unswap_block_fp8(qg[b], g8);
+        unswap_block_fp8(qu[b], u8);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          gv[g] = unpack_fp8x4(g8[g]);
+          uv[g] = unpack_fp8x4(u8[g]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            gv[g][r] *= qs[blk / RN][0];
+            uv[g][r] *= qs[blk / RN][1];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          gv[g] = f32x4{bf_lo(hg[b][g][0]), bf_hi(hg[b][g][0]), bf_lo(hg[b][g][1]), bf_hi(hg[b][g][1])};
+          uv[g] = f32x4{bf_lo(hu[b][g][0]), bf_hi(hu[b][g][0]), bf_lo(hu[b][g][1]), bf_hi(hu[b][g][1])};
+        }
+      }
     };
     load_block(0, 0);
     float part = 0.f;
@@ -1295,10 +1460,11 @@ struct OpDH {
         const int m0 = wm0 + 32 * i;
         if (m0 < ti.mrows && (PLAIN || col_of(j) < n)) {
           u32x2 vg[4], vu[4], va[4];
+          f32x4 gvs[4], uvs[4];
+          values(blk, b, gvs, uvs);
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const float gv[4] = {bf_lo(hg[b][g][0]), bf_hi(hg[b][g][0]), bf_lo(hg[b][g][1]), bf_hi(hg[b][g][1])};
-            const float uv[4] = {bf_lo(hu[b][g][0]), bf_hi(hu[b][g][0]), bf_lo(hu[b][g][1]), bf_hi(hu[b][g][1])};
+            const f32x4 gv = gvs[g], uv = uvs[g];
             float dg[4], du[4], apv[4];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
@@ -1337,10 +1503,11 @@ struct OpDH {
         uint16_t* ap = p.a.Ap + row * n;
         const int col = col_of(j);
         u32x2 vg[4], vu[4], va[4];
+        f32x4 gvs[4], uvs[4];
+        values(blk, b, gvs, uvs);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const float gv[4] = {bf_lo(hg[b][g][0]), bf_hi(hg[b][g][0]), bf_lo(hg[b][g][1]), bf_hi(hg[b][g][1])};
-          const float uv[4] = {bf_lo(hu[b][g][0]), bf_hi(hu[b][g][0]), bf_lo(hu[b][g][1]), bf_hi(hu[b][g][1])};
+          const f32x4 gv = gvs[g], uv = uvs[g];
           float dg[4], du[4], apv[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -1666,6 +1833,13 @@ hipError_t launch_up(const UpArgs& a, hipStream_t s) {
   return w == 256 ? run<OpUp<C256x256w>>({a}, grid, s) : run<OpUp<C256x128>>({a}, grid, s);
 }
 
+// (a block of 128 columns needs the 256-wide tile)
+hipError_t launch_up_ckpt(const UpArgs& a, hipStream_t s) {
+  const int N = 2 * a.n, grid = pad8(mtiles_bound(a.capacity, a.E, 256) * n_tiles(N, 256));
+  if (plain_256(N)) return run<OpUpCkpt<C256x256w, true>>({a}, grid, s);
+  return run<OpUpCkpt<C256x256w>>({a}, grid, s);
+}
+
 hipError_t launch_down(const DownArgs& a, hipStream_t s) {
   const int w = tile_width(kTimesDown, a.mt, a.d);
   const int grid = pad8(mtiles_bound(a.capacity, a.E, 256) * n_tiles(a.d, w));
@@ -1692,6 +1866,14 @@ int dh_n_tiles(int n, int64_t mt) { return n_tiles(n, tile_width(kTimesDH, mt, n
 hipError_t launch_dh(const DHArgs& a, hipStream_t s) {
   const int w = tile_width(kTimesDH, a.mt, a.n);
   const int grid = pad8(mtiles_bound(a.capacity, a.E, 256) * n_tiles(a.n, w));
+  if (a.H8) {
+    if (w == 256 && plain_256(a.n)) return run<OpDH<C256x256w, true, true>>({a}, grid, s);
+    switch (w) {
+      case 256: return run<OpDH<C256x256w, false, true>>({a}, grid, s);
+      case 128: return run<OpDH<C256x128, false, true>>({a}, grid, s);
+      default: return run<OpDH<C256x64, false, true>>({a}, grid, s);
+    }
+  }
   if (w == 256 && plain_256(a.n)) return run<OpDH<C256x256w, true>>({a}, grid, s);
   switch (w) {
     case 256: return run<OpDH<C256x256w>>({a}, grid, s);

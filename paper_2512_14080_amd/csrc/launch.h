@@ -100,8 +100,11 @@ struct UpArgs {
   const uint16_t* X; const uint16_t* W1; const int32_t* offsets; const int32_t* row_token;
   uint16_t* H; uint16_t* A; int d, n, E, capacity; int64_t mt; const int32_t* mtiles;
   const float* b1;  // [E,2n] expert bias added to H, or null
+  // H kept in 8-bit blocks instead (launch_up_ckpt)
+  uint8_t* H8 = nullptr; uint8_t* Hs = nullptr;
 };
 hipError_t launch_up(const UpArgs& a, hipStream_t s);
+hipError_t launch_up_ckpt(const UpArgs& a, hipStream_t s);
 
 struct DownArgs {
   const uint16_t* A; const uint16_t* W2; const int32_t* offsets; uint16_t* Y; int d, n, E, capacity;
@@ -136,6 +139,8 @@ struct DHArgs {
   // <dO_t, b2_e> of the expert-bias dS term as two fp32 halves [T][2E]
   // (columns e and E + e; see launch_bias_split), or null
   const float* bq;
+  // H in 8-bit blocks (then H is null)
+  const uint8_t* H8 = nullptr; const uint8_t* Hs = nullptr;
 };
 int dh_n_tiles(int n, int64_t mt);  // dS partials per row
 inline int dh_max_n_tiles(int n) { return (n + 63) / 64; }  // at the narrowest tile
@@ -203,6 +208,32 @@ inline size_t colsum_part_bytes(int64_t capacity, int E, int d, int n) {
   return (size_t)(capacity / kMTile + E) * (2 * n + d) * 4;
 }
 hipError_t launch_expert_colsum(const ExpertColsumArgs& a, hipStream_t s);
+
+// The 8-bit block format (fp8_block.h).  rows * blocks of a row < 2^31
+hipError_t launch_quantize_rows(const uint16_t* X, int64_t rows, int cols, uint8_t* q, uint8_t* scale, hipStream_t s);
+hipError_t launch_dequantize_rows(const uint8_t* q, const uint8_t* scale, int64_t rows, int cols, uint16_t* X,
+                                  hipStream_t s);
+struct QExpertsArgs {
+  const uint16_t* W1; const uint16_t* W2;                  // (quantize)
+  uint8_t* W1q; uint8_t* W1s; uint8_t* W2q; uint8_t* W2s;
+  uint16_t* W1out; uint16_t* W2out;                        // (dequantize)
+  int d, n, E;
+};
+hipError_t launch_quantize_experts(const QExpertsArgs& a, hipStream_t s);
+hipError_t launch_dequantize_experts(const QExpertsArgs& a, hipStream_t s);
+
+// The 8-bit forward (gemm_fp8.hip): launch_quant_up writes A8, As (and H8, Hs where
+// given) from X8, Xs; launch_quant_down Y from A8, As.
+struct QuantArgs {
+  const uint8_t* X8; const uint8_t* Xs;
+  const uint8_t* W1q; const uint8_t* W1s; const uint8_t* W2q; const uint8_t* W2s;
+  const int32_t* offsets; const int32_t* row_token; const int32_t* row_expert; const int32_t* mtiles;
+  const float* b1; const float* b2;
+  float* H32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
+  int d, n, E, capacity;
+};
+hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s);
+hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s);
 
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);

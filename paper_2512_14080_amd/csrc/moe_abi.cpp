@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "fp8_block.h"
 #include "launch.h"
 
 namespace {
@@ -188,6 +189,81 @@ size_t bwd_layout(const moe_dims& m, int64_t cap, char* base, BwdWs* w) {
   return off;
 }
 
+// moe_bwd_ckpt: the backward workspace, then X in bf16 (where the kept one is used)
+size_t bwd_ckpt_layout(const moe_dims& m, int64_t cap, char* base, BwdWs* w, uint16_t** X) {
+  size_t off = bwd_layout(m, cap, base, w);
+  off = carve(base, off, (size_t)m.T * m.d * 2, (void**)X);
+  return off;
+}
+
+// moe_fwd_quant: X and A in 8-bit blocks (X's in the checkpoint where it is kept)
+struct QuantWs {
+  uint8_t* X8;
+  uint8_t* Xs;
+  float* H32;
+  uint8_t* A8;
+  uint8_t* As;
+  uint16_t* Y;
+  int32_t* mtiles;
+};
+size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
+  const int np = smoe::q_pad(m.n);
+  size_t off = 0;
+  off = carve(base, off, (size_t)m.T * m.d, w ? (void**)&w->X8 : nullptr);
+  off = carve(base, off, (size_t)m.T * smoe::q_stride(m.d / smoe::kQBlock), w ? (void**)&w->Xs : nullptr);
+  off = carve(base, off, (size_t)cap * 2 * np * 4, w ? (void**)&w->H32 : nullptr);
+  off = carve(base, off, (size_t)cap * np, w ? (void**)&w->A8 : nullptr);
+  off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
+  off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);
+  off = carve(base, off, smoe::mtiles_bytes(cap, m.E), w ? (void**)&w->mtiles : nullptr);
+  return off;
+}
+
+size_t qexperts_layout(const moe_dims& m, char* base, moe_qexperts* q) {
+  size_t off = 0;
+  off = carve(base, off, m.E * smoe::w1q_bytes(m.d, m.n), q ? (void**)&q->W1 : nullptr);
+  off = carve(base, off, m.E * smoe::w1s_bytes(m.d, m.n), q ? (void**)&q->W1s : nullptr);
+  off = carve(base, off, m.E * smoe::w2q_bytes(m.d, m.n), q ? (void**)&q->W2 : nullptr);
+  off = carve(base, off, m.E * smoe::w2s_bytes(m.d, m.n), q ? (void**)&q->W2s : nullptr);
+  return off;
+}
+
+size_t ckpt_layout(const moe_dims& m, int64_t cap, int flags, char* base, moe_ckpt* c) {
+  const bool x = flags & MOE_CKPT_X;
+  size_t off = 0;
+  off = carve(base, off, (size_t)cap * 2 * m.n, c ? (void**)&c->H : nullptr);
+  off = carve(base, off, (size_t)cap * smoe::h8_stride(m.n), c ? (void**)&c->Hs : nullptr);
+  off = carve(base, off, x ? (size_t)m.T * m.d : 0, c ? (void**)&c->X : nullptr);
+  off = carve(base, off, x ? (size_t)m.T * smoe::q_stride(m.d / smoe::kQBlock) : 0, c ? (void**)&c->Xs : nullptr);
+  if (c && !x) c->X = c->Xs = nullptr;
+  return off;
+}
+
+int check_qexperts(const moe_dims& m, const moe_qexperts* q, bool written) {
+  if (!q) return fail(MOE_ERR_INVALID_ARG, "the 8-bit weights must not be null");
+  if (!q->W1 || !q->W1s || !q->W2 || !q->W2s)
+    return fail(MOE_ERR_INVALID_ARG, "the 8-bit weights have a null array (initialise them with moe_qexperts_init)");
+  if (q->d != m.d || q->n != m.n || q->E != m.E)
+    return fail(MOE_ERR_INVALID_ARG, "the 8-bit weights are of d = %d, n = %d, E = %d, not of the call's %d, %d, %d", q->d,
+                q->n, q->E, m.d, m.n, m.E);
+  if (written && q->state != MOE_HELD_WRITTEN)
+    return fail(MOE_ERR_INVALID_ARG, "the 8-bit weights are not written (moe_quantize_experts does it)");
+  return MOE_OK;
+}
+
+int check_ckpt(const moe_dims& m, const moe_routing* r, const moe_ckpt* c, bool written) {
+  if (!c) return fail(MOE_ERR_INVALID_ARG, "the checkpoint must not be null");
+  if (!c->H || !c->Hs || !c->X != !c->Xs)
+    return fail(MOE_ERR_INVALID_ARG, "the checkpoint has a null array (initialise it with moe_ckpt_init)");
+  if (c->T != m.T || c->d != m.d || c->n != m.n || c->capacity != r->capacity)
+    return fail(MOE_ERR_INVALID_ARG,
+                "the checkpoint is of T = %d, d = %d, n = %d, capacity %d, not of the call's %d, %d, %d, %d", c->T, c->d,
+                c->n, c->capacity, m.T, m.d, m.n, r->capacity);
+  if (written && c->state != MOE_HELD_WRITTEN)
+    return fail(MOE_ERR_INVALID_ARG, "the checkpoint is not written (moe_fwd_ckpt or moe_fwd_quant does it)");
+  return MOE_OK;
+}
+
 // byte offset of the rounding selection's lists in the routing scratch
 size_t round_lists_offset(const moe_dims& m) {
   const int W = (m.T + 63) / 64;
@@ -357,6 +433,9 @@ size_t moe_workspace_bytes(moe_dims dims, int32_t capacity, int which) {
     float* o32;
     return abl_layout(dims, capacity, nullptr, nullptr, &dst, &o32);
   }
+  if (which == MOE_WS_FWD_QUANT) return quant_layout(dims, capacity, nullptr, nullptr);
+  if (which == MOE_WS_FWD_CKPT) return fwd_layout(dims, capacity, nullptr, nullptr);
+  if (which == MOE_WS_BWD_CKPT) return bwd_ckpt_layout(dims, capacity, nullptr, nullptr, nullptr);
   return 0;
 }
 
@@ -589,9 +668,11 @@ int moe_fwd_aggregation_ablation(moe_dims m, const moe_bf16* X, const moe_bf16* 
   return MOE_OK;
 }
 
-int moe_bwd(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H, const moe_bf16* W1,
-            const moe_bf16* W2, const moe_expert_bias* eb, const moe_bf16* Wr, const moe_routing* r, moe_bf16* dX, moe_bf16* dW1, moe_bf16* dW2,
-            float* dWr, float* dbias, float* dS, void* ws, size_t ws_bytes, void* stream_) {
+// moe_bwd and moe_bwd_ckpt: with ck, its H in the place of H, and its X where X is null
+static int backward(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H, const moe_ckpt* ck,
+                    const moe_bf16* W1, const moe_bf16* W2, const moe_expert_bias* eb, const moe_bf16* Wr,
+                    const moe_routing* r, moe_bf16* dX, moe_bf16* dW1, moe_bf16* dW2, float* dWr, float* dbias, float* dS,
+                    void* ws, size_t ws_bytes, void* stream_) {
   int rc = check_dims(m);
   if (rc) return rc;
   rc = check_routing(m, r, 1, "r");
@@ -599,8 +680,15 @@ int moe_bwd(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H
   rc = check_built(r, "r");
   if (rc) return rc;
   CHECK_PTR(dO, 16);
-  CHECK_PTR(X, 16);
-  CHECK_PTR(H, 16);
+  if (ck) {
+    rc = check_ckpt(m, r, ck, true);
+    if (rc) return rc;
+    if (!X && !ck->X) return fail(MOE_ERR_INVALID_ARG, "X must not be null: the checkpoint does not keep it (MOE_CKPT_X)");
+    if (!aligned(X, 16)) return fail(MOE_ERR_INVALID_ARG, "X must be 16-byte aligned");
+  } else {
+    CHECK_PTR(X, 16);
+    CHECK_PTR(H, 16);
+  }
   CHECK_PTR(W1, 16);
   CHECK_PTR(W2, 16);
   CHECK_PTR(dX, 16);
@@ -614,12 +702,20 @@ int moe_bwd(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H
   rc = check_expert_bias(eb);
   if (rc) return rc;
   const float* b2 = eb ? eb->b2 : nullptr;
-  const size_t need = bwd_layout(m, r->capacity, nullptr, nullptr);
+  uint16_t* x16 = nullptr;
+  const size_t need = ck ? bwd_ckpt_layout(m, r->capacity, nullptr, nullptr, nullptr) : bwd_layout(m, r->capacity, nullptr, nullptr);
   if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "backward workspace %zu < required %zu", ws_bytes, need);
   CHECK_PTR(ws, kAlign);
   BwdWs w;
-  bwd_layout(m, r->capacity, (char*)ws, &w);
+  if (ck)
+    bwd_ckpt_layout(m, r->capacity, (char*)ws, &w, &x16);
+  else
+    bwd_layout(m, r->capacity, (char*)ws, &w);
   hipStream_t stream = (hipStream_t)stream_;
+  if (!X) {
+    LAUNCH(MOE_KC_QUANTIZE, smoe::launch_dequantize_rows(ck->X, ck->Xs, m.T, m.d, x16, stream), "kept X");
+    X = x16;
+  }
   float* dS_out = dS ? dS : w.dS;
   const int64_t rows = (int64_t)m.T * m.K, mt = smoe::expected_mtiles(m, *r);
   const int nnt = smoe::dh_n_tiles(m.n, mt);
@@ -633,7 +729,7 @@ int moe_bwd(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H
   }
   LAUNCH(MOE_KC_DH,
          smoe::launch_dh({dO, W2, H, r->offsets, r->row_token, r->row_w, w.dH, w.Ap, dS_out, w.dS_part, m.d, m.n, m.E,
-                          r->capacity, mt, w.mtiles, b2 ? w.bq : nullptr},
+                          r->capacity, mt, w.mtiles, b2 ? w.bq : nullptr, ck ? ck->H : nullptr, ck ? ck->Hs : nullptr},
                          stream),
          "dH");
   // dS in parts (one per N tile of dH): a few are summed where they are read,
@@ -666,6 +762,194 @@ int moe_bwd(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H
   return MOE_OK;
 }
 
+int moe_bwd(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_bf16* H, const moe_bf16* W1, const moe_bf16* W2,
+            const moe_expert_bias* eb, const moe_bf16* Wr, const moe_routing* r, moe_bf16* dX, moe_bf16* dW1,
+            moe_bf16* dW2, float* dWr, float* dbias, float* dS, void* ws, size_t ws_bytes, void* stream) {
+  return backward(m, dO, X, H, nullptr, W1, W2, eb, Wr, r, dX, dW1, dW2, dWr, dbias, dS, ws, ws_bytes, stream);
+}
+
+int32_t moe_scale_stride(int32_t cols) { return cols < 1 ? 0 : smoe::q_stride((cols - 1) / smoe::kQBlock + 1); }
+
+static int check_rows(int64_t rows, int32_t cols) {
+  if (rows < 0) return fail(MOE_ERR_INVALID_ARG, "rows must be >= 0 (got %lld)", (long long)rows);
+  if (cols < 8 || cols % 8) return fail(MOE_ERR_UNSUPPORTED, "cols must be a positive multiple of 8 (got %d)", cols);
+  if (rows > INT32_MAX || rows * ((cols - 1) / smoe::kQBlock + 1) > INT32_MAX)
+    return fail(MOE_ERR_UNSUPPORTED, "%lld rows of %d columns have 2^31 blocks or more", (long long)rows, cols);
+  return MOE_OK;
+}
+
+int moe_quantize_rows(int64_t rows, int32_t cols, const moe_bf16* X, moe_fp8* q, uint8_t* scale, void* stream_) {
+  int rc = check_rows(rows, cols);
+  if (rc || rows == 0) return rc;
+  CHECK_PTR(X, 16);
+  CHECK_PTR(q, 8);
+  CHECK_PTR(scale, 4);
+  hipStream_t stream = (hipStream_t)stream_;
+  LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, rows, cols, q, scale, stream), "quantize rows");
+  return MOE_OK;
+}
+
+int moe_dequantize_rows(int64_t rows, int32_t cols, const moe_fp8* q, const uint8_t* scale, moe_bf16* X, void* stream_) {
+  int rc = check_rows(rows, cols);
+  if (rc || rows == 0) return rc;
+  CHECK_PTR(q, 8);
+  CHECK_PTR(scale, 4);
+  CHECK_PTR(X, 16);
+  hipStream_t stream = (hipStream_t)stream_;
+  LAUNCH(MOE_KC_QUANTIZE, smoe::launch_dequantize_rows(q, scale, rows, cols, X, stream), "dequantize rows");
+  return MOE_OK;
+}
+
+size_t moe_qexperts_bytes(moe_dims m) { return check_dims(m) == MOE_OK ? qexperts_layout(m, nullptr, nullptr) : 0; }
+
+int moe_qexperts_init(moe_dims m, void* buf, size_t bytes, moe_qexperts* q) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  if (!q) return fail(MOE_ERR_INVALID_ARG, "q must not be null");
+  CHECK_PTR(buf, kAlign);
+  const size_t need = qexperts_layout(m, nullptr, nullptr);
+  if (bytes < need) return fail(MOE_ERR_INVALID_ARG, "buffer of %zu bytes < required %zu", bytes, need);
+  *q = moe_qexperts{m.d, m.n, m.E, MOE_HELD_EMPTY, nullptr, nullptr, nullptr, nullptr};
+  qexperts_layout(m, (char*)buf, q);
+  return MOE_OK;
+}
+
+int moe_quantize_experts(moe_dims m, const moe_bf16* W1, const moe_bf16* W2, moe_qexperts* q, void* stream_) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  rc = check_qexperts(m, q, false);
+  if (rc) return rc;
+  CHECK_PTR(W1, 16);
+  CHECK_PTR(W2, 16);
+  hipStream_t stream = (hipStream_t)stream_;
+  q->state = MOE_HELD_EMPTY;  // until the launch is enqueued
+  LAUNCH(MOE_KC_QUANTIZE,
+         smoe::launch_quantize_experts({W1, W2, q->W1, q->W1s, q->W2, q->W2s, nullptr, nullptr, m.d, m.n, m.E}, stream),
+         "quantize experts");
+  q->state = MOE_HELD_WRITTEN;
+  return MOE_OK;
+}
+
+int moe_dequantize_experts(moe_dims m, const moe_qexperts* q, moe_bf16* W1, moe_bf16* W2, void* stream_) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  rc = check_qexperts(m, q, true);
+  if (rc) return rc;
+  CHECK_PTR(W1, 16);
+  CHECK_PTR(W2, 16);
+  hipStream_t stream = (hipStream_t)stream_;
+  LAUNCH(MOE_KC_QUANTIZE,
+         smoe::launch_dequantize_experts({nullptr, nullptr, q->W1, q->W1s, q->W2, q->W2s, W1, W2, m.d, m.n, m.E}, stream),
+         "dequantize experts");
+  return MOE_OK;
+}
+
+size_t moe_ckpt_bytes(moe_dims m, int32_t capacity, int flags) {
+  if (check_dims(m) != MOE_OK || capacity < 1 || (flags & ~MOE_CKPT_X)) return 0;
+  return ckpt_layout(m, capacity, flags, nullptr, nullptr);
+}
+
+int moe_ckpt_init(moe_dims m, int32_t capacity, int flags, void* buf, size_t bytes, moe_ckpt* c) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  if (!c) return fail(MOE_ERR_INVALID_ARG, "c must not be null");
+  if (capacity < 1) return fail(MOE_ERR_CAPACITY, "capacity must be >= 1 (got %d)", capacity);
+  if (flags & ~MOE_CKPT_X) return fail(MOE_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  CHECK_PTR(buf, kAlign);
+  const size_t need = ckpt_layout(m, capacity, flags, nullptr, nullptr);
+  if (bytes < need) return fail(MOE_ERR_INVALID_ARG, "checkpoint buffer of %zu bytes < required %zu", bytes, need);
+  *c = moe_ckpt{m.T, m.d, m.n, capacity, MOE_HELD_EMPTY, 0, nullptr, nullptr, nullptr, nullptr};
+  ckpt_layout(m, capacity, flags, (char*)buf, c);
+  return MOE_OK;
+}
+
+int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const moe_expert_bias* eb, const moe_routing* r,
+                  moe_ckpt* c, moe_bf16* O, void* ws, size_t ws_bytes, void* stream_) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  rc = check_routing(m, r, 1, "r");
+  if (rc) return rc;
+  rc = check_built(r, "r");
+  if (rc) return rc;
+  rc = check_qexperts(m, q, true);
+  if (rc) return rc;
+  if (c) {
+    rc = check_ckpt(m, r, c, false);
+    if (rc) return rc;
+  }
+  CHECK_PTR(X, 16);
+  CHECK_PTR(O, 16);
+  rc = check_expert_bias(eb);
+  if (rc) return rc;
+  const size_t need = quant_layout(m, r->capacity, nullptr, nullptr);
+  if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "8-bit forward workspace %zu < required %zu", ws_bytes, need);
+  CHECK_PTR(ws, kAlign);
+  QuantWs w;
+  quant_layout(m, r->capacity, (char*)ws, &w);
+  hipStream_t stream = (hipStream_t)stream_;
+  if (c) c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
+  uint8_t* X8 = c && c->X ? c->X : w.X8;
+  uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
+  LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, X8, Xs, stream), "quantize X");
+  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
+  const smoe::QuantArgs a{X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, r->row_expert, w.mtiles,
+                          eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.H32, w.A8, w.As, c ? c->H : nullptr,
+                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity};
+  LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
+  LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
+  LAUNCH(MOE_KC_AGG_O, smoe::launch_agg_o(w.Y, *r, O, m.T, m.d, stream), "aggregation");
+  if (c) c->state = MOE_HELD_WRITTEN;
+  return MOE_OK;
+}
+
+int moe_fwd_ckpt(moe_dims m, const moe_bf16* X, const moe_bf16* W1, const moe_bf16* W2, const moe_expert_bias* eb,
+                 const moe_routing* r, moe_ckpt* c, moe_bf16* O, void* ws, size_t ws_bytes, void* stream_) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  rc = check_routing(m, r, 1, "r");
+  if (rc) return rc;
+  rc = check_built(r, "r");
+  if (rc) return rc;
+  rc = check_ckpt(m, r, c, false);
+  if (rc) return rc;
+  CHECK_PTR(X, 16);
+  CHECK_PTR(W1, 16);
+  CHECK_PTR(W2, 16);
+  CHECK_PTR(O, 16);
+  rc = check_expert_bias(eb);
+  if (rc) return rc;
+  const size_t need = fwd_layout(m, r->capacity, nullptr, nullptr);
+  if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "forward workspace %zu < required %zu", ws_bytes, need);
+  CHECK_PTR(ws, kAlign);
+  FwdWs w;
+  fwd_layout(m, r->capacity, (char*)ws, &w);
+  hipStream_t stream = (hipStream_t)stream_;
+  c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
+  const int64_t mt = smoe::expected_mtiles(m, *r);
+  if (c->X) LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, c->X, c->Xs, stream), "quantize X");
+  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
+  LAUNCH(MOE_KC_UP,
+         smoe::launch_up_ckpt({X, W1, r->offsets, r->row_token, nullptr, w.A, m.d, m.n, m.E, r->capacity, mt, w.mtiles,
+                               eb ? eb->b1 : nullptr, c->H, c->Hs},
+                              stream),
+         "up-proj");
+  LAUNCH(MOE_KC_DOWN,
+         Projections(m, *r).run_down({w.A, W2, r->offsets, w.Y, m.d, m.n, m.E, r->capacity, mt, w.mtiles, eb ? eb->b2 : nullptr},
+                                     MOE_AGG_GATHER_SUM, stream),
+         "down-proj");
+  LAUNCH(MOE_KC_AGG_O, smoe::launch_agg_o(w.Y, *r, O, m.T, m.d, stream), "aggregation");
+  c->state = MOE_HELD_WRITTEN;
+  return MOE_OK;
+}
+
+int moe_bwd_ckpt(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_ckpt* c, const moe_bf16* W1,
+                 const moe_bf16* W2, const moe_expert_bias* eb, const moe_bf16* Wr, const moe_routing* r, moe_bf16* dX,
+                 moe_bf16* dW1, moe_bf16* dW2, float* dWr, float* dbias, float* dS, void* ws, size_t ws_bytes,
+                 void* stream) {
+  if (!c) return fail(MOE_ERR_INVALID_ARG, "the checkpoint must not be null");
+  return backward(m, dO, X, nullptr, c, W1, W2, eb, Wr, r, dX, dW1, dW2, dWr, dbias, dS, ws, ws_bytes, stream);
+}
+
 int moe_prof_select(int kc) {
   if (kc < -1 || kc >= MOE_KC_COUNT) return fail(MOE_ERR_INVALID_ARG, "unknown kernel class %d", kc);
   std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -696,7 +980,8 @@ int moe_prof_read(double* ms, int32_t* launches) {
 const char* moe_kernel_class_name(int kc) {
   static const char* names[MOE_KC_COUNT] = {"router_gemm", "topk", "routing_meta", "token_round", "up_proj",
                                             "down_proj", "aggregate_O", "dH", "dW2", "dXtilde",
-                                            "dW1", "aggregate_dX", "dWr", "router_topk"};
+                                            "dW1", "aggregate_dX", "dWr", "router_topk", "quantize",
+                                            "up_proj_quant", "down_proj_quant"};
   return (kc >= 0 && kc < MOE_KC_COUNT) ? names[kc] : "unknown";
 }
 

@@ -1,0 +1,226 @@
+// The 8-bit block format (fp8_block.h) to and from bf16: rows of activations, and
+// the expert weights in the layout that the 8-bit products read.
+#include "fp8_block.h"
+#include "launch.h"
+
+namespace smoe {
+
+constexpr int kRowThreads = 256;
+
+// bf16 pairs: the larger |x| of finite halves as bf16 bits in each half
+__device__ __forceinline__ uint32_t finite_abs_bits(uint32_t h) {
+  h &= 0x7FFFu;
+  return h < 0x7F80u ? h : 0u;
+}
+
+// ---------------------------------------------------------------- rows
+// 16 lanes per block of 128 columns, 8 columns (16 bytes) each: the largest |x| of
+// the block is a maximum over the lane's values and the 16 lanes.
+__global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const uint16_t* __restrict__ X, int units, int blocks,
+                                                                    int cols, int stride, uint8_t* __restrict__ q,
+                                                                    uint8_t* __restrict__ scale) {
+  const int u = blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4), l = threadIdx.x & 15;
+  if (u >= units) return;
+  const int row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
+  u32x4 v = {0, 0, 0, 0};
+  if (c < cols) v = *(const u32x4*)(X + (size_t)row * cols + c);
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max(m, max(finite_abs_bits(v[i]), finite_abs_bits(v[i] >> 16)));
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 16));
+  const int sb = scale_byte(m << 16);
+  const float inv = scale_inverse(sb);
+  u32x2 out;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    out[i] = pack_fp8x4(bf_lo(v[2 * i]) * inv, bf_hi(v[2 * i]) * inv, bf_lo(v[2 * i + 1]) * inv, bf_hi(v[2 * i + 1]) * inv);
+  if (c < cols) *(u32x2*)(q + (size_t)row * cols + c) = out;
+  // (the last block's first lanes also fill the row's scales to a whole dword)
+  if (l == 0 || (b == blocks - 1 && b + l < stride)) scale[(size_t)row * stride + b + l] = l ? 127 : sb;
+}
+
+__global__ __launch_bounds__(kRowThreads) void dequantize_rows_kernel(const uint8_t* __restrict__ q,
+                                                                      const uint8_t* __restrict__ scale, int units,
+                                                                      int blocks, int cols, int stride,
+                                                                      uint16_t* __restrict__ X) {
+  const int u = blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4), l = threadIdx.x & 15;
+  if (u >= units) return;
+  const int row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
+  if (c >= cols) return;
+  const float s = scale_value(scale[(size_t)row * stride + b]);
+  const u32x2 v = *(const u32x2*)(q + (size_t)row * cols + c);
+  u32x4 out;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f32x4 x = unpack_fp8x4(v[i]);
+    out[2 * i] = pack_bf2(x[0] * s, x[1] * s);
+    out[2 * i + 1] = pack_bf2(x[2] * s, x[3] * s);
+  }
+  *(u32x4*)(X + (size_t)row * cols + c) = out;
+}
+
+static int row_units(int64_t rows, int cols) { return (int)(rows * q_blocks(cols)); }
+
+hipError_t launch_quantize_rows(const uint16_t* X, int64_t rows, int cols, uint8_t* q, uint8_t* scale, hipStream_t s) {
+  const int units = row_units(rows, cols), per = kRowThreads / 16;
+  quantize_rows_kernel<<<(units + per - 1) / per, kRowThreads, 0, s>>>(X, units, q_blocks(cols), cols,
+                                                                       q_stride(q_blocks(cols)), q, scale);
+  return hipGetLastError();
+}
+hipError_t launch_dequantize_rows(const uint8_t* q, const uint8_t* scale, int64_t rows, int cols, uint16_t* X,
+                                  hipStream_t s) {
+  const int units = row_units(rows, cols), per = kRowThreads / 16;
+  dequantize_rows_kernel<<<(units + per - 1) / per, kRowThreads, 0, s>>>(q, scale, units, q_blocks(cols), cols,
+                                                                         q_stride(q_blocks(cols)), X);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- expert weights
+// One 128 x 128 block of one matrix: k rows k0 .., columns c0 .. of a half.
+struct WeightBlock {
+  int e, kb, nb, up;   // expert, block of k, block of columns, half (W1)
+  bool w1;
+  __device__ __forceinline__ bool init(const QExpertsArgs& a, int id) {
+    const int kd = a.d / kQBlock, nn = q_blocks(a.n);
+    w1 = id < a.E * kd * nn * 2;
+    if (w1) {
+      kb = id % kd;
+      id /= kd;
+      up = id & 1;
+      id >>= 1;
+      nb = id % nn;
+      e = id / nn;
+    } else {
+      id -= a.E * kd * nn * 2;
+      kb = id % nn;
+      id /= nn;
+      nb = id % kd;
+      e = id / kd;
+      up = 0;
+    }
+    return e < a.E;
+  }
+  // first element of the block in the bf16 matrix, its leading dimension, and the
+  // columns and k rows that exist
+  __device__ __forceinline__ size_t source(const QExpertsArgs& a, int* ld, int* cols, int* ks) const {
+    if (w1) {
+      *ld = 2 * a.n;
+      *cols = a.n - kQBlock * nb;
+      *ks = kQBlock;
+      return ((size_t)e * a.d + kQBlock * kb) * (2 * a.n) + (size_t)up * a.n + kQBlock * nb;
+    }
+    *ld = a.d;
+    *cols = kQBlock;
+    *ks = a.n - kQBlock * kb;
+    return ((size_t)e * a.n + kQBlock * kb) * a.d + kQBlock * nb;
+  }
+  // codes of column c of the block, from the block's first k on
+  __device__ __forceinline__ size_t codes(const QExpertsArgs& a, int c) const {
+    if (w1) return (size_t)e * w1q_bytes(a.d, a.n) + (size_t)(256 * nb + w1q_row(c, up)) * a.d + kQBlock * kb;
+    return (size_t)e * w2q_bytes(a.d, a.n) + (size_t)(kQBlock * nb + c) * q_pad(a.n) + kQBlock * kb;
+  }
+  __device__ __forceinline__ size_t scales(const QExpertsArgs& a, int* blocks) const {
+    if (w1) {
+      *blocks = a.d / kQBlock;
+      return (size_t)e * w1s_bytes(a.d, a.n) + (size_t)(2 * nb + up) * q_stride(*blocks) + kb;
+    }
+    *blocks = q_blocks(a.n);
+    return (size_t)e * w2s_bytes(a.d, a.n) + (size_t)nb * q_stride(*blocks) + kb;
+  }
+};
+
+constexpr int kPitch = kQBlock + 16;  // LDS bytes of a column's 128 codes
+
+// A thread loads 8 columns of 8 consecutive k rows and so holds 8 codes of each of
+// its columns; they go through LDS, and out as whole 128-byte runs of k.
+__global__ __launch_bounds__(256) void quantize_experts_kernel(const QExpertsArgs a) {
+  __shared__ __attribute__((aligned(16))) char tile[kQBlock * kPitch];
+  __shared__ uint32_t wmax[4];
+  WeightBlock w;
+  if (!w.init(a, blockIdx.x)) return;
+  int ld, cols, ks;
+  const uint16_t* src = (w.w1 ? a.W1 : a.W2) + w.source(a, &ld, &cols, &ks);
+  const int c = 8 * (threadIdx.x & 15), k = 8 * (threadIdx.x >> 4);
+  u32x4 v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = u32x4{0, 0, 0, 0};
+    if (c < cols && k + i < ks) v[i] = *(const u32x4*)(src + (size_t)(k + i) * ld + c);
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max(m, max(finite_abs_bits(v[i][j]), finite_abs_bits(v[i][j] >> 16)));
+  m = dpp_reduce(m, [](uint32_t x, uint32_t y) { return max(x, y); });
+  if (lane_id() == 0) wmax[threadIdx.x >> 6] = m;
+  __syncthreads();
+  const int sb = scale_byte(max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3])) << 16);
+  const float inv = scale_inverse(sb);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (j & 1 ? bf_hi(v[i][j >> 1]) : bf_lo(v[i][j >> 1])) * inv;
+    *(u32x2*)(tile + (c + j) * kPitch + k) = u32x2{pack_fp8x4(x[0], x[1], x[2], x[3]), pack_fp8x4(x[4], x[5], x[6], x[7])};
+  }
+  __syncthreads();
+  uint8_t* q = w.w1 ? a.W1q : a.W2q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = (threadIdx.x >> 3) + 32 * i, at = 16 * (threadIdx.x & 7);
+    *(u32x4*)(q + w.codes(a, col) + at) = *(const u32x4*)(tile + col * kPitch + at);
+  }
+  int blocks;
+  uint8_t* s = (w.w1 ? a.W1s : a.W2s) + w.scales(a, &blocks);
+  const int i = threadIdx.x;
+  if (i == 0 || (w.kb == blocks - 1 && w.kb + i < q_stride(blocks))) s[i] = i ? 127 : sb;
+}
+
+__global__ __launch_bounds__(256) void dequantize_experts_kernel(const QExpertsArgs a) {
+  __shared__ __attribute__((aligned(16))) char tile[kQBlock * kPitch];
+  WeightBlock w;
+  if (!w.init(a, blockIdx.x)) return;
+  const uint8_t* q = w.w1 ? a.W1q : a.W2q;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = (threadIdx.x >> 3) + 32 * i, at = 16 * (threadIdx.x & 7);
+    *(u32x4*)(tile + col * kPitch + at) = *(const u32x4*)(q + w.codes(a, col) + at);
+  }
+  int blocks, ld, cols, ks;
+  const float s = scale_value(((w.w1 ? a.W1s : a.W2s) + w.scales(a, &blocks))[0]);
+  uint16_t* dst = (w.w1 ? a.W1out : a.W2out) + w.source(a, &ld, &cols, &ks);
+  __syncthreads();
+  const int c = 8 * (threadIdx.x & 15), k = 8 * (threadIdx.x >> 4);
+  if (c >= cols || k >= ks) return;  // (n is a multiple of 64: eight k rows all exist or none)
+  f32x4 lo[8], hi[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const u32x2 v = *(const u32x2*)(tile + (c + j) * kPitch + k);
+    lo[j] = unpack_fp8x4(v[0]);
+    hi[j] = unpack_fp8x4(v[1]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    u32x4 o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      o[j] = i < 4 ? pack_bf2(lo[2 * j][i & 3] * s, lo[2 * j + 1][i & 3] * s)
+                   : pack_bf2(hi[2 * j][i & 3] * s, hi[2 * j + 1][i & 3] * s);
+    *(u32x4*)(dst + (size_t)(k + i) * ld + c) = o;
+  }
+}
+
+static int weight_blocks(const QExpertsArgs& a) { return a.E * (a.d / kQBlock) * q_blocks(a.n) * 3; }
+
+hipError_t launch_quantize_experts(const QExpertsArgs& a, hipStream_t s) {
+  quantize_experts_kernel<<<weight_blocks(a), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_dequantize_experts(const QExpertsArgs& a, hipStream_t s) {
+  dequantize_experts_kernel<<<weight_blocks(a), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace smoe

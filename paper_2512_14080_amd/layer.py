@@ -39,10 +39,15 @@ class DeviceLayer:
 
     ``round_mode`` None runs token-choice routing only; otherwise the layer is
     run on the token-rounded routing with tile ``m_tile``.
+
+    ``held8`` keeps the activations for the backward in 8 bits: "ckpt" with the
+    16-bit forward, "quant" with the forward in 8-bit expert products (the
+    weights are quantised in every forward, as after an optimiser's step);
+    ``keep_x``: X too, and the backward reads that.
     """
 
     def __init__(self, inputs, round_mode=None, m_tile=None, scores_in=None, u=None, device="cuda",
-                 router_grad=True, b1=None, b2=None, keep_logits=True):
+                 router_grad=True, b1=None, b2=None, keep_logits=True, held8=None, keep_x=False):
         import torch
         cfg = inputs.cfg
         T, d, n, E, K = inputs.X.shape[0], cfg.d, cfg.n, cfg.E, cfg.K
@@ -70,10 +75,15 @@ class DeviceLayer:
             self.route_flags = B.MOE_ROUTE_SCORES_IN | for_round
         self.u = None if u is None else torch.from_numpy(np.asarray(u, np.float32)).to(device)
         cap = self.routing.capacity
-        self.H = torch.empty((cap, 2 * n), dtype=torch.bfloat16, device=device)
+        self.held8, self.keep_x = held8, keep_x
+        ws_f, ws_b = {None: (B.MOE_WS_FWD, B.MOE_WS_BWD), "ckpt": (B.MOE_WS_FWD_CKPT, B.MOE_WS_BWD_CKPT),
+                      "quant": (B.MOE_WS_FWD_QUANT, B.MOE_WS_BWD_CKPT)}[held8]
+        self.H = torch.empty((cap, 2 * n), dtype=torch.bfloat16, device=device) if held8 is None else None
+        self.ckpt = None if held8 is None else B.Checkpoint(self.D, cap, keep_x, device)
+        self.qw = B.QExperts(self.D, device) if held8 == "quant" else None
         self.O = torch.empty((T, d), dtype=torch.bfloat16, device=device)
-        self.ws_f = _aligned_empty(B.moe_workspace_bytes(self.D, cap, B.MOE_WS_FWD), device)
-        self.ws_b = _aligned_empty(B.moe_workspace_bytes(self.D, cap, B.MOE_WS_BWD), device)
+        self.ws_f = _aligned_empty(B.moe_workspace_bytes(self.D, cap, ws_f), device)
+        self.ws_b = _aligned_empty(B.moe_workspace_bytes(self.D, cap, ws_b), device)
         self.dX = torch.empty((T, d), dtype=torch.bfloat16, device=device)
         self.dW1 = torch.empty((E, d, 2 * n), dtype=torch.bfloat16, device=device)
         self.dW2 = torch.empty((E, n, d), dtype=torch.bfloat16, device=device)
@@ -99,9 +109,22 @@ class DeviceLayer:
             B.moe_round_tokens(self.D, self.m_tile, self.round_mode, self.u, self.tc, self.tr, stream)
 
     def forward(self, stream=None):
+        if self.held8 == "ckpt":
+            B.moe_fwd_ckpt(self.D, self.X, self.W1, self.W2, self.routing, self.ckpt, self.O, self.ws_f, stream,
+                           eb=self.eb)
+            return
+        if self.held8 == "quant":
+            B.moe_quantize_experts(self.D, self.W1, self.W2, self.qw, stream)
+            B.moe_fwd_quant(self.D, self.X, self.qw, self.routing, self.ckpt, self.O, self.ws_f, stream, eb=self.eb)
+            return
         B.moe_fwd(self.D, self.X, self.W1, self.W2, self.routing, self.H, self.O, self.ws_f, stream, eb=self.eb)
 
     def backward(self, stream=None):
+        if self.held8:
+            B.moe_bwd_ckpt(self.D, self.dO, None if self.keep_x else self.X, self.ckpt, self.W1, self.W2,
+                           self.Wr if self.router_grad else None, self.routing, self.dX, self.dW1, self.dW2, self.dWr,
+                           self.dbias, self.dS, self.ws_b, stream, eb=self.eb)
+            return
         B.moe_bwd(self.D, self.dO, self.X, self.H, self.W1, self.W2, self.Wr if self.router_grad else None,
                   self.routing, self.dX, self.dW1, self.dW2, self.dWr, self.dbias, self.dS, self.ws_b, stream,
                   eb=self.eb)
