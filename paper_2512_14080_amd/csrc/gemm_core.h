@@ -416,6 +416,29 @@ struct EpiStores : std::integral_constant<int, 0> {};
 template <class Op>
 struct EpiStores<Op, std::void_t<decltype(Op::EPI_STORES)>> : std::integral_constant<int, Op::EPI_STORES> {};
 
+// Ops on 8-bit operands (F8 = true; rows of codes with k contiguous, handled in
+// units of two codes, so that BK = 64 is 128 k, one block of the scales) define
+//   static constexpr int W_SCALES                          -- weight scales of a tile, 1 or 2
+//   const uint8_t* scale_row(const Params&, const TileInfo&, int r, uint32_t idx_lds)
+//                                                          -- the scales of the tile's row r (dwords of four blocks)
+//   void weight_scales(const Params&, const TileInfo&, int g, uint32_t (&)[W_SCALES])
+//                                                          -- four blocks' bytes from block 4 g on
+// Accumulator columns j >= RN / W_SCALES take the second weight scale.  scale_row of
+// an op that gathers reads the row indices that other waves loaded: its epilogue
+// has a workgroup barrier, before which the next tile's may not be requested.
+template <class Op, class = void>
+struct IsF8 : std::false_type {};
+template <class Op>
+struct IsF8<Op, std::void_t<decltype(Op::F8)>> : std::true_type {};
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+// the 32 codes of each lane for sub-step s (64 k) of a stage
+template <class Side>
+__device__ __forceinline__ i32x8 frag8(const char* lds_side, int r0, int s) {
+  const u32x4 a = __builtin_bit_cast(u32x4, Side::frag(lds_side, r0, 2 * s));
+  const u32x4 b = __builtin_bit_cast(u32x4, Side::frag(lds_side, r0, 2 * s + 1));
+  return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
 template <class Op, class = void>
 struct HasCountTail : std::false_type {};
 template <class Op>
@@ -450,7 +473,9 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
   constexpr bool kSplit = Cfg::SPLIT;
   // (its ops gather nothing: row-major M side, N side without k-row indices)
   static_assert(!kSplit || (Op::M_MODE == ROWS && kIdxLds == 0 && Op::EPI_LDS == 0), "split-ring ops");
-  constexpr int kSmem = kSplit ? Cfg::LDS_BYTES : Cfg::LDS_BYTES + kEpiBytes + kIdxLds;
+  constexpr bool kF8 = IsF8<Op>::value;
+  constexpr int kScaleLds = kF8 ? 2 * BM * 4 : 0;  // two groups of four blocks' scales, a dword per row
+  constexpr int kSmem = kSplit ? Cfg::LDS_BYTES : Cfg::LDS_BYTES + kEpiBytes + kIdxLds + kScaleLds;
   static_assert(kSmem <= 160 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) char smem[kSmem];
   int* sh = nullptr;  // [0..3], [4..7]: tile lookups of even / odd k; [8..9]: tile counts
@@ -479,10 +504,32 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
   if constexpr (kIdxLds > 0) ms.idx_lds = ms_next.idx_lds = lds0 + Cfg::LDS_BYTES + kEpiBytes;
   Op::init_m(p, ti, ms);
   Op::init_n(p, ti, ns);
-  if constexpr (kIdxLds > 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the first tile's index DMA
+  // the first tile's index DMA (of every wave, for the scales' rows)
+  if constexpr (kIdxLds > 0 && IsF8<Op>::value)
+    wait_vm_barrier<0>();
+  else if constexpr (kIdxLds > 0)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   ms.commit();
   ns.commit();
   const int wave = threadIdx.x >> 6;
+  // 8-bit operands: the rows' scales come by DMA like the rows, a dword (four
+  // blocks) of 64 rows per instruction, which the first BM / 64 waves issue; group g
+  // goes to half g % 2 of its area
+  const uint32_t scale_lds = lds0 + Cfg::LDS_BYTES + kEpiBytes + kIdxLds;
+  const uint8_t* scale_ptr = nullptr;  // this lane's row
+  auto scale_rows = [&](const TileInfo& t) {
+    if constexpr (kF8) {
+      if (wave < BM / 64)
+        scale_ptr = Op::scale_row(p, t, min(64 * wave + (int)(threadIdx.x & 63), t.mrows - 1), ms.idx_lds);
+    }
+  };
+  auto scale_issue = [&](int g) {
+    if constexpr (kF8) {
+      const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      if (w < BM / 64) dma4(scale_ptr + 4 * g, scale_lds + (g & 1) * (BM * 4) + w * 256);
+    }
+  };
+  scale_rows(ti);
   const int wm0 = Cfg::wave_m(wave) * (BM / Cfg::WM);
   const int wn0 = Cfg::wave_n(wave) * (BN / Cfg::WN);
   constexpr int kPerStage = Cfg::QM + Cfg::QN;  // DMA ops per wave per stage
@@ -500,6 +547,7 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
   // the next tile's sides after the k loop: that is plain arithmetic, and its
   // registers would otherwise be held across the loop (with the interleaved
   // DMA the 256x256 loop then spilled).
+  // (So do 8-bit operands that gather nothing.)
   constexpr bool kLateSides = Op::M_MODE == KOUTER && Op::N_MODE == KOUTER;
   // The two-stage schedule with its barrier before the last sub-step (below)
   // needs a stage's instructions to fit every second MFMA of one sub-step.
@@ -513,6 +561,7 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
   // stages 0 .. S-2 of a tile, and the row indices of stage S-1 (gathered k)
   auto prologue = [&](const TileInfo& t, MSide& a, NSide& b) {
     const int nk = (t.k_len + BK - 1) / BK;
+    scale_issue(0);  // (older than stage 0, whose wait covers it)
     if constexpr (kSplit) {
       // A0, B0, A1 (in this order: the waits count on it)
       if (nk > 0) {
@@ -557,8 +606,8 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
     // this tile's k loop; the weight-gradient sides (plain arithmetic) set up
     // after it, so their registers are free during the k loop.
     if (idn >= 0 && !kLateSides) {
-      Op::init_m(p, tn, ms_next);
-      Op::init_n(p, tn, ns_next);
+      if constexpr (!kF8 || kIdxLds > 0) Op::init_m(p, tn, ms_next);
+      if constexpr (!kF8) Op::init_n(p, tn, ns_next);
     }
     const int nk = (ti.k_len + BK - 1) / BK;
     // a wave whose rows all lie past the tile's valid rows skips its MFMAs
@@ -726,6 +775,80 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
         k_loop(std::true_type{});
       else
         k_loop(std::false_type{});
+    } else if constexpr (kF8) {
+      // 8-bit operands, two stages of 128 k: two sub-steps of 64 k per stage, each
+      // MFMA as long as two of the bf16 ones, so a DMA instruction before every one
+      // of the first keeps the stage's requests in the first half of the step.  A
+      // fragment is two 16-byte chunks of its row; which k a chunk holds does not
+      // matter as long as both operands agree, and the scales cover the whole stage.
+      static_assert(!kF8 || (S == 2 && Cfg::RN % 2 == 0 && BK == 64 && Op::M_MODE == ROWS && Op::N_MODE == ROWS), "8-bit ops");
+      constexpr int NS = Op::W_SCALES;
+      uint32_t ws[NS], ws_next[NS], xs[Cfg::RM];
+      Op::weight_scales(p, ti, 0, ws_next);
+      const int groups = (nk + 3) >> 2;
+      for (int kt = 0; kt < nk; ++kt) {
+        // (a tile of one step: the next tile's index loads are to be complete after it)
+        if (kt == 0 && prev_full && nk > 1)
+          wait_vm_barrier<(EpiStores<Op>::value < 63 ? EpiStores<Op>::value : 63)>();
+        else
+          wait_vm_barrier<0>();
+        const int g = kt >> 2;
+        if ((kt & 3) == 0) {
+          const SMOE_LDS uint32_t* sl = (const SMOE_LDS uint32_t*)(uintptr_t)(scale_lds + (g & 1) * (BM * 4));
+#pragma unroll
+          for (int i = 0; i < Cfg::RM; ++i) xs[i] = sl[wm0 + 32 * i + (threadIdx.x & 31)];
+#pragma unroll
+          for (int q = 0; q < NS; ++q) ws[q] = ws_next[q];
+          if (g + 1 < groups) Op::weight_scales(p, ti, g + 1, ws_next);
+        }
+        const int knext = kt + 1;
+        const bool issue_next = knext < nk;
+        const uint32_t st_next = lds0 + (knext & 1) * Cfg::STAGE_BYTES;
+        const char* lm = smem + (kt & 1) * Cfg::STAGE_BYTES;
+        const char* ln = lm + Cfg::M_BYTES;
+        auto issue_one = [&](int d) {
+          if (d < Cfg::QM)
+            ms.issue(st_next, knext * BK, d, Cfg::QM);
+          else
+            ns.issue(st_next + Cfg::M_BYTES, knext * BK, d - Cfg::QM, Cfg::QN);
+        };
+        if (active) {
+          // one column fragment ahead: the one of the next column is read while this
+          // one's MFMAs issue
+          i32x8 fm[Cfg::RM], fn[2];
+#pragma unroll
+          for (int i = 0; i < Cfg::RM; ++i) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, 0);
+          fn[0] = frag8<NSide>(ln, wn0, 0);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < Cfg::RN; ++j) {
+              if (j + 1 < Cfg::RN)
+                fn[(j + 1) & 1] = frag8<NSide>(ln, wn0 + 32 * (j + 1), s);
+              else if (s == 0)
+                fn[(j + 1) & 1] = frag8<NSide>(ln, wn0, 1);
+#pragma unroll
+              for (int i = 0; i < Cfg::RM; ++i) {
+                const int c = (s * Cfg::RN + j) * Cfg::RM + i;
+                __builtin_amdgcn_sched_barrier(0);
+                if (c < kPerStage && issue_next) issue_one(c);
+                __builtin_amdgcn_sched_barrier(0);
+                acc.acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                    fn[j & 1], fm[i], acc.acc[i][j], 0, 0, 0, (int)ws[j * NS / Cfg::RN], 0, (int)xs[i]);
+                if (s == 0 && j == Cfg::RN - 1) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, 1);
+              }
+            }
+        } else if (issue_next) {
+          ms.issue(st_next, knext * BK);
+          ns.issue(st_next + Cfg::M_BYTES, knext * BK);
+        }
+        // the next group's scales, complete at the top of the step after
+        if ((kt & 3) == 1 && g + 1 < groups) scale_issue(g + 1);
+#pragma unroll
+        for (int i = 0; i < Cfg::RM; ++i) xs[i] >>= 8;
+#pragma unroll
+        for (int q = 0; q < NS; ++q) ws[q] >>= 8;
+      }
     } else {
       for (int kt = 0; kt < nk; ++kt) {
         // stage kt is complete when at most (stages issued after it) * kPerStage
@@ -805,15 +928,14 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
     }
     barrier_lds();  // every wave is done with the stage buffers
     if (idn >= 0) {
-      if constexpr (kLateSides) {
-        Op::init_m(p, tn, ms_next);
-        Op::init_n(p, tn, ns_next);
-      }
+      if constexpr (kLateSides || (kF8 && kIdxLds == 0)) Op::init_m(p, tn, ms_next);
+      if constexpr (kLateSides || kF8) Op::init_n(p, tn, ns_next);
       // the last step's full drain covered the next tile's index loads
       ms_next.commit();
       ns_next.commit();
       ms = ms_next;
       ns = ns_next;
+      scale_rows(tn);
       prologue(tn, ms, ns);
     }
     Op::epilogue(p, ti, acc, smem + Cfg::LDS_BYTES);

@@ -1333,6 +1333,181 @@ struct OpDown {
   }
 };
 
+// ================================================================== 8-bit projections
+// The same two products on 8-bit blocks (fp8_block.h): X~ gathered and W1~_e, A~ and
+// W2~_e, with k contiguous on both sides.  K in units of two codes.
+struct F8Rows {
+  static constexpr bool F8 = true;
+  static constexpr int M_MODE = ROWS, N_MODE = ROWS;
+};
+
+// N tile: 128 gate columns and the matching up columns, in the order the weights
+// are laid out in, so a wave's first 64 are gate columns and its last 64 the up ones.
+// A leaves as codes of blocks of 128: the two waves of a row group hold 64 columns
+// each, and their largest |A| meet in LDS (as do H's where it is kept).
+template <class Cfg_>
+struct OpUp8 : F8Rows {
+  using Cfg = Cfg_;
+  static constexpr int W_SCALES = 2;
+  static_assert(Cfg::BM == 256 && Cfg::BN == 256 && Cfg::WN == 2 && Cfg::RN == 4, "two waves share a block of 128 columns");
+  struct Params { QuantArgs a; };
+  static constexpr int IDX_LDS = Cfg::NW * Cfg::QM * 256;
+  static constexpr int EPI_LDS = 3 * 2 * Cfg::BM * 4;  // [gate, up, A][column group][row]
+  static constexpr int EPI_STORES = Cfg::RM * 2;       // A's
+  static __device__ int count(const Params& p, int*) { return count_varlen_m<256>(p.a.mtiles, 2 * q_pad(p.a.n)); }
+  static __device__ int count_tail(const Params& p, const int*) {
+    return count_varlen_m_tail<256>(p.a.mtiles, 2 * q_pad(p.a.n));
+  }
+  static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
+    return tile_varlen_m<Cfg::BM, Cfg::BN>(p.a.mtiles, p.a.E, 2 * q_pad(p.a.n), p.a.d / 2, id, ti);
+  }
+  static __device__ void init_m(const Params& p, const TileInfo& ti, RowsSide<Cfg::BM, Cfg::BK, Cfg::NW, true>& s) {
+    s.init((const uint16_t*)p.a.X8, p.a.d / 2, p.a.row_token, ti.row_base, ti.mrows);
+  }
+  static __device__ void init_n(const Params& p, const TileInfo& ti, RowsSide<Cfg::BN, Cfg::BK, Cfg::NW>& s) {
+    s.init((const uint16_t*)(p.a.W1q + (size_t)ti.e * w1q_bytes(p.a.d, p.a.n)), p.a.d / 2, nullptr, ti.n0, ti.ncols);
+  }
+  static __device__ const uint8_t* scale_row(const Params& p, const TileInfo&, int r, uint32_t idx_lds) {
+    // row r was loaded by instruction j of wave w (RowsSide), in all eight lanes of its place
+    const int q = r >> 3, w = q % Cfg::NW, j = q / Cfg::NW;
+    const int t = *(const SMOE_LDS int32_t*)(uintptr_t)(idx_lds + (w * Cfg::QM + j) * 256 + (r & 7) * 32);
+    return p.a.Xs + (size_t)t * q_stride(p.a.d / kQBlock);
+  }
+  static __device__ void weight_scales(const Params& p, const TileInfo& ti, int g, uint32_t (&ws)[2]) {
+    const int st = q_stride(p.a.d / kQBlock);
+    const SMOE_CONST uint8_t* s = (const SMOE_CONST uint8_t*)p.a.W1s + (size_t)ti.e * w1s_bytes(p.a.d, p.a.n) +
+                                  (size_t)(ti.n0 / Cfg::BN) * 2 * st + 4 * g;
+    ws[0] = *(const SMOE_CONST uint32_t*)s;
+    ws[1] = *(const SMOE_CONST uint32_t*)(s + st);
+  }
+  static __device__ void epilogue(const Params& p, const TileInfo& ti, Acc<Cfg>& t, char* epi) {
+    const QuantArgs& a = p.a;
+    const int n = a.n, np = q_pad(n), nb = np / kQBlock, b = ti.n0 / Cfg::BN;  // block of A's columns
+    const int lane = epilogue_lane(), wn = t.wave_n(), h = lane >> 5;
+    const int wm0 = Cfg::wave_m(threadIdx.x >> 6) * (Cfg::BM / Cfg::WM);
+    const int col = kQBlock * b + 64 * wn;  // this wave's first column
+    const bool live = col < n;              // (past n everything is zero, and is stored as A's padding)
+    float* amax = (float*)epi;
+    auto put = [&](int which, int i, float m) {
+      m = fmaxf(m, __shfl_xor(m, 32, kWave));
+      if (h == 0) amax[(which * 2 + wn) * Cfg::BM + wm0 + 32 * i + lane] = m;
+    };
+    auto block_scale = [&](int which, int m) {
+      return scale_byte(__float_as_uint(fmaxf(amax[which * 2 * Cfg::BM + m], amax[(which * 2 + 1) * Cfg::BM + m])));
+    };
+    // the 64 codes of this wave and row block i, accumulator columns j0 .. j0 + 1 (both
+    // lanes of a row are in a branch on it, so the swaps find their partners)
+    auto store = [&](int i, int j0, float inv, uint8_t* row) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        uint32_t v[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const auto& x = t.acc[i][j0 + q];
+          v[g] = pack_fp8x4(x[4 * g] * inv, x[4 * g + 1] * inv, x[4 * g + 2] * inv, x[4 * g + 3] * inv);
+        }
+        *(u32x4*)(row + 32 * q + 16 * h) = swap_block_fp8(v[0], v[1], v[2], v[3]);
+      }
+    };
+    if (a.b1 && live) {
+      const float* b1 = a.b1 + (size_t)ti.e * (2 * n) + col + 4 * h;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 v = *(const f32x4*)(b1 + (j >> 1) * n + 32 * (j & 1) + 8 * g);
+#pragma unroll
+          for (int i = 0; i < Cfg::RM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) t.acc[i][j][4 * g + r] += v[r];
+        }
+    }
+    if (a.H8) {
+#pragma unroll
+      for (int i = 0; i < Cfg::RM; ++i)
+#pragma unroll
+        for (int up = 0; up < 2; ++up) {
+          float x[32];
+#pragma unroll
+          for (int q = 0; q < 32; ++q) x[q] = t.acc[i][2 * up + q / 16][q % 16];
+          put(up, i, finite_amax(x));
+        }
+      barrier_lds();
+#pragma unroll
+      for (int i = 0; i < Cfg::RM; ++i) {
+        const int m = wm0 + 32 * i + (lane & 31);
+        const int sg = block_scale(0, m), su = block_scale(1, m);
+        const size_t row = (size_t)ti.row_base + m;
+        if (m < ti.mrows && live) {
+          uint8_t* h8 = a.H8 + row * (2 * n) + col;
+          store(i, 0, scale_inverse(sg), h8);
+          store(i, 2, scale_inverse(su), h8 + n);
+        }
+        if (h == 0 && wn == 0 && m < ti.mrows) {
+          uint8_t* hs = a.Hs + row * h8_stride(n) + b;
+          hs[0] = sg;
+          hs[nb] = su;
+        }
+      }
+    }
+    // A in the place of the gate columns
+#pragma unroll
+    for (int i = 0; i < Cfg::RM; ++i) {
+      float x[32];
+#pragma unroll
+      for (int q = 0; q < 32; ++q) {
+        float sg;
+        x[q] = silu_sig(t.acc[i][q / 16][q % 16], &sg) * t.acc[i][2 + q / 16][q % 16];
+        t.acc[i][q / 16][q % 16] = x[q];
+      }
+      put(2, i, finite_amax(x));
+    }
+    barrier_lds();
+#pragma unroll
+    for (int i = 0; i < Cfg::RM; ++i) {
+      const int m = wm0 + 32 * i + (lane & 31);
+      const int sa = block_scale(2, m);
+      const size_t row = (size_t)ti.row_base + m;
+      if (m < ti.mrows) store(i, 0, scale_inverse(sa), a.A8 + row * np + col);
+      if (h == 0 && wn == 0 && m < ti.mrows) a.As[row * q_stride(nb) + b] = sa;
+    }
+  }
+};
+
+template <class Cfg_>
+struct OpDown8 : F8Rows {
+  using Cfg = Cfg_;
+  static constexpr int W_SCALES = 1;
+  static_assert(Cfg::BN / Cfg::WN <= kQBlock, "a wave's columns lie in one block");
+  struct Params { QuantArgs a; };
+  static constexpr int EPI_LDS = 0;
+  static constexpr int EPI_STORES = kStoresPerFullTile<Cfg>;
+  static __device__ int count(const Params& p, int*) { return count_varlen_m<Cfg::BN>(p.a.mtiles, p.a.d); }
+  static __device__ int count_tail(const Params& p, const int*) { return count_varlen_m_tail<Cfg::BN>(p.a.mtiles, p.a.d); }
+  static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
+    return tile_varlen_m<Cfg::BM, Cfg::BN>(p.a.mtiles, p.a.E, p.a.d, q_pad(p.a.n) / 2, id, ti);
+  }
+  static __device__ void init_m(const Params& p, const TileInfo& ti, RowsSide<Cfg::BM, Cfg::BK, Cfg::NW>& s) {
+    s.init((const uint16_t*)p.a.A8, q_pad(p.a.n) / 2, nullptr, ti.row_base, ti.mrows);
+  }
+  static __device__ void init_n(const Params& p, const TileInfo& ti, RowsSide<Cfg::BN, Cfg::BK, Cfg::NW>& s) {
+    s.init((const uint16_t*)(p.a.W2q + (size_t)ti.e * w2q_bytes(p.a.d, p.a.n)), q_pad(p.a.n) / 2, nullptr, ti.n0, ti.ncols);
+  }
+  static __device__ const uint8_t* scale_row(const Params& p, const TileInfo& ti, int r, uint32_t) {
+    return p.a.As + (size_t)(ti.row_base + r) * q_stride(q_blocks(p.a.n));
+  }
+  static __device__ void weight_scales(const Params& p, const TileInfo& ti, int g, uint32_t (&ws)[1]) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nb = min(ti.n0 + Cfg::wave_n(wave) * (Cfg::BN / Cfg::WN), p.a.d - kQBlock) / kQBlock;
+    ws[0] = *(const SMOE_CONST uint32_t*)((const SMOE_CONST uint8_t*)p.a.W2s + (size_t)ti.e * w2s_bytes(p.a.d, p.a.n) +
+                                          (size_t)nb * q_stride(q_blocks(p.a.n)) + 4 * g);
+  }
+  static __device__ void epilogue(const Params& p, const TileInfo& ti, Acc<Cfg>& t, char* epi) {
+    if (p.a.b2) add_col_bias<Cfg>(t, p.a.b2 + (size_t)ti.e * p.a.d, ColOffset{ti.n0}, p.a.d);
+    store_rows_bf16_any<Cfg>(p.a.Y, p.a.d, ti.row_base, ti.mrows, ti.n0, ti.ncols, t, epi);
+  }
+};
+
 // ================================================================== dH
 // Epilogue (down-proj backward): with A recomputed from the cached H,
 // dS = <dA', A> (reduced over this tile's n columns), dA = s dA',
@@ -1859,6 +2034,13 @@ hipError_t launch_down_ablation(const DownArgs& a, int strategy, hipStream_t s) 
     return run<OpDown<C256x128, kAggAtomic>>({a}, g128, s);
   }
   return launch_down(a, s);
+}
+
+hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s) {
+  return run<OpUp8<C256x256w>>({a}, pad8(mtiles_bound(a.capacity, a.E, 256) * q_blocks(a.n)), s);
+}
+hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s) {
+  return run<OpDown8<C256x256w>>({a}, pad8(mtiles_bound(a.capacity, a.E, 256) * n_tiles(a.d, 256)), s);
 }
 
 int dh_n_tiles(int n, int64_t mt) { return n_tiles(n, tile_width(kTimesDH, mt, n)); }

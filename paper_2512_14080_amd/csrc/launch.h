@@ -222,14 +222,14 @@ struct QExpertsArgs {
 hipError_t launch_quantize_experts(const QExpertsArgs& a, hipStream_t s);
 hipError_t launch_dequantize_experts(const QExpertsArgs& a, hipStream_t s);
 
-// The 8-bit forward (gemm_fp8.hip): launch_quant_up writes A8, As (and H8, Hs where
+// The 8-bit projections: launch_quant_up writes A8, As (and H8, Hs where
 // given) from X8, Xs; launch_quant_down Y from A8, As.
 struct QuantArgs {
   const uint8_t* X8; const uint8_t* Xs;
   const uint8_t* W1q; const uint8_t* W1s; const uint8_t* W2q; const uint8_t* W2s;
-  const int32_t* offsets; const int32_t* row_token; const int32_t* row_expert; const int32_t* mtiles;
+  const int32_t* offsets; const int32_t* row_token; const int32_t* mtiles;
   const float* b1; const float* b2;
-  float* H32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
+  uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
   int d, n, E, capacity;
 };
 hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s);

@@ -200,7 +200,6 @@ size_t bwd_ckpt_layout(const moe_dims& m, int64_t cap, char* base, BwdWs* w, uin
 struct QuantWs {
   uint8_t* X8;
   uint8_t* Xs;
-  float* H32;
   uint8_t* A8;
   uint8_t* As;
   uint16_t* Y;
@@ -211,7 +210,6 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   size_t off = 0;
   off = carve(base, off, (size_t)m.T * m.d, w ? (void**)&w->X8 : nullptr);
   off = carve(base, off, (size_t)m.T * smoe::q_stride(m.d / smoe::kQBlock), w ? (void**)&w->Xs : nullptr);
-  off = carve(base, off, (size_t)cap * 2 * np * 4, w ? (void**)&w->H32 : nullptr);
   off = carve(base, off, (size_t)cap * np, w ? (void**)&w->A8 : nullptr);
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
   off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);
@@ -892,8 +890,8 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
   LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, X8, Xs, stream), "quantize X");
   HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
-  const smoe::QuantArgs a{X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, r->row_expert, w.mtiles,
-                          eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.H32, w.A8, w.As, c ? c->H : nullptr,
+  const smoe::QuantArgs a{X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles,
+                          eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A8, w.As, c ? c->H : nullptr,
                           c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity};
   LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
   LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
