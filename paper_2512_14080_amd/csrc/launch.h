@@ -225,15 +225,20 @@ hipError_t launch_dequantize_experts(const QExpertsArgs& a, hipStream_t s);
 // The 8-bit projections: launch_quant_up writes A8, As (and H8, Hs where
 // given) from X8, Xs; launch_quant_down Y from A8, As.
 struct QuantArgs {
-  const uint8_t* X8; const uint8_t* Xs;
+  const uint16_t* X; const uint8_t* X8; const uint8_t* Xs;
   const uint8_t* W1q; const uint8_t* W1s; const uint8_t* W2q; const uint8_t* W2s;
   const int32_t* offsets; const int32_t* row_token; const int32_t* mtiles;
   const float* b1; const float* b2;
-  uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
+  float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
   int d, n, E, capacity;
 };
 hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s);
 hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s);
+// The same for few rows per expert, from X in bf16 (stream_gemm.hip); stream8_shape:
+// mb = 0 where the tiled ones are the better ones
+StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile);
+hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s);    // writes A32
+hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s);  // from A32
 
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);

@@ -196,10 +196,13 @@ size_t bwd_ckpt_layout(const moe_dims& m, int64_t cap, char* base, BwdWs* w, uin
   return off;
 }
 
-// moe_fwd_quant: X and A in 8-bit blocks (X's in the checkpoint where it is kept)
+// moe_fwd_quant: X and A in 8-bit blocks (X's in the checkpoint where it is kept), or
+// A in fp32 where the streaming projections may run (a rounding's m_tile only makes
+// that rarer)
 struct QuantWs {
   uint8_t* X8;
   uint8_t* Xs;
+  float* A32;
   uint8_t* A8;
   uint8_t* As;
   uint16_t* Y;
@@ -210,6 +213,7 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   size_t off = 0;
   off = carve(base, off, (size_t)m.T * m.d, w ? (void**)&w->X8 : nullptr);
   off = carve(base, off, (size_t)m.T * smoe::q_stride(m.d / smoe::kQBlock), w ? (void**)&w->Xs : nullptr);
+  off = carve(base, off, smoe::stream8_shape(m, (int)cap, 0).mb ? (size_t)cap * m.n * 4 : 0, w ? (void**)&w->A32 : nullptr);
   off = carve(base, off, (size_t)cap * np, w ? (void**)&w->A8 : nullptr);
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
   off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);
@@ -888,13 +892,20 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   if (c) c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
   uint8_t* X8 = c && c->X ? c->X : w.X8;
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
-  LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, X8, Xs, stream), "quantize X");
-  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
-  const smoe::QuantArgs a{X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles,
-                          eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A8, w.As, c ? c->H : nullptr,
+  const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles,
+                          eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A32, w.A8, w.As, c ? c->H : nullptr,
                           c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity};
-  LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
-  LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
+  // (what is kept is written by the tiled projections)
+  const smoe::StreamShape few = c ? smoe::StreamShape{0, 0} : smoe::stream8_shape(m, r->capacity, smoe::rounding_tile(*r));
+  if (few.mb) {
+    LAUNCH(MOE_KC_UP_QUANT, smoe::launch_stream8_up(a, few, stream), "8-bit up-proj");
+    LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_stream8_down(a, few, stream), "8-bit down-proj");
+  } else {
+    LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, X8, Xs, stream), "quantize X");
+    HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
+    LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
+    LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
+  }
   LAUNCH(MOE_KC_AGG_O, smoe::launch_agg_o(w.Y, *r, O, m.T, m.d, stream), "aggregation");
   if (c) c->state = MOE_HELD_WRITTEN;
   return MOE_OK;

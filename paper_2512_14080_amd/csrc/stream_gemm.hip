@@ -23,7 +23,7 @@
 //     added in wave order by the epilogue.
 #include <algorithm>
 
-#include "device_common.h"
+#include "fp8_block.h"
 #include "launch.h"
 
 namespace smoe {
@@ -410,6 +410,252 @@ hipError_t launch_router_part(const uint16_t* X, const uint16_t* Wr, float* part
   const int mb = router_row_blocks(T, E, &groups);
   const dim3 grid((E + kStreamCols - 1) / kStreamCols, slices, groups);
   return run_stream<StreamRouter>({X, Wr, part, T, d, E, slice}, grid, mb, slice, s);
+}
+
+// ---------------------------------------------------------------- 8-bit weights
+// The same for the 8-bit forward.  MFMA 16x16x128 takes one block of 128 k at a time,
+// so a wave's step is one block, with one scale byte of the weights and one of the
+// row.  A workgroup computes 64 weight columns (8 KB of codes a step and wave); lane l
+// loads, of weight column l % 16, the codes of k 16 (l / 16) + [0, 16) and the same 64
+// further on: whole 64-byte runs of k per instruction.  The rows are quantised as they
+// are loaded (each block by one wave of the workgroup, its largest |x| a maximum over
+// the four lanes that share the row), so neither X nor A needs a launch or a buffer of
+// codes of its own; A passes between the two products in fp32.  D = W x X: a lane ends
+// with four consecutive columns of one row.
+typedef int i32x8s __attribute__((ext_vector_type(8)));
+constexpr int kStream8Cols = 64;
+typedef f32x4 Stream8Part[16][kStream8Cols / 4 + 1];  // one wave's 16 x 64 partial (padded rows)
+
+// the largest of the lanes l % 16 + {0, 16, 32, 48}
+__device__ __forceinline__ uint32_t max_of_row(uint32_t m) {
+  m = max(m, (uint32_t)__shfl_xor((int)m, 16, kWave));
+  return max(m, (uint32_t)__shfl_xor((int)m, 32, kWave));
+}
+
+// A lane's 32 values of a row's block of 128, from bf16 (4 x 8) or fp32 (8 x 4), and
+// their codes and scale byte
+template <bool F32>
+struct RowBlock8 {
+  static constexpr int N = F32 ? 8 : 4;
+  u32x4 v[N];
+  // x: the row; k: 16 g of the block's first k; valid: whether the block's second half exists
+  __device__ __forceinline__ void load(const void* x, uint32_t k, bool second) {
+    const char* p = (const char*)x + (size_t)k * (F32 ? 4 : 2);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool hi = i >= N / 2;
+      v[i] = !hi || second ? *(const u32x4*)(p + (hi ? 64 * (F32 ? 4 : 2) : 0) + 16 * (i % (N / 2))) : u32x4{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ float value(int i) const {  // of 32
+    if constexpr (F32) return __uint_as_float(v[i / 4][i % 4]);
+    return i & 1 ? bf_hi(v[i / 8][i / 2 % 4]) : bf_lo(v[i / 8][i / 2 % 4]);
+  }
+  __device__ __forceinline__ i32x8s codes(int* scale) const {
+    float a[32], m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      a[i] = value(i);
+      m = fmaxf(m, fabsf(a[i]));  // (passes over NaN)
+    }
+    if (__any(m == INFINITY)) {
+      m = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) m = fmaxf(m, finite_abs(a[i]));
+    }
+    const int b = scale_byte(max_of_row(__float_as_uint(m)));
+    const float inv = scale_inverse(b);
+    i32x8s q;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      q[i] = (int)pack_fp8x4(a[4 * i] * inv, a[4 * i + 1] * inv, a[4 * i + 2] * inv, a[4 * i + 3] * inv);
+    *scale = b;
+    return q;
+  }
+};
+
+// grid: as stream_gemm_kernel's of the experts.  Op supplies
+//   F32: whether rows come in fp32 (else bf16),
+//   int blocks(p), k(p): blocks of the reduction, and its length,
+//   const void* row(p, r), const uint8_t* w(p, e), const uint8_t* ws(p, e, tile, half),
+//   uint32_t w_row(p, tile, c): offset of weight column c of the tile,
+//   finish(p, e, tile, row0, rows, part)
+template <class Op, int MB, int KW, int NBUF, int OCC>
+__global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantArgs p) {
+  __shared__ Stream8Part part[KW];
+  const int tile = blockIdx.x;
+  int e = blockIdx.y, m0 = 0;
+  if (e >= p.E && !find_group<64 * KW>(p.offsets, p.E, 16 * MB, e - p.E, (int*)part, &e, &m0)) return;
+  const int off = p.offsets[e], cnt = p.offsets[e + 1] - off;
+  if (m0 >= cnt) return;
+  const int lane = lane_id(), g = lane >> 4, l = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int ns = (Op::blocks(p) - wave + KW - 1) / KW;  // this wave's steps
+  const uint8_t* wbase = Op::w(p, e);
+  const uint8_t* ws0 = Op::ws(p, e, tile, 0);
+  const uint8_t* ws1 = Op::ws(p, e, tile, 1);
+  uint32_t wrow[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) wrow[j] = Op::w_row(p, tile, 16 * j + l) + 16 * g;
+  const void* xp[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) xp[b] = Op::row(p, off + min(m0 + 16 * b + l, cnt - 1));
+  f32x4 acc[MB][4];
+#pragma unroll
+  for (int b = 0; b < MB; ++b)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  u32x4 wv[NBUF][4][2];
+  int sv[NBUF][2];
+  RowBlock8<Op::F32> xv[NBUF][MB];
+  // step s of this wave; a step past the end reads the step 0 addresses (cached, unused)
+  auto load = [&](int buf, int s) {
+    const uint32_t kb = s < ns ? wave + KW * s : wave, k = kQBlock * kb;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      wv[buf][j][0] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k));
+      wv[buf][j][1] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k + 64));
+    }
+    sv[buf][0] = ws0[kb];
+    sv[buf][1] = ws1[kb];
+#pragma unroll
+    for (int b = 0; b < MB; ++b) xv[buf][b].load(xp[b], k + 16 * g, (int)k + 64 < Op::k(p));
+  };
+  if (ns > 0) {
+#pragma unroll
+    for (int q = 0; q < NBUF; ++q) load(q, q);
+    for (int s = 0;; s += NBUF) {
+#pragma unroll
+      for (int q = 0; q < NBUF; ++q) {
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+          int xs;
+          const i32x8s x = xv[q][b].codes(&xs);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const u32x4 lo = wv[q][j][0], hi = wv[q][j][1];
+            const i32x8s w = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+            acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[b][j], 0, 0, 0, sv[q][j >> 1], 0, xs);
+          }
+        }
+        if (s + q + 1 >= ns) goto done;
+        load(q, s + q + NBUF);
+      }
+    }
+  done:;
+  }
+#pragma unroll
+  for (int b = 0; b < MB; ++b) {
+    if (m0 + 16 * b >= cnt) break;
+    __syncthreads();  // the previous rows' sums have been read
+#pragma unroll
+    for (int j = 0; j < 4; ++j) part[wave][l][4 * j + g] = acc[b][j];
+    __syncthreads();
+    Op::template finish<KW>(p, e, tile, off + m0 + 16 * b, min(16, cnt - m0 - 16 * b), part);
+  }
+}
+
+// the sum over the waves of columns 4 c4 .. 4 c4 + 3 of the tile
+template <int KW>
+__device__ __forceinline__ f32x4 stream8_sum(const Stream8Part* part, int row, int c4) {
+  f32x4 s = part[0][row][c4];
+#pragma unroll
+  for (int w = 1; w < KW; ++w)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s[q] += part[w][row][c4][q];
+  return s;
+}
+
+// 32 gate columns and the matching up columns; A in fp32
+struct Stream8Up {
+  static constexpr bool F32 = false;
+  static __device__ int blocks(const QuantArgs& p) { return p.d / kQBlock; }
+  static __device__ int k(const QuantArgs& p) { return p.d; }
+  static __device__ const void* row(const QuantArgs& p, int r) { return p.X + (size_t)p.row_token[r] * p.d; }
+  static __device__ const uint8_t* w(const QuantArgs& p, int e) { return p.W1q + (size_t)e * w1q_bytes(p.d, p.n); }
+  static __device__ const uint8_t* ws(const QuantArgs& p, int e, int tile, int half) {
+    return p.W1s + (size_t)e * w1s_bytes(p.d, p.n) + (size_t)(2 * (tile / 4) + half) * q_stride(p.d / kQBlock);
+  }
+  static __device__ uint32_t w_row(const QuantArgs& p, int tile, int c) {
+    return (uint32_t)(256 * (tile / 4) + w1q_row(32 * (tile % 4) + (c & 31), c >> 5)) * p.d;
+  }
+  template <int KW>
+  static __device__ void finish(const QuantArgs& p, int e, int tile, int row0, int rows, const Stream8Part* part) {
+    for (int i = threadIdx.x; i < 128; i += 64 * KW) {
+      const int row = i >> 3, c4 = i & 7;
+      if (row >= rows) break;
+      f32x4 hg = stream8_sum<KW>(part, row, c4), hu = stream8_sum<KW>(part, row, c4 + 8), a;
+      const int c = 32 * tile + 4 * c4;
+      const float* b1 = p.b1 ? p.b1 + (size_t)e * 2 * p.n + c : nullptr;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (b1) {
+          hg[q] += b1[q];
+          hu[q] += b1[p.n + q];
+        }
+        float sg;
+        a[q] = silu_sig(hg[q], &sg) * hu[q];
+      }
+      *(f32x4*)(p.A32 + (size_t)(row0 + row) * p.n + c) = a;
+    }
+  }
+};
+
+struct Stream8Down {
+  static constexpr bool F32 = true;
+  static __device__ int blocks(const QuantArgs& p) { return q_blocks(p.n); }
+  static __device__ int k(const QuantArgs& p) { return p.n; }
+  static __device__ const void* row(const QuantArgs& p, int r) { return p.A32 + (size_t)r * p.n; }
+  static __device__ const uint8_t* w(const QuantArgs& p, int e) { return p.W2q + (size_t)e * w2q_bytes(p.d, p.n); }
+  static __device__ const uint8_t* ws(const QuantArgs& p, int e, int tile, int) {
+    return p.W2s + (size_t)e * w2s_bytes(p.d, p.n) + (size_t)(tile / 2) * q_stride(q_blocks(p.n));
+  }
+  static __device__ uint32_t w_row(const QuantArgs& p, int tile, int c) { return (uint32_t)(64 * tile + c) * q_pad(p.n); }
+  template <int KW>
+  static __device__ void finish(const QuantArgs& p, int e, int tile, int row0, int rows, const Stream8Part* part) {
+    for (int i = threadIdx.x; i < 256; i += 64 * KW) {
+      const int row = i >> 4, c4 = i & 15;
+      if (row >= rows) break;
+      f32x4 y = stream8_sum<KW>(part, row, c4);
+      const int c = 64 * tile + 4 * c4;
+      if (p.b2) {
+        const f32x4 b = *(const f32x4*)(p.b2 + (size_t)e * p.d + c);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] += b[q];
+      }
+      *(u32x2*)(p.Y + (size_t)(row0 + row) * p.d + c) = pack_bf16x4(y[0], y[1], y[2], y[3]);
+    }
+  }
+};
+
+template <class Op>
+static hipError_t run_stream8(const QuantArgs& p, dim3 grid, int mb, int blocks, hipStream_t s) {
+  if (mb == 1 && blocks > 4)
+    stream8_gemm_kernel<Op, 1, 8, 2, 2><<<grid, dim3(512), 0, s>>>(p);
+  else if (mb == 1 && blocks > 2)
+    stream8_gemm_kernel<Op, 1, 4, 1, 4><<<grid, dim3(256), 0, s>>>(p);
+  else if (mb == 1)
+    stream8_gemm_kernel<Op, 1, 2, 1, 4><<<grid, dim3(128), 0, s>>>(p);
+  else if (mb == 2 && blocks > 4)
+    stream8_gemm_kernel<Op, 2, 8, 1, 2><<<grid, dim3(512), 0, s>>>(p);
+  else if (mb == 2)
+    stream8_gemm_kernel<Op, 2, 2, 1, 3><<<grid, dim3(128), 0, s>>>(p);
+  else
+    stream8_gemm_kernel<Op, 4, 4, 1, 2><<<grid, dim3(256), 0, s>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
+  return run_stream8<Stream8Up>(a, stream_grid(a.n / 32, a.E, t), t.mb, a.d / kQBlock, s);
+}
+hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
+  return run_stream8<Stream8Down>(a, stream_grid(a.d / kStream8Cols, a.E, t), t.mb, q_blocks(a.n), s);
+}
+
+// up's tiles decide for both, since A passes between the two in one of two forms
+StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile) {
+  if (2 * (int64_t)m.d * q_pad(m.n) > INT32_MAX) return {0, 0};  // 32-bit offsets within an expert's codes
+  return stream_shape(m, capacity, m_tile, q_blocks(m.n));
 }
 
 }  // namespace smoe

@@ -230,20 +230,32 @@ def test_held_layers_full_rows_per_expert():
     check_held(W.MoEConfig("long", T=5000, d=128, n=64, E=8, K=4, m_tile=128), "quant", 5, "nearest", True)
 
 
-def test_forward_without_a_checkpoint():
-    """The same O, and the checkpoint's bytes untouched."""
+FORWARD = SHAPES + [
+    W.MoEConfig("t10", T=10, d=896, n=320, E=8, K=8, m_tile=16),        # one row block of 10 rows, K = E
+    W.MoEConfig("t16", T=16, d=768, n=256, E=8, K=8, m_tile=16),        # its last size
+    W.MoEConfig("t17", T=17, d=768, n=256, E=8, K=8, m_tile=16),        # two row blocks
+    W.MoEConfig("m20", T=20, d=256, n=128, E=16, K=16, m_tile=16),      # two at their largest mean
+    W.MoEConfig("m21", T=21, d=256, n=128, E=16, K=16, m_tile=16),      # four
+    W.MoEConfig("t128", T=128, d=640, n=192, E=8, K=4, m_tile=16),      # rows past one group of four
+    W.MoEConfig("t150", T=150, d=256, n=64, E=120, K=8, m_tile=16, zipf_s=1.5),   # hot experts of many groups
+    W.MoEConfig("t140", T=140, d=640, n=192, E=24, K=8, m_tile=16, zipf_s=3.0),
+    W.MoEConfig("t5", T=5, d=1280, n=1152, E=8, K=3, m_tile=16),        # nine blocks of n, ten of d, on eight waves
+]
+
+
+@pytest.mark.parametrize("cfg", FORWARD, ids=lambda c: c.name)
+@pytest.mark.parametrize("biased", [False, True])
+def test_forward_without_a_checkpoint(cfg, biased):
     torch = _torch()
     from paper_2512_14080_amd import binding as B
-    cfg = SHAPES[3]
-    _, _, layer, _, _ = _layer(cfg, "quant")
+    inp, R, layer, b1, b2 = _layer(cfg, "quant", seed=10, biased=biased)
     layer.route()
-    layer.forward()
-    O = layer.O.clone()
-    layer.ckpt.buf.fill_(0xAB)
-    layer.O.zero_()
-    B.moe_fwd_quant(layer.D, layer.X, layer.qw, layer.routing, None, layer.O, layer.ws_f)
+    B.moe_quantize_experts(layer.D, layer.W1, layer.W2, layer.qw)
+    layer.ws_f.fill_(0xFF)  # NaN in every type: nothing unwritten is used
+    B.moe_fwd_quant(layer.D, layer.X, layer.qw, layer.routing, None, layer.O, layer.ws_f, eb=layer.eb)
     torch.cuda.synchronize()
-    assert rel_err(layer.O.float().cpu().numpy(), O.float().cpu().numpy()) <= TOL
+    fw = block8.forward_quant(inp.f32("X"), inp.f32("W1"), inp.f32("W2"), R, b1, b2)
+    _check_o(layer.O.double().cpu().numpy(), fw, R, fw["W2q"], True)
     assert (layer.ckpt.buf == 0xAB).all()
 
 
@@ -252,6 +264,7 @@ def test_forward_without_a_checkpoint():
 def test_one_broken_token_stays_one(bad, T):
     """A value that is not finite reaches its own token's output only."""
     torch = _torch()
+    from paper_2512_14080_amd import binding as B
 
     def edit(inp):
         inp.X[5, 17] = W.bf16_bits_from_f32(np.array([1.0], np.float32))[0]  # (the scores are the sound token's)
@@ -259,14 +272,19 @@ def test_one_broken_token_stays_one(bad, T):
     cfg = W.MoEConfig("broken", T=T, d=256, n=128, E=16, K=2, m_tile=16)
     inp, R, layer, _, _ = _layer(cfg, "quant", seed=6, edit=edit)
     layer.route()
-    layer.forward()
-    want = layer.O.clone()
-    layer.X[5, 17] = float(bad)
-    layer.forward()
-    torch.cuda.synchronize()
+    sound = layer.X.clone()
     keep = torch.arange(T, device="cuda") != 5
-    assert torch.isnan(layer.O[5]).any()
-    assert torch.equal(layer.O[keep], want[keep])
+    for ckpt in (layer.ckpt, None):
+        out = []
+        for value in (1.0, float(bad)):
+            layer.X.copy_(sound)
+            layer.X[5, 17] = value
+            B.moe_quantize_experts(layer.D, layer.W1, layer.W2, layer.qw)
+            B.moe_fwd_quant(layer.D, layer.X, layer.qw, layer.routing, ckpt, layer.O, layer.ws_f)
+            torch.cuda.synchronize()
+            out.append(layer.O.clone())
+        assert torch.isnan(out[1][5]).any()
+        assert torch.equal(out[1][keep], out[0][keep])
 
 
 def test_steps_in_a_graph_and_on_another_stream():
