@@ -41,22 +41,63 @@ __host__ __device__ inline int h8_stride(int n) { return q_stride(2 * q_blocks(n
 // and one more where its fraction is above 1.75
 __device__ __forceinline__ int scale_byte(uint32_t amax_bits) { return max((int)((amax_bits + 0x1FFFFFu) >> 23) - 8, 1); }
 __device__ __forceinline__ float scale_value(int b) { return __uint_as_float((uint32_t)b << 23); }
-__device__ __forceinline__ float scale_inverse(int b) { return __uint_as_float((uint32_t)(254 - b) << 23); }
 
-// four values (|x| <= 448, or not finite) -> four codes
-__device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d) {
-  const int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+// The scaled conversions divide or multiply by the scale as they convert: for every
+// scale byte, the codes of x * 2^-e and the values of code * 2^e, bit for bit.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+// four values (|x| <= 448 * scale, or not finite) -> four codes
+__device__ __forceinline__ uint32_t pack_fp8x4(float a, float b, float c, float d, float scale) {
+  const i16x2 v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(i16x2{0, 0}, a, b, scale, false);
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, c, d, scale, true));
+}
+// the same from two bf16 pairs
+__device__ __forceinline__ uint32_t pack_fp8x4_bf16(uint32_t ab, uint32_t cd, float scale) {
+  const i16x2 v = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(i16x2{0, 0}, __builtin_bit_cast(bf16x2v, ab), scale, false);
+  return __builtin_bit_cast(uint32_t,
+                            __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(v, __builtin_bit_cast(bf16x2v, cd), scale, true));
 }
 // four codes -> four values
-__device__ __forceinline__ f32x4 unpack_fp8x4(uint32_t v) {
-  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, true);
+__device__ __forceinline__ f32x4 unpack_fp8x4(uint32_t v, float scale) {
+  const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, scale, false);
+  const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, scale, true);
   return f32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+// the largest |x| of N bf16 pairs, finite ones only, as bf16 bits
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <int N>
+__device__ __forceinline__ uint32_t finite_amax_bf16(const uint32_t (&w)[N]) {
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+  uint32_t a = max((uint32_t)m[0], (uint32_t)m[1]);
+  if (__builtin_expect(__any(a >= 0x7F80u), 0)) {
+    a = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t lo = w[i] & 0x7FFFu, hi = w[i] >> 16 & 0x7FFFu;
+      a = max(a, max(lo < 0x7F80u ? lo : 0u, hi < 0x7F80u ? hi : 0u));
+    }
+  }
+  return a;
 }
 // |x|, 0 for what is not finite
 __device__ __forceinline__ float finite_abs(float x) {
   const float a = fabsf(x);
   return a < INFINITY ? a : 0.f;
+}
+
+// the largest |x| of N fp32 values, finite ones only
+template <int N>
+__device__ __forceinline__ float finite_amax(const float (&x)[N]) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]));  // (passes over NaN)
+  if (__builtin_expect(__any(m == INFINITY), 0)) {
+    m = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, finite_abs(x[i]));
+  }
+  return m;
 }
 
 }  // namespace smoe

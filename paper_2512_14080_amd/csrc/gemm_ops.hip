@@ -1104,20 +1104,6 @@ struct OpUp {
   }
 };
 
-// The largest finite |x| of N values per lane
-template <int N>
-__device__ __forceinline__ float finite_amax(const float (&x)[N]) {
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) m = fmaxf(m, fabsf(x[i]));  // (passes over NaN)
-  if (__builtin_expect(__any(m == INFINITY), 0)) {
-    m = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, finite_abs(x[i]));
-  }
-  return m;
-}
-
 // Up-projection whose H is kept in 8-bit blocks: A leaves as in OpUp, H as codes and
 // scale bytes, both from the fp32 accumulators.  The 128 gate (or up) columns of a
 // tile are one block: each of the two waves of a row group holds 64 of them, so the
@@ -1167,7 +1153,7 @@ struct OpUpCkpt : OpUp<Cfg_, PLAIN> {
 #pragma unroll
       for (int up = 0; up < 2; ++up)
         sb[up] = scale_byte(__float_as_uint(fmaxf(amax[up * 2 * Cfg::BM + m], amax[(up * 2 + 1) * Cfg::BM + m])));
-      const float ig = scale_inverse(sb[0]), iu = scale_inverse(sb[1]);
+      const float vg = scale_value(sb[0]), vu = scale_value(sb[1]);
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         u32x2 ha[4];
@@ -1183,8 +1169,8 @@ struct OpUpCkpt : OpUp<Cfg_, PLAIN> {
             av[r] = silu_sig(gv[r], &sg) * uv[r];
           }
           ha[g] = pack_bf16x4(av[0], av[1], av[2], av[3]);
-          cg[g] = pack_fp8x4(gv[0] * ig, gv[1] * ig, gv[2] * ig, gv[3] * ig);
-          cu[g] = pack_fp8x4(uv[0] * iu, uv[1] * iu, uv[2] * iu, uv[3] * iu);
+          cg[g] = pack_fp8x4(gv[0], gv[1], gv[2], gv[3], vg);
+          cu[g] = pack_fp8x4(uv[0], uv[1], uv[2], uv[3], vu);
         }
         stage_block32(st, q, ha);
         const u32x4 xg = swap_block_fp8(cg[0], cg[1], cg[2], cg[3]), xu = swap_block_fp8(cu[0], cu[1], cu[2], cu[3]);
@@ -1397,14 +1383,14 @@ struct OpUp8 : F8Rows {
     };
     // the 64 codes of this wave and row block i, accumulator columns j0 .. j0 + 1 (both
     // lanes of a row are in a branch on it, so the swaps find their partners)
-    auto store = [&](int i, int j0, float inv, uint8_t* row) {
+    auto store = [&](int i, int j0, float scale, uint8_t* row) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         uint32_t v[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const auto& x = t.acc[i][j0 + q];
-          v[g] = pack_fp8x4(x[4 * g] * inv, x[4 * g + 1] * inv, x[4 * g + 2] * inv, x[4 * g + 3] * inv);
+          v[g] = pack_fp8x4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3], scale);
         }
         *(u32x4*)(row + 32 * q + 16 * h) = swap_block_fp8(v[0], v[1], v[2], v[3]);
       }
@@ -1440,8 +1426,8 @@ struct OpUp8 : F8Rows {
         const size_t row = (size_t)ti.row_base + m;
         if (m < ti.mrows && live) {
           uint8_t* h8 = a.H8 + row * (2 * n) + col;
-          store(i, 0, scale_inverse(sg), h8);
-          store(i, 2, scale_inverse(su), h8 + n);
+          store(i, 0, scale_value(sg), h8);
+          store(i, 2, scale_value(su), h8 + n);
         }
         if (h == 0 && wn == 0 && m < ti.mrows) {
           uint8_t* hs = a.Hs + row * h8_stride(n) + b;
@@ -1468,7 +1454,7 @@ struct OpUp8 : F8Rows {
       const int m = wm0 + 32 * i + (lane & 31);
       const int sa = block_scale(2, m);
       const size_t row = (size_t)ti.row_base + m;
-      if (m < ti.mrows) store(i, 0, scale_inverse(sa), a.A8 + row * np + col);
+      if (m < ti.mrows) store(i, 0, scale_value(sa), a.A8 + row * np + col);
       if (h == 0 && wn == 0 && m < ti.mrows) a.As[row * q_stride(nb) + b] = sa;
     }
   }
@@ -1600,13 +1586,8 @@ struct OpDH {
         unswap_block_fp8(qu[b], u8);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          gv[g] = unpack_fp8x4(g8[g]);
-          uv[g] = unpack_fp8x4(u8[g]);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            gv[g][r] *= qs[blk / RN][0];
-            uv[g][r] *= qs[blk / RN][1];
-          }
+          gv[g] = unpack_fp8x4(g8[g], qs[blk / RN][0]);
+          uv[g] = unpack_fp8x4(u8[g], qs[blk / RN][1]);
         }
       } else {
 #pragma unroll

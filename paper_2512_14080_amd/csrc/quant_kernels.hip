@@ -7,12 +7,6 @@ namespace smoe {
 
 constexpr int kRowThreads = 256;
 
-// bf16 pairs: the larger |x| of finite halves as bf16 bits in each half
-__device__ __forceinline__ uint32_t finite_abs_bits(uint32_t h) {
-  h &= 0x7FFFu;
-  return h < 0x7F80u ? h : 0u;
-}
-
 // ---------------------------------------------------------------- rows
 // 16 lanes per block of 128 columns, 8 columns (16 bytes) each: the largest |x| of
 // the block is a maximum over the lane's values and the 16 lanes.
@@ -24,17 +18,13 @@ __global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const uint16
   const int row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
   u32x4 v = {0, 0, 0, 0};
   if (c < cols) v = *(const u32x4*)(X + (size_t)row * cols + c);
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) m = max(m, max(finite_abs_bits(v[i]), finite_abs_bits(v[i] >> 16)));
+  const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+  uint32_t m = finite_amax_bf16(w);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 16));
   const int sb = scale_byte(m << 16);
-  const float inv = scale_inverse(sb);
-  u32x2 out;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    out[i] = pack_fp8x4(bf_lo(v[2 * i]) * inv, bf_hi(v[2 * i]) * inv, bf_lo(v[2 * i + 1]) * inv, bf_hi(v[2 * i + 1]) * inv);
+  const float sv = scale_value(sb);
+  const u32x2 out = {pack_fp8x4_bf16(v[0], v[1], sv), pack_fp8x4_bf16(v[2], v[3], sv)};
   if (c < cols) *(u32x2*)(q + (size_t)row * cols + c) = out;
   // (the last block's first lanes also fill the row's scales to a whole dword)
   if (l == 0 || (b == blocks - 1 && b + l < stride)) scale[(size_t)row * stride + b + l] = l ? 127 : sb;
@@ -53,9 +43,9 @@ __global__ __launch_bounds__(kRowThreads) void dequantize_rows_kernel(const uint
   u32x4 out;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const f32x4 x = unpack_fp8x4(v[i]);
-    out[2 * i] = pack_bf2(x[0] * s, x[1] * s);
-    out[2 * i + 1] = pack_bf2(x[2] * s, x[3] * s);
+    const f32x4 x = unpack_fp8x4(v[i], s);
+    out[2 * i] = pack_bf2(x[0], x[1]);
+    out[2 * i + 1] = pack_bf2(x[2], x[3]);
   }
   *(u32x4*)(X + (size_t)row * cols + c) = out;
 }
@@ -148,22 +138,23 @@ __global__ __launch_bounds__(256) void quantize_experts_kernel(const QExpertsArg
     v[i] = u32x4{0, 0, 0, 0};
     if (c < cols && k + i < ks) v[i] = *(const u32x4*)(src + (size_t)(k + i) * ld + c);
   }
-  uint32_t m = 0;
+  uint32_t words[32];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = max(m, max(finite_abs_bits(v[i][j]), finite_abs_bits(v[i][j] >> 16)));
+  for (int i = 0; i < 32; ++i) words[i] = v[i / 4][i % 4];
+  uint32_t m = finite_amax_bf16(words);
   m = dpp_reduce(m, [](uint32_t x, uint32_t y) { return max(x, y); });
   if (lane_id() == 0) wmax[threadIdx.x >> 6] = m;
   __syncthreads();
   const int sb = scale_byte(max(max(wmax[0], wmax[1]), max(wmax[2], wmax[3])) << 16);
-  const float inv = scale_inverse(sb);
+  const float sv = scale_value(sb);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float x[8];
+    // column c + j of eight rows as bf16 pairs
+    uint32_t x[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = (j & 1 ? bf_hi(v[i][j >> 1]) : bf_lo(v[i][j >> 1])) * inv;
-    *(u32x2*)(tile + (c + j) * kPitch + k) = u32x2{pack_fp8x4(x[0], x[1], x[2], x[3]), pack_fp8x4(x[4], x[5], x[6], x[7])};
+    for (int i = 0; i < 4; ++i)
+      x[i] = __builtin_amdgcn_perm(v[2 * i + 1][j >> 1], v[2 * i][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+    *(u32x2*)(tile + (c + j) * kPitch + k) = u32x2{pack_fp8x4_bf16(x[0], x[1], sv), pack_fp8x4_bf16(x[2], x[3], sv)};
   }
   __syncthreads();
   uint8_t* q = w.w1 ? a.W1q : a.W2q;
@@ -198,16 +189,15 @@ __global__ __launch_bounds__(256) void dequantize_experts_kernel(const QExpertsA
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const u32x2 v = *(const u32x2*)(tile + (c + j) * kPitch + k);
-    lo[j] = unpack_fp8x4(v[0]);
-    hi[j] = unpack_fp8x4(v[1]);
+    lo[j] = unpack_fp8x4(v[0], s);
+    hi[j] = unpack_fp8x4(v[1], s);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     u32x4 o;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      o[j] = i < 4 ? pack_bf2(lo[2 * j][i & 3] * s, lo[2 * j + 1][i & 3] * s)
-                   : pack_bf2(hi[2 * j][i & 3] * s, hi[2 * j + 1][i & 3] * s);
+      o[j] = i < 4 ? pack_bf2(lo[2 * j][i & 3], lo[2 * j + 1][i & 3]) : pack_bf2(hi[2 * j][i & 3], hi[2 * j + 1][i & 3]);
     *(u32x4*)(dst + (size_t)(k + i) * ld + c) = o;
   }
 }

@@ -421,10 +421,12 @@ hipError_t launch_router_part(const uint16_t* X, const uint16_t* Wr, float* part
 // are loaded (each block by one wave of the workgroup, its largest |x| a maximum over
 // the four lanes that share the row), so neither X nor A needs a launch or a buffer of
 // codes of its own; A passes between the two products in fp32.  D = W x X: a lane ends
-// with four consecutive columns of one row.
+// with four consecutive columns of one row.  What keeps loads in flight is many waves,
+// each with one step's: two steps in flight per wave cost registers, and with them
+// waves (d = 4096, n = 512, E = 128, 256 tokens: up 127 -> 117 us, down 113 -> 73).
 typedef int i32x8s __attribute__((ext_vector_type(8)));
-constexpr int kStream8Cols = 64;
-typedef f32x4 Stream8Part[16][kStream8Cols / 4 + 1];  // one wave's 16 x 64 partial (padded rows)
+template <int NJ>
+using Stream8Part = f32x4[16][4 * NJ + 1];  // one wave's 16 x 16 NJ partial (padded rows)
 
 // the largest of the lanes l % 16 + {0, 16, 32, 48}
 __device__ __forceinline__ uint32_t max_of_row(uint32_t m) {
@@ -447,29 +449,31 @@ struct RowBlock8 {
       v[i] = !hi || second ? *(const u32x4*)(p + (hi ? 64 * (F32 ? 4 : 2) : 0) + 16 * (i % (N / 2))) : u32x4{0, 0, 0, 0};
     }
   }
-  __device__ __forceinline__ float value(int i) const {  // of 32
-    if constexpr (F32) return __uint_as_float(v[i / 4][i % 4]);
-    return i & 1 ? bf_hi(v[i / 8][i / 2 % 4]) : bf_lo(v[i / 8][i / 2 % 4]);
-  }
   __device__ __forceinline__ i32x8s codes(int* scale) const {
-    float a[32], m = 0.f;
+    uint32_t m;
+    if constexpr (F32) {
+      float a[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      a[i] = value(i);
-      m = fmaxf(m, fabsf(a[i]));  // (passes over NaN)
-    }
-    if (__any(m == INFINITY)) {
-      m = 0.f;
+      for (int i = 0; i < 32; ++i) a[i] = __uint_as_float(v[i / 4][i % 4]);
+      m = __float_as_uint(finite_amax(a));
+    } else {
+      uint32_t w[16];
 #pragma unroll
-      for (int i = 0; i < 32; ++i) m = fmaxf(m, finite_abs(a[i]));
+      for (int i = 0; i < 16; ++i) w[i] = v[i / 4][i % 4];
+      m = finite_amax_bf16(w) << 16;
     }
-    const int b = scale_byte(max_of_row(__float_as_uint(m)));
-    const float inv = scale_inverse(b);
+    *scale = scale_byte(max_of_row(m));
+    const float sv = scale_value(*scale);
     i32x8s q;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      q[i] = (int)pack_fp8x4(a[4 * i] * inv, a[4 * i + 1] * inv, a[4 * i + 2] * inv, a[4 * i + 3] * inv);
-    *scale = b;
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (F32) {
+        const u32x4 x = v[i];
+        q[i] = (int)pack_fp8x4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3]), sv);
+      } else {
+        q[i] = (int)pack_fp8x4_bf16(v[i / 2][2 * (i & 1)], v[i / 2][2 * (i & 1) + 1], sv);
+      }
+    }
     return q;
   }
 };
@@ -480,9 +484,10 @@ struct RowBlock8 {
 //   const void* row(p, r), const uint8_t* w(p, e), const uint8_t* ws(p, e, tile, half),
 //   uint32_t w_row(p, tile, c): offset of weight column c of the tile,
 //   finish(p, e, tile, row0, rows, part)
-template <class Op, int MB, int KW, int NBUF, int OCC>
+template <template <int> class OpT, int NJ, int MB, int KW, int OCC>
 __global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantArgs p) {
-  __shared__ Stream8Part part[KW];
+  using Op = OpT<NJ>;
+  __shared__ Stream8Part<NJ> part[KW];
   const int tile = blockIdx.x;
   int e = blockIdx.y, m0 = 0;
   if (e >= p.E && !find_group<64 * KW>(p.offsets, p.E, 16 * MB, e - p.E, (int*)part, &e, &m0)) return;
@@ -490,74 +495,59 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantA
   if (m0 >= cnt) return;
   const int lane = lane_id(), g = lane >> 4, l = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ns = (Op::blocks(p) - wave + KW - 1) / KW;  // this wave's steps
   const uint8_t* wbase = Op::w(p, e);
   const uint8_t* ws0 = Op::ws(p, e, tile, 0);
   const uint8_t* ws1 = Op::ws(p, e, tile, 1);
-  uint32_t wrow[4];
+  uint32_t wrow[NJ];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) wrow[j] = Op::w_row(p, tile, 16 * j + l) + 16 * g;
+  for (int j = 0; j < NJ; ++j) wrow[j] = Op::w_row(p, tile, 16 * j + l) + 16 * g;
   const void* xp[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) xp[b] = Op::row(p, off + min(m0 + 16 * b + l, cnt - 1));
-  f32x4 acc[MB][4];
+  f32x4 acc[MB][NJ];
 #pragma unroll
   for (int b = 0; b < MB; ++b)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 wv[NBUF][4][2];
-  int sv[NBUF][2];
-  RowBlock8<Op::F32> xv[NBUF][MB];
-  // step s of this wave; a step past the end reads the step 0 addresses (cached, unused)
-  auto load = [&](int buf, int s) {
-    const uint32_t kb = s < ns ? wave + KW * s : wave, k = kQBlock * kb;
+    for (int j = 0; j < NJ; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int blocks = Op::blocks(p);
+  for (int kb = wave; kb < blocks; kb += KW) {
+    const uint32_t k = kQBlock * kb;
+    u32x4 wv[NJ][2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      wv[buf][j][0] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k));
-      wv[buf][j][1] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k + 64));
+    for (int j = 0; j < NJ; ++j) {
+      wv[j][0] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k));
+      wv[j][1] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k + 64));
     }
-    sv[buf][0] = ws0[kb];
-    sv[buf][1] = ws1[kb];
+    const int sv[2] = {ws0[kb], ws1[kb]};
+    RowBlock8<Op::F32> xv[MB];
 #pragma unroll
-    for (int b = 0; b < MB; ++b) xv[buf][b].load(xp[b], k + 16 * g, (int)k + 64 < Op::k(p));
-  };
-  if (ns > 0) {
+    for (int b = 0; b < MB; ++b) xv[b].load(xp[b], k + 16 * g, (int)k + 64 < Op::k(p));
 #pragma unroll
-    for (int q = 0; q < NBUF; ++q) load(q, q);
-    for (int s = 0;; s += NBUF) {
+    for (int b = 0; b < MB; ++b) {
+      int xs;
+      const i32x8s x = xv[b].codes(&xs);
 #pragma unroll
-      for (int q = 0; q < NBUF; ++q) {
-#pragma unroll
-        for (int b = 0; b < MB; ++b) {
-          int xs;
-          const i32x8s x = xv[q][b].codes(&xs);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const u32x4 lo = wv[q][j][0], hi = wv[q][j][1];
-            const i32x8s w = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-            acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[b][j], 0, 0, 0, sv[q][j >> 1], 0, xs);
-          }
-        }
-        if (s + q + 1 >= ns) goto done;
-        load(q, s + q + NBUF);
+      for (int j = 0; j < NJ; ++j) {
+        const u32x4 lo = wv[j][0], hi = wv[j][1];
+        const i32x8s w = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+        acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[b][j], 0, 0, 0, sv[2 * j / NJ], 0, xs);
       }
     }
-  done:;
   }
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
     if (m0 + 16 * b >= cnt) break;
     __syncthreads();  // the previous rows' sums have been read
 #pragma unroll
-    for (int j = 0; j < 4; ++j) part[wave][l][4 * j + g] = acc[b][j];
+    for (int j = 0; j < NJ; ++j) part[wave][l][4 * j + g] = acc[b][j];
     __syncthreads();
     Op::template finish<KW>(p, e, tile, off + m0 + 16 * b, min(16, cnt - m0 - 16 * b), part);
   }
 }
 
 // the sum over the waves of columns 4 c4 .. 4 c4 + 3 of the tile
-template <int KW>
-__device__ __forceinline__ f32x4 stream8_sum(const Stream8Part* part, int row, int c4) {
+template <int KW, int NJ>
+__device__ __forceinline__ f32x4 stream8_sum(const Stream8Part<NJ>* part, int row, int c4) {
   f32x4 s = part[0][row][c4];
 #pragma unroll
   for (int w = 1; w < KW; ++w)
@@ -566,26 +556,30 @@ __device__ __forceinline__ f32x4 stream8_sum(const Stream8Part* part, int row, i
   return s;
 }
 
-// 32 gate columns and the matching up columns; A in fp32
+// 8 NJ gate columns and the matching up columns; A in fp32
+template <int NJ>
 struct Stream8Up {
   static constexpr bool F32 = false;
+  static constexpr int kCols = 8 * NJ;
   static __device__ int blocks(const QuantArgs& p) { return p.d / kQBlock; }
   static __device__ int k(const QuantArgs& p) { return p.d; }
   static __device__ const void* row(const QuantArgs& p, int r) { return p.X + (size_t)p.row_token[r] * p.d; }
   static __device__ const uint8_t* w(const QuantArgs& p, int e) { return p.W1q + (size_t)e * w1q_bytes(p.d, p.n); }
   static __device__ const uint8_t* ws(const QuantArgs& p, int e, int tile, int half) {
-    return p.W1s + (size_t)e * w1s_bytes(p.d, p.n) + (size_t)(2 * (tile / 4) + half) * q_stride(p.d / kQBlock);
+    return p.W1s + (size_t)e * w1s_bytes(p.d, p.n) + (size_t)(2 * (kCols * tile / kQBlock) + half) * q_stride(p.d / kQBlock);
   }
   static __device__ uint32_t w_row(const QuantArgs& p, int tile, int c) {
-    return (uint32_t)(256 * (tile / 4) + w1q_row(32 * (tile % 4) + (c & 31), c >> 5)) * p.d;
+    const int col = kCols * tile + c % kCols;
+    return (uint32_t)(256 * (col / kQBlock) + w1q_row(col % kQBlock, c / kCols)) * p.d;
   }
   template <int KW>
-  static __device__ void finish(const QuantArgs& p, int e, int tile, int row0, int rows, const Stream8Part* part) {
-    for (int i = threadIdx.x; i < 128; i += 64 * KW) {
-      const int row = i >> 3, c4 = i & 7;
+  static __device__ void finish(const QuantArgs& p, int e, int tile, int row0, int rows, const Stream8Part<NJ>* part) {
+    constexpr int C4 = kCols / 4;
+    for (int i = threadIdx.x; i < 16 * C4; i += 64 * KW) {
+      const int row = i / C4, c4 = i % C4;
       if (row >= rows) break;
-      f32x4 hg = stream8_sum<KW>(part, row, c4), hu = stream8_sum<KW>(part, row, c4 + 8), a;
-      const int c = 32 * tile + 4 * c4;
+      f32x4 hg = stream8_sum<KW, NJ>(part, row, c4), hu = stream8_sum<KW, NJ>(part, row, c4 + C4), a;
+      const int c = kCols * tile + 4 * c4;
       const float* b1 = p.b1 ? p.b1 + (size_t)e * 2 * p.n + c : nullptr;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -601,23 +595,26 @@ struct Stream8Up {
   }
 };
 
+template <int NJ>
 struct Stream8Down {
   static constexpr bool F32 = true;
+  static constexpr int kCols = 16 * NJ;
   static __device__ int blocks(const QuantArgs& p) { return q_blocks(p.n); }
   static __device__ int k(const QuantArgs& p) { return p.n; }
   static __device__ const void* row(const QuantArgs& p, int r) { return p.A32 + (size_t)r * p.n; }
   static __device__ const uint8_t* w(const QuantArgs& p, int e) { return p.W2q + (size_t)e * w2q_bytes(p.d, p.n); }
   static __device__ const uint8_t* ws(const QuantArgs& p, int e, int tile, int) {
-    return p.W2s + (size_t)e * w2s_bytes(p.d, p.n) + (size_t)(tile / 2) * q_stride(q_blocks(p.n));
+    return p.W2s + (size_t)e * w2s_bytes(p.d, p.n) + (size_t)(kCols * tile / kQBlock) * q_stride(q_blocks(p.n));
   }
-  static __device__ uint32_t w_row(const QuantArgs& p, int tile, int c) { return (uint32_t)(64 * tile + c) * q_pad(p.n); }
+  static __device__ uint32_t w_row(const QuantArgs& p, int tile, int c) { return (uint32_t)(kCols * tile + c) * q_pad(p.n); }
   template <int KW>
-  static __device__ void finish(const QuantArgs& p, int e, int tile, int row0, int rows, const Stream8Part* part) {
-    for (int i = threadIdx.x; i < 256; i += 64 * KW) {
-      const int row = i >> 4, c4 = i & 15;
+  static __device__ void finish(const QuantArgs& p, int e, int tile, int row0, int rows, const Stream8Part<NJ>* part) {
+    constexpr int C4 = kCols / 4;
+    for (int i = threadIdx.x; i < 16 * C4; i += 64 * KW) {
+      const int row = i / C4, c4 = i % C4;
       if (row >= rows) break;
-      f32x4 y = stream8_sum<KW>(part, row, c4);
-      const int c = 64 * tile + 4 * c4;
+      f32x4 y = stream8_sum<KW, NJ>(part, row, c4);
+      const int c = kCols * tile + 4 * c4;
       if (p.b2) {
         const f32x4 b = *(const f32x4*)(p.b2 + (size_t)e * p.d + c);
 #pragma unroll
@@ -628,28 +625,38 @@ struct Stream8Down {
   }
 };
 
-template <class Op>
-static hipError_t run_stream8(const QuantArgs& p, dim3 grid, int mb, int blocks, hipStream_t s) {
-  if (mb == 1 && blocks > 4)
-    stream8_gemm_kernel<Op, 1, 8, 2, 2><<<grid, dim3(512), 0, s>>>(p);
-  else if (mb == 1 && blocks > 2)
-    stream8_gemm_kernel<Op, 1, 4, 1, 4><<<grid, dim3(256), 0, s>>>(p);
-  else if (mb == 1)
-    stream8_gemm_kernel<Op, 1, 2, 1, 4><<<grid, dim3(128), 0, s>>>(p);
-  else if (mb == 2 && blocks > 4)
-    stream8_gemm_kernel<Op, 2, 8, 1, 2><<<grid, dim3(512), 0, s>>>(p);
-  else if (mb == 2)
-    stream8_gemm_kernel<Op, 2, 2, 1, 3><<<grid, dim3(128), 0, s>>>(p);
-  else
-    stream8_gemm_kernel<Op, 4, 4, 1, 2><<<grid, dim3(256), 0, s>>>(p);
+template <template <int> class Op, int NJ, int MB, int KW, int OCC>
+static hipError_t run_stream8(const QuantArgs& p, const StreamShape& t, int cols, hipStream_t s) {
+  stream8_gemm_kernel<Op, NJ, MB, KW, OCC><<<stream_grid(cols / Op<NJ>::kCols, p.E, t), dim3(64 * KW), 0, s>>>(p);
   return hipGetLastError();
 }
 
+// us of up / down by columns and waves of a workgroup (weights read at 5.0 to 5.6 TB/s
+// in the large ones):
+//   up                                       64, 4 waves   64, 8   128, 4   128, 8
+//     d = 1536, n = 256, E = 128, T = 4       11.5          9.8     14.9     9.6
+//     d = 1024, n = 256, E = 64, T = 64       9.2           10.3    10.9     10.4
+//     d = 1536, n = 256, E = 128, T = 128     22.9          24.1    21.9     25.1
+//     d = 4096, n = 512, E = 128, T = 256     117           119     112      125
+//   down                                     64, 2 waves   64, 4   128, 1   128, 2   128, 4
+//     d = 1536, n = 256, E = 128, T = 1       3.8           4.3              3.9      5.1
+//     d = 4096, n = 512, E = 128, T = 64      44.6          44.9             44.1     40.8
+//     d = 1024, n = 256, E = 64, T = 64       7.0           8.1     7.8      6.9      6.9
+//     d = 1536, n = 256, E = 128, T = 128     14.6          17.1    12.6     16.1     15.4
+//     d = 2048, n = 128, E = 256, T = 128     17.9          26.0    15.1     18.0     24.1
+//     d = 4096, n = 512, E = 128, T = 256     71.5          72.9    58.9     59.0     59.8
 hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
-  return run_stream8<Stream8Up>(a, stream_grid(a.n / 32, a.E, t), t.mb, a.d / kQBlock, s);
+  if (t.mb == 1) return run_stream8<Stream8Up, 4, 1, 8, 4>(a, t, a.n, s);
+  if (t.mb == 2) return run_stream8<Stream8Up, 4, 2, 4, 4>(a, t, a.n, s);
+  return run_stream8<Stream8Up, 4, 4, 4, 2>(a, t, a.n, s);
 }
 hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
-  return run_stream8<Stream8Down>(a, stream_grid(a.d / kStream8Cols, a.E, t), t.mb, q_blocks(a.n), s);
+  const int blocks = q_blocks(a.n);
+  if (t.mb == 1 && blocks <= 2) return run_stream8<Stream8Down, 4, 1, 2, 4>(a, t, a.d, s);
+  if (t.mb == 1) return run_stream8<Stream8Down, 4, 1, 4, 4>(a, t, a.d, s);
+  if (t.mb == 2 && blocks <= 2 && a.E * (a.d / kQBlock) > 768) return run_stream8<Stream8Down, 8, 2, 1, 2>(a, t, a.d, s);
+  if (t.mb == 2) return run_stream8<Stream8Down, 8, 2, 2, 2>(a, t, a.d, s);
+  return run_stream8<Stream8Down, 4, 4, 4, 2>(a, t, a.d, s);
 }
 
 // up's tiles decide for both, since A passes between the two in one of two forms
