@@ -23,13 +23,11 @@ __host__ __device__ inline int q_pad(int cols) { return q_blocks(cols) * kQBlock
 __host__ __device__ inline int q_stride(int blocks) { return (blocks + 3) / 4 * 4; }
 
 // Expert weights as the products read them, k contiguous (np = q_pad(n)):
-//   W1q [E][np / 128][2 halves of 64][gate, up][64 columns][d]   W1s [E][np / 128][gate, up][q_stride(d / 128)]
-//   W2q [E][d columns][np]                                       W2s [E][d / 128][q_stride(np / 128)]
-// W1's rows come in the order of a tile of 128 gate and 128 up columns whose two
-// column groups of waves hold 64 of each; columns and k past n are zero.
-__host__ __device__ inline int w1q_row(int col, int up) {
-  return ((col >> 6) * 2 + up) * 64 + (col & 63);
-}
+//   W1q [E][np / 128][4 quarters][gate, up][32 columns][d]   W1s [E][np / 128][gate, up][q_stride(d / 128)]
+//   W2q [E][d columns][np]                                   W2s [E][d / 128][q_stride(np / 128)]
+// W1's rows alternate between 32 gate and the 32 matching up columns, so that any
+// wave of a tile holds both; columns and k past n are zero.
+__host__ __device__ inline int w1q_row(int col, int up) { return ((col >> 5) * 2 + up) * 32 + (col & 31); }
 __host__ __device__ inline size_t w1q_bytes(int d, int n) { return (size_t)2 * q_pad(n) * d; }
 __host__ __device__ inline size_t w2q_bytes(int d, int n) { return (size_t)d * q_pad(n); }
 __host__ __device__ inline size_t w1s_bytes(int d, int n) { return (size_t)q_blocks(n) * 2 * q_stride(d / kQBlock); }

@@ -423,7 +423,7 @@ struct EpiStores<Op, std::void_t<decltype(Op::EPI_STORES)>> : std::integral_cons
 //                                                          -- the scales of the tile's row r (dwords of four blocks)
 //   void weight_scales(const Params&, const TileInfo&, int g, uint32_t (&)[W_SCALES])
 //                                                          -- four blocks' bytes from block 4 g on
-// Accumulator columns j >= RN / W_SCALES take the second weight scale.  scale_row of
+// Accumulator column j takes weight scale j % W_SCALES.  scale_row of
 // an op that gathers reads the row indices that other waves loaded: its epilogue
 // has a workgroup barrier, before which the next tile's may not be requested.
 template <class Op, class = void>
@@ -776,24 +776,36 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
       else
         k_loop(std::false_type{});
     } else if constexpr (kF8) {
-      // 8-bit operands, two stages of 128 k: two sub-steps of 64 k per stage, each
-      // MFMA as long as two of the bf16 ones, so a DMA instruction before every one
-      // of the first keeps the stage's requests in the first half of the step.  A
-      // fragment is two 16-byte chunks of its row; which k a chunk holds does not
-      // matter as long as both operands agree, and the scales cover the whole stage.
-      static_assert(!kF8 || (S == 2 && Cfg::RN % 2 == 0 && BK == 64 && Op::M_MODE == ROWS && Op::N_MODE == ROWS), "8-bit ops");
-      constexpr int NS = Op::W_SCALES;
+      // 8-bit operands: a stage is BK / 32 sub-steps of 64 k, each MFMA as long as two
+      // of the bf16 ones, so a DMA instruction before every one of the first keeps the
+      // stage's requests early in the step.  A fragment is two 16-byte chunks of its
+      // row; which k a chunk holds does not matter as long as both operands agree, and
+      // a scale covers two sub-steps.
+      static_assert(!kF8 || (Cfg::RN % 2 == 0 && Op::M_MODE == ROWS && Op::N_MODE == ROWS), "8-bit ops");
+      constexpr int NS = Op::W_SCALES, SUB8 = BK / 32, SPB = 64 / BK;  // steps per block of 128 k
       uint32_t ws[NS], ws_next[NS], xs[Cfg::RM];
       Op::weight_scales(p, ti, 0, ws_next);
-      const int groups = (nk + 3) >> 2;
+      const int groups = (nk + 4 * SPB - 1) / (4 * SPB);  // of four blocks
+      constexpr int kYoung = (S - 2) * kPerStage;
+      constexpr int kYoungEpi = kYoung + EpiStores<Op>::value < 63 ? kYoung + EpiStores<Op>::value : 63;
       for (int kt = 0; kt < nk; ++kt) {
-        // (a tile of one step: the next tile's index loads are to be complete after it)
-        if (kt == 0 && prev_full && nk > 1)
-          wait_vm_barrier<(EpiStores<Op>::value < 63 ? EpiStores<Op>::value : 63)>();
+        // as below; scale DMA among the younger operations only makes a wait stricter
+        // (where the loop has fewer steps than stages: full drains, which the next
+        // tile's index loads need after its last step)
+        const int ahead = kt == 0 ? 0 : min(S - 2, nk - 1 - kt);
+        if (kt == 0 && nk > S - 1 && (kYoung > 0 || prev_full)) {
+          if (prev_full)
+            wait_vm_barrier<kYoungEpi>();
+          else
+            wait_vm_barrier<kYoung>();
+        } else if (ahead >= 2)
+          wait_vm_barrier<(S >= 4 ? 2 : 0) * kPerStage>();
+        else if (ahead == 1)
+          wait_vm_barrier<(S >= 3 ? 1 : 0) * kPerStage>();
         else
           wait_vm_barrier<0>();
-        const int g = kt >> 2;
-        if ((kt & 3) == 0) {
+        const int g = kt / (4 * SPB), kg = kt % (4 * SPB);
+        if (kg == 0) {
           const SMOE_LDS uint32_t* sl = (const SMOE_LDS uint32_t*)(uintptr_t)(scale_lds + (g & 1) * (BM * 4));
 #pragma unroll
           for (int i = 0; i < Cfg::RM; ++i) xs[i] = sl[wm0 + 32 * i + (threadIdx.x & 31)];
@@ -801,10 +813,10 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
           for (int q = 0; q < NS; ++q) ws[q] = ws_next[q];
           if (g + 1 < groups) Op::weight_scales(p, ti, g + 1, ws_next);
         }
-        const int knext = kt + 1;
+        const int knext = kt + S - 1;
         const bool issue_next = knext < nk;
-        const uint32_t st_next = lds0 + (knext & 1) * Cfg::STAGE_BYTES;
-        const char* lm = smem + (kt & 1) * Cfg::STAGE_BYTES;
+        const uint32_t st_next = lds0 + (knext % S) * Cfg::STAGE_BYTES;
+        const char* lm = smem + (kt % S) * Cfg::STAGE_BYTES;
         const char* ln = lm + Cfg::M_BYTES;
         auto issue_one = [&](int d) {
           if (d < Cfg::QM)
@@ -820,13 +832,13 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
           for (int i = 0; i < Cfg::RM; ++i) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, 0);
           fn[0] = frag8<NSide>(ln, wn0, 0);
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < SUB8; ++s)
 #pragma unroll
             for (int j = 0; j < Cfg::RN; ++j) {
               if (j + 1 < Cfg::RN)
                 fn[(j + 1) & 1] = frag8<NSide>(ln, wn0 + 32 * (j + 1), s);
-              else if (s == 0)
-                fn[(j + 1) & 1] = frag8<NSide>(ln, wn0, 1);
+              else if (s + 1 < SUB8)
+                fn[(j + 1) & 1] = frag8<NSide>(ln, wn0, s + 1);
 #pragma unroll
               for (int i = 0; i < Cfg::RM; ++i) {
                 const int c = (s * Cfg::RN + j) * Cfg::RM + i;
@@ -834,20 +846,22 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
                 if (c < kPerStage && issue_next) issue_one(c);
                 __builtin_amdgcn_sched_barrier(0);
                 acc.acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                    fn[j & 1], fm[i], acc.acc[i][j], 0, 0, 0, (int)ws[j * NS / Cfg::RN], 0, (int)xs[i]);
-                if (s == 0 && j == Cfg::RN - 1) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, 1);
+                    fn[j & 1], fm[i], acc.acc[i][j], 0, 0, 0, (int)ws[j % NS], 0, (int)xs[i]);
+                if (s + 1 < SUB8 && j == Cfg::RN - 1) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, s + 1);
               }
             }
         } else if (issue_next) {
           ms.issue(st_next, knext * BK);
           ns.issue(st_next + Cfg::M_BYTES, knext * BK);
         }
-        // the next group's scales, complete at the top of the step after
-        if ((kt & 3) == 1 && g + 1 < groups) scale_issue(g + 1);
+        // the next group's scales, complete long before its first step
+        if (kg == 1 && g + 1 < groups) scale_issue(g + 1);
+        if ((kt + 1) % SPB == 0) {
 #pragma unroll
-        for (int i = 0; i < Cfg::RM; ++i) xs[i] >>= 8;
+          for (int i = 0; i < Cfg::RM; ++i) xs[i] >>= 8;
 #pragma unroll
-        for (int q = 0; q < NS; ++q) ws[q] >>= 8;
+          for (int q = 0; q < NS; ++q) ws[q] >>= 8;
+        }
       }
     } else {
       for (int kt = 0; kt < nk; ++kt) {

@@ -68,7 +68,8 @@ __device__ __forceinline__ void unswap_block_fp8(const u32x4& x, uint32_t (&v)[4
 
 // ---------------------------------------------------------------- scheduling
 // ---------------------------------------------------------------- m-tile list
-// The varlen-M m-tiles (BM = kMTile rows) as a list, built on the device from
+// The varlen-M m-tiles (BM = kMTile rows, or another power of two for the 8-bit
+// projections) as a list, built on the device from
 // the expert offsets: int32 header {all m-tiles, partial m-tiles, 0, 0}, then
 // one {expert, m0, rows, first global row} entry per m-tile, the full tiles
 // of every expert in expert order first and the partial last tiles after
@@ -76,12 +77,13 @@ __device__ __forceinline__ void unswap_block_fp8(const u32x4& x, uint32_t (&v)[4
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 #define SMOE_CONST __attribute__((address_space(4)))
 
-size_t mtiles_bytes(int64_t capacity, int E) { return 16 * (size_t)(1 + capacity / kMTile + E); }
+size_t mtiles_bytes(int64_t capacity, int E, int rows) { return 16 * (size_t)(1 + capacity / rows + E); }
 
 constexpr int kMTilesThreads = 1024;
 // pf, pp: LDS [4097] each (per-expert exclusive prefix of full / partial m-tiles)
-__device__ __forceinline__ void mtiles_body(const int32_t* __restrict__ offsets, int E, int32_t* __restrict__ out,
-                                            int* pf, int* pp, int* scan_lds) {
+__device__ __forceinline__ void mtiles_body(const int32_t* __restrict__ offsets, int E, int log2_rows,
+                                            int32_t* __restrict__ out, int* pf, int* pp, int* scan_lds) {
+  const int rows = 1 << log2_rows;
   const int tid = threadIdx.x;
   // thread t owns experts 4t .. 4t+3 (E <= 4096)
   int nf[4], np[4], sf = 0, sp = 0;
@@ -89,8 +91,8 @@ __device__ __forceinline__ void mtiles_body(const int32_t* __restrict__ offsets,
   for (int q = 0; q < 4; ++q) {
     const int e = 4 * tid + q;
     const int cnt = e < E ? offsets[e + 1] - offsets[e] : 0;
-    nf[q] = cnt / kMTile;
-    np[q] = cnt % kMTile != 0;
+    nf[q] = cnt >> log2_rows;
+    np[q] = (cnt & (rows - 1)) != 0;
     sf += nf[q];
     sp += np[q];
   }
@@ -124,21 +126,23 @@ __device__ __forceinline__ void mtiles_body(const int32_t* __restrict__ offsets,
       if (pre[mid] <= key) lo = mid; else hi = mid;
     }
     const int off = offsets[lo], cnt = offsets[lo + 1] - off;
-    const int m0 = part ? (cnt / kMTile) * kMTile : (key - pre[lo]) * kMTile;
-    *(i32x4*)(out + 4 + 4 * t) = i32x4{lo, m0, min(kMTile, cnt - m0), off + m0};
+    const int m0 = part ? cnt & ~(rows - 1) : (key - pre[lo]) << log2_rows;
+    *(i32x4*)(out + 4 + 4 * t) = i32x4{lo, m0, min(rows, cnt - m0), off + m0};
   }
 }
 
-__global__ __launch_bounds__(kMTilesThreads) void mtiles_kernel(const int32_t* __restrict__ offsets, int E,
+__global__ __launch_bounds__(kMTilesThreads) void mtiles_kernel(const int32_t* __restrict__ offsets, int E, int log2_rows,
                                                                int32_t* __restrict__ out) {
   __shared__ int pf[4097], pp[4097];
   __shared__ int scan_lds[kMTilesThreads / 64];
-  mtiles_body(offsets, E, out, pf, pp, scan_lds);
+  mtiles_body(offsets, E, log2_rows, out, pf, pp, scan_lds);
 }
 
-hipError_t launch_mtiles(const int32_t* offsets, int E, int32_t* out, hipStream_t s) {
-  if (E > 4096) return hipErrorInvalidValue;
-  mtiles_kernel<<<1, kMTilesThreads, 0, s>>>(offsets, E, out);
+constexpr int kMTileLog2 = 8;
+static_assert(1 << kMTileLog2 == kMTile);
+hipError_t launch_mtiles(const int32_t* offsets, int E, int rows, int32_t* out, hipStream_t s) {
+  if (E > 4096 || (rows & (rows - 1))) return hipErrorInvalidValue;
+  mtiles_kernel<<<1, kMTilesThreads, 0, s>>>(offsets, E, __builtin_ctz(rows), out);
   return hipGetLastError();
 }
 
@@ -289,7 +293,7 @@ __global__ __launch_bounds__(kMTilesThreads) void bwd_lists_kernel(const int32_t
   __shared__ int scan_lds[kMTilesThreads / 64];
   __shared__ int sh_kc;
   if (blockIdx.x == 0) {
-    mtiles_body(offsets, E, mtiles, lds, lds + 4097, scan_lds);
+    mtiles_body(offsets, E, kMTileLog2, mtiles, lds, lds + 4097, scan_lds);
   } else if (blockIdx.x == 1) {
     kchunks_body(offsets, E, tpe2, slabs2, keep2, klist2, lds, scan_lds, &sh_kc);
   } else if (blockIdx.x == 2) {
@@ -432,12 +436,11 @@ __device__ __forceinline__ void store_part_f32(float* out, int64_t ld, int m0, i
 
 // Logical tile ids run over the tiles of their class (full m-tiles, then the
 // partial ones) in tile_order, so neighbouring ids share the rows of an m-tile
-// and the weights of an expert.  The list entry is
+// and the weights of an expert.  The list is of tiles of BM rows.  The list entry is
 // read with a scalar load (the id is workgroup-uniform).  PLAIN: N is a multiple
 // of BN and less than 8 BN, so the tiles are whole and go row by row.
 template <int BM, int BN, bool PLAIN = false>
 __device__ __forceinline__ bool tile_varlen_m(const int32_t* mtiles, int E, int N, int K, int id, TileInfo& ti) {
-  static_assert(BM == kMTile, "varlen-M tiles are the m-tile list's tiles");
   const int nnt = PLAIN ? N / BN : (N + BN - 1) / BN;
   const bool partial = (id & kPartialTile) != 0;
   id &= kPartialTile - 1;
@@ -1328,18 +1331,19 @@ struct F8Rows {
 };
 
 // N tile: 128 gate columns and the matching up columns, in the order the weights
-// are laid out in, so a wave's first 64 are gate columns and its last 64 the up ones.
-// A leaves as codes of blocks of 128: the two waves of a row group hold 64 columns
-// each, and their largest |A| meet in LDS (as do H's where it is kept).
+// are laid out in: accumulator column blocks alternate between 32 gate and 32 up
+// columns.  A leaves as codes of blocks of 128: the WN waves of a row group hold
+// 128 / WN columns each, and their largest |A| meet in LDS (as do H's where it is
+// kept).
 template <class Cfg_>
 struct OpUp8 : F8Rows {
   using Cfg = Cfg_;
-  static constexpr int W_SCALES = 2;
-  static_assert(Cfg::BM == 256 && Cfg::BN == 256 && Cfg::WN == 2 && Cfg::RN == 4, "two waves share a block of 128 columns");
+  static constexpr int W_SCALES = 2, WN = Cfg::WN, CB = Cfg::RN / 2;  // CB: blocks of 32 gate columns of a wave
+  static_assert(Cfg::BN == 256 && Cfg::RN % 2 == 0, "a tile holds one block of 128 columns of A");
   struct Params { QuantArgs a; };
   static constexpr int IDX_LDS = Cfg::NW * Cfg::QM * 256;
-  static constexpr int EPI_LDS = 3 * 2 * Cfg::BM * 4;  // [gate, up, A][column group][row]
-  static constexpr int EPI_STORES = Cfg::RM * 2;       // A's
+  static constexpr int EPI_LDS = 3 * WN * Cfg::BM * 4;  // [gate, up, A][column group][row]
+  static constexpr int EPI_STORES = Cfg::RM * CB;       // A's
   static __device__ int count(const Params& p, int*) { return count_varlen_m<256>(p.a.mtiles, 2 * q_pad(p.a.n)); }
   static __device__ int count_tail(const Params& p, const int*) {
     return count_varlen_m_tail<256>(p.a.mtiles, 2 * q_pad(p.a.n));
@@ -1354,9 +1358,10 @@ struct OpUp8 : F8Rows {
     s.init((const uint16_t*)(p.a.W1q + (size_t)ti.e * w1q_bytes(p.a.d, p.a.n)), p.a.d / 2, nullptr, ti.n0, ti.ncols);
   }
   static __device__ const uint8_t* scale_row(const Params& p, const TileInfo&, int r, uint32_t idx_lds) {
-    // row r was loaded by instruction j of wave w (RowsSide), in all eight lanes of its place
-    const int q = r >> 3, w = q % Cfg::NW, j = q / Cfg::NW;
-    const int t = *(const SMOE_LDS int32_t*)(uintptr_t)(idx_lds + (w * Cfg::QM + j) * 256 + (r & 7) * 32);
+    // row r was loaded by instruction j of wave w (RowsSide), in all C lanes of its place
+    constexpr int C = Cfg::BK / 8, RPI = 64 / C;
+    const int q = r / RPI, w = q % Cfg::NW, j = q / Cfg::NW;
+    const int t = *(const SMOE_LDS int32_t*)(uintptr_t)(idx_lds + (w * Cfg::QM + j) * 256 + (r % RPI) * C * 4);
     return p.a.Xs + (size_t)t * q_stride(p.a.d / kQBlock);
   }
   static __device__ void weight_scales(const Params& p, const TileInfo& ti, int g, uint32_t (&ws)[2]) {
@@ -1371,25 +1376,28 @@ struct OpUp8 : F8Rows {
     const int n = a.n, np = q_pad(n), nb = np / kQBlock, b = ti.n0 / Cfg::BN;  // block of A's columns
     const int lane = epilogue_lane(), wn = t.wave_n(), h = lane >> 5;
     const int wm0 = Cfg::wave_m(threadIdx.x >> 6) * (Cfg::BM / Cfg::WM);
-    const int col = kQBlock * b + 64 * wn;  // this wave's first column
-    const bool live = col < n;              // (past n everything is zero, and is stored as A's padding)
+    const int col = kQBlock * b + 32 * CB * wn;  // this wave's first column
+    const bool live = col < n;                   // (past n everything is zero, and is stored as A's padding)
     float* amax = (float*)epi;
     auto put = [&](int which, int i, float m) {
       m = fmaxf(m, __shfl_xor(m, 32, kWave));
-      if (h == 0) amax[(which * 2 + wn) * Cfg::BM + wm0 + 32 * i + lane] = m;
+      if (h == 0) amax[(which * WN + wn) * Cfg::BM + wm0 + 32 * i + lane] = m;
     };
     auto block_scale = [&](int which, int m) {
-      return scale_byte(__float_as_uint(fmaxf(amax[which * 2 * Cfg::BM + m], amax[(which * 2 + 1) * Cfg::BM + m])));
-    };
-    // the 64 codes of this wave and row block i, accumulator columns j0 .. j0 + 1 (both
-    // lanes of a row are in a branch on it, so the swaps find their partners)
-    auto store = [&](int i, int j0, float scale, uint8_t* row) {
+      float x = amax[which * WN * Cfg::BM + m];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
+      for (int w = 1; w < WN; ++w) x = fmaxf(x, amax[(which * WN + w) * Cfg::BM + m]);
+      return scale_byte(__float_as_uint(x));
+    };
+    // this wave's codes of row block i of the gate (or A's) or the up columns (both
+    // lanes of a row are in a branch on it, so the swaps find their partners)
+    auto store = [&](int i, int up, float scale, uint8_t* row) {
+#pragma unroll
+      for (int q = 0; q < CB; ++q) {
         uint32_t v[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const auto& x = t.acc[i][j0 + q];
+          const auto& x = t.acc[i][2 * q + up];
           v[g] = pack_fp8x4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3], scale);
         }
         *(u32x4*)(row + 32 * q + 16 * h) = swap_block_fp8(v[0], v[1], v[2], v[3]);
@@ -1398,10 +1406,10 @@ struct OpUp8 : F8Rows {
     if (a.b1 && live) {
       const float* b1 = a.b1 + (size_t)ti.e * (2 * n) + col + 4 * h;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < Cfg::RN; ++j)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const f32x4 v = *(const f32x4*)(b1 + (j >> 1) * n + 32 * (j & 1) + 8 * g);
+          const f32x4 v = *(const f32x4*)(b1 + (j & 1) * n + 32 * (j >> 1) + 8 * g);
 #pragma unroll
           for (int i = 0; i < Cfg::RM; ++i)
 #pragma unroll
@@ -1413,9 +1421,9 @@ struct OpUp8 : F8Rows {
       for (int i = 0; i < Cfg::RM; ++i)
 #pragma unroll
         for (int up = 0; up < 2; ++up) {
-          float x[32];
+          float x[16 * CB];
 #pragma unroll
-          for (int q = 0; q < 32; ++q) x[q] = t.acc[i][2 * up + q / 16][q % 16];
+          for (int q = 0; q < 16 * CB; ++q) x[q] = t.acc[i][2 * (q / 16) + up][q % 16];
           put(up, i, finite_amax(x));
         }
       barrier_lds();
@@ -1427,7 +1435,7 @@ struct OpUp8 : F8Rows {
         if (m < ti.mrows && live) {
           uint8_t* h8 = a.H8 + row * (2 * n) + col;
           store(i, 0, scale_value(sg), h8);
-          store(i, 2, scale_value(su), h8 + n);
+          store(i, 1, scale_value(su), h8 + n);
         }
         if (h == 0 && wn == 0 && m < ti.mrows) {
           uint8_t* hs = a.Hs + row * h8_stride(n) + b;
@@ -1439,12 +1447,12 @@ struct OpUp8 : F8Rows {
     // A in the place of the gate columns
 #pragma unroll
     for (int i = 0; i < Cfg::RM; ++i) {
-      float x[32];
+      float x[16 * CB];
 #pragma unroll
-      for (int q = 0; q < 32; ++q) {
+      for (int q = 0; q < 16 * CB; ++q) {
         float sg;
-        x[q] = silu_sig(t.acc[i][q / 16][q % 16], &sg) * t.acc[i][2 + q / 16][q % 16];
-        t.acc[i][q / 16][q % 16] = x[q];
+        x[q] = silu_sig(t.acc[i][2 * (q / 16)][q % 16], &sg) * t.acc[i][2 * (q / 16) + 1][q % 16];
+        t.acc[i][2 * (q / 16)][q % 16] = x[q];
       }
       put(2, i, finite_amax(x));
     }
@@ -2017,11 +2025,37 @@ hipError_t launch_down_ablation(const DownArgs& a, int strategy, hipStream_t s) 
   return launch_down(a, s);
 }
 
+#ifdef V1
+using F128u = GemmCfg<128, 256, 2, 4, 3>;
+using F128d = GemmCfg<128, 256, 2, 4, 3>;
+#elif defined(V2)
+using F128u = GemmCfg<128, 256, 2, 4, 2>;
+using F128d = GemmCfg<128, 128, 2, 2, 2, kBK, 2>;
+#elif defined(V3)
+using F128u = GemmCfg<128, 256, 2, 4, 3>;
+using F128d = GemmCfg<128, 128, 4, 2, 4>;
+#elif defined(V4)
+using F128u = GemmCfg<128, 256, 4, 2, 3>;
+using F128d = GemmCfg<128, 128, 4, 2, 2, kBK, 2>;
+#else
+using F128u = GemmCfg<128, 256, 2, 4, 3>;
+using F128d = GemmCfg<128, 256, 2, 4, 3>;
+#endif
+int quant_tile_rows(const moe_dims& m, int64_t mt) {
+#ifdef VF
+  return VF;
+#else
+  return 256;
+#endif
+}
 hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s) {
-  return run<OpUp8<C256x256w>>({a}, pad8(mtiles_bound(a.capacity, a.E, 256) * q_blocks(a.n)), s);
+  const int grid = pad8(mtiles_bound(a.capacity, a.E, a.tile_rows) * q_blocks(a.n));
+  return a.tile_rows == 128 ? run<OpUp8<F128u>>({a}, grid, s) : run<OpUp8<C256x256w>>({a}, grid, s);
 }
 hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s) {
-  return run<OpDown8<C256x256w>>({a}, pad8(mtiles_bound(a.capacity, a.E, 256) * n_tiles(a.d, 256)), s);
+  const int mt = mtiles_bound(a.capacity, a.E, a.tile_rows);
+  return a.tile_rows == 128 ? run<OpDown8<F128d>>({a}, pad8(mt * n_tiles(a.d, F128d::BN)), s)
+                            : run<OpDown8<C256x256w>>({a}, pad8(mt * n_tiles(a.d, 256)), s);
 }
 
 int dh_n_tiles(int n, int64_t mt) { return n_tiles(n, tile_width(kTimesDH, mt, n)); }

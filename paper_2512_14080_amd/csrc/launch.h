@@ -89,10 +89,10 @@ inline int rounding_mode(const moe_routing& r) { return r.reserved >> 16; }
 // The varlen-M m-tile list (mtiles_kernel): built from the expert offsets
 // once per forward / backward call, read by the up, down, dH and dX~ GEMMs.
 constexpr int kMTile = 256;  // rows of an m-tile
-size_t mtiles_bytes(int64_t capacity, int E);
+size_t mtiles_bytes(int64_t capacity, int E, int rows = kMTile);
 // about how many m-tiles a routing has
 int64_t expected_mtiles(const moe_dims& m, const moe_routing& r);
-hipError_t launch_mtiles(const int32_t* offsets, int E, int32_t* out, hipStream_t s);
+hipError_t launch_mtiles(const int32_t* offsets, int E, int rows, int32_t* out, hipStream_t s);
 
 // mt: the m-tiles to expect (expected_mtiles), for the choice of the tiles; capacity
 // bounds the rows.
@@ -230,8 +230,10 @@ struct QuantArgs {
   const int32_t* offsets; const int32_t* row_token; const int32_t* mtiles;
   const float* b1; const float* b2;
   float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
-  int d, n, E, capacity;
+  int d, n, E, capacity, tile_rows;  // (tile_rows: of the m-tile list)
 };
+// rows of the tiles of the 8-bit projections: 256, or 128
+int quant_tile_rows(const moe_dims& m, int64_t mt);
 hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s);
 hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s);
 // The same for few rows per expert, from X in bf16 (stream_gemm.hip); stream8_shape:

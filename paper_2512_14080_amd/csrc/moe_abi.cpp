@@ -217,7 +217,7 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   off = carve(base, off, (size_t)cap * np, w ? (void**)&w->A8 : nullptr);
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
   off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);
-  off = carve(base, off, smoe::mtiles_bytes(cap, m.E), w ? (void**)&w->mtiles : nullptr);
+  off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles : nullptr);
   return off;
 }
 
@@ -334,7 +334,7 @@ struct Projections {
       : up(smoe::stream_shape(m, r.capacity, smoe::rounding_tile(r), (2 * m.n + 255) / 256)),
         down(smoe::stream_shape(m, r.capacity, smoe::rounding_tile(r), (m.d + 255) / 256)) {}
   hipError_t lists(const int32_t* offsets, int E, int32_t* mtiles, hipStream_t s) const {
-    return up.mb && down.mb ? hipSuccess : smoe::launch_mtiles(offsets, E, mtiles, s);
+    return up.mb && down.mb ? hipSuccess : smoe::launch_mtiles(offsets, E, smoe::kMTile, mtiles, s);
   }
   hipError_t run_up(const smoe::UpArgs& a, hipStream_t s) const {
     return up.mb ? smoe::launch_stream_up(a, up, s) : smoe::launch_up(a, s);
@@ -894,7 +894,7 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
   const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles,
                           eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A32, w.A8, w.As, c ? c->H : nullptr,
-                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity};
+                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity, smoe::quant_tile_rows(m, smoe::expected_mtiles(m, *r))};
   // (what is kept is written by the tiled projections)
   const smoe::StreamShape few = c ? smoe::StreamShape{0, 0} : smoe::stream8_shape(m, r->capacity, smoe::rounding_tile(*r));
   if (few.mb) {
@@ -902,7 +902,7 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_stream8_down(a, few, stream), "8-bit down-proj");
   } else {
     LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, X8, Xs, stream), "quantize X");
-    HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
+    HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, a.tile_rows, w.mtiles, stream), "m-tile list");
     LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
   }
@@ -936,7 +936,7 @@ int moe_fwd_ckpt(moe_dims m, const moe_bf16* X, const moe_bf16* W1, const moe_bf
   c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
   const int64_t mt = smoe::expected_mtiles(m, *r);
   if (c->X) LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, c->X, c->Xs, stream), "quantize X");
-  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
+  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, smoe::kMTile, w.mtiles, stream), "m-tile list");
   LAUNCH(MOE_KC_UP,
          smoe::launch_up_ckpt({X, W1, r->offsets, r->row_token, nullptr, w.A, m.d, m.n, m.E, r->capacity, mt, w.mtiles,
                                eb ? eb->b1 : nullptr, c->H, c->Hs},
