@@ -98,4 +98,23 @@ __device__ __forceinline__ float finite_amax(const float (&x)[N]) {
   return m;
 }
 
+// Block u of the rows X [.., cols] (`blocks` blocks a row), by 16 lanes with 8 columns
+// (16 bytes) each: the largest |x| is a maximum over the lane's values and the lanes.
+__device__ __forceinline__ void quantize_unit(const uint16_t* __restrict__ X, int u, int blocks, int cols, int stride,
+                                              uint8_t* __restrict__ q, uint8_t* __restrict__ scale) {
+  const int l = threadIdx.x & 15, row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
+  u32x4 v = {0, 0, 0, 0};
+  if (c < cols) v = *(const u32x4*)(X + (size_t)row * cols + c);
+  const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+  uint32_t m = finite_amax_bf16(w);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 16));
+  const int sb = scale_byte(m << 16);
+  const float sv = scale_value(sb);
+  if (c < cols)
+    *(u32x2*)(q + (size_t)row * cols + c) = u32x2{pack_fp8x4_bf16(v[0], v[1], sv), pack_fp8x4_bf16(v[2], v[3], sv)};
+  // (the last block's first lanes also fill the row's scales to a whole dword)
+  if (l == 0 || (b == blocks - 1 && b + l < stride)) scale[(size_t)row * stride + b + l] = l ? 127 : sb;
+}
+
 }  // namespace smoe

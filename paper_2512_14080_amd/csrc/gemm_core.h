@@ -783,6 +783,7 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
       // a scale covers two sub-steps.
       static_assert(!kF8 || (Cfg::RN % 2 == 0 && Op::M_MODE == ROWS && Op::N_MODE == ROWS), "8-bit ops");
       constexpr int NS = Op::W_SCALES, SUB8 = BK / 32, SPB = 64 / BK;  // steps per block of 128 k
+      static_assert(!kF8 || kPerStage <= SUB8 * Cfg::RM * Cfg::RN, "every DMA instruction has an MFMA after it");
       uint32_t ws[NS], ws_next[NS], xs[Cfg::RM];
       Op::weight_scales(p, ti, 0, ws_next);
       const int groups = (nk + 4 * SPB - 1) / (4 * SPB);  // of four blocks

@@ -138,6 +138,26 @@ __global__ __launch_bounds__(kMTilesThreads) void mtiles_kernel(const int32_t* _
   mtiles_body(offsets, E, log2_rows, out, pf, pp, scan_lds);
 }
 
+// The 8-bit forward's first launch: workgroup 0 writes the m-tile list (and 1 a second
+// one, of 128-row tiles), the others quantise X, 64 blocks each.  Two launches of 4 to 5
+// us in one.
+__global__ __launch_bounds__(kMTilesThreads) void quant_prepare_kernel(const int32_t* __restrict__ offsets, int E,
+                                                                      int log2_rows, int32_t* __restrict__ out,
+                                                                      int32_t* __restrict__ out128,
+                                                                      const uint16_t* __restrict__ X, int units,
+                                                                      int blocks, uint8_t* __restrict__ q,
+                                                                      uint8_t* __restrict__ scale) {
+  __shared__ int pf[4097], pp[4097];
+  __shared__ int scan_lds[kMTilesThreads / 64];
+  const int lists = out128 ? 2 : 1;
+  if ((int)blockIdx.x < lists) {
+    mtiles_body(offsets, E, blockIdx.x ? 7 : log2_rows, blockIdx.x ? out128 : out, pf, pp, scan_lds);
+    return;
+  }
+  const int u = (blockIdx.x - lists) * (kMTilesThreads / 16) + (threadIdx.x >> 4);
+  if (u < units) quantize_unit(X, u, blocks, kQBlock * blocks, q_stride(blocks), q, scale);
+}
+
 constexpr int kMTileLog2 = 8;
 static_assert(1 << kMTileLog2 == kMTile);
 hipError_t launch_mtiles(const int32_t* offsets, int E, int rows, int32_t* out, hipStream_t s) {
@@ -151,13 +171,13 @@ hipError_t launch_mtiles(const int32_t* offsets, int E, int rows, int32_t* out, 
 // and none where that is 0, so a rounding to large tiles leaves fewer experts than
 // the token choice's (with E m-tiles expected, T = 643, d = 1792, n = 448, E = 88, K
 // = 3 rounded to 256, about ten experts left: dH in 256 wide tiles 56 us, in 64 26).
-int64_t expected_mtiles(const moe_dims& m, const moe_routing& r) {
+int64_t expected_mtiles(const moe_dims& m, const moe_routing& r, int tile_rows) {
   const int64_t rows = (int64_t)m.T * m.K;
   const int t = rounding_tile(r);
-  if (t == 0 || rows > 2 * kMTile * (int64_t)m.E) return std::max<int64_t>(m.E, rows / kMTile + m.E / 2);
+  if (t == 0 || rows > 2 * tile_rows * (int64_t)m.E) return std::max<int64_t>(m.E, rows / tile_rows + m.E / 2);
   const int64_t lo = rows / m.E / t * t, hi = lo + t;
   auto tiles = [&](int64_t f) -> double {
-    return t >= 128 ? (f + kMTile - 1) / kMTile : f ? std::max(1., f / (double)kMTile + .5) : 0.;
+    return t >= 128 ? (f + tile_rows - 1) / tile_rows : f ? std::max(1., f / (double)tile_rows + .5) : 0.;
   };
   double up = (rows / (double)m.E - lo) / t;  // share of the experts rounded up
   if (rounding_mode(r) == MOE_ROUND_UP) up = hi <= m.T;
@@ -2025,37 +2045,50 @@ hipError_t launch_down_ablation(const DownArgs& a, int strategy, hipStream_t s) 
   return launch_down(a, s);
 }
 
-#ifdef V1
-using F128u = GemmCfg<128, 256, 2, 4, 3>;
-using F128d = GemmCfg<128, 256, 2, 4, 3>;
-#elif defined(V2)
-using F128u = GemmCfg<128, 256, 2, 4, 2>;
-using F128d = GemmCfg<128, 128, 2, 2, 2, kBK, 2>;
-#elif defined(V3)
-using F128u = GemmCfg<128, 256, 2, 4, 3>;
-using F128d = GemmCfg<128, 128, 4, 2, 4>;
-#elif defined(V4)
-using F128u = GemmCfg<128, 256, 4, 2, 3>;
-using F128d = GemmCfg<128, 128, 4, 2, 2, kBK, 2>;
-#else
-using F128u = GemmCfg<128, 256, 2, 4, 3>;
-using F128d = GemmCfg<128, 256, 2, 4, 3>;
-#endif
-int quant_tile_rows(const moe_dims& m, int64_t mt) {
-#ifdef VF
-  return VF;
-#else
-  return 256;
-#endif
+// Tiles of the 8-bit projections: 256 x 256, or 128 rows where an expert has few.
+//   up    128 x 256, where the mean is at most 128 rows and they take no more rounds:
+//         us, 256 rows / 128:  d = 1536, n = 512, E = 64   mean 50: 30.6 / 27.1   111: 33.4 / 37.4   219: 52 / 54
+//                              d = 1024, n = 256, E = 64   mean 125: 21 / 16.8    250: 22 / 26.8
+//                              d = 4096, n = 512, E = 128  mean 62: 142 / 132     125: 141 / 161
+//   down  128 x 128, two workgroups to a CU, where the mean is at most 96 rows; and in
+//         up to four rounds, by rounds times time (58% of a 256 x 256 tile's over a
+//         short k, 67% over a long one), beyond which only the tile's own rate counts:
+//                              d = 1536, n = 512, E = 64   mean 50: 22.4 / 17.6   111: 25.2 / 21.8   500: 54 / 58
+//                              d = 1024, n = 256, E = 64   mean 250: 18.7 / 15.1  500: 26.3 / 22.6
+//                              d = 4096, n = 512, E = 128  mean 62: 73.8 / 68.5   125: 88 / 96   250: 143 / 152
+//                              d = 4096, n = 14336, E = 8  mean 1024: 608 / 686
+using F128x256 = GemmCfg<128, 256, 4, 2, 3>;
+using F128x128 = GemmCfg<128, 128, 4, 2, 2, kBK, 2>;
+QuantTiles quant_tiles(const moe_dims& m, const moe_routing& r) {
+  const int64_t mt256 = expected_mtiles(m, r, 256), mt128 = expected_mtiles(m, r, 128), cus = cu_count();
+  auto rounds = [](int64_t tiles, int64_t slots) { return (tiles + slots - 1) / slots; };
+  QuantTiles q{256, 256};
+  const int nu = q_blocks(m.n);
+  if ((int64_t)m.T * m.K <= 128 * (int64_t)m.E && rounds(mt128 * nu, cus) <= rounds(mt256 * nu, cus)) q.up = 128;
+  const int64_t wide = rounds(mt256 * n_tiles(m.d, 256), cus), narrow = rounds(mt128 * (m.d / 128), 2 * cus);
+  if ((int64_t)m.T * m.K <= 96 * (int64_t)m.E || (wide <= 4 && narrow * (m.n <= 1024 ? 58 : 67) < 97 * wide)) q.down = 128;
+  return q;
 }
-hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s) {
-  const int grid = pad8(mtiles_bound(a.capacity, a.E, a.tile_rows) * q_blocks(a.n));
-  return a.tile_rows == 128 ? run<OpUp8<F128u>>({a}, grid, s) : run<OpUp8<C256x256w>>({a}, grid, s);
+
+hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s) {
+  if (a.E > 4096) return hipErrorInvalidValue;
+  const bool two = a.tiles.up != a.tiles.down;
+  const int blocks = a.d / kQBlock, units = T * blocks, per = kMTilesThreads / 16;
+  quant_prepare_kernel<<<1 + two + (units + per - 1) / per, kMTilesThreads, 0, s>>>(
+      a.offsets, a.E, two || a.tiles.up == 256 ? 8 : 7, a.mtiles, two ? a.mtiles128 : nullptr, a.X, units, blocks, a.X8, a.Xs);
+  return hipGetLastError();
 }
-hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s) {
-  const int mt = mtiles_bound(a.capacity, a.E, a.tile_rows);
-  return a.tile_rows == 128 ? run<OpDown8<F128d>>({a}, pad8(mt * n_tiles(a.d, F128d::BN)), s)
-                            : run<OpDown8<C256x256w>>({a}, pad8(mt * n_tiles(a.d, 256)), s);
+hipError_t launch_quant_up(QuantArgs a, hipStream_t s) {
+  const int grid = pad8(mtiles_bound(a.capacity, a.E, a.tiles.up) * q_blocks(a.n));
+  if (a.tiles.up == 256) return run<OpUp8<C256x256w>>({a}, grid, s);
+  if (a.tiles.down == 256) a.mtiles = a.mtiles128;
+  return run<OpUp8<F128x256>>({a}, grid, s);
+}
+hipError_t launch_quant_down(QuantArgs a, hipStream_t s) {
+  const int mt = mtiles_bound(a.capacity, a.E, a.tiles.down);
+  if (a.tiles.down == 256) return run<OpDown8<C256x256w>>({a}, pad8(mt * n_tiles(a.d, 256)), s);
+  if (a.tiles.up == 256) a.mtiles = a.mtiles128;
+  return run<OpDown8<F128x128>>({a}, pad8(mt * (a.d / 128)), s);
 }
 
 int dh_n_tiles(int n, int64_t mt) { return n_tiles(n, tile_width(kTimesDH, mt, n)); }

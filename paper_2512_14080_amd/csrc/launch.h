@@ -91,7 +91,7 @@ inline int rounding_mode(const moe_routing& r) { return r.reserved >> 16; }
 constexpr int kMTile = 256;  // rows of an m-tile
 size_t mtiles_bytes(int64_t capacity, int E, int rows = kMTile);
 // about how many m-tiles a routing has
-int64_t expected_mtiles(const moe_dims& m, const moe_routing& r);
+int64_t expected_mtiles(const moe_dims& m, const moe_routing& r, int tile_rows = kMTile);
 hipError_t launch_mtiles(const int32_t* offsets, int E, int rows, int32_t* out, hipStream_t s);
 
 // mt: the m-tiles to expect (expected_mtiles), for the choice of the tiles; capacity
@@ -222,20 +222,23 @@ struct QExpertsArgs {
 hipError_t launch_quantize_experts(const QExpertsArgs& a, hipStream_t s);
 hipError_t launch_dequantize_experts(const QExpertsArgs& a, hipStream_t s);
 
-// The 8-bit projections: launch_quant_up writes A8, As (and H8, Hs where
-// given) from X8, Xs; launch_quant_down Y from A8, As.
+// The 8-bit projections: launch_quant_prepare writes X8, Xs and the m-tile lists,
+// launch_quant_up A8, As (and H8, Hs where given) from them, launch_quant_down Y.
+struct QuantTiles { int up, down; };  // rows of the tiles, 256 or 128
+QuantTiles quant_tiles(const moe_dims& m, const moe_routing& r);
 struct QuantArgs {
-  const uint16_t* X; const uint8_t* X8; const uint8_t* Xs;
+  const uint16_t* X; uint8_t* X8; uint8_t* Xs;
   const uint8_t* W1q; const uint8_t* W1s; const uint8_t* W2q; const uint8_t* W2s;
-  const int32_t* offsets; const int32_t* row_token; const int32_t* mtiles;
+  const int32_t* offsets; const int32_t* row_token;
+  int32_t* mtiles; int32_t* mtiles128;  // (the second where the two differ)
   const float* b1; const float* b2;
   float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
-  int d, n, E, capacity, tile_rows;  // (tile_rows: of the m-tile list)
+  int d, n, E, capacity;
+  QuantTiles tiles;
 };
-// rows of the tiles of the 8-bit projections: 256, or 128
-int quant_tile_rows(const moe_dims& m, int64_t mt);
-hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s);
-hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s);
+hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s);
+hipError_t launch_quant_up(QuantArgs a, hipStream_t s);
+hipError_t launch_quant_down(QuantArgs a, hipStream_t s);
 // The same for few rows per expert, from X in bf16 (stream_gemm.hip); stream8_shape:
 // mb = 0 where the tiled ones are the better ones
 StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile);

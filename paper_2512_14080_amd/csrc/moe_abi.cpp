@@ -207,6 +207,7 @@ struct QuantWs {
   uint8_t* As;
   uint16_t* Y;
   int32_t* mtiles;
+  int32_t* mtiles128;
 };
 size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   const int np = smoe::q_pad(m.n);
@@ -218,6 +219,7 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
   off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);
   off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles : nullptr);
+  off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles128 : nullptr);
   return off;
 }
 
@@ -892,17 +894,16 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   if (c) c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
   uint8_t* X8 = c && c->X ? c->X : w.X8;
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
-  const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles,
+  const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles, w.mtiles128,
                           eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A32, w.A8, w.As, c ? c->H : nullptr,
-                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity, smoe::quant_tile_rows(m, smoe::expected_mtiles(m, *r))};
+                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity, smoe::quant_tiles(m, *r)};
   // (what is kept is written by the tiled projections)
   const smoe::StreamShape few = c ? smoe::StreamShape{0, 0} : smoe::stream8_shape(m, r->capacity, smoe::rounding_tile(*r));
   if (few.mb) {
     LAUNCH(MOE_KC_UP_QUANT, smoe::launch_stream8_up(a, few, stream), "8-bit up-proj");
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_stream8_down(a, few, stream), "8-bit down-proj");
   } else {
-    LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, X8, Xs, stream), "quantize X");
-    HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, a.tile_rows, w.mtiles, stream), "m-tile list");
+    LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quant_prepare(a, m.T, stream), "quantize X and m-tile lists");
     LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
   }

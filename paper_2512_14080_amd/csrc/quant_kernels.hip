@@ -8,26 +8,11 @@ namespace smoe {
 constexpr int kRowThreads = 256;
 
 // ---------------------------------------------------------------- rows
-// 16 lanes per block of 128 columns, 8 columns (16 bytes) each: the largest |x| of
-// the block is a maximum over the lane's values and the 16 lanes.
 __global__ __launch_bounds__(kRowThreads) void quantize_rows_kernel(const uint16_t* __restrict__ X, int units, int blocks,
                                                                     int cols, int stride, uint8_t* __restrict__ q,
                                                                     uint8_t* __restrict__ scale) {
-  const int u = blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4), l = threadIdx.x & 15;
-  if (u >= units) return;
-  const int row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
-  u32x4 v = {0, 0, 0, 0};
-  if (c < cols) v = *(const u32x4*)(X + (size_t)row * cols + c);
-  const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
-  uint32_t m = finite_amax_bf16(w);
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 16));
-  const int sb = scale_byte(m << 16);
-  const float sv = scale_value(sb);
-  const u32x2 out = {pack_fp8x4_bf16(v[0], v[1], sv), pack_fp8x4_bf16(v[2], v[3], sv)};
-  if (c < cols) *(u32x2*)(q + (size_t)row * cols + c) = out;
-  // (the last block's first lanes also fill the row's scales to a whole dword)
-  if (l == 0 || (b == blocks - 1 && b + l < stride)) scale[(size_t)row * stride + b + l] = l ? 127 : sb;
+  const int u = blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4);
+  if (u < units) quantize_unit(X, u, blocks, cols, stride, q, scale);
 }
 
 __global__ __launch_bounds__(kRowThreads) void dequantize_rows_kernel(const uint8_t* __restrict__ q,

@@ -301,6 +301,11 @@ struct StreamDown {
 // A rounded routing's experts have no rows or m_tile and more, whatever the mean:
 //   T = 512, d = 1536, n = 256, E = 256, K = 8 (mean 16), rounded up to 256:
 //   forward call 1088 us streaming, 350 tiled; d = 4096, n = 512, up to 128: 2923, 826
+static StreamShape stream_groups(const moe_dims& m, int capacity, int mb) {
+  // further groups of at most `capacity` rows over experts of at most T
+  const int64_t rows = 16 * mb, further = std::min(capacity / rows, m.E * ((m.T - 1) / rows));
+  return m.E + further <= 65535 ? StreamShape{mb, (int)further} : StreamShape{0, 0};
+}
 StreamShape stream_shape(const moe_dims& m, int capacity, int m_tile, int64_t tiles_per_expert) {
   const StreamShape tiled{0, 0};
   if ((int64_t)m.d * 2 * m.n > INT32_MAX) return tiled;  // 32-bit offsets within an expert's weights
@@ -315,9 +320,7 @@ StreamShape stream_shape(const moe_dims& m, int capacity, int m_tile, int64_t ti
     mb = 4;
   else
     return tiled;
-  // further groups of at most `capacity` rows over experts of at most T
-  const int64_t rows = 16 * mb, further = std::min(capacity / rows, m.E * ((m.T - 1) / rows));
-  return m.E + further <= 65535 ? StreamShape{mb, (int)further} : tiled;
+  return stream_groups(m, capacity, mb);
 }
 
 // Partial router logits of k slice y: part[y][t][e] = sum over the slice of X W_r
@@ -638,31 +641,38 @@ static hipError_t run_stream8(const QuantArgs& p, const StreamShape& t, int cols
 //     d = 1024, n = 256, E = 64, T = 64       9.2           10.3    10.9     10.4
 //     d = 1536, n = 256, E = 128, T = 128     22.9          24.1    21.9     25.1
 //     d = 4096, n = 512, E = 128, T = 256     117           119     112      125
-//   down                                     64, 2 waves   64, 4   128, 1   128, 2   128, 4
-//     d = 1536, n = 256, E = 128, T = 1       3.8           4.3              3.9      5.1
-//     d = 4096, n = 512, E = 128, T = 64      44.6          44.9             44.1     40.8
-//     d = 1024, n = 256, E = 64, T = 64       7.0           8.1     7.8      6.9      6.9
-//     d = 1536, n = 256, E = 128, T = 128     14.6          17.1    12.6     16.1     15.4
-//     d = 2048, n = 128, E = 256, T = 128     17.9          26.0    15.1     18.0     24.1
-//     d = 4096, n = 512, E = 128, T = 256     71.5          72.9    58.9     59.0     59.8
+//     d = 1536, n = 1024, E = 16, K = 2, T = 512     34.1   39.7     31.6
+//   and one token (d = 1536, n = 256, 8 rows): 64 columns and 8 waves 8.4, 32 and 16 waves
+//   6.4; d = 4096, n = 512: 19.6, 14.3; but d = 4096, n = 14336, 2 rows (the CUs are full): 40, 52
+//   down                                     32, 2   64, 2   64, 4   128, 1   128, 2   128, 4
+//     d = 1536, n = 256, E = 128, T = 1       3.6     3.9     4.2              3.9      5.1
+//     d = 4096, n = 14336, E = 8, T = 1       47.6    60.4    35.4 (32, 4 waves: 32.1)
+//     d = 4096, n = 512, E = 128, T = 64              44.6    44.9             44.1     40.8
+//     d = 1024, n = 256, E = 64, T = 64               7.0     8.1     7.8      6.9      6.9
+//     d = 1536, n = 256, E = 128, T = 128             14.6    17.1    12.6     16.1     15.4
+//     d = 2048, n = 128, E = 256, T = 128             17.9    26.0    15.1     18.0     24.1
+//     d = 4096, n = 512, E = 128, T = 256             71.5    72.9    58.9     59.0     59.8
 hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
+  if (t.mb == 1 && (int64_t)a.capacity * (a.n / 32) <= 128) return run_stream8<Stream8Up, 2, 1, 16, 4>(a, t, a.n, s);
   if (t.mb == 1) return run_stream8<Stream8Up, 4, 1, 8, 4>(a, t, a.n, s);
-  if (t.mb == 2) return run_stream8<Stream8Up, 4, 2, 4, 4>(a, t, a.n, s);
-  return run_stream8<Stream8Up, 4, 4, 4, 2>(a, t, a.n, s);
+  return run_stream8<Stream8Up, 4, 2, 4, 4>(a, t, a.n, s);
 }
 hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
   const int blocks = q_blocks(a.n);
-  if (t.mb == 1 && blocks <= 2) return run_stream8<Stream8Down, 4, 1, 2, 4>(a, t, a.d, s);
-  if (t.mb == 1) return run_stream8<Stream8Down, 4, 1, 4, 4>(a, t, a.d, s);
-  if (t.mb == 2 && blocks <= 2 && a.E * (a.d / kQBlock) > 768) return run_stream8<Stream8Down, 8, 2, 1, 2>(a, t, a.d, s);
-  if (t.mb == 2) return run_stream8<Stream8Down, 8, 2, 2, 2>(a, t, a.d, s);
-  return run_stream8<Stream8Down, 4, 4, 4, 2>(a, t, a.d, s);
+  if (t.mb == 1 && blocks <= 2) return run_stream8<Stream8Down, 2, 1, 2, 4>(a, t, a.d, s);
+  if (t.mb == 1) return run_stream8<Stream8Down, 2, 1, 4, 4>(a, t, a.d, s);
+  if (blocks <= 2 && a.E * (a.d / kQBlock) > 768) return run_stream8<Stream8Down, 8, 2, 1, 2>(a, t, a.d, s);
+  return run_stream8<Stream8Down, 8, 2, 2, 2>(a, t, a.d, s);
 }
 
-// up's tiles decide for both, since A passes between the two in one of two forms
+// up's tiles decide for both, since A passes between the two in one of two forms; two
+// row blocks where the 16-bit products take four (d = 1536, n = 1024, E = 16, 32 rows
+// each: up 21.1 / 21.3 us, down 16.5 / 19.1)
 StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile) {
   if (2 * (int64_t)m.d * q_pad(m.n) > INT32_MAX) return {0, 0};  // 32-bit offsets within an expert's codes
-  return stream_shape(m, capacity, m_tile, q_blocks(m.n));
+  StreamShape t = stream_shape(m, capacity, m_tile, q_blocks(m.n));
+  if (t.mb == 4) t = stream_groups(m, capacity, 2);
+  return t;
 }
 
 }  // namespace smoe
