@@ -92,7 +92,7 @@ constexpr int kMTile = 256;  // rows of an m-tile
 size_t mtiles_bytes(int64_t capacity, int E, int rows = kMTile);
 // about how many m-tiles a routing has
 int64_t expected_mtiles(const moe_dims& m, const moe_routing& r, int tile_rows = kMTile);
-hipError_t launch_mtiles(const int32_t* offsets, int E, int rows, int32_t* out, hipStream_t s);
+hipError_t launch_mtiles(const int32_t* offsets, int E, int32_t* out, hipStream_t s);
 
 // mt: the m-tiles to expect (expected_mtiles), for the choice of the tiles; capacity
 // bounds the rows.

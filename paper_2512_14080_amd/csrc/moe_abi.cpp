@@ -336,7 +336,7 @@ struct Projections {
       : up(smoe::stream_shape(m, r.capacity, smoe::rounding_tile(r), (2 * m.n + 255) / 256)),
         down(smoe::stream_shape(m, r.capacity, smoe::rounding_tile(r), (m.d + 255) / 256)) {}
   hipError_t lists(const int32_t* offsets, int E, int32_t* mtiles, hipStream_t s) const {
-    return up.mb && down.mb ? hipSuccess : smoe::launch_mtiles(offsets, E, smoe::kMTile, mtiles, s);
+    return up.mb && down.mb ? hipSuccess : smoe::launch_mtiles(offsets, E, mtiles, s);
   }
   hipError_t run_up(const smoe::UpArgs& a, hipStream_t s) const {
     return up.mb ? smoe::launch_stream_up(a, up, s) : smoe::launch_up(a, s);
@@ -937,7 +937,7 @@ int moe_fwd_ckpt(moe_dims m, const moe_bf16* X, const moe_bf16* W1, const moe_bf
   c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
   const int64_t mt = smoe::expected_mtiles(m, *r);
   if (c->X) LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, c->X, c->Xs, stream), "quantize X");
-  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, smoe::kMTile, w.mtiles, stream), "m-tile list");
+  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
   LAUNCH(MOE_KC_UP,
          smoe::launch_up_ckpt({X, W1, r->offsets, r->row_token, nullptr, w.A, m.d, m.n, m.E, r->capacity, mt, w.mtiles,
                                eb ? eb->b1 : nullptr, c->H, c->Hs},

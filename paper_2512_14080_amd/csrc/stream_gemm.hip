@@ -665,14 +665,23 @@ hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStre
   return run_stream8<Stream8Down, 8, 2, 2, 2>(a, t, a.d, s);
 }
 
-// up's tiles decide for both, since A passes between the two in one of two forms; two
-// row blocks where the 16-bit products take four (d = 1536, n = 1024, E = 16, 32 rows
-// each: up 21.1 / 21.3 us, down 16.5 / 19.1)
+// One rule for both projections, since A passes between the two in one of two forms.
+// us a call, streaming / tiled (128-row tiles, gemm_ops.hip), by rows per expert:
+//                                  8          12         16         20
+//   d = 768, n = 256, E = 128      25 / 27    26 / 28    29 / 28
+//   d = 1024, n = 256, E = 64      20 / 24    22 / 25               24 / 25
+//   d = 1536, n = 256, E = 512     131 / 130  142 / 133  152 / 134
+//   d = 2048, n = 512, E = 64                 56 / 53    59 / 55    63 / 55
+//   d = 4096, n = 256, E = 256                176 / 197  187 / 199  200 / 200
+//   d = 4096, n = 512, E = 128     163 / 190  172 / 194  183 / 192  194 / 196
+//   d = 4096, n = 1024, E = 64                176 / 187  183 / 187  195 / 189
+//   d = 4096, n = 4096, E = 16                180 / 198  189 / 198  197 / 199
+//   d = 4096, n = 14336, E = 8     288 / 293  303 / 294  320 / 296
 StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile) {
   if (2 * (int64_t)m.d * q_pad(m.n) > INT32_MAX) return {0, 0};  // 32-bit offsets within an expert's codes
-  StreamShape t = stream_shape(m, capacity, m_tile, q_blocks(m.n));
-  if (t.mb == 4) t = stream_groups(m, capacity, 2);
-  return t;
+  const int64_t mean = std::max<int64_t>(((int64_t)m.T * m.K + m.E - 1) / m.E, m_tile);
+  if (m.T <= 16 || mean <= 2) return stream_groups(m, capacity, 1);
+  return mean <= (m.d >= 4096 && m.n <= 4096 ? 16 : 10) ? stream_groups(m, capacity, 2) : StreamShape{0, 0};
 }
 
 }  // namespace smoe
