@@ -117,4 +117,21 @@ __device__ __forceinline__ void quantize_unit(const uint16_t* __restrict__ X, in
   if (l == 0 || (b == blocks - 1 && b + l < stride)) scale[(size_t)row * stride + b + l] = l ? 127 : sb;
 }
 
+// and back
+__device__ __forceinline__ void dequantize_unit(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scale, int u,
+                                                int blocks, int cols, int stride, uint16_t* __restrict__ X) {
+  const int l = threadIdx.x & 15, row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
+  if (c >= cols) return;
+  const float s = scale_value(scale[(size_t)row * stride + b]);
+  const u32x2 v = *(const u32x2*)(q + (size_t)row * cols + c);
+  u32x4 out;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const f32x4 x = unpack_fp8x4(v[i], s);
+    out[2 * i] = pack_bf2(x[0], x[1]);
+    out[2 * i + 1] = pack_bf2(x[2], x[3]);
+  }
+  *(u32x4*)(X + (size_t)row * cols + c) = out;
+}
+
 }  // namespace smoe

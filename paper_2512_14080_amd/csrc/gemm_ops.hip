@@ -145,9 +145,10 @@ __global__ __launch_bounds__(kMTilesThreads) void mtiles_kernel(const int32_t* _
   mtiles_body(offsets, E, kMTileLog2, out, pf, pp, scan_lds);
 }
 
-// The 8-bit forward's first launch: workgroup 0 writes the m-tile list (and 1 a second
-// one, of 128-row tiles), the others quantise X, 64 blocks each.  Two launches of 4 to 5
-// us in one.
+// The first launch of a forward that quantises X: workgroup 0 writes the m-tile list
+// (and 1 a second one, of 128-row tiles), the others quantise X, 64 blocks each.  Two
+// launches of 4 to 5 us in one.  BY_EXPERT: of the 8-bit projections, else of the 16-bit ones.
+template <bool BY_EXPERT>
 __global__ __launch_bounds__(kMTilesThreads) void quant_prepare_kernel(const int32_t* __restrict__ offsets, int E,
                                                                       int log2_rows, int32_t* __restrict__ out,
                                                                       int32_t* __restrict__ out128,
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(kMTilesThreads) void quant_prepare_kernel(const int
   __shared__ int scan_lds[kMTilesThreads / 64];
   const int lists = out128 ? 2 : 1;
   if ((int)blockIdx.x < lists) {
-    mtiles_body<true>(offsets, E, blockIdx.x ? kMTileLog2 - 1 : log2_rows, blockIdx.x ? out128 : out, pf, pp, scan_lds);
+    mtiles_body<BY_EXPERT>(offsets, E, blockIdx.x ? kMTileLog2 - 1 : log2_rows, blockIdx.x ? out128 : out, pf, pp, scan_lds);
     return;
   }
   const int u = (blockIdx.x - lists) * (kMTilesThreads / 16) + (threadIdx.x >> 4);
@@ -306,14 +307,16 @@ __device__ __forceinline__ void kchunks_body(const int32_t* __restrict__ offsets
 }
 
 // The backward's tile lists in one launch: workgroup 0 the m-tile list,
-// 1 and 2 the k-chunk lists of dW2 and dW1.
+// 1 and 2 the k-chunk lists of dW2 and dW1; the next ones transpose W_r, and the last
+// give an X kept in 8 bits its bf16 form (tr_blocks and kept.units may be 0).
 static_assert(kMTilesThreads == kKChunksThreads, "one workgroup size");
 __global__ __launch_bounds__(kMTilesThreads) void bwd_lists_kernel(const int32_t* __restrict__ offsets, int E,
                                                                   int32_t* __restrict__ mtiles, int tpe2, int slabs2, int keep2,
                                                                   int32_t* __restrict__ klist2, int tpe1, int slabs1, int keep1,
                                                                   int32_t* __restrict__ klist1,
                                                                   const uint16_t* __restrict__ Wr,
-                                                                  uint16_t* __restrict__ WrT, int d) {
+                                                                  uint16_t* __restrict__ WrT, int d, int tr_blocks,
+                                                                  const KeptX kept) {
   __shared__ int lds[2 * 4097];
   __shared__ int scan_lds[kMTilesThreads / 64];
   __shared__ int sh_kc;
@@ -323,6 +326,10 @@ __global__ __launch_bounds__(kMTilesThreads) void bwd_lists_kernel(const int32_t
     kchunks_body(offsets, E, tpe2, slabs2, keep2, klist2, lds, scan_lds, &sh_kc);
   } else if (blockIdx.x == 2) {
     kchunks_body(offsets, E, tpe1, slabs1, keep1, klist1, lds, scan_lds, &sh_kc);
+  } else if ((int)blockIdx.x >= 3 + tr_blocks) {
+    const int u = (blockIdx.x - 3 - tr_blocks) * (kMTilesThreads / 16) + (threadIdx.x >> 4);
+    const int blocks = d / kQBlock;
+    if (u < kept.units) dequantize_unit(kept.q, kept.scale, u, blocks, d, q_stride(blocks), kept.X);
   } else {  // W_r transpose, one element per thread
     const int idx = (blockIdx.x - 3) * kMTilesThreads + threadIdx.x;
     if (idx < d * E) {
@@ -1358,9 +1365,9 @@ struct F8Rows {
 // N tile: 128 gate columns and the matching up columns, in the order the weights
 // are laid out in: accumulator column blocks alternate between 32 gate and 32 up
 // columns.  A leaves as codes of blocks of 128: the WN waves of a row group hold
-// 128 / WN columns each, and their largest |A| meet in LDS (as do H's where it is
-// kept).
-template <class Cfg_>
+// 128 / WN columns each, and their largest |A| meet in LDS (as do H's, where
+// KEEP writes it to the checkpoint).
+template <class Cfg_, bool KEEP>
 struct OpUp8 : F8Rows {
   using Cfg = Cfg_;
   static constexpr int W_SCALES = 2, WN = Cfg::WN, CB = Cfg::RN / 2;  // CB: blocks of 32 gate columns of a wave
@@ -1368,7 +1375,7 @@ struct OpUp8 : F8Rows {
   struct Params { QuantArgs a; };
   static constexpr int IDX_LDS = Cfg::NW * Cfg::QM * 256;
   static constexpr int EPI_LDS = 3 * WN * Cfg::BM * 4;  // [gate, up, A][column group][row]
-  static constexpr int EPI_STORES = Cfg::RM * CB;       // A's
+  static constexpr int EPI_STORES = Cfg::RM * CB * (KEEP ? 3 : 1);  // A's codes, and H's
   static __device__ int count(const Params& p, int*) { return count_varlen_m<256>(p.a.mtiles, 2 * q_pad(p.a.n)); }
   static __device__ int count_tail(const Params& p, const int*) {
     return count_varlen_m_tail<256>(p.a.mtiles, 2 * q_pad(p.a.n));
@@ -1441,7 +1448,7 @@ struct OpUp8 : F8Rows {
             for (int r = 0; r < 4; ++r) t.acc[i][j][4 * g + r] += v[r];
         }
     }
-    if (a.H8) {
+    if constexpr (KEEP) {
 #pragma unroll
       for (int i = 0; i < Cfg::RM; ++i)
 #pragma unroll
@@ -2079,15 +2086,24 @@ hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s) {
   if (a.E > 4096) return hipErrorInvalidValue;
   const bool two = a.tiles.up != a.tiles.down;
   const int blocks = a.d / kQBlock, units = T * blocks, per = kMTilesThreads / 16;
-  quant_prepare_kernel<<<1 + two + (units + per - 1) / per, kMTilesThreads, 0, s>>>(
-      a.offsets, a.E, two || a.tiles.up == 256 ? kMTileLog2 : kMTileLog2 - 1, a.mtiles, two ? a.mtiles128 : nullptr, a.X, units, blocks, a.X8, a.Xs);
+  quant_prepare_kernel<true><<<1 + two + (units + per - 1) / per, kMTilesThreads, 0, s>>>(
+      a.offsets, a.E, two || a.tiles.up == 256 ? kMTileLog2 : kMTileLog2 - 1, a.mtiles, two ? a.mtiles128 : nullptr, a.X,
+      units, blocks, a.X8, a.Xs);
+  return hipGetLastError();
+}
+hipError_t launch_ckpt_prepare(const int32_t* offsets, int E, int32_t* mtiles, const uint16_t* X, int T, int d, uint8_t* X8,
+                               uint8_t* Xs, hipStream_t s) {
+  if (E > 4096) return hipErrorInvalidValue;
+  const int blocks = d / kQBlock, units = T * blocks, per = kMTilesThreads / 16;
+  quant_prepare_kernel<false><<<1 + (units + per - 1) / per, kMTilesThreads, 0, s>>>(offsets, E, kMTileLog2, mtiles, nullptr,
+                                                                                   X, units, blocks, X8, Xs);
   return hipGetLastError();
 }
 hipError_t launch_quant_up(QuantArgs a, hipStream_t s) {
   const int grid = pad8(mtiles_bound(a.capacity, a.E, a.tiles.up) * q_blocks(a.n));
-  if (a.tiles.up == 256) return run<OpUp8<C256x256w>>({a}, grid, s);
+  if (a.tiles.up == 256) return a.H8 ? run<OpUp8<C256x256w, true>>({a}, grid, s) : run<OpUp8<C256x256w, false>>({a}, grid, s);
   if (a.tiles.down == 256) a.mtiles = a.mtiles128;
-  return run<OpUp8<F128x256>>({a}, grid, s);
+  return a.H8 ? run<OpUp8<F128x256, true>>({a}, grid, s) : run<OpUp8<F128x256, false>>({a}, grid, s);
 }
 hipError_t launch_quant_down(QuantArgs a, hipStream_t s) {
   const int mt = mtiles_bound(a.capacity, a.E, a.tiles.down);
@@ -2187,15 +2203,16 @@ static int kchunk_keep_whole(int E, int tpe) {
 }
 
 hipError_t launch_bwd_lists(const int32_t* offsets, int T, int64_t rows, int E, int d, int n, int32_t* mtiles, int32_t* klist2,
-                            int32_t* klist1, const uint16_t* Wr, uint16_t* WrT, hipStream_t s) {
+                            int32_t* klist1, const uint16_t* Wr, uint16_t* WrT, const KeptX& kept, hipStream_t s) {
   if (E > 4096) return hipErrorInvalidValue;
   const DwTile t2 = dw_tile(n, d, E, rows), t1 = dw_tile(d, 2 * n, E, rows);
   const int tpe2 = n_tiles(n, t2.bm) * n_tiles(d, t2.bn), tpe1 = n_tiles(d, t1.bm) * n_tiles(2 * n, t1.bn);
   const int tr_blocks = Wr ? (d * E + kMTilesThreads - 1) / kMTilesThreads : 0;
-  bwd_lists_kernel<<<3 + tr_blocks, kMTilesThreads, 0, s>>>(offsets, E, mtiles, tpe2, dw_slabs(T, (int64_t)n * d),
+  const int x_blocks = (kept.units + kMTilesThreads / 16 - 1) / (kMTilesThreads / 16);
+  bwd_lists_kernel<<<3 + tr_blocks + x_blocks, kMTilesThreads, 0, s>>>(offsets, E, mtiles, tpe2, dw_slabs(T, (int64_t)n * d),
                                                            kchunk_keep_whole(E, tpe2), klist2, tpe1,
                                                            dw_slabs(T, (int64_t)d * 2 * n), kchunk_keep_whole(E, tpe1),
-                                                           klist1, Wr, WrT, d);
+                                                           klist1, Wr, WrT, d, tr_blocks, kept);
   return hipGetLastError();
 }
 

@@ -165,8 +165,10 @@ inline size_t dw_part_bytes(int T, int64_t mn) { return (size_t)dw_slabs(T, mn) 
 // the backward's m-tile list (as launch_mtiles) and the k-chunk lists of dW2
 // and dW1, in one launch; with Wr non-null the same launch writes WrT[e][i] =
 // Wr[i][e] (the dX aggregation's router term reads W_r by expert)
+// with kept.units, X of a checkpoint into bf16.
+struct KeptX { const uint8_t* q; const uint8_t* scale; uint16_t* X; int units; };  // units: blocks of 128 columns
 hipError_t launch_bwd_lists(const int32_t* offsets, int T, int64_t rows, int E, int d, int n, int32_t* mtiles, int32_t* klist2,
-                            int32_t* klist1, const uint16_t* Wr, uint16_t* WrT, hipStream_t s);
+                            int32_t* klist1, const uint16_t* Wr, uint16_t* WrT, const KeptX& kept, hipStream_t s);
 
 struct DW2Args {
   const uint16_t* Ap; const uint16_t* dO; const int32_t* offsets; const int32_t* row_token; uint16_t* dW2;
@@ -237,6 +239,9 @@ struct QuantArgs {
   QuantTiles tiles;
 };
 hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s);
+// the m-tile list of the 16-bit projections, and X into 8-bit blocks
+hipError_t launch_ckpt_prepare(const int32_t* offsets, int E, int32_t* mtiles, const uint16_t* X, int T, int d, uint8_t* X8,
+                               uint8_t* Xs, hipStream_t s);
 hipError_t launch_quant_up(QuantArgs a, hipStream_t s);
 hipError_t launch_quant_down(QuantArgs a, hipStream_t s);
 // The same for few rows per expert, from X in bf16 (stream_gemm.hip); stream8_shape:

@@ -716,16 +716,17 @@ static int backward(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe
   else
     bwd_layout(m, r->capacity, (char*)ws, &w);
   hipStream_t stream = (hipStream_t)stream_;
+  smoe::KeptX kept{nullptr, nullptr, nullptr, 0};
   if (!X) {
-    LAUNCH(MOE_KC_QUANTIZE, smoe::launch_dequantize_rows(ck->X, ck->Xs, m.T, m.d, x16, stream), "kept X");
+    kept = smoe::KeptX{ck->X, ck->Xs, x16, m.T * (m.d / smoe::kQBlock)};
     X = x16;
   }
   float* dS_out = dS ? dS : w.dS;
   const int64_t rows = (int64_t)m.T * m.K, mt = smoe::expected_mtiles(m, *r);
   const int nnt = smoe::dh_n_tiles(m.n, mt);
   HIP_TRY(smoe::launch_bwd_lists(r->offsets, m.T, rows, m.E, m.d, m.n, w.mtiles, w.klist2, w.klist1, Wr, Wr ? w.WrT : nullptr,
-                                 stream),
-          "tile lists and W_r transpose");
+                                 kept, stream),
+          "tile lists, W_r transpose and the kept X");
   if (b2) {
     // <dO_t, b2_e> for every (t, e): dO times b2^T split into bf16 high and low parts
     HIP_TRY(smoe::launch_bias_split(b2, m.E, m.d, w.b2s, stream), "expert-bias split");
@@ -936,8 +937,11 @@ int moe_fwd_ckpt(moe_dims m, const moe_bf16* X, const moe_bf16* W1, const moe_bf
   hipStream_t stream = (hipStream_t)stream_;
   c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
   const int64_t mt = smoe::expected_mtiles(m, *r);
-  if (c->X) LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quantize_rows(X, m.T, m.d, c->X, c->Xs, stream), "quantize X");
-  HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
+  if (c->X)
+    LAUNCH(MOE_KC_QUANTIZE, smoe::launch_ckpt_prepare(r->offsets, m.E, w.mtiles, X, m.T, m.d, c->X, c->Xs, stream),
+           "quantize X and m-tile list");
+  else
+    HIP_TRY(smoe::launch_mtiles(r->offsets, m.E, w.mtiles, stream), "m-tile list");
   LAUNCH(MOE_KC_UP,
          smoe::launch_up_ckpt({X, W1, r->offsets, r->row_token, nullptr, w.A, m.d, m.n, m.E, r->capacity, mt, w.mtiles,
                                eb ? eb->b1 : nullptr, c->H, c->Hs},

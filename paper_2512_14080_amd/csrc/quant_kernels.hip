@@ -19,20 +19,8 @@ __global__ __launch_bounds__(kRowThreads) void dequantize_rows_kernel(const uint
                                                                       const uint8_t* __restrict__ scale, int units,
                                                                       int blocks, int cols, int stride,
                                                                       uint16_t* __restrict__ X) {
-  const int u = blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4), l = threadIdx.x & 15;
-  if (u >= units) return;
-  const int row = u / blocks, b = u - row * blocks, c = b * kQBlock + 8 * l;
-  if (c >= cols) return;
-  const float s = scale_value(scale[(size_t)row * stride + b]);
-  const u32x2 v = *(const u32x2*)(q + (size_t)row * cols + c);
-  u32x4 out;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const f32x4 x = unpack_fp8x4(v[i], s);
-    out[2 * i] = pack_bf2(x[0], x[1]);
-    out[2 * i + 1] = pack_bf2(x[2], x[3]);
-  }
-  *(u32x4*)(X + (size_t)row * cols + c) = out;
+  const int u = blockIdx.x * (kRowThreads / 16) + (threadIdx.x >> 4);
+  if (u < units) dequantize_unit(q, scale, u, blocks, cols, stride, X);
 }
 
 static int row_units(int64_t rows, int cols) { return (int)(rows * q_blocks(cols)); }
