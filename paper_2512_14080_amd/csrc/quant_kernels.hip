@@ -23,18 +23,19 @@ __global__ __launch_bounds__(kRowThreads) void dequantize_rows_kernel(const uint
   if (u < units) dequantize_unit(q, scale, u, blocks, cols, stride, X);
 }
 
-static int row_units(int64_t rows, int cols) { return (int)(rows * q_blocks(cols)); }
+static int row_units(int64_t rows, int cols) { return (int)(rows * q_blocks(cols)); }  // below 2^31
+static int row_groups(int units) { return (int)(((int64_t)units + kRowThreads / 16 - 1) / (kRowThreads / 16)); }
 
 hipError_t launch_quantize_rows(const uint16_t* X, int64_t rows, int cols, uint8_t* q, uint8_t* scale, hipStream_t s) {
-  const int units = row_units(rows, cols), per = kRowThreads / 16;
-  quantize_rows_kernel<<<(units + per - 1) / per, kRowThreads, 0, s>>>(X, units, q_blocks(cols), cols,
+  const int units = row_units(rows, cols);
+  quantize_rows_kernel<<<row_groups(units), kRowThreads, 0, s>>>(X, units, q_blocks(cols), cols,
                                                                        q_stride(q_blocks(cols)), q, scale);
   return hipGetLastError();
 }
 hipError_t launch_dequantize_rows(const uint8_t* q, const uint8_t* scale, int64_t rows, int cols, uint16_t* X,
                                   hipStream_t s) {
-  const int units = row_units(rows, cols), per = kRowThreads / 16;
-  dequantize_rows_kernel<<<(units + per - 1) / per, kRowThreads, 0, s>>>(q, scale, units, q_blocks(cols), cols,
+  const int units = row_units(rows, cols);
+  dequantize_rows_kernel<<<row_groups(units), kRowThreads, 0, s>>>(q, scale, units, q_blocks(cols), cols,
                                                                          q_stride(q_blocks(cols)), X);
   return hipGetLastError();
 }
