@@ -1500,12 +1500,14 @@ struct OpUp8 : F8Rows {
   }
 };
 
-template <class Cfg_>
+// PART: all tiles; those of DownRounds::whole; those of DownRounds::rest in quarters
+enum { kDownAll, kDownWhole, kDownQuarters };
+template <class Cfg_, int PART = kDownAll>
 struct OpDown8 : F8Rows {
   using Cfg = Cfg_;
   static constexpr int W_SCALES = 1;
   static_assert(Cfg::BN / Cfg::WN <= kQBlock, "a wave's columns lie in one block");
-  struct Params { QuantArgs a; };
+  struct Params { QuantArgs a; int slots; };  // slots: of DownRounds
   static constexpr int EPI_LDS = 0;
   static constexpr int EPI_STORES = kStoresPerFullTile<Cfg>;
   static __device__ int count(const Params& p, int*) { return count_varlen_m<Cfg::BN>(p.a.mtiles, p.a.d); }
@@ -1531,6 +1533,56 @@ struct OpDown8 : F8Rows {
   static __device__ void epilogue(const Params& p, const TileInfo& ti, Acc<Cfg>& t, char* epi) {
     if (p.a.b2) add_col_bias<Cfg>(t, p.a.b2 + (size_t)ti.e * p.a.d, ColOffset{ti.n0}, p.a.d);
     store_rows_bf16_any<Cfg>(p.a.Y, p.a.d, ti.row_base, ti.mrows, ti.n0, ti.ncols, t, epi);
+  }
+};
+
+// The end of a launch of 256 x 256 tiles with a long k: where the last round of an
+// XCD's `slots` workgroups holds at most half of them, its tiles run as quarters, in a
+// launch of their own (a tile's k stays in one, so the sums are the same).  A round
+// takes 200 us at n = 14336 and one of quarters with four stages 90; a second one starts
+// as the first one's workgroups end, and the quarters past an expert's last row end at
+// once (two stages, two workgroups to a CU: 135 for both).  us, d = 4096, n = 14336,
+// E = 8, whole / with quarters: T = 2048 418 / 328, 4096 600 / 491, 8192 1040 / 922.
+struct DownRounds {
+  int begin, whole, rest;  // an XCD's tiles: the first, those of the 256 x 256 launch, those in quarters
+  __device__ __forceinline__ DownRounds(const QuantArgs& a, int slots, int xcd) {
+    const int tiles = count_varlen_m<256>(a.mtiles, a.d), per = (tiles + 7) >> 3;  // as Sched::init
+    begin = xcd * per;
+    whole = max(0, min(per, tiles - begin));
+    rest = whole % slots;
+    if (2 * rest > slots) rest = 0;
+    whole -= rest;
+  }
+};
+template <class Cfg_>
+struct OpDown8<Cfg_, kDownWhole> : OpDown8<Cfg_> {
+  using Params = typename OpDown8<Cfg_>::Params;
+  static_assert(Cfg_::BM == 256 && Cfg_::BN == 256, "DownRounds");
+  static __device__ void xcd_range(const Params& p, int xcd, int* begin, int* count) {
+    const DownRounds r(p.a, p.slots, xcd);
+    *begin = r.begin;
+    *count = r.whole;
+  }
+};
+// (launched with 2 slots workgroups per XCD, so that none has a second tile)
+template <class Cfg_>
+struct OpDown8<Cfg_, kDownQuarters> : OpDown8<Cfg_> {
+  using Params = typename OpDown8<Cfg_>::Params;
+  static_assert(Cfg_::BM == 128 && Cfg_::BN == 128, "quarters of 256 x 256");
+  static __device__ void xcd_range(const Params& p, int xcd, int* begin, int* count) {
+    const DownRounds r(p.a, p.slots, xcd);
+    *begin = 4 * (r.begin + r.whole);
+    *count = 4 * r.rest;
+  }
+  static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
+    if (!tile_varlen_m<256, 256>(p.a.mtiles, p.a.E, p.a.d, q_pad(p.a.n) / 2, id >> 2, ti)) return false;
+    const int r0 = 128 * ((id >> 1) & 1), c0 = 128 * (id & 1);
+    ti.m0 += r0;
+    ti.row_base += r0;
+    ti.mrows = min(128, ti.mrows - r0);
+    ti.n0 += c0;
+    ti.ncols = min(128, ti.ncols - c0);
+    return ti.mrows > 0 && ti.ncols > 0;
   }
 };
 
@@ -1926,11 +1978,14 @@ static int cu_count() {
 }
 
 template <class Op>
+static int run_grid(int tiles_bound) {
+  return (std::min(tiles_bound, cu_count() * Op::Cfg::OCC) + 7) & ~7;
+}
+template <class Op>
 static hipError_t run(const typename Op::Params& p, int tiles_bound, hipStream_t s) {
   if (tiles_bound <= 0) return hipSuccess;
   using Cfg = typename Op::Cfg;
-  const int grid = (std::min(tiles_bound, cu_count() * Cfg::OCC) + 7) & ~7;
-  grouped_gemm_kernel<Op><<<dim3(grid), dim3(Cfg::THREADS), 0, s>>>(p);
+  grouped_gemm_kernel<Op><<<dim3(run_grid<Op>(tiles_bound)), dim3(Cfg::THREADS), 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -2071,6 +2126,10 @@ hipError_t launch_down_ablation(const DownArgs& a, int strategy, hipStream_t s) 
 //                              d = 4096, n = 14336, E = 8  mean 1024: 608 / 686
 using F128x256 = GemmCfg<128, 256, 4, 2, 3>;
 using F128x128 = GemmCfg<128, 128, 4, 2, 2, kBK, 2>;
+using F128x128q = GemmCfg<128, 128, 4, 2, 4>;
+// The launch of the quarters costs 1.5 us where no XCD has any; the gain where they have
+// some (us): 5 of 72 at n = 2048, 10 of 128 at 4096, 94 of 422 at 14336.
+constexpr int kQuartersMinK = 4096;
 QuantTiles quant_tiles(const moe_dims& m, const moe_routing& r) {
   const int64_t mt256 = expected_mtiles(m, r, 256), mt128 = expected_mtiles(m, r, 128), cus = cu_count();
   auto rounds = [](int64_t tiles, int64_t slots) { return (tiles + slots - 1) / slots; };
@@ -2107,9 +2166,16 @@ hipError_t launch_quant_up(QuantArgs a, hipStream_t s) {
 }
 hipError_t launch_quant_down(QuantArgs a, hipStream_t s) {
   const int mt = mtiles_bound(a.capacity, a.E, a.tiles.down);
-  if (a.tiles.down == 256) return run<OpDown8<C256x256w>>({a}, pad8(mt * n_tiles(a.d, 256)), s);
+  if (a.tiles.down == 256 && a.n >= kQuartersMinK) {
+    const int bound = pad8(mt * n_tiles(a.d, 256)), slots = run_grid<OpDown8<C256x256w, kDownWhole>>(bound) / 8;
+    const hipError_t err = run<OpDown8<C256x256w, kDownWhole>>({a, slots}, bound, s);
+    if (err != hipSuccess) return err;
+    grouped_gemm_kernel<OpDown8<F128x128q, kDownQuarters>><<<16 * slots, F128x128q::THREADS, 0, s>>>({a, slots});
+    return hipGetLastError();
+  }
+  if (a.tiles.down == 256) return run<OpDown8<C256x256w>>({a, 0}, pad8(mt * n_tiles(a.d, 256)), s);
   if (a.tiles.up == 256) a.mtiles = a.mtiles128;
-  return run<OpDown8<F128x128>>({a}, pad8(mt * (a.d / 128)), s);
+  return run<OpDown8<F128x128>>({a, 0}, pad8(mt * (a.d / 128)), s);
 }
 
 int dh_n_tiles(int n, int64_t mt) { return n_tiles(n, tile_width(kTimesDH, mt, n)); }

@@ -102,6 +102,19 @@ def test_tile_rows(tmp_path, dims, up, down):
     assert l[0][1] == 1 + (up != down) + -(-dims[0] * (dims[1] // 128) // per)
 
 
+@pytest.mark.parametrize("dims,quarters", [
+    ((4096, 4096, 14336, 8, 2), True), ((4096, 4096, 4096, 16, 2), True), ((4096, 4096, 4032, 16, 2), False),
+    ((300, 4096, 14336, 8, 2), False),  # in tiles of 128 rows
+])
+def test_the_last_round_of_a_long_k_in_quarters(tmp_path, dims, quarters):
+    l, = launches([(dims, "quant", 0, False)], tmp_path)
+    down = [(re.search(r"OpDown8INS_7GemmCfgILi(\d+)E.*EELi(\d)E", name).groups(), x) for name, x, _ in l if "OpDown8" in name]
+    if quarters:  # (a round may leave half of its workgroups' tiles, each four quarters)
+        assert [g for g, _ in down] == [("256", "1"), ("128", "2")] and [x for _, x in down] == [256, 512]
+    else:
+        assert len(down) == 1 and down[0][0][1] == "0"
+
+
 def test_kept_x_needs_no_launch_of_its_own(tmp_path):
     dims = (5003, 896, 192, 40, 3)
     fwd, fwd_x, bwd, bwd_x = launches([(dims, k, 0, x) for k in ("ckpt", "bwd") for x in (False, True)], tmp_path)

@@ -259,6 +259,38 @@ def test_forward_without_a_checkpoint(cfg, biased):
     assert (layer.ckpt.buf == 0xAB).all()
 
 
+def test_a_tokens_output_does_not_depend_on_its_tile():
+    """Many rows behind a long n: whole rounds of tiles and a last one in quarters (282 to 298 tiles of 256 x 256, two per
+    m-tile, the second of 128 columns), every token with the bits that it gets among few."""
+    torch = _torch()
+    from paper_2512_14080_amd import binding as B
+    small = W.MoEConfig("few", T=450, d=384, n=4096, E=8, K=2, m_tile=16)
+    big = W.MoEConfig("many", T=18000, d=384, n=4096, E=8, K=2, m_tile=16)
+
+    def forward(layer):
+        layer.route()
+        layer.ws_f.fill_(0xFF)
+        layer.O.fill_(7.0)
+        B.moe_fwd_quant(layer.D, layer.X, layer.qw, layer.routing, None, layer.O, layer.ws_f, eb=layer.eb)
+
+    inp, R, few, b1, b2 = _layer(small, "quant", seed=12, biased=True)
+    B.moe_quantize_experts(few.D, few.W1, few.W2, few.qw)
+    forward(few)
+    torch.cuda.synchronize()
+    fw = block8.forward_quant(inp.f32("X"), inp.f32("W1"), inp.f32("W2"), R, b1, b2)
+    _check_o(few.O.double().cpu().numpy(), fw, R, fw["W2q"], True)
+    _, R, many, _, _ = _layer(big, "quant", seed=13, biased=True)
+    tiles = 2 * -(-np.diff(R.offsets) // 256).sum()
+    assert 256 < tiles <= 256 + 64, tiles
+    many.qw, many.eb = few.qw, few.eb
+    forward(many)
+    for t in range(0, big.T, small.T):
+        few.X.copy_(many.X[t:t + small.T])
+        few.tc.arrays()["scores"].copy_(many.tc.arrays()["scores"][t:t + small.T])
+        forward(few)
+        assert torch.equal(few.O, many.O[t:t + small.T]), t
+
+
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
 @pytest.mark.parametrize("T", [9, 400])
 def test_one_broken_token_stays_one(bad, T):
