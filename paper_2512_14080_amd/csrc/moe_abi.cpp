@@ -197,8 +197,7 @@ size_t bwd_ckpt_layout(const moe_dims& m, int64_t cap, char* base, BwdWs* w, uin
 }
 
 // moe_fwd_quant: X and A in 8-bit blocks (X's in the checkpoint where it is kept), or
-// A in fp32 where the streaming projections may run (a rounding's m_tile only makes
-// that rarer)
+// A in fp32 where the streaming projections may run, with or without a rounding
 struct QuantWs {
   uint8_t* X8;
   uint8_t* Xs;
@@ -211,10 +210,13 @@ struct QuantWs {
 };
 size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   const int np = smoe::q_pad(m.n);
+  // (a rounding raises the mean rows of an expert, above 2 at the least: the wider of the
+  // two row groups, which may fit a grid where the narrow ones of 2 rows do not)
+  const bool streams = smoe::stream8_shape(m, (int)cap, 0).mb || smoe::stream8_shape(m, (int)cap, 3).mb;
   size_t off = 0;
   off = carve(base, off, (size_t)m.T * m.d, w ? (void**)&w->X8 : nullptr);
   off = carve(base, off, (size_t)m.T * smoe::q_stride(m.d / smoe::kQBlock), w ? (void**)&w->Xs : nullptr);
-  off = carve(base, off, smoe::stream8_shape(m, (int)cap, 0).mb ? (size_t)cap * m.n * 4 : 0, w ? (void**)&w->A32 : nullptr);
+  off = carve(base, off, streams ? (size_t)cap * m.n * 4 : 0, w ? (void**)&w->A32 : nullptr);
   off = carve(base, off, (size_t)cap * np, w ? (void**)&w->A8 : nullptr);
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
   off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);

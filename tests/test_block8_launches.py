@@ -133,5 +133,15 @@ def test_workspace_size_does_not_depend_on_the_device(tmp_path, dims, which):
     assert len(set(sizes)) == 1, sizes
 
 
+def test_workspace_of_a_rounding_that_streams_in_wider_groups(tmp_path):
+    """A capacity whose groups of 16 rows pass the grid's 65535 and whose groups of 32 do not: an A in fp32 is there."""
+    D = B.dims(1024, 128, 64, 4096, 8)
+    cap = 1 << 20
+    assert D.E + cap // 16 > 65535 >= D.E + cap // 32
+    n = B.lib().moe_workspace_bytes(D, cap, B.MOE_WS_FWD_QUANT)
+    parts = cap * (4 * D.n + 128 + 4 + 2 * D.d) + D.T * (D.d + 4)  # A32, A8, their scales, Y; X and its scales
+    assert n >= parts
+
+
 if __name__ == "__main__":
     _main()
