@@ -424,8 +424,9 @@ int moe_fwd_quant(moe_dims dims, const moe_bf16 *X, const moe_qexperts *w, const
                   const moe_routing *r, moe_ckpt *c, moe_bf16 *O, void *ws, size_t ws_bytes, void *stream);
 
 /*
- * moe_fwd that keeps its activations in 8 bits: the same O; in the place of H,
- * c receives q(H) (from the fp32 H) and, with MOE_CKPT_X, q(X).
+ * moe_fwd that keeps its activations in 8 bits: the same O (up to the order of
+ * sums, where moe_fwd streams the weights past few rows); in the place of H, c
+ * receives q(H) (from the fp32 H) and, with MOE_CKPT_X, q(X).
  *   ws   moe_workspace_bytes(dims, r->capacity, MOE_WS_FWD_CKPT) bytes
  */
 int moe_fwd_ckpt(moe_dims dims, const moe_bf16 *X, const moe_bf16 *W1, const moe_bf16 *W2, const moe_expert_bias *eb,
@@ -461,8 +462,8 @@ enum {
   MOE_KC_DH, MOE_KC_DW2, MOE_KC_DXT, MOE_KC_DW1, MOE_KC_AGG_DX, MOE_KC_DWR,
   MOE_KC_ROUTER_TOPK, /* the router GEMM with fused softmax/top-K; for few tokens
                          (see moe_route) two launches, counted as one */
-  MOE_KC_QUANTIZE, /* activations into or out of the 8-bit block format */
-  MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT,
+  MOE_KC_QUANTIZE, /* rows and weights into or out of the 8-bit block format (moe_fwd_quant: and its m-tile lists) */
+  MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT, /* (two launches over a long n, counted as one) */
   MOE_KC_COUNT
 };
 int moe_prof_select(int kernel_class);

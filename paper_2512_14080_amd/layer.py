@@ -49,6 +49,10 @@ class DeviceLayer:
     def __init__(self, inputs, round_mode=None, m_tile=None, scores_in=None, u=None, device="cuda",
                  router_grad=True, b1=None, b2=None, keep_logits=True, held8=None, keep_x=False):
         import torch
+        if held8 not in (None, "ckpt", "quant"):
+            raise ValueError(f'held8 must be None, "ckpt" or "quant" (got {held8!r})')
+        if keep_x and held8 is None:
+            raise ValueError("keep_x needs held8: the 16-bit layer's backward reads X itself")
         cfg = inputs.cfg
         T, d, n, E, K = inputs.X.shape[0], cfg.d, cfg.n, cfg.E, cfg.K
         self.D = B.dims(T, d, n, E, K)

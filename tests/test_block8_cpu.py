@@ -216,3 +216,10 @@ def test_gradient_formula_against_differences():
         args[1][i][at] -= 1e-6
         diff = (loss(*args[0])[0] - loss(*args[1])[0]) / 2e-6
         assert abs(diff - g[name][at]) <= 1e-6 * max(1, abs(diff)), name
+
+
+@pytest.mark.parametrize("kw", [{"held8": "fp8"}, {"held8": True}, {"keep_x": True}])
+def test_layer_refuses(kw):
+    from paper_2512_14080_amd.layer import DeviceLayer
+    with pytest.raises(ValueError):
+        DeviceLayer(None, **kw)
