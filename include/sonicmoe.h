@@ -410,7 +410,8 @@ int moe_ckpt_init(moe_dims dims, int32_t capacity, int flags, void *buf, size_t 
  *   H = gather(q(X)) q(W1_e) (+ b1_e);  A = SiLU(H_gate) * H_up
  *   Y = q(A) q(W2_e) (+ b2_e);          O_t = sum_{rows of t} s * Y
  * Products accumulate in fp32; A is quantised from fp32 (blocks of 128 columns of a row), Y
- * is held in bf16 as in moe_fwd.
+ * is held in bf16 as in moe_fwd (in fp32 where T * K <= E / 2 without a rounding and
+ * without c).
  *   w    weights in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of the
  *        same d, n and E
  *   c    nullable: then nothing is kept for a backward.  Otherwise q(H) (and
@@ -463,7 +464,8 @@ enum {
   MOE_KC_ROUTER_TOPK, /* the router GEMM with fused softmax/top-K; for few tokens
                          (see moe_route) two launches, counted as one */
   MOE_KC_QUANTIZE, /* rows and weights into or out of the 8-bit block format (moe_fwd_quant: and its m-tile lists) */
-  MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT, /* (two launches over a long n, counted as one) */
+  MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT, /* (two launches over a long n, counted as one; for few
+                                          tokens with the aggregation in it) */
   MOE_KC_COUNT
 };
 int moe_prof_select(int kernel_class);

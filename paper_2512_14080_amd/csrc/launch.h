@@ -81,8 +81,10 @@ hipError_t launch_topk_few(const float* in, int slices, const float* bias, float
 hipError_t launch_tc_metadata_few(const moe_routing& r, int T, int E, int K, bool counts_only, hipStream_t s);
 
 // What built a routing, as moe_routing.reserved keeps it: 0 for token choice, else
-// the rounding's m_tile and mode.  It guides the choice of kernels.
+// the rounding's m_tile and mode.  It guides the choice of kernels (a token choice has
+// at most T K rows).
 inline int rounding_word(int m_tile, int mode) { return m_tile | mode << 16; }
+inline bool token_choice(const moe_routing& r) { return r.reserved == 0; }
 inline int rounding_tile(const moe_routing& r) { return r.reserved & 0xffff; }
 inline int rounding_mode(const moe_routing& r) { return r.reserved >> 16; }
 
@@ -237,6 +239,7 @@ struct QuantArgs {
   float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
   int d, n, E, capacity;
   QuantTiles tiles;
+  const int32_t* row_expert; const float* row_w; const int32_t* tok_offsets; const int32_t* tok_rows; uint16_t* O;
 };
 hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s);
 // the m-tile list of the 16-bit projections, and X into 8-bit blocks
@@ -249,6 +252,10 @@ hipError_t launch_quant_down(QuantArgs a, hipStream_t s);
 StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile);
 hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s);    // writes A32
 hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s);  // from A32
+// and for few tokens of a token choice, by row and by token: O without Y
+bool stream8_by_token(const moe_dims& m, const moe_routing& r);
+hipError_t launch_stream8_row_up(const QuantArgs& a, int T, int K, hipStream_t s);
+hipError_t launch_stream8_token_down(const QuantArgs& a, int T, hipStream_t s);
 
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);

@@ -899,9 +899,15 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
   const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles, w.mtiles128,
                           eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A32, w.A8, w.As, c ? c->H : nullptr,
-                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity, smoe::quant_tiles(m, *r)};
+                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity, smoe::quant_tiles(m, *r),
+                          r->row_expert, r->row_w, r->tok_offsets, r->tok_rows, O};
   // (what is kept is written by the tiled projections)
   const smoe::StreamShape few = c ? smoe::StreamShape{0, 0} : smoe::stream8_shape(m, r->capacity, smoe::rounding_tile(*r));
+  if (few.mb && smoe::stream8_by_token(m, *r)) {
+    LAUNCH(MOE_KC_UP_QUANT, smoe::launch_stream8_row_up(a, m.T, m.K, stream), "8-bit up-proj");
+    LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_stream8_token_down(a, m.T, stream), "8-bit down-proj and aggregation");
+    return MOE_OK;
+  }
   if (few.mb) {
     LAUNCH(MOE_KC_UP_QUANT, smoe::launch_stream8_up(a, few, stream), "8-bit up-proj");
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_stream8_down(a, few, stream), "8-bit down-proj");

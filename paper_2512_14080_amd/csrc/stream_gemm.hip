@@ -481,21 +481,34 @@ struct RowBlock8 {
   }
 };
 
+// A lane's codes of NJ times 16 weight columns and one block of 128 k
+template <int NJ>
+struct Weights8 {
+  u32x4 v[NJ][2];
+  __device__ __forceinline__ void load(const uint8_t* w, const uint32_t (&row)[NJ], uint32_t k) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      v[j][0] = *(const u32x4*)(w + (size_t)(row[j] + k));
+      v[j][1] = *(const u32x4*)(w + (size_t)(row[j] + k + 64));
+    }
+  }
+  __device__ __forceinline__ i32x8s frag(int j) const {
+    const u32x4 lo = v[j][0], hi = v[j][1];
+    return i32x8s{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  }
+};
+
 // grid: as stream_gemm_kernel's of the experts.  Op supplies
 //   F32: whether rows come in fp32 (else bf16),
 //   int blocks(p), k(p): blocks of the reduction, and its length,
 //   const void* row(p, r), const uint8_t* w(p, e), const uint8_t* ws(p, e, tile, half),
 //   uint32_t w_row(p, tile, c): offset of weight column c of the tile,
 //   finish(p, e, tile, row0, rows, part)
-template <template <int> class OpT, int NJ, int MB, int KW, int OCC>
-__global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantArgs p) {
+// stream8_rows: rows [m0, cnt) of the expert's, at most 16 MB; xp: those that the lanes load
+template <template <int> class OpT, int NJ, int MB, int KW>
+__device__ __forceinline__ void stream8_rows(const QuantArgs& p, int tile, int e, int off, int cnt, int m0,
+                                             const void* const (&xp)[MB], Stream8Part<NJ>* part) {
   using Op = OpT<NJ>;
-  __shared__ Stream8Part<NJ> part[KW];
-  const int tile = blockIdx.x;
-  int e = blockIdx.y, m0 = 0;
-  if (e >= p.E && !find_group<64 * KW>(p.offsets, p.E, 16 * MB, e - p.E, (int*)part, &e, &m0)) return;
-  const int off = p.offsets[e], cnt = p.offsets[e + 1] - off;
-  if (m0 >= cnt) return;
   const int lane = lane_id(), g = lane >> 4, l = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint8_t* wbase = Op::w(p, e);
@@ -504,9 +517,6 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantA
   uint32_t wrow[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) wrow[j] = Op::w_row(p, tile, 16 * j + l) + 16 * g;
-  const void* xp[MB];
-#pragma unroll
-  for (int b = 0; b < MB; ++b) xp[b] = Op::row(p, off + min(m0 + 16 * b + l, cnt - 1));
   f32x4 acc[MB][NJ];
 #pragma unroll
   for (int b = 0; b < MB; ++b)
@@ -515,12 +525,8 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantA
   const int blocks = Op::blocks(p);
   for (int kb = wave; kb < blocks; kb += KW) {
     const uint32_t k = kQBlock * kb;
-    u32x4 wv[NJ][2];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      wv[j][0] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k));
-      wv[j][1] = *(const u32x4*)(wbase + (size_t)(wrow[j] + k + 64));
-    }
+    Weights8<NJ> wv;
+    wv.load(wbase, wrow, k);
     const int sv[2] = {ws0[kb], ws1[kb]};
     RowBlock8<Op::F32> xv[MB];
 #pragma unroll
@@ -530,11 +536,8 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantA
       int xs;
       const i32x8s x = xv[b].codes(&xs);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const u32x4 lo = wv[j][0], hi = wv[j][1];
-        const i32x8s w = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-        acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc[b][j], 0, 0, 0, sv[2 * j / NJ], 0, xs);
-      }
+      for (int j = 0; j < NJ; ++j)
+        acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv.frag(j), x, acc[b][j], 0, 0, 0, sv[2 * j / NJ], 0, xs);
     }
   }
 #pragma unroll
@@ -548,11 +551,25 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantA
   }
 }
 
+template <template <int> class OpT, int NJ, int MB, int KW, int OCC>
+__global__ __launch_bounds__(64 * KW, OCC) void stream8_gemm_kernel(const QuantArgs p) {
+  __shared__ Stream8Part<NJ> part[KW];
+  const int tile = blockIdx.x;
+  int e = blockIdx.y, m0 = 0;
+  if (e >= p.E && !find_group<64 * KW>(p.offsets, p.E, 16 * MB, e - p.E, (int*)part, &e, &m0)) return;
+  const int off = p.offsets[e], cnt = p.offsets[e + 1] - off;
+  if (m0 >= cnt) return;
+  const void* xp[MB];
+#pragma unroll
+  for (int b = 0; b < MB; ++b) xp[b] = OpT<NJ>::row(p, off + min(m0 + 16 * b + (lane_id() & 15), cnt - 1));
+  stream8_rows<OpT, NJ, MB, KW>(p, tile, e, off, cnt, m0, xp, part);
+}
+
 // the sum over the waves of columns 4 c4 .. 4 c4 + 3 of the tile
 template <int KW, int NJ>
 __device__ __forceinline__ f32x4 stream8_sum(const Stream8Part<NJ>* part, int row, int c4) {
   f32x4 s = part[0][row][c4];
-#pragma unroll
+#pragma unroll 7  // (all 15 of 16 waves at once spilled)
   for (int w = 1; w < KW; ++w)
 #pragma unroll
     for (int q = 0; q < 4; ++q) s[q] += part[w][row][c4][q];
@@ -628,6 +645,67 @@ struct Stream8Down {
   }
 };
 
+// Few tokens: a workgroup per row instead of one per expert, most of which have no
+// rows (rows of the same expert read its weights again)
+template <int NJ, int KW, int OCC>
+__global__ __launch_bounds__(64 * KW, OCC) void stream8_row_up_kernel(const QuantArgs p) {
+  __shared__ Stream8Part<NJ> part[KW];
+  const int r = blockIdx.y, e = p.row_expert[r], t = p.row_token[r];  // (the grid is within the capacity)
+  if (r >= p.offsets[p.E]) return;
+  const void* xp[1] = {p.X + (size_t)t * p.d};
+  stream8_rows<Stream8Up, NJ, 1, KW>(p, blockIdx.x, e, r, 1, 0, xp, part);
+}
+
+// and the down-projection by token, with the sum over the token's rows: a wave's step is
+// one block of one row, its product weighted as it is added (Y stays in fp32)
+template <int NJ, int KW, int OCC>
+__global__ __launch_bounds__(64 * KW, OCC) void stream8_token_down_kernel(const QuantArgs p) {
+  using Op = Stream8Down<NJ>;
+  __shared__ f32x4 part[KW][4 * NJ];
+  const int tile = blockIdx.x, t = blockIdx.y;
+  const int lane = lane_id(), g = lane >> 4, l = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blocks = Op::blocks(p), j0 = p.tok_offsets[t], steps = (p.tok_offsets[t + 1] - j0) * blocks;
+  uint32_t wrow[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) wrow[j] = Op::w_row(p, tile, 16 * j + l) + 16 * g;
+  f32x4 acc[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = wave; i < steps; i += KW) {
+    const int kb = i % blocks, r = p.tok_rows[j0 + i / blocks], e = p.row_expert[r];
+    const float s = p.row_w[r];
+    const uint32_t k = kQBlock * kb;
+    Weights8<NJ> wv;
+    wv.load(Op::w(p, e), wrow, k);
+    const int sv = Op::ws(p, e, tile, 0)[kb];
+    RowBlock8<true> xv;
+    xv.load(Op::row(p, r), k + 16 * g, (int)k + 64 < p.n);
+    int xs;
+    const i32x8s x = xv.codes(&xs);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (kb == 0 && p.b2) y = *(const f32x4*)(p.b2 + (size_t)e * p.d + Op::kCols * tile + 16 * j + 4 * g);
+      y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv.frag(j), x, y, 0, 0, 0, sv, 0, xs);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) acc[j][q] += s * y[q];
+    }
+  }
+  if (l == 0)  // (all 16 rows of the product are this one)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) part[wave][4 * j + g] = acc[j];
+  __syncthreads();
+  if (threadIdx.x < 4 * NJ) {
+    f32x4 o = part[0][threadIdx.x];
+#pragma unroll
+    for (int w = 1; w < KW; ++w)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) o[q] += part[w][threadIdx.x][q];
+    *(u32x2*)(p.O + (size_t)t * p.d + Op::kCols * tile + 4 * threadIdx.x) = pack_bf16x4(o[0], o[1], o[2], o[3]);
+  }
+}
+
 template <template <int> class Op, int NJ, int MB, int KW, int OCC>
 static hipError_t run_stream8(const QuantArgs& p, const StreamShape& t, int cols, hipStream_t s) {
   stream8_gemm_kernel<Op, NJ, MB, KW, OCC><<<stream_grid(cols / Op<NJ>::kCols, p.E, t), dim3(64 * KW), 0, s>>>(p);
@@ -663,6 +741,33 @@ hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStre
   if (t.mb == 1) return run_stream8<Stream8Down, 2, 1, 4, 4>(a, t, a.d, s);
   if (blocks <= 2 && a.E * (a.d / kQBlock) > 768) return run_stream8<Stream8Down, 8, 2, 1, 2>(a, t, a.d, s);
   return run_stream8<Stream8Down, 8, 2, 2, 2>(a, t, a.d, s);
+}
+
+// Up to E / 2 rows of a token choice: by row and by token.  us a call, by expert (three
+// launches) / so, by tokens; where rows repeat experts, their weights are read again:
+//     T =                                1          2           4           8           12          16
+//   d = 1536, n = 256, E = 128, K = 8    13.8/11.1  17.3/12.3   19.8/13.7   22.0/19.7   26.6/25.5   29.0/29.1
+//   d = 1024, n = 256, E = 64, K = 8     10.9/10.3  12.9/10.6   15.0/11.8   16.7/14.2
+//   d = 2048, n = 128, E = 256, K = 10   17.1/10.5              23.6/13.1               28.1/24.9   34.2/28.9
+//   d = 4096, n = 512, E = 128, K = 8    26.6/19.4  34.7/23.4   48.8/43.4   73.4/72.4   91/99       105/124
+//   d = 2048, n = 1024, E = 32, K = 4    18.7/16.3  24.1/17.6   28.3/22.1   33.8/37.3
+//   d = 4096, n = 14336, E = 8, K = 2    91.3/90.6  140/128     173/234
+// Columns and waves as above; of the down-projection: 32 and 8 (16 waves: coarse 102
+// instead of 91 a call; 64 columns and 16 or 4 waves: +2 to 25).
+bool stream8_by_token(const moe_dims& m, const moe_routing& r) {
+  return token_choice(r) && 2 * (int64_t)m.T * m.K <= m.E;
+}
+hipError_t launch_stream8_row_up(const QuantArgs& a, int T, int K, hipStream_t s) {
+  const int rows = std::min(T * K, a.capacity);
+  if ((int64_t)rows * (a.n / 32) <= 128)
+    stream8_row_up_kernel<2, 16, 4><<<dim3(a.n / 16, rows), 64 * 16, 0, s>>>(a);
+  else
+    stream8_row_up_kernel<4, 8, 4><<<dim3(a.n / 32, rows), 64 * 8, 0, s>>>(a);
+  return hipGetLastError();
+}
+hipError_t launch_stream8_token_down(const QuantArgs& a, int T, hipStream_t s) {
+  stream8_token_down_kernel<2, 8, 4><<<dim3(a.d / 32, T), 64 * 8, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 // One rule for both projections, since A passes between the two in one of two forms.

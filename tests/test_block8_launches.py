@@ -80,6 +80,21 @@ def test_few_rows_stream(tmp_path, dims, m_tile, stream):
     assert "stream8" not in _names(kept) and "OpUp8" in _names(kept)
 
 
+@pytest.mark.parametrize("dims,tiles", [
+    ((1, 1536, 256, 128, 8), 16), ((2, 1536, 256, 128, 8), 16), ((3, 1536, 256, 128, 8), 8), ((8, 1536, 256, 128, 8), 8),
+    ((1, 4096, 14336, 8, 2), 448), ((32, 768, 512, 64, 1), 16), ((9, 1536, 256, 128, 8), 0), ((5, 1024, 256, 64, 8), 0),
+])
+def test_few_tokens_by_row_and_token(tmp_path, dims, tiles):
+    """Two launches up to E / 2 rows; three where there are more, with a rounding, or with a checkpoint."""
+    T, d, _, _, K = dims
+    l, rounded, kept = launches([(dims, "quant", 0, False), (dims, "quant", 8, False), (dims, "kept", 0, False)], tmp_path)
+    if tiles:
+        assert [(re.search("stream8_(row_up|token_down)", name).group(1), x, y) for name, x, y in l] == [
+            ("row_up", tiles, T * K), ("token_down", d // 32, T)]
+    for x in (rounded, kept) if tiles else (l, rounded, kept):
+        assert not re.search("stream8_(row_up|token_down)", _names(x)) and "agg_o" in _names(x)
+
+
 @pytest.mark.parametrize("T,E,K,rows", [(40, 512, 8, 16), (100, 128, 8, 32), (300, 2048, 8, 16), (9, 8, 8, 16)])
 def test_streaming_grid_holds_a_hot_experts_groups(tmp_path, T, E, K, rows):
     l, = launches([((T, 1536, 256, E, K), "quant", 0, False)], tmp_path)

@@ -259,6 +259,37 @@ def test_forward_without_a_checkpoint(cfg, biased):
     assert (layer.ckpt.buf == 0xAB).all()
 
 
+FEW = [
+    (W.MoEConfig("k16", T=1, d=256, n=1152, E=32, K=16, m_tile=16), None),               # 144 steps on eight waves
+    (W.MoEConfig("half", T=8, d=640, n=320, E=64, K=4, m_tile=16), None),                # E / 2 rows, an uneven n
+    (W.MoEConfig("t32", T=32, d=128, n=64, E=64, K=1, m_tile=16), None),                 # one step a token
+    (W.MoEConfig("same", T=6, d=384, n=192, E=48, K=4, m_tile=16, zipf_s=3.0), None),    # tokens that share experts
+    (W.MoEConfig("up", T=9, d=384, n=192, E=64, K=3, m_tile=8), "up"),                   # rounded: more rows than T K
+    (W.MoEConfig("down", T=9, d=384, n=192, E=64, K=3, m_tile=8), "down"),               # and hardly any
+]
+
+
+@pytest.mark.parametrize("cfg,mode", FEW, ids=lambda c: getattr(c, "name", ""))
+@pytest.mark.parametrize("biased", [False, True])
+def test_few_tokens(cfg, mode, biased):
+    """At most E / 2 rows: by row and by token where they are a token choice's."""
+    torch = _torch()
+    from paper_2512_14080_amd import binding as B
+    inp, R, layer, b1, b2 = _layer(cfg, "quant", seed=21, mode=mode, biased=biased)
+    layer.route()
+    B.moe_quantize_experts(layer.D, layer.W1, layer.W2, layer.qw)
+    fw = block8.forward_quant(inp.f32("X"), inp.f32("W1"), inp.f32("W2"), R, b1, b2)
+    out = []
+    for _ in range(2):
+        layer.ws_f.fill_(0xFF)
+        layer.O.fill_(7.0)
+        B.moe_fwd_quant(layer.D, layer.X, layer.qw, layer.routing, None, layer.O, layer.ws_f, eb=layer.eb)
+        out.append(layer.O.clone())
+    torch.cuda.synchronize()
+    assert torch.equal(*out)
+    _check_o(out[0].double().cpu().numpy(), fw, R, fw["W2q"], True)
+
+
 def test_a_tokens_output_does_not_depend_on_its_tile():
     """Many rows behind a long n: whole rounds of tiles and a last one in quarters (282 to 298 tiles of 256 x 256, two per
     m-tile, the second of 128 columns), every token with the bits that it gets among few."""
@@ -292,8 +323,8 @@ def test_a_tokens_output_does_not_depend_on_its_tile():
 
 
 @pytest.mark.parametrize("bad", [np.nan, np.inf])
-@pytest.mark.parametrize("T", [9, 400])
-def test_one_broken_token_stays_one(bad, T):
+@pytest.mark.parametrize("T,E", [(9, 16), (400, 16), (9, 64)])
+def test_one_broken_token_stays_one(bad, T, E):
     """A value that is not finite reaches its own token's output only."""
     torch = _torch()
     from paper_2512_14080_amd import binding as B
@@ -301,7 +332,7 @@ def test_one_broken_token_stays_one(bad, T):
     def edit(inp):
         inp.X[5, 17] = W.bf16_bits_from_f32(np.array([1.0], np.float32))[0]  # (the scores are the sound token's)
 
-    cfg = W.MoEConfig("broken", T=T, d=256, n=128, E=16, K=2, m_tile=16)
+    cfg = W.MoEConfig("broken", T=T, d=256, n=128, E=E, K=2, m_tile=16)
     inp, R, layer, _, _ = _layer(cfg, "quant", seed=6, edit=edit)
     layer.route()
     sound = layer.X.clone()
