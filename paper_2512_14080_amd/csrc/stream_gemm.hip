@@ -498,17 +498,34 @@ struct Weights8 {
   }
 };
 
+// codes 8 i .. 8 i + 7 as bf16 (exact)
+__device__ __forceinline__ bf16x8 codes_bf16(const i32x8s& q, int i) {
+  u32x4 v;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    v[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + h], 1.f, false));
+    v[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + h], 1.f, true));
+  }
+  return __builtin_bit_cast(bf16x8, v);
+}
+
 // grid: as stream_gemm_kernel's of the experts.  Op supplies
 //   F32: whether rows come in fp32 (else bf16),
 //   int blocks(p), k(p): blocks of the reduction, and its length,
 //   const void* row(p, r), const uint8_t* w(p, e), const uint8_t* ws(p, e, tile, half),
 //   uint32_t w_row(p, tile, c): offset of weight column c of the tile,
 //   finish(p, e, tile, row0, rows, part)
-// stream8_rows: rows [m0, cnt) of the expert's, at most 16 MB; xp: those that the lanes load
+// stream8_rows: rows [m0, cnt) of the expert's, at most 16 MB; xp: those that the lanes load.
+// The 8-bit instruction adds its products to 1.3e-5 of the result, which moves some of
+// A's codes to the other side of a step.  With few rows single ones show in O (one
+// token, d = 1536, n = 256: O 2.7e-3 off, 1.7e-3 without): there the up-projection
+// multiplies the same codes in bf16, which is exact but for fp32 sums, at 11.5 instead
+// of 11.3 us a call.  With two row blocks it would cost 7 to 12%.
 template <template <int> class OpT, int NJ, int MB, int KW>
 __device__ __forceinline__ void stream8_rows(const QuantArgs& p, int tile, int e, int off, int cnt, int m0,
                                              const void* const (&xp)[MB], Stream8Part<NJ>* part) {
   using Op = OpT<NJ>;
+  constexpr bool kInBf16 = MB == 1 && !Op::F32;
   const int lane = lane_id(), g = lane >> 4, l = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint8_t* wbase = Op::w(p, e);
@@ -536,8 +553,19 @@ __device__ __forceinline__ void stream8_rows(const QuantArgs& p, int tile, int e
       int xs;
       const i32x8s x = xv[b].codes(&xs);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
-        acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv.frag(j), x, acc[b][j], 0, 0, 0, sv[2 * j / NJ], 0, xs);
+      for (int j = 0; j < NJ; ++j) {
+        const int ws = sv[2 * j / NJ];
+        if constexpr (kInBf16) {
+          f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16(wv.frag(j), i), codes_bf16(x, i), y, 0, 0, 0);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) acc[b][j][q] += ldexpf(y[q], ws + xs - 254);
+        } else {
+          acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv.frag(j), x, acc[b][j], 0, 0, 0, ws, 0, xs);
+        }
+      }
     }
   }
 #pragma unroll
