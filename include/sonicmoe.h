@@ -410,8 +410,8 @@ int moe_ckpt_init(moe_dims dims, int32_t capacity, int flags, void *buf, size_t 
  *   H = gather(q(X)) q(W1_e) (+ b1_e);  A = SiLU(H_gate) * H_up
  *   Y = q(A) q(W2_e) (+ b2_e);          O_t = sum_{rows of t} s * Y
  * Products accumulate in fp32; A is quantised from fp32 (blocks of 128 columns of a row), Y
- * is held in bf16 as in moe_fwd (in fp32 where T * K <= E / 2 without a rounding and
- * without c).
+ * is held in bf16 as in moe_fwd, or in fp32 for few rows (without c: T <= 16, or a mean of up
+ * to 10 rows per expert, 16 where d is large).
  *   w    weights in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of the
  *        same d, n and E
  *   c    nullable: then nothing is kept for a backward.  Otherwise q(H) (and

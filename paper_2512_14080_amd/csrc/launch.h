@@ -236,7 +236,7 @@ struct QuantArgs {
   const int32_t* offsets; const int32_t* row_token;
   int32_t* mtiles; int32_t* mtiles128;  // (the second where the two differ)
   const float* b1; const float* b2;
-  float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y;
+  float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y; float* Y32;
   int d, n, E, capacity;
   QuantTiles tiles;
   const int32_t* row_expert; const float* row_w; const int32_t* tok_offsets; const int32_t* tok_rows; uint16_t* O;
@@ -251,7 +251,7 @@ hipError_t launch_quant_down(QuantArgs a, hipStream_t s);
 // mb = 0 where the tiled ones are the better ones
 StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile);
 hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s);    // writes A32
-hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s);  // from A32
+hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s);  // Y32 from A32
 // and for few tokens of a token choice, by row and by token: O without Y
 bool stream8_by_token(const moe_dims& m, const moe_routing& r);
 hipError_t launch_stream8_row_up(const QuantArgs& a, int T, int K, hipStream_t s);
@@ -259,6 +259,7 @@ hipError_t launch_stream8_token_down(const QuantArgs& a, int T, hipStream_t s);
 
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);
+hipError_t launch_agg_o_f32(const float* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);
 // aggregation ablation: dst[tok_rows[j]] = j (token-major slot of each row);
 // O from token-major (contiguous) Y rows; fp32 buffer fill and fp32 -> bf16
 hipError_t launch_tok_slots(const moe_routing& r, int T, int P_bound, int32_t* dst, hipStream_t s);

@@ -205,6 +205,7 @@ struct QuantWs {
   uint8_t* A8;
   uint8_t* As;
   uint16_t* Y;
+  float* Y32;
   int32_t* mtiles;
   int32_t* mtiles128;
 };
@@ -219,7 +220,8 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   off = carve(base, off, streams ? (size_t)cap * m.n * 4 : 0, w ? (void**)&w->A32 : nullptr);
   off = carve(base, off, (size_t)cap * np, w ? (void**)&w->A8 : nullptr);
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
-  off = carve(base, off, (size_t)cap * m.d * 2, w ? (void**)&w->Y : nullptr);
+  off = carve(base, off, (size_t)cap * m.d * (streams ? 4 : 2), w ? (void**)&w->Y : nullptr);
+  if (w) w->Y32 = (float*)w->Y;
   off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles : nullptr);
   off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles128 : nullptr);
   return off;
@@ -899,7 +901,7 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
   const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles, w.mtiles128,
                           eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A32, w.A8, w.As, c ? c->H : nullptr,
-                          c ? c->Hs : nullptr, w.Y, m.d, m.n, m.E, r->capacity, smoe::quant_tiles(m, *r),
+                          c ? c->Hs : nullptr, w.Y, w.Y32, m.d, m.n, m.E, r->capacity, smoe::quant_tiles(m, *r),
                           r->row_expert, r->row_w, r->tok_offsets, r->tok_rows, O};
   // (what is kept is written by the tiled projections)
   const smoe::StreamShape few = c ? smoe::StreamShape{0, 0} : smoe::stream8_shape(m, r->capacity, smoe::rounding_tile(*r));
@@ -911,12 +913,13 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   if (few.mb) {
     LAUNCH(MOE_KC_UP_QUANT, smoe::launch_stream8_up(a, few, stream), "8-bit up-proj");
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_stream8_down(a, few, stream), "8-bit down-proj");
+    LAUNCH(MOE_KC_AGG_O, smoe::launch_agg_o_f32(w.Y32, *r, O, m.T, m.d, stream), "aggregation");
   } else {
     LAUNCH(MOE_KC_QUANTIZE, smoe::launch_quant_prepare(a, m.T, stream), "quantize X and m-tile lists");
     LAUNCH(MOE_KC_UP_QUANT, smoe::launch_quant_up(a, stream), "8-bit up-proj");
     LAUNCH(MOE_KC_DOWN_QUANT, smoe::launch_quant_down(a, stream), "8-bit down-proj");
+    LAUNCH(MOE_KC_AGG_O, smoe::launch_agg_o(w.Y, *r, O, m.T, m.d, stream), "aggregation");
   }
-  LAUNCH(MOE_KC_AGG_O, smoe::launch_agg_o(w.Y, *r, O, m.T, m.d, stream), "aggregation");
   if (c) c->state = MOE_HELD_WRITTEN;
   return MOE_OK;
 }
