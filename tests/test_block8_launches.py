@@ -82,10 +82,11 @@ def test_few_rows_stream(tmp_path, dims, m_tile, stream):
 
 @pytest.mark.parametrize("dims,tiles", [
     ((1, 1536, 256, 128, 8), 16), ((2, 1536, 256, 128, 8), 16), ((3, 1536, 256, 128, 8), 8), ((8, 1536, 256, 128, 8), 8),
-    ((1, 4096, 14336, 8, 2), 448), ((32, 768, 512, 64, 1), 16), ((9, 1536, 256, 128, 8), 0), ((5, 1024, 256, 64, 8), 0),
+    ((1, 4096, 14336, 8, 2), 448), ((32, 768, 512, 64, 1), 16), ((9, 1536, 256, 128, 8), 8),  # 85 MB of weights
+    ((16, 1536, 256, 128, 8), 0), ((9, 1024, 256, 64, 8), 0), ((8, 2048, 1024, 32, 4), 0),
 ])
 def test_few_tokens_by_row_and_token(tmp_path, dims, tiles):
-    """Two launches up to E / 2 rows; three where there are more, with a rounding, or with a checkpoint."""
+    """Two launches up to E / 2 rows, or E of few weights; three where there are more, with a rounding, or with a checkpoint."""
     T, d, _, _, K = dims
     l, rounded, kept = launches([(dims, "quant", 0, False), (dims, "quant", 8, False), (dims, "kept", 0, False)], tmp_path)
     if tiles:

@@ -263,6 +263,7 @@ FEW = [
     (W.MoEConfig("k16", T=1, d=256, n=1152, E=32, K=16, m_tile=16), None),               # 144 steps on eight waves
     (W.MoEConfig("half", T=8, d=640, n=320, E=64, K=4, m_tile=16), None),                # E / 2 rows, an uneven n
     (W.MoEConfig("t32", T=32, d=128, n=64, E=64, K=1, m_tile=16), None),                 # one step a token
+    (W.MoEConfig("t64", T=64, d=256, n=128, E=64, K=1, m_tile=16), None),                # E rows
     (W.MoEConfig("same", T=6, d=384, n=192, E=48, K=4, m_tile=16, zipf_s=3.0), None),    # tokens that share experts
     (W.MoEConfig("up", T=9, d=384, n=192, E=64, K=3, m_tile=8), "up"),                   # rounded: more rows than T K
     (W.MoEConfig("down", T=9, d=384, n=192, E=64, K=3, m_tile=8), "down"),               # and hardly any
@@ -272,7 +273,7 @@ FEW = [
 @pytest.mark.parametrize("cfg,mode", FEW, ids=lambda c: getattr(c, "name", ""))
 @pytest.mark.parametrize("biased", [False, True])
 def test_few_tokens(cfg, mode, biased):
-    """At most E / 2 rows: by row and by token where they are a token choice's."""
+    """At most E / 2 rows, or E of few weights: by row and by token where they are a token choice's."""
     torch = _torch()
     from paper_2512_14080_amd import binding as B
     inp, R, layer, b1, b2 = _layer(cfg, "quant", seed=21, mode=mode, biased=biased)
