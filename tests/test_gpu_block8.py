@@ -291,6 +291,42 @@ def test_few_tokens(cfg, mode, biased):
     _check_o(out[0].double().cpu().numpy(), fw, R, fw["W2q"], True)
 
 
+def test_decode_steps_in_a_graph():
+    """Routing and the forward of few tokens, captured once and replayed on other tokens between eager calls."""
+    torch = _torch()
+    from paper_2512_14080_amd import binding as B
+    cfg = W.MoEConfig("decode", T=4, d=384, n=192, E=40, K=3, m_tile=16)
+    _, _, layer, _, _ = _layer(cfg, "quant", seed=31, biased=True)
+    B.moe_quantize_experts(layer.D, layer.W1, layer.W2, layer.qw)
+    layer.route_flags &= ~B.MOE_ROUTE_SCORES_IN
+
+    def step():
+        layer.route()
+        B.moe_fwd_quant(layer.D, layer.X, layer.qw, layer.routing, None, layer.O, layer.ws_f, eb=layer.eb)
+
+    tokens = [torch.randn_like(layer.X) for _ in range(4)]
+    want = []
+    for x in tokens:
+        layer.X.copy_(x)
+        step()
+        want.append(layer.O.clone())
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    for i in (2, 0, 3, 1, 1):
+        layer.X.copy_(tokens[i])
+        layer.O.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(layer.O, want[i]), i
+        step()
+        assert torch.equal(layer.O, want[i]), i
+
+
 def test_a_tokens_output_does_not_depend_on_its_tile():
     """Many rows behind a long n: whole rounds of tiles and a last one in quarters (282 to 298 tiles of 256 x 256, two per
     m-tile, the second of 128 columns), every token with the bits that it gets among few."""
