@@ -396,7 +396,7 @@ hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, in
 __global__ __launch_bounds__(256) void agg_o_f32_kernel(const float* __restrict__ Y, const int32_t* __restrict__ tok_offsets,
                                                         const int32_t* __restrict__ tok_rows, const float* __restrict__ row_w,
                                                         uint16_t* __restrict__ O, int d) {
-  const int t = blockIdx.y, c = 4 * (256 * blockIdx.x + threadIdx.x), cl = min(c, d - 4);
+  const int t = blockIdx.x, c = 4 * (256 * blockIdx.y + threadIdx.x), cl = min(c, d - 4);
   const int j0 = tok_offsets[t], j1 = tok_offsets[t + 1];
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int jb = j0; jb < j1; jb += kAggBatch) {
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256) void agg_o_f32_kernel(const float* __restrict_
 }
 
 hipError_t launch_agg_o_f32(const float* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s) {
-  agg_o_f32_kernel<<<dim3((d + 1023) / 1024, T), 256, 0, s>>>(Y, r.tok_offsets, r.tok_rows, r.row_w, O, d);
+  agg_o_f32_kernel<<<dim3(T, (d + 1023) / 1024), 256, 0, s>>>(Y, r.tok_offsets, r.tok_rows, r.row_w, O, d);
   return hipGetLastError();
 }
 

@@ -96,6 +96,13 @@ def test_few_tokens_by_row_and_token(tmp_path, dims, tiles):
         assert not re.search("stream8_(row_up|token_down)", _names(x)) and "agg_o" in _names(x)
 
 
+def test_grids_of_the_most_tokens_that_stream(tmp_path):
+    """16 rows of each of 4096 experts: no grid past 65535 workgroups but along x."""
+    l, = launches([((65536, 4096, 64, 4096, 1), "quant", 0, False)], tmp_path)
+    assert "stream8" in _names(l) and "agg_o_f32" in _names(l)
+    assert all(y <= 65535 for _, _, y in l), l
+
+
 @pytest.mark.parametrize("T,E,K,rows", [(40, 512, 8, 16), (100, 128, 8, 32), (300, 2048, 8, 16), (9, 8, 8, 16)])
 def test_streaming_grid_holds_a_hot_experts_groups(tmp_path, T, E, K, rows):
     l, = launches([((T, 1536, 256, E, K), "quant", 0, False)], tmp_path)
