@@ -781,6 +781,8 @@ hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStre
 //   d = 1024, n = 256, E = 64, K = 8     10.9/10.3  12.9/10.6   15.0/11.8   16.7/14.2
 //   d = 2048, n = 128, E = 256, K = 10   17.1/10.5              23.6/13.1               28.1/24.9   34.2/28.9
 //     (25 tokens, 196 MB: 35.5/40.0)
+//   d = 4096, n = 64, E = 64, K = 4                                                          19.6/21.9
+//   d = 640, n = 768, E = 16, K = 2, 7 tokens: 13.6/12.0; d = 768, n = 512, E = 64, K = 2, 32: 20.3/20.6
 //   d = 4096, n = 512, E = 128, K = 8    26.6/19.4  34.7/23.4   48.8/43.4   73.4/72.4   91/99       105/124
 //   d = 2048, n = 1024, E = 32, K = 4    18.7/16.3  24.1/17.6   28.3/22.1   33.8/37.3
 //   d = 4096, n = 14336, E = 8, K = 2    91.3/90.6  140/128     173/234
