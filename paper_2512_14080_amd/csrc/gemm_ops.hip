@@ -1375,7 +1375,10 @@ struct OpUp8 : F8Rows {
   struct Params { QuantArgs a; };
   static constexpr int IDX_LDS = Cfg::NW * Cfg::QM * 256;
   static constexpr int EPI_LDS = 3 * WN * Cfg::BM * 4;  // [gate, up, A][column group][row]
-  static constexpr int EPI_STORES = Cfg::RM * CB * (KEEP ? 3 : 1);  // A's codes, and H's
+  // A's codes, which every wave stores.  Not H's: the tiles cover n padded to whole
+  // blocks, so a tile counts as full although its last columns may not exist, and a
+  // wave of such columns stores A's padding alone.
+  static constexpr int EPI_STORES = Cfg::RM * CB;
   static __device__ int count(const Params& p, int*) { return count_varlen_m<256>(p.a.mtiles, 2 * q_pad(p.a.n)); }
   static __device__ int count_tail(const Params& p, const int*) {
     return count_varlen_m_tail<256>(p.a.mtiles, 2 * q_pad(p.a.n));
