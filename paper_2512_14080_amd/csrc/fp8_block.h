@@ -98,6 +98,10 @@ __device__ __forceinline__ float finite_amax(const float (&x)[N]) {
   return m;
 }
 
+// Rows of `blocks` blocks that one launch takes, 16 lanes a block: it holds fewer than
+// 2^32 work-items, and 2^27 blocks (32 GB of whole ones, 2 GB of rows of 8 columns) are half
+inline int64_t quant_rows(int blocks) { return (1 << 27) / blocks; }
+
 // Block u of the rows X [.., cols] (`blocks` blocks a row), by 16 lanes with 8 columns
 // (16 bytes) each: the largest |x| is a maximum over the lane's values and the lanes.
 __device__ __forceinline__ void quantize_unit(const uint16_t* __restrict__ X, int u, int blocks, int cols, int stride,

@@ -2144,22 +2144,30 @@ QuantTiles quant_tiles(const moe_dims& m, const moe_routing& r) {
   return q;
 }
 
+// the rows from `first` on, where X is more than one launch's
+static hipError_t quantize_from(int64_t first, const uint16_t* X, int T, int d, uint8_t* X8, uint8_t* Xs, hipStream_t s) {
+  return launch_quantize_rows(X + first * d, T - first, d, X8 + first * d, Xs + first * q_stride(d / kQBlock), s);
+}
 hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s) {
   if (a.E > 4096) return hipErrorInvalidValue;
   const bool two = a.tiles.up != a.tiles.down;
-  const int blocks = a.d / kQBlock, units = T * blocks, per = kMTilesThreads / 16;
+  const int blocks = a.d / kQBlock, first = (int)std::min<int64_t>(T, quant_rows(blocks));
+  const int units = first * blocks, per = kMTilesThreads / 16;
   quant_prepare_kernel<true><<<1 + two + (units + per - 1) / per, kMTilesThreads, 0, s>>>(
       a.offsets, a.E, two || a.tiles.up == 256 ? kMTileLog2 : kMTileLog2 - 1, a.mtiles, two ? a.mtiles128 : nullptr, a.X,
       units, blocks, a.X8, a.Xs);
-  return hipGetLastError();
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess ? quantize_from(first, a.X, T, a.d, a.X8, a.Xs, s) : err;
 }
 hipError_t launch_ckpt_prepare(const int32_t* offsets, int E, int32_t* mtiles, const uint16_t* X, int T, int d, uint8_t* X8,
                                uint8_t* Xs, hipStream_t s) {
   if (E > 4096) return hipErrorInvalidValue;
-  const int blocks = d / kQBlock, units = T * blocks, per = kMTilesThreads / 16;
+  const int blocks = d / kQBlock, first = (int)std::min<int64_t>(T, quant_rows(blocks));
+  const int units = first * blocks, per = kMTilesThreads / 16;
   quant_prepare_kernel<false><<<1 + (units + per - 1) / per, kMTilesThreads, 0, s>>>(offsets, E, kMTileLog2, mtiles, nullptr,
                                                                                    X, units, blocks, X8, Xs);
-  return hipGetLastError();
+  const hipError_t err = hipGetLastError();
+  return err == hipSuccess ? quantize_from(first, X, T, d, X8, Xs, s) : err;
 }
 hipError_t launch_quant_up(QuantArgs a, hipStream_t s) {
   const int grid = pad8(mtiles_bound(a.capacity, a.E, a.tiles.up) * q_blocks(a.n));
@@ -2277,12 +2285,18 @@ hipError_t launch_bwd_lists(const int32_t* offsets, int T, int64_t rows, int E, 
   const DwTile t2 = dw_tile(n, d, E, rows), t1 = dw_tile(d, 2 * n, E, rows);
   const int tpe2 = n_tiles(n, t2.bm) * n_tiles(d, t2.bn), tpe1 = n_tiles(d, t1.bm) * n_tiles(2 * n, t1.bn);
   const int tr_blocks = Wr ? (d * E + kMTilesThreads - 1) / kMTilesThreads : 0;
-  const int x_blocks = (kept.units + kMTilesThreads / 16 - 1) / (kMTilesThreads / 16);
+  const int blocks = d / kQBlock, per = kMTilesThreads / 16;
+  const int64_t first = kept.units ? std::min<int64_t>(T, quant_rows(blocks)) : T;  // rows of X in this launch
+  KeptX part = kept;
+  part.units = kept.units ? (int)first * blocks : 0;
+  const int x_blocks = (part.units + per - 1) / per;
   bwd_lists_kernel<<<3 + tr_blocks + x_blocks, kMTilesThreads, 0, s>>>(offsets, E, mtiles, tpe2, dw_slabs(T, (int64_t)n * d),
                                                            kchunk_keep_whole(E, tpe2), klist2, tpe1,
                                                            dw_slabs(T, (int64_t)d * 2 * n), kchunk_keep_whole(E, tpe1),
-                                                           klist1, Wr, WrT, d, tr_blocks, kept);
-  return hipGetLastError();
+                                                           klist1, Wr, WrT, d, tr_blocks, part);
+  const hipError_t err = hipGetLastError();
+  if (err != hipSuccess || first == T) return err;
+  return launch_dequantize_rows(kept.q + first * d, kept.scale + first * q_stride(blocks), T - first, d, kept.X + first * d, s);
 }
 
 // the GEMM over the k-chunk list (its split experts are summed by
