@@ -16,7 +16,8 @@ namespace smoe {
 
 constexpr int kQBlock = 128;
 
-__host__ __device__ inline int q_blocks(int cols) { return (cols + kQBlock - 1) / kQBlock; }
+// (cols >= 1, up to the largest int)
+__host__ __device__ inline int q_blocks(int cols) { return (cols - 1) / kQBlock + 1; }
 // columns padded to whole blocks
 __host__ __device__ inline int q_pad(int cols) { return q_blocks(cols) * kQBlock; }
 // bytes of a row's scales: whole dwords, which the products load

@@ -20,7 +20,7 @@ def _record(calls, tmp_path):
     so = os.path.join(str(tmp_path), "launch_recorder.so")
     subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-o", so, os.path.join(HERE, "launch_recorder.c")], check=True)
     r = subprocess.run([sys.executable, os.path.abspath(__file__), so], input=json.dumps(calls), text=True,
-                       capture_output=True, cwd=ROOT, env={**os.environ, "PYTHONPATH": ROOT + os.pathsep + HERE})
+                       capture_output=True, cwd=ROOT, timeout=60, env={**os.environ, "PYTHONPATH": ROOT + os.pathsep + HERE})
     assert r.returncode == 0, r.stderr
     return json.loads(r.stdout)
 
@@ -57,7 +57,8 @@ def _main():
 
 
 @built
-@pytest.mark.parametrize("rows,cols", [(1 << 28, 8), ((1 << 31) - 1, 128), (1 << 26, 4096 // 8), (1 << 20, 1 << 17)])
+@pytest.mark.parametrize("rows,cols", [(1 << 28, 8), ((1 << 31) - 1, 128), (1 << 26, 4096 // 8), (1 << 20, 1 << 17),
+                                       (127, (1 << 31) - 8)])
 def test_rows_grids(tmp_path, rows, cols):
     l, = _record([{"rows": (rows, cols)}], tmp_path)
     blocks = -(-cols // 128)
@@ -104,6 +105,32 @@ def test_rows_past_a_launchs_work_items():
         whole = rows // base
         assert (got[:whole * base].view(whole, base, -1) == w).all()
         assert torch.equal(got[whole * base:], w[:rows - whole * base])
+
+
+@pytest.mark.gpu
+def test_one_row_of_the_most_columns():
+    """2^31 - 8 columns: blocks of the last columns as of the first."""
+    torch = _torch()
+    base, cols = 128 * 1021, (1 << 31) - 8
+    g = torch.Generator(device="cuda").manual_seed(2)
+    small = torch.randn((base,), generator=g, device="cuda")
+    small = (small * torch.exp2(torch.randint(-30, 30, (base,), generator=g, device="cuda").float())).to(torch.bfloat16)
+
+    def through(x):
+        n = x.shape[0]
+        q = torch.full((n,), 0xAB, dtype=torch.uint8, device="cuda")
+        s = torch.full((B.scale_stride(n),), 0xCD, dtype=torch.uint8, device="cuda")
+        back = torch.full((n,), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.moe_quantize_rows(1, n, x, q, s)
+        B.moe_dequantize_rows(1, n, q, s, back)
+        return q, s[:-(-n // 128)], back
+
+    X = small.repeat(-(-cols // base))[:cols]
+    whole = cols // base
+    want, tail = through(small), through(X[whole * base:].clone())
+    for got, w, t, per in zip(through(X), want, tail, (1, 128, 1)):
+        n = whole * base // per
+        assert (got[:n].view(whole, -1) == w).all() and torch.equal(got[n:], t)
 
 
 if __name__ == "__main__":
