@@ -468,11 +468,13 @@ __device__ __forceinline__ void store_part_f32(float* out, int64_t ld, int m0, i
 
 // Logical tile ids run over the tiles of their class (full m-tiles, then the
 // partial ones) in tile_order, so neighbouring ids share the rows of an m-tile
-// and the weights of an expert.  The list is of tiles of BM rows.  The list entry is
+// and the weights of an expert.  The list entry is
 // read with a scalar load (the id is workgroup-uniform).  PLAIN: N is a multiple
 // of BN and less than 8 BN, so the tiles are whole and go row by row.
-template <int BM, int BN, bool PLAIN = false>
+// LIST_ROWS: rows of the list's tiles
+template <int BM, int BN, bool PLAIN = false, int LIST_ROWS = kMTile>
 __device__ __forceinline__ bool tile_varlen_m(const int32_t* mtiles, int E, int N, int K, int id, TileInfo& ti) {
+  static_assert(BM == LIST_ROWS, "varlen-M tiles are the m-tile list's tiles");
   const int nnt = PLAIN ? N / BN : (N + BN - 1) / BN;
   const bool partial = (id & kPartialTile) != 0;
   id &= kPartialTile - 1;
@@ -1361,6 +1363,16 @@ struct F8Rows {
   static constexpr bool F8 = true;
   static constexpr int M_MODE = ROWS, N_MODE = ROWS;
 };
+// the list of m-tiles of BM rows, and a tile of it
+template <int BM>
+__device__ __forceinline__ const int32_t* quant_list(const QuantArgs& a) {
+  static_assert(BM == 256 || BM == 128, "the lists that launch_quant_prepare writes");
+  return BM == 256 ? a.mtiles256 : a.mtiles128;
+}
+template <int BM, int BN>
+__device__ __forceinline__ bool quant_tile(const QuantArgs& a, int N, int K, int id, TileInfo& ti) {
+  return tile_varlen_m<BM, BN, false, BM>(quant_list<BM>(a), a.E, N, K, id, ti);
+}
 
 // N tile: 128 gate columns and the matching up columns, in the order the weights
 // are laid out in: accumulator column blocks alternate between 32 gate and 32 up
@@ -1379,12 +1391,12 @@ struct OpUp8 : F8Rows {
   // blocks, so a tile counts as full although its last columns may not exist, and a
   // wave of such columns stores A's padding alone.
   static constexpr int EPI_STORES = Cfg::RM * CB;
-  static __device__ int count(const Params& p, int*) { return count_varlen_m<256>(p.a.mtiles, 2 * q_pad(p.a.n)); }
+  static __device__ int count(const Params& p, int*) { return count_varlen_m<256>(quant_list<Cfg::BM>(p.a), 2 * q_pad(p.a.n)); }
   static __device__ int count_tail(const Params& p, const int*) {
-    return count_varlen_m_tail<256>(p.a.mtiles, 2 * q_pad(p.a.n));
+    return count_varlen_m_tail<256>(quant_list<Cfg::BM>(p.a), 2 * q_pad(p.a.n));
   }
   static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
-    return tile_varlen_m<Cfg::BM, Cfg::BN>(p.a.mtiles, p.a.E, 2 * q_pad(p.a.n), p.a.d / 2, id, ti);
+    return quant_tile<Cfg::BM, Cfg::BN>(p.a, 2 * q_pad(p.a.n), p.a.d / 2, id, ti);
   }
   static __device__ void init_m(const Params& p, const TileInfo& ti, RowsSide<Cfg::BM, Cfg::BK, Cfg::NW, true>& s) {
     s.init((const uint16_t*)p.a.X8, p.a.d / 2, p.a.row_token, ti.row_base, ti.mrows);
@@ -1513,10 +1525,12 @@ struct OpDown8 : F8Rows {
   struct Params { QuantArgs a; int slots; };  // slots: of DownRounds
   static constexpr int EPI_LDS = 0;
   static constexpr int EPI_STORES = kStoresPerFullTile<Cfg>;
-  static __device__ int count(const Params& p, int*) { return count_varlen_m<Cfg::BN>(p.a.mtiles, p.a.d); }
-  static __device__ int count_tail(const Params& p, const int*) { return count_varlen_m_tail<Cfg::BN>(p.a.mtiles, p.a.d); }
+  static __device__ int count(const Params& p, int*) { return count_varlen_m<Cfg::BN>(quant_list<Cfg::BM>(p.a), p.a.d); }
+  static __device__ int count_tail(const Params& p, const int*) {
+    return count_varlen_m_tail<Cfg::BN>(quant_list<Cfg::BM>(p.a), p.a.d);
+  }
   static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
-    return tile_varlen_m<Cfg::BM, Cfg::BN>(p.a.mtiles, p.a.E, p.a.d, q_pad(p.a.n) / 2, id, ti);
+    return quant_tile<Cfg::BM, Cfg::BN>(p.a, p.a.d, q_pad(p.a.n) / 2, id, ti);
   }
   static __device__ void init_m(const Params& p, const TileInfo& ti, RowsSide<Cfg::BM, Cfg::BK, Cfg::NW>& s) {
     s.init((const uint16_t*)p.a.A8, q_pad(p.a.n) / 2, nullptr, ti.row_base, ti.mrows);
@@ -1549,7 +1563,7 @@ struct OpDown8 : F8Rows {
 struct DownRounds {
   int begin, whole, rest;  // an XCD's tiles: the first, those of the 256 x 256 launch, those in quarters
   __device__ __forceinline__ DownRounds(const QuantArgs& a, int slots, int xcd) {
-    const int tiles = count_varlen_m<256>(a.mtiles, a.d), per = (tiles + 7) >> 3;  // as Sched::init
+    const int tiles = count_varlen_m<256>(quant_list<256>(a), a.d), per = (tiles + 7) >> 3;  // as Sched::init
     begin = xcd * per;
     whole = max(0, min(per, tiles - begin));
     rest = whole % slots;
@@ -1578,7 +1592,7 @@ struct OpDown8<Cfg_, kDownQuarters> : OpDown8<Cfg_> {
     *count = 4 * r.rest;
   }
   static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
-    if (!tile_varlen_m<256, 256>(p.a.mtiles, p.a.E, p.a.d, q_pad(p.a.n) / 2, id >> 2, ti)) return false;
+    if (!quant_tile<256, 256>(p.a, p.a.d, q_pad(p.a.n) / 2, id >> 2, ti)) return false;
     const int r0 = 128 * ((id >> 1) & 1), c0 = 128 * (id & 1);
     ti.m0 += r0;
     ti.row_base += r0;
@@ -2150,12 +2164,12 @@ static hipError_t quantize_from(int64_t first, const uint16_t* X, int T, int d, 
 }
 hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s) {
   if (a.E > 4096) return hipErrorInvalidValue;
-  const bool two = a.tiles.up != a.tiles.down;
+  const bool two = a.tiles.up != a.tiles.down, wide = two || a.tiles.up == 256;
   const int blocks = a.d / kQBlock, first = (int)std::min<int64_t>(T, quant_rows(blocks));
   const int units = first * blocks, per = kMTilesThreads / 16;
   quant_prepare_kernel<true><<<1 + two + (units + per - 1) / per, kMTilesThreads, 0, s>>>(
-      a.offsets, a.E, two || a.tiles.up == 256 ? kMTileLog2 : kMTileLog2 - 1, a.mtiles, two ? a.mtiles128 : nullptr, a.X,
-      units, blocks, a.X8, a.Xs);
+      a.offsets, a.E, wide ? kMTileLog2 : kMTileLog2 - 1, wide ? a.mtiles256 : a.mtiles128, two ? a.mtiles128 : nullptr,
+      a.X, units, blocks, a.X8, a.Xs);
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? quantize_from(first, a.X, T, a.d, a.X8, a.Xs, s) : err;
 }
@@ -2169,13 +2183,12 @@ hipError_t launch_ckpt_prepare(const int32_t* offsets, int E, int32_t* mtiles, c
   const hipError_t err = hipGetLastError();
   return err == hipSuccess ? quantize_from(first, X, T, d, X8, Xs, s) : err;
 }
-hipError_t launch_quant_up(QuantArgs a, hipStream_t s) {
+hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s) {
   const int grid = pad8(mtiles_bound(a.capacity, a.E, a.tiles.up) * q_blocks(a.n));
   if (a.tiles.up == 256) return a.H8 ? run<OpUp8<C256x256w, true>>({a}, grid, s) : run<OpUp8<C256x256w, false>>({a}, grid, s);
-  if (a.tiles.down == 256) a.mtiles = a.mtiles128;
   return a.H8 ? run<OpUp8<F128x256, true>>({a}, grid, s) : run<OpUp8<F128x256, false>>({a}, grid, s);
 }
-hipError_t launch_quant_down(QuantArgs a, hipStream_t s) {
+hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s) {
   const int mt = mtiles_bound(a.capacity, a.E, a.tiles.down);
   if (a.tiles.down == 256 && a.n >= kQuartersMinK) {
     const int bound = pad8(mt * n_tiles(a.d, 256)), slots = run_grid<OpDown8<C256x256w, kDownWhole>>(bound) / 8;
@@ -2185,7 +2198,6 @@ hipError_t launch_quant_down(QuantArgs a, hipStream_t s) {
     return hipGetLastError();
   }
   if (a.tiles.down == 256) return run<OpDown8<C256x256w>>({a, 0}, pad8(mt * n_tiles(a.d, 256)), s);
-  if (a.tiles.up == 256) a.mtiles = a.mtiles128;
   return run<OpDown8<F128x128>>({a, 0}, pad8(mt * (a.d / 128)), s);
 }
 

@@ -234,7 +234,7 @@ struct QuantArgs {
   const uint16_t* X; uint8_t* X8; uint8_t* Xs;
   const uint8_t* W1q; const uint8_t* W1s; const uint8_t* W2q; const uint8_t* W2s;
   const int32_t* offsets; const int32_t* row_token;
-  int32_t* mtiles; int32_t* mtiles128;  // (the second where the two differ)
+  int32_t* mtiles256; int32_t* mtiles128;  // of the tiles' rows (`tiles`: either or both)
   const float* b1; const float* b2;
   float* A32; uint8_t* A8; uint8_t* As; uint8_t* H8; uint8_t* Hs; uint16_t* Y; float* Y32;
   int d, n, E, capacity;
@@ -245,8 +245,8 @@ hipError_t launch_quant_prepare(const QuantArgs& a, int T, hipStream_t s);
 // the m-tile list of the 16-bit projections, and X into 8-bit blocks
 hipError_t launch_ckpt_prepare(const int32_t* offsets, int E, int32_t* mtiles, const uint16_t* X, int T, int d, uint8_t* X8,
                                uint8_t* Xs, hipStream_t s);
-hipError_t launch_quant_up(QuantArgs a, hipStream_t s);
-hipError_t launch_quant_down(QuantArgs a, hipStream_t s);
+hipError_t launch_quant_up(const QuantArgs& a, hipStream_t s);
+hipError_t launch_quant_down(const QuantArgs& a, hipStream_t s);
 // The same for few rows per expert, from X in bf16 (stream_gemm.hip); stream8_shape:
 // mb = 0 where the tiled ones are the better ones
 StreamShape stream8_shape(const moe_dims& m, int capacity, int m_tile);

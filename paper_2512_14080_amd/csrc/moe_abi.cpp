@@ -206,7 +206,7 @@ struct QuantWs {
   uint8_t* As;
   uint16_t* Y;
   float* Y32;
-  int32_t* mtiles;
+  int32_t* mtiles256;
   int32_t* mtiles128;
 };
 size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
@@ -222,7 +222,7 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   off = carve(base, off, (size_t)cap * smoe::q_stride(smoe::q_blocks(m.n)), w ? (void**)&w->As : nullptr);
   off = carve(base, off, (size_t)cap * m.d * (streams ? 4 : 2), w ? (void**)&w->Y : nullptr);
   if (w) w->Y32 = (float*)w->Y;
-  off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles : nullptr);
+  off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 256), w ? (void**)&w->mtiles256 : nullptr);
   off = carve(base, off, smoe::mtiles_bytes(cap, m.E, 128), w ? (void**)&w->mtiles128 : nullptr);
   return off;
 }
@@ -899,7 +899,7 @@ int moe_fwd_quant(moe_dims m, const moe_bf16* X, const moe_qexperts* q, const mo
   if (c) c->state = MOE_HELD_EMPTY;  // until all of it is enqueued
   uint8_t* X8 = c && c->X ? c->X : w.X8;
   uint8_t* Xs = c && c->X ? c->Xs : w.Xs;
-  const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles, w.mtiles128,
+  const smoe::QuantArgs a{X, X8, Xs, q->W1, q->W1s, q->W2, q->W2s, r->offsets, r->row_token, w.mtiles256, w.mtiles128,
                           eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, w.A32, w.A8, w.As, c ? c->H : nullptr,
                           c ? c->Hs : nullptr, w.Y, w.Y32, m.d, m.n, m.E, r->capacity, smoe::quant_tiles(m, *r),
                           r->row_expert, r->row_w, r->tok_offsets, r->tok_rows, O};
