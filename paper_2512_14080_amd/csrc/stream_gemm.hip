@@ -752,24 +752,42 @@ static hipError_t run_stream8(const QuantArgs& p, const StreamShape& t, int cols
 //     d = 1536, n = 1024, E = 16, K = 2, T = 512     34.1   39.7     31.6
 //   and one token (d = 1536, n = 256, 8 rows): 64 columns and 8 waves 8.4, 32 and 16 waves
 //   6.4; d = 4096, n = 512: 19.6, 14.3; but d = 4096, n = 14336, 2 rows (the CUs are full): 40, 52
-//   down                                     32, 2   64, 2   64, 4   128, 1   128, 2   128, 4
-//     d = 1536, n = 256, E = 128, T = 1       3.6     3.9     4.2              3.9      5.1
-//     d = 4096, n = 14336, E = 8, T = 1       47.6    60.4    35.4 (32, 4 waves: 32.1)
-//     d = 4096, n = 512, E = 128, T = 64              44.6    44.9             44.1     40.8
-//     d = 1024, n = 256, E = 64, T = 64               7.0     8.1     7.8      6.9      6.9
-//     d = 1536, n = 256, E = 128, T = 128             14.6    17.1    12.6     16.1     15.4
-//     d = 2048, n = 128, E = 256, T = 128             17.9    26.0    15.1     18.0     24.1
-//     d = 4096, n = 512, E = 128, T = 256             71.5    72.9    58.9     59.0     59.8
+//   down, Y in fp32                          32, 2   32, 4   64, 2   64, 4   128, 1   128, 2   128, 4
+//    16-row groups
+//     d = 1536, n = 256, E = 128, T = 16      9.1     9.6     8.3     9.4     15.3     13.8     17.3
+//     d = 768, n = 256, E = 8, T = 16         3.7     3.6     3.8     4.0     8.3      5.8      5.8
+//     d = 896, n = 320, E = 8, T = 10         4.2     3.6     4.4     4.0     12.4     9.6      6.4
+//     d = 1280, n = 1152, E = 8, T = 5        6.7     6.0     7.6     6.4     35.5     22.0     14.8
+//     d = 1024, n = 1024, E = 16, T = 8       6.8     6.5     6.8     5.9     32.6     19.4     12.4
+//     d = 4096, n = 14336, E = 8, T = 4       87.2    92.1    79.8    74.8    557      363      206
+//     d = 4096, n = 512, E = 128, K = 8, T = 32     51.4    48.6    44.4    40.9    78.1   72.2     76.1
+//    32-row groups
+//     d = 1024, n = 256, E = 64, T = 64       8.6     9.2     7.2     8.0     8.2      7.2      7.7
+//     d = 1536, n = 256, E = 128, T = 128     19.5    22.6    15.9    19.4    16.0     18.1     17.7
+//     d = 2048, n = 128, E = 256, T = 128     23.6    38.0    20.2    30.8    17.4     20.5     29.0
+//     d = 1024, n = 512, E = 16, T = 20       6.1     4.9     5.0     5.3     8.6      6.5      5.4
+//     d = 768, n = 1024, E = 32, K = 2, T = 64      10.0    10.2    10.7    10.3    13.9   11.2     9.5
+//     d = 2048, n = 1024, E = 32, T = 64      28.2    26.9    21.4    21.0    24.3     17.8     19.4
+//     d = 4096, n = 512, E = 128, T = 256     106     109     73.6    73.6    67.1     64.9     65.7
+//     d = 2048, n = 2048, E = 16, K = 1, T = 100    26.8    24.9    20.5    20.2    29.9   22.2     18.4
+//     d = 4096, n = 4096, E = 16, K = 2, T = 64     93.5    89.6    73.0    66.8    73.9   70.7     62.6
+//     d = 4096, n = 14336, E = 8, K = 2, T = 20     152     146     98.3    102     191    125      86.8
+//   so: more waves over a long k, or where there are few workgroups; 64 columns of 16 rows
+//   where they are a workgroup to a CU at least
 hipError_t launch_stream8_up(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
   if (t.mb == 1 && (int64_t)a.capacity * (a.n / 32) <= 128) return run_stream8<Stream8Up, 2, 1, 16, 4>(a, t, a.n, s);
   if (t.mb == 1) return run_stream8<Stream8Up, 4, 1, 8, 4>(a, t, a.n, s);
   return run_stream8<Stream8Up, 4, 2, 4, 4>(a, t, a.n, s);
 }
 hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStream_t s) {
-  const int blocks = q_blocks(a.n);
-  if (t.mb == 1 && blocks <= 2) return run_stream8<Stream8Down, 2, 1, 2, 4>(a, t, a.d, s);
-  if (t.mb == 1) return run_stream8<Stream8Down, 2, 1, 4, 4>(a, t, a.d, s);
-  if (blocks <= 2 && a.E * (a.d / kQBlock) > 768) return run_stream8<Stream8Down, 8, 2, 1, 2>(a, t, a.d, s);
+  const int blocks = q_blocks(a.n), groups = a.E * (a.d / kQBlock);
+  if (t.mb == 1) {
+    if (blocks <= 2) return run_stream8<Stream8Down, 2, 1, 2, 4>(a, t, a.d, s);
+    if (2 * groups < 256) return run_stream8<Stream8Down, 2, 1, 4, 4>(a, t, a.d, s);
+    return run_stream8<Stream8Down, 4, 1, 4, 4>(a, t, a.d, s);
+  }
+  if (blocks <= 2 && groups > 768) return run_stream8<Stream8Down, 8, 2, 1, 2>(a, t, a.d, s);
+  if (blocks >= 16 || (blocks > 2 && groups <= 256)) return run_stream8<Stream8Down, 8, 2, 4, 2>(a, t, a.d, s);
   return run_stream8<Stream8Down, 8, 2, 2, 2>(a, t, a.d, s);
 }
 
