@@ -792,23 +792,34 @@ hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStre
 }
 
 // Up to E / 2 rows of a token choice, and up to E where the rows' weights are at most 128
-// MB: by row and by token.  us a call, by expert (three launches) / so, by tokens; where
-// rows repeat experts, their weights are read again:
+// MB, of tokens that make at most 1024 workgroups of 32 columns: by row and by token.  us a
+// call, by expert (three launches) / so, by tokens; where rows repeat experts, their
+// weights are read again:
 //     T =                                1          2           4           8           12          16
 //   d = 1536, n = 256, E = 128, K = 8    13.8/11.1  17.3/12.3   19.8/13.7   22.0/19.7   26.6/25.5   29.0/29.1
 //   d = 1024, n = 256, E = 64, K = 8     10.9/10.3  12.9/10.6   15.0/11.8   16.7/14.2
 //   d = 2048, n = 128, E = 256, K = 10   17.1/10.5              23.6/13.1               28.1/24.9   34.2/28.9
 //     (25 tokens, 196 MB: 35.5/40.0)
-//   d = 4096, n = 64, E = 64, K = 4                                                          19.6/21.9
 //   d = 640, n = 768, E = 16, K = 2, 7 tokens: 13.6/12.0; d = 768, n = 512, E = 64, K = 2, 32: 20.3/20.6
-//   d = 4096, n = 512, E = 128, K = 8    26.6/19.4  34.7/23.4   48.8/43.4   73.4/72.4   91/99       105/124
+//   d = 4096, n = 512, E = 128, K = 8    26.6/19.4  34.7/23.4   48.8/43.4   64.6/69.0   91/99       105/124
 //   d = 2048, n = 1024, E = 32, K = 4    18.7/16.3  24.1/17.6   28.3/22.1   33.8/37.3
 //   d = 4096, n = 14336, E = 8, K = 2    91.3/90.6  140/128     173/234
+// Many workgroups of one or a few steps each lose what the third launch costs (T d / 32):
+//   n = 64    d = 4096, E = 64, K = 4, 16 tokens (2048 of them): 19.6/21.8
+//             d = 4096, E = 128: K = 8, 8 (1024): 26.6/20.1; K = 1, 64 (8192): 25.8/35.2
+//             d = 4096, E = 256, K = 4, 32 (4096): 36.6/34.4; d = 1024, K = 8, 32 (1024): 19.6/18.7
+//             d = 2048, E = 256: K = 8, 32 (2048): 26.5/30.1; K = 1, 128 (8192): 22.1/34.5
+//             d = 1536, E = 128, K = 2, 64 (3072): 15.0/20.3
+//   n = 128   d = 2048, E = 64, K = 2, 16 (1024): 16.0/11.2; d = 1024, E = 128, K = 2, 64 (2048): 15.3/18.4
+//             d = 4096, E = 256, K = 8, 16 (2048): 37.7/40.7
+//   n = 256   d = 2048, E = 64, K = 1, 32 (2048): 20.5/18.6
+//   n = 512   d = 2048, E = 64, K = 2, 16 (1024): 24.1/22.7; d = 4096, E = 128, K = 1, 64 (8192): 62/81
 // Columns and waves as above; of the down-projection: 32 and 8 (16 waves: coarse 102
 // instead of 91 a call; 64 columns and 16 or 4 waves: +2 to 25).
 bool stream8_by_token(const moe_dims& m, const moe_routing& r) {
   const int64_t rows = (int64_t)m.T * m.K;
-  return token_choice(r) && (2 * rows <= m.E || (rows <= m.E && rows * 3 * m.d * m.n <= 128 << 20));
+  return token_choice(r) && (int64_t)m.T * (m.d / 32) <= 1024 &&
+         (2 * rows <= m.E || (rows <= m.E && rows * 3 * m.d * m.n <= 128 << 20));
 }
 hipError_t launch_stream8_row_up(const QuantArgs& a, int T, int K, hipStream_t s) {
   const int rows = std::min(T * K, a.capacity);

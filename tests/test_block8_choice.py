@@ -1,4 +1,5 @@
-"""Columns and waves of the streaming 8-bit down-projection, without a GPU and each form on one."""
+"""Columns and waves of the streaming 8-bit down-projection, without a GPU and each form on one, and which few tokens go by
+row and token."""
 import re
 
 import pytest
@@ -23,6 +24,17 @@ from test_gpu_block8 import _check_o, _layer, _torch
 def test_shape_of_the_streaming_down_projection(tmp_path, dims, shape):
     l, = launches([(dims, "quant", 0, False)], tmp_path)
     assert re.search(r"stream8_gemm_kernel.*Stream8DownELi(\d)ELi(\d)ELi(\d+)E", _names(l)).groups() == tuple(map(str, shape))
+
+
+@built
+@pytest.mark.parametrize("dims,by_token", [  # workgroups of the down-projection by token: T d / 32
+    ((8, 4096, 64, 128, 8), True), ((16, 2048, 128, 64, 2), True), ((32, 1024, 64, 256, 8), True),
+    ((16, 4096, 64, 64, 4), False), ((64, 1536, 64, 128, 2), False), ((64, 4096, 64, 128, 1), False),
+    ((64, 1024, 128, 128, 2), False), ((64, 4096, 512, 128, 1), False),
+])
+def test_few_tokens_of_many_workgroups_go_by_expert(tmp_path, dims, by_token):
+    l, = launches([(dims, "quant", 0, False)], tmp_path)
+    assert ("stream8_token_down" in _names(l)) == by_token
 
 
 @pytest.mark.gpu
