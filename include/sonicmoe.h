@@ -386,9 +386,11 @@ int moe_dequantize_experts(moe_dims dims, const moe_qexperts *q, moe_bf16 *W1, m
  * The activations a forward keeps for the backward, in the 8-bit block format:
  * H (blocks of 128 columns within the gate and the up half: a row's scales are
  * its ceil(n/128) gate blocks, then its up blocks) and, with MOE_CKPT_X, X.  2 P n (+ T d)
- * bytes instead of 4 P n (+ 2 T d).  One caller-allocated device buffer, laid out
- * by moe_ckpt_init, written by moe_fwd_ckpt or moe_fwd_quant, read by
- * moe_bwd_ckpt.
+ * bytes instead of 4 P n (+ 2 T d), held from the forward to the backward.  The
+ * workspaces hold the other form of X all the same, whether or not a call uses it:
+ * MOE_WS_BWD_CKPT is MOE_WS_BWD and 2 T d bytes, MOE_WS_FWD_QUANT has a q(X) of T d.
+ * One caller-allocated device buffer, laid out by moe_ckpt_init, written by
+ * moe_fwd_ckpt or moe_fwd_quant, read by moe_bwd_ckpt.
  */
 typedef struct {
   int32_t T, d, n, capacity;
@@ -409,15 +411,18 @@ int moe_ckpt_init(moe_dims dims, int32_t capacity, int flags, void *buf, size_t 
  * Forward with 8-bit expert products: with q() the block format,
  *   H = gather(q(X)) q(W1_e) (+ b1_e);  A = SiLU(H_gate) * H_up
  *   Y = q(A) q(W2_e) (+ b2_e);          O_t = sum_{rows of t} s * Y
- * Products accumulate in fp32; A is quantised from fp32 (blocks of 128 columns of a row), Y
- * is held in bf16 as in moe_fwd, or in fp32 for few rows (without c: T <= 16, or a mean of up
- * to 10 rows per expert, 16 where d is large).
+ * The block-scaled 8-bit matrix instruction sums a product to 1.3e-5 of its value (fp32 sums:
+ * 1e-7); A is quantised from fp32 (blocks of 128 columns of a row); Y is rounded to bf16
+ * before its weighted sum, as in moe_fwd.  For few rows and without c, Y stays in fp32 (T <=
+ * 16, or a mean of up to 10 rows per expert, 16 where d >= 4096 and n <= 4096), and for fewer
+ * the up-projection's codes are multiplied with fp32 sums (T <= 16, or a mean of up to 2).
+ * O's error to this definition in 64 bits is 2.7e-3 of it, 2.1e-3 and 1.7e-3 in that order;
+ * one rounding to bf16 alone is 1.7e-3.
  *   w    weights in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of the
  *        same d, n and E
  *   c    nullable: then nothing is kept for a backward.  Otherwise q(H) (and
- *        q(X)) are written and c->state becomes MOE_HELD_WRITTEN: moe_bwd_ckpt
- *        with the 16-bit weights is the backward of this forward, its
- *        roundings taken to carry no gradient
+ *        q(X)) are written and c->state becomes MOE_HELD_WRITTEN, for
+ *        moe_bwd_ckpt (which see: an approximation of this forward's gradient)
  *   ws   moe_workspace_bytes(dims, r->capacity, MOE_WS_FWD_QUANT) bytes
  * Other arguments as moe_fwd.
  */
@@ -435,7 +440,15 @@ int moe_fwd_ckpt(moe_dims dims, const moe_bf16 *X, const moe_bf16 *W1, const moe
 
 /*
  * moe_bwd from an 8-bit checkpoint: the gradients of moe_bwd with the kept
- * values in the place of H and, where X is null, of X.
+ * values in the place of H and, where X is null, of X.  So W1, W2 and a given X
+ * enter as they are, and A is SwiGLU of the kept H, without a rounding of its own.
+ * After moe_fwd_ckpt that is the layer's backward but for the rounding of what is
+ * kept.  After moe_fwd_quant it is the 16-bit layer's backward at that forward's
+ * H, not the gradient of its 8-bit products: with every rounding passed straight
+ * through, that has q(W1), q(W2), q(X) and q(A) in their place.  The two are 4 to
+ * 5% of the gradients' norm apart, 7% for dWr (a code is up to 2^-4 of its value
+ * off); with the weights of moe_dequantize_experts and the kept X 3 to 6%, the rest
+ * being A's and H's roundings.
  *   c    checkpoint in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of
  *        the same T, d, n and capacity
  *   X    [T,d] bf16, or null to use the kept one (then c needs MOE_CKPT_X)
