@@ -853,17 +853,22 @@ int moe_dequantize_experts(moe_dims m, const moe_qexperts* q, moe_bf16* W1, moe_
   return MOE_OK;
 }
 
+static int check_ckpt_size(const moe_dims& m, int32_t capacity, int flags) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  if (capacity < 1) return fail(MOE_ERR_CAPACITY, "capacity must be >= 1 (got %d)", capacity);
+  if (flags & ~MOE_CKPT_X) return fail(MOE_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  return MOE_OK;
+}
+
 size_t moe_ckpt_bytes(moe_dims m, int32_t capacity, int flags) {
-  if (check_dims(m) != MOE_OK || capacity < 1 || (flags & ~MOE_CKPT_X)) return 0;
-  return ckpt_layout(m, capacity, flags, nullptr, nullptr);
+  return check_ckpt_size(m, capacity, flags) == MOE_OK ? ckpt_layout(m, capacity, flags, nullptr, nullptr) : 0;
 }
 
 int moe_ckpt_init(moe_dims m, int32_t capacity, int flags, void* buf, size_t bytes, moe_ckpt* c) {
-  int rc = check_dims(m);
+  int rc = check_ckpt_size(m, capacity, flags);
   if (rc) return rc;
   if (!c) return fail(MOE_ERR_INVALID_ARG, "c must not be null");
-  if (capacity < 1) return fail(MOE_ERR_CAPACITY, "capacity must be >= 1 (got %d)", capacity);
-  if (flags & ~MOE_CKPT_X) return fail(MOE_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   CHECK_PTR(buf, kAlign);
   const size_t need = ckpt_layout(m, capacity, flags, nullptr, nullptr);
   if (bytes < need) return fail(MOE_ERR_INVALID_ARG, "checkpoint buffer of %zu bytes < required %zu", bytes, need);
