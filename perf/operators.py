@@ -351,6 +351,10 @@ def _prepare_own(B, s, case, S):
     B.moe_route(D, None, None, None, B.MOE_ROUTE_SCORES_IN | (B.MOE_ROUTE_WRITE_SCORES_T if M else 0), tc)
     s["r"] = tc
     if M:
+        # an expert's own tokens in the selection's order: that of S + 2 in 32 bits, where scores less than 2^-22 apart are equal
+        a = tc.arrays()
+        picked = torch.zeros((T, E), dtype=torch.bool, device="cuda").scatter_(1, a["topk_idx"].long(), True)
+        a["scores_t"].copy_(torch.where(picked, S + 2 - 2, S).t())
         s["r"] = B.Routing(D, B.moe_round_capacity(D, M))
         B.moe_round_tokens(D, M, "nearest", None, tc, s["r"])
     cap = s["r"].capacity
