@@ -417,7 +417,8 @@ int moe_ckpt_init(moe_dims dims, int32_t capacity, int flags, void *buf, size_t 
  * 16, or a mean of up to 10 rows per expert, 16 where d >= 4096 and n <= 4096), and for fewer
  * the up-projection's codes are multiplied with fp32 sums (T <= 16, or a mean of up to 2).
  * O's error to this definition in 64 bits is 2.7e-3 of it, 2.1e-3 and 1.7e-3 in that order;
- * one rounding to bf16 alone is 1.7e-3.
+ * one rounding to bf16 alone is 1.7e-3.  With c the up-projection's sums are fp32 too, so that
+ * the codes of H that a backward reads are the definition's but for a few in 10^6 (O: 2.4e-3).
  *   w    weights in state MOE_HELD_WRITTEN (otherwise MOE_ERR_INVALID_ARG), of the
  *        same d, n and E
  *   c    nullable: then nothing is kept for a backward.  Otherwise q(H) (and

@@ -61,6 +61,18 @@ __device__ __forceinline__ f32x4 unpack_fp8x4(uint32_t v, float scale) {
   const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, scale, true);
   return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
+// codes 8 i .. 8 i + 7 of a fragment as bf16 values, code * scale (exact above bf16's
+// smallest, 2^-133)
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ bf16x8 codes_bf16(const i32x8& q, int i, float scale) {
+  u32x4 v;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    v[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + h], scale, false));
+    v[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + h], scale, true));
+  }
+  return __builtin_bit_cast(bf16x8, v);
+}
 // the largest |x| of N bf16 pairs, finite ones only, as bf16 bits
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 template <int N>

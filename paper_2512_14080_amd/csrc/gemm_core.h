@@ -38,7 +38,7 @@
 #pragma once
 #include <type_traits>
 
-#include "device_common.h"
+#include "fp8_block.h"
 
 namespace smoe {
 
@@ -430,7 +430,14 @@ template <class Op, class = void>
 struct IsF8 : std::false_type {};
 template <class Op>
 struct IsF8<Op, std::void_t<decltype(Op::F8)>> : std::true_type {};
-typedef int i32x8 __attribute__((ext_vector_type(8)));
+// Such an op may also define  static constexpr bool FP32_SUMS  = true: the same codes are
+// multiplied in bf16 (exact products, summed in fp32), four MFMAs to an 8-bit one.  The
+// 8-bit instruction sums to 1.3e-5 of the result, which moves 3 in 10^4 values that are
+// quantised next to the other side of a step.
+template <class Op, class = void>
+struct Fp32Sums : std::false_type {};
+template <class Op>
+struct Fp32Sums<Op, std::void_t<decltype(Op::FP32_SUMS)>> : std::integral_constant<bool, Op::FP32_SUMS> {};
 // the 32 codes of each lane for sub-step s (64 k) of a stage
 template <class Side>
 __device__ __forceinline__ i32x8 frag8(const char* lds_side, int r0, int s) {
@@ -832,7 +839,57 @@ __global__ __launch_bounds__(Op::Cfg::THREADS, Op::Cfg::OCC) void grouped_gemm_k
           else
             ns.issue(st_next + Cfg::M_BYTES, knext * BK, d - Cfg::QM, Cfg::QN);
         };
-        if (live) {
+        if constexpr (Fp32Sums<Op>::value) {
+          if (live) {
+            // rows' fragments become bf16 once a sub-step, and the next sub-step's are read
+            // into their place; a column's are converted eight codes at a time
+            i32x8 fm[Cfg::RM], fn[2];
+            bf16x8 mb[Cfg::RM][4];
+            float xv[Cfg::RM], wv[NS];
+#pragma unroll
+            for (int i = 0; i < Cfg::RM; ++i) xv[i] = scale_value(xs[i] & 255);
+#pragma unroll
+            for (int q = 0; q < NS; ++q) wv[q] = scale_value(ws[q] & 255);
+#pragma unroll
+            for (int i = 0; i < Cfg::RM; ++i) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, 0);
+            fn[0] = frag8<NSide>(ln, wn0, 0);
+#pragma unroll
+            for (int s = 0; s < SUB8; ++s) {
+#pragma unroll
+              for (int i = 0; i < Cfg::RM; ++i) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g) mb[i][g] = codes_bf16(fm[i], g, xv[i]);
+                if (s + 1 < SUB8) fm[i] = frag8<MSide>(lm, wm0 + 32 * i, s + 1);
+              }
+#pragma unroll
+              for (int j = 0; j < Cfg::RN; ++j) {
+                if (j + 1 < Cfg::RN)
+                  fn[(j + 1) & 1] = frag8<NSide>(ln, wn0 + 32 * (j + 1), s);
+                else if (s + 1 < SUB8)
+                  fn[(j + 1) & 1] = frag8<NSide>(ln, wn0, s + 1);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                  const bf16x8 nb = codes_bf16(fn[j & 1], g, wv[j % NS]);
+#pragma unroll
+                  for (int i = 0; i < Cfg::RM; ++i) {
+                    const int c = ((s * Cfg::RN + j) * 4 + g) * Cfg::RM + i;
+                    if constexpr (ISSUE) {
+                      if (c < 2 * kPerStage && c % 2 == 0) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        issue_one(c / 2);
+                        __builtin_amdgcn_sched_barrier(0);
+                      }
+                    }
+                    acc.acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nb, mb[i][g], acc.acc[i][j], 0, 0, 0);
+                  }
+                }
+              }
+            }
+          } else if constexpr (ISSUE) {
+            ms.issue(st_next, knext * BK);
+            ns.issue(st_next + Cfg::M_BYTES, knext * BK);
+          }
+        } else if (live) {
           // one column fragment ahead: the one of the next column is read while this
           // one's MFMAs issue
           i32x8 fm[Cfg::RM], fn[2];

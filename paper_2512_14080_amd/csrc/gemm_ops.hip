@@ -1383,6 +1383,13 @@ template <class Cfg_, bool KEEP>
 struct OpUp8 : F8Rows {
   using Cfg = Cfg_;
   static constexpr int W_SCALES = 2, WN = Cfg::WN, CB = Cfg::RN / 2;  // CB: blocks of 32 gate columns of a wave
+  // What a backward reads takes fp32 sums: of a checkpoint's codes the 8-bit instruction's
+  // own put 3 in 10^4 on the other side of a step (fp32: 1 to 3 in 10^6), and one of them
+  // times a large column of X moved an element of dW1 by up to 0.9 of dW1's root mean
+  // square (0.2).  us a call: T = 16384, d = 1024, n = 256, E = 64, K = 8 214 -> 260, T =
+  // 32768, d = 1536, E = 128 651 -> 760, T = 4096, d = 4096, n = 512, E = 64, K = 4 243 ->
+  // 281; where the DMA instructions stand between the MFMAs makes no difference.
+  static constexpr bool FP32_SUMS = KEEP;
   static_assert(Cfg::BN == 256 && Cfg::RN % 2 == 0, "a tile holds one block of 128 columns of A");
   struct Params { QuantArgs a; };
   static constexpr int IDX_LDS = Cfg::NW * Cfg::QM * 256;

@@ -429,7 +429,6 @@ hipError_t launch_router_part(const uint16_t* X, const uint16_t* Wr, float* part
 // with four consecutive columns of one row.  What keeps loads in flight is many waves,
 // each with one step's: two steps in flight per wave cost registers, and with them
 // waves (d = 4096, n = 512, E = 128, 256 tokens: up 127 -> 117 us, down 113 -> 73).
-typedef int i32x8s __attribute__((ext_vector_type(8)));
 template <int NJ>
 using Stream8Part = f32x4[16][4 * NJ + 1];  // one wave's 16 x 16 NJ partial (padded rows)
 
@@ -454,7 +453,7 @@ struct RowBlock8 {
       v[i] = !hi || second ? *(const u32x4*)(p + (hi ? 64 * (F32 ? 4 : 2) : 0) + 16 * (i % (N / 2))) : u32x4{0, 0, 0, 0};
     }
   }
-  __device__ __forceinline__ i32x8s codes(int* scale) const {
+  __device__ __forceinline__ i32x8 codes(int* scale) const {
     uint32_t m;
     if constexpr (F32) {
       float a[32];
@@ -469,7 +468,7 @@ struct RowBlock8 {
     }
     *scale = scale_byte(max_of_row(m));
     const float sv = scale_value(*scale);
-    i32x8s q;
+    i32x8 q;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (F32) {
@@ -494,22 +493,11 @@ struct Weights8 {
       v[j][1] = *(const u32x4*)(w + (size_t)(row[j] + k + 64));
     }
   }
-  __device__ __forceinline__ i32x8s frag(int j) const {
+  __device__ __forceinline__ i32x8 frag(int j) const {
     const u32x4 lo = v[j][0], hi = v[j][1];
-    return i32x8s{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   }
 };
-
-// codes 8 i .. 8 i + 7 as bf16 (exact)
-__device__ __forceinline__ bf16x8 codes_bf16(const i32x8s& q, int i) {
-  u32x4 v;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    v[2 * h] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + h], 1.f, false));
-    v[2 * h + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[2 * i + h], 1.f, true));
-  }
-  return __builtin_bit_cast(bf16x8, v);
-}
 
 // grid: as stream_gemm_kernel's of the experts.  Op supplies
 //   F32: whether rows come in fp32 (else bf16),
@@ -553,7 +541,7 @@ __device__ __forceinline__ void stream8_rows(const QuantArgs& p, int tile, int e
 #pragma unroll
     for (int b = 0; b < MB; ++b) {
       int xs;
-      const i32x8s x = xv[b].codes(&xs);
+      const i32x8 x = xv[b].codes(&xs);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const int ws = sv[2 * j / NJ];
@@ -561,7 +549,7 @@ __device__ __forceinline__ void stream8_rows(const QuantArgs& p, int tile, int e
           f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16(wv.frag(j), i), codes_bf16(x, i), y, 0, 0, 0);
+            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16(wv.frag(j), i, 1.f), codes_bf16(x, i, 1.f), y, 0, 0, 0);
 #pragma unroll
           for (int q = 0; q < 4; ++q) acc[b][j][q] += ldexpf(y[q], ws + xs - 254);
         } else {
@@ -712,7 +700,7 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream8_token_down_kernel(const 
     RowBlock8<true> xv;
     xv.load(Op::row(p, r), k + 16 * g, (int)k + 64 < p.n);
     int xs;
-    const i32x8s x = xv.codes(&xs);
+    const i32x8 x = xv.codes(&xs);
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};

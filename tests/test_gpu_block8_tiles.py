@@ -1,12 +1,13 @@
 """The 8-bit up-projection that keeps H, where a workgroup computes several full tiles and the last block of n is a half.
 
 A wave whose columns lie past n stores less than the others behind a tile that counts as full, and the next tile's first
-wait counts stores.  H is compared with its products in 64 bits, O bit for bit with the call that keeps nothing.
+wait counts stores.  H is compared with its products in 64 bits, O with that of the call that keeps nothing.
 """
 import pytest
 
 from test_block8_cpu import built
 from test_block8_launches import _names, launches
+from test_gpu_block8_accuracy import OFF
 from test_gpu_parity import _torch
 
 # (dims, m_tile of a rounding up or 0, rows of the up-projection's tiles)
@@ -70,7 +71,10 @@ def test_several_full_tiles_of_a_half_block(dims, m_tile, rows):
         B.moe_fwd_quant(D, X, qw, r, c, O, ws, eb=eb)
         out.append((O, {k: v.clone() for k, v in ckpt.arrays().items()}))
     torch.cuda.synchronize()
-    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][0], out[2][0])
+    assert torch.equal(out[0][0], out[2][0])
+    # without a checkpoint: other sums, and so a few other codes of A
+    kept, plain = (out[i][0].double() for i in (0, 1))
+    assert ((kept - plain).norm() / plain.norm()).item() <= 2 * OFF["tiled"]
     first = int(r.arrays()["offsets"][E])
     for k in ("H", "Hs"):
         assert torch.equal(out[0][1][k][:first], out[2][1][k][:first]), k
