@@ -1558,7 +1558,7 @@ struct OpDown8 : F8Rows {
     if (p.a.b2) add_col_bias<Cfg>(t, p.a.b2 + (size_t)ti.e * p.a.d, ColOffset{ti.n0}, p.a.d);
     // Y in bf16, as the 16-bit forward's: in fp32 it would take O's error from 2.7e-3 to
     // 2.1e-3, and twice Y's bytes out and in (T = 16384, d = 1024, K = 8: 268 MB more each
-    // way, 108 of a training step's 920 us)
+    // way, about 108 us of a training step's 1020)
     store_rows_bf16_any<Cfg>(p.a.Y, p.a.d, ti.row_base, ti.mrows, ti.n0, ti.ncols, t, epi);
   }
 };
