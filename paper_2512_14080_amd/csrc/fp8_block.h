@@ -61,8 +61,8 @@ __device__ __forceinline__ f32x4 unpack_fp8x4(uint32_t v, float scale) {
   const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, scale, true);
   return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
-// codes 8 i .. 8 i + 7 of a fragment as bf16 values, code * scale (exact above bf16's
-// smallest, 2^-133)
+// codes 8 i .. 8 i + 7 of a fragment as bf16 values, code * scale: exact within bf16's
+// range (2^-133 up; a value above 3.3e38 may have a code that stands for 2^128)
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 __device__ __forceinline__ bf16x8 codes_bf16(const i32x8& q, int i, float scale) {
   u32x4 v;
