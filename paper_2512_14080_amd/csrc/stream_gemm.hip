@@ -797,7 +797,7 @@ hipError_t launch_stream8_down(const QuantArgs& a, const StreamShape& t, hipStre
 //             d = 4096, E = 128: K = 8, 8 (1024): 26.6/20.1; K = 1, 64 (8192): 25.8/35.2
 //             d = 4096, E = 256, K = 4, 32 (4096): 36.6/34.4; d = 1024, K = 8, 32 (1024): 19.6/18.7
 //             d = 2048, E = 256: K = 8, 32 (2048): 26.5/30.1; K = 1, 128 (8192): 22.1/34.5
-//             d = 1536, E = 128, K = 2, 64 (3072): 15.0/20.3
+//             d = 1536, E = 128, K = 2, 64 (2048 and a half as many again): 15.0/20.3
 //   n = 128   d = 2048, E = 64, K = 2, 16 (1024): 16.0/11.2; d = 1024, E = 128, K = 2, 64 (2048): 15.3/18.4
 //             d = 4096, E = 256, K = 8, 16 (2048): 37.7/40.7
 //   n = 256   d = 2048, E = 64, K = 1, 32 (2048): 20.5/18.6
