@@ -231,10 +231,12 @@ typedef struct {
 
 /* Workspace bytes for moe_fwd (which = 1), moe_bwd (which = 2),
  * moe_fwd_aggregation_ablation (which = 3), moe_fwd_quant (which = 4),
- * moe_fwd_ckpt (which = 5) and moe_bwd_ckpt (which = 6). */
+ * moe_fwd_ckpt (which = 5), moe_bwd_ckpt (which = 6) and moe_decode (which = 7, whatever
+ * the capacity). */
 enum {
   MOE_WS_FWD = 1, MOE_WS_BWD = 2, MOE_WS_FWD_AGG_ABLATION = 3,
-  MOE_WS_FWD_QUANT = 4, MOE_WS_FWD_CKPT = 5, MOE_WS_BWD_CKPT = 6
+  MOE_WS_FWD_QUANT = 4, MOE_WS_FWD_CKPT = 5, MOE_WS_BWD_CKPT = 6,
+  MOE_WS_DECODE = 7
 };
 size_t moe_workspace_bytes(moe_dims dims, int32_t capacity, int which);
 
@@ -460,6 +462,26 @@ int moe_bwd_ckpt(moe_dims dims, const moe_bf16 *dO, const moe_bf16 *X, const moe
                  moe_bf16 *dW1, moe_bf16 *dW2, float *dWr, float *dbias, float *dS, void *ws, size_t ws_bytes,
                  void *stream);
 
+/*
+ * The whole layer for a few tokens in two launches: token-choice routing as moe_route's,
+ * then the experts and the sum of moe_fwd, without a routing or an H.
+ *   O = R + sum over t's K experts of s * (SwiGLU(X W1_e + b1_e) W2_e + b2_e)
+ * A is rounded to bf16 between the products; H, Y and the sum are fp32, O is rounded once.
+ *   dims  T at most MOE_DECODE_MAX_T, E at most 1024, an expert's W1 below 2^31 bytes
+ *   bias  [E] fp32, of the router, nullable;  eb  b1 and b2 are read, nullable
+ *   R     [T,d] bf16, what the layer's output is added to, nullable; may be O itself.
+ *         O must not overlap X.
+ *   topk_idx, topk_w   [T,K] out, nullable: the selection by (score descending, expert
+ *         ascending) and its weights, as moe_route writes them
+ *   ws    moe_workspace_bytes(dims, capacity, MOE_WS_DECODE) bytes.  Calls that share
+ *         one must be ordered, like those of moe_fwd: of two at once either waits
+ *         (for seconds at most) for counts that the other took, and then writes NaN.
+ */
+enum { MOE_DECODE_MAX_T = 64 };
+int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float *bias, const moe_bf16 *W1,
+               const moe_bf16 *W2, const moe_expert_bias *eb, const moe_bf16 *R, moe_bf16 *O, int32_t *topk_idx,
+               float *topk_w, void *ws, size_t ws_bytes, void *stream);
+
 /* Static description of an error code. */
 const char *moe_strerror(int code);
 /* Thread-local description of the last error returned on this thread. */
@@ -480,6 +502,7 @@ enum {
   MOE_KC_QUANTIZE, /* rows and weights into or out of the 8-bit block format (moe_fwd_quant: and its m-tile lists) */
   MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT, /* (two launches over a long n, counted as one; for few
                                           tokens with the aggregation in it) */
+  MOE_KC_DECODE, /* moe_decode: its two launches, counted as one */
   MOE_KC_COUNT
 };
 int moe_prof_select(int kernel_class);

@@ -42,6 +42,9 @@ MOE_WS_FWD_AGG_ABLATION = 3
 MOE_WS_FWD_QUANT = 4
 MOE_WS_FWD_CKPT = 5
 MOE_WS_BWD_CKPT = 6
+MOE_WS_DECODE = 7
+
+MOE_DECODE_MAX_T = 64
 
 MOE_HELD_EMPTY = 0
 MOE_HELD_WRITTEN = 1
@@ -51,14 +54,14 @@ AGG_STRATEGIES = {"gather_sum": 0, "scatter_sum": 1, "atomic_f32": 2}
 
 KERNEL_CLASSES = ["router_gemm", "topk", "routing_meta", "token_round", "up_proj", "down_proj", "aggregate_O",
                   "dH", "dW2", "dXtilde", "dW1", "aggregate_dX", "dWr", "router_topk", "quantize", "up_proj_quant",
-                  "down_proj_quant"]
+                  "down_proj_quant", "decode"]
 
 EXPORTS = ["moe_routing_bytes", "moe_routing_init", "moe_round_capacity", "moe_route", "moe_round_tokens",
            "moe_workspace_bytes", "moe_fwd", "moe_bwd", "moe_strerror", "moe_last_error", "moe_prof_select",
            "moe_prof_read", "moe_kernel_class_name", "moe_fwd_aggregation_ablation", "moe_fwd_static",
            "moe_fwd_static_max_bytes", "moe_scale_stride", "moe_quantize_rows", "moe_dequantize_rows",
            "moe_qexperts_bytes", "moe_qexperts_init", "moe_quantize_experts", "moe_dequantize_experts",
-           "moe_ckpt_bytes", "moe_ckpt_init", "moe_fwd_quant", "moe_fwd_ckpt", "moe_bwd_ckpt"]
+           "moe_ckpt_bytes", "moe_ckpt_init", "moe_fwd_quant", "moe_fwd_ckpt", "moe_bwd_ckpt", "moe_decode"]
 
 
 class MoeDims(ctypes.Structure):
@@ -140,6 +143,7 @@ def lib():
         "moe_fwd_quant": (ctypes.c_int, [D, vp, Q, EB, R, C, vp, vp, sz, vp]),
         "moe_fwd_ckpt": (ctypes.c_int, [D, vp, vp, vp, EB, R, C, vp, vp, sz, vp]),
         "moe_bwd_ckpt": (ctypes.c_int, [D, vp, vp, C, vp, vp, EB, vp, R, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "moe_decode": (ctypes.c_int, [D, vp, vp, vp, vp, vp, EB, vp, vp, vp, vp, vp, sz, vp]),
         "moe_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         "moe_last_error": (ctypes.c_char_p, []),
         "moe_prof_select": (ctypes.c_int, [ctypes.c_int]),
@@ -388,6 +392,14 @@ def moe_bwd_ckpt(D, dO, X, ckpt: Checkpoint, W1, W2, Wr, r: Routing, dX, dW1, dW
                                               ctypes.byref(r.struct), _ptr(dX), _ptr(dW1), _ptr(dW2), _ptr(dWr),
                                               _ptr(dbias), _ptr(dS), _ptr(ws), ws.numel() * ws.element_size(),
                                               _stream(stream)))
+
+
+# ------------------------------------------------------------------ few tokens
+def moe_decode(D, X, Wr, bias, W1, W2, R, O, ws, topk_idx=None, topk_w=None, stream=None, eb=None):
+    """The whole layer for at most MOE_DECODE_MAX_T tokens; R None: O is the layer's output alone."""
+    _check("moe_decode", lib().moe_decode(D, _ptr(X), _ptr(Wr), _ptr(bias), _ptr(W1), _ptr(W2), _eb(eb), _ptr(R),
+                                          _ptr(O), _ptr(topk_idx), _ptr(topk_w), _ptr(ws),
+                                          ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def moe_prof_select(kernel_class):

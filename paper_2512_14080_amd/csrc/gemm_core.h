@@ -50,7 +50,7 @@ typedef short v4i16 __attribute__((ext_vector_type(4)));
 #define SMOE_LDS __attribute__((address_space(3)))
 
 // read-only zero page for masked k rows / columns of KOUTER operands
-__device__ __attribute__((aligned(4096))) uint32_t g_zero_page[1024];
+static __device__ __attribute__((aligned(4096))) uint32_t g_zero_page[1024];
 
 struct TileInfo {
   int e;        // expert (group)

@@ -257,6 +257,21 @@ bool stream8_by_token(const moe_dims& m, const moe_routing& r);
 hipError_t launch_stream8_row_up(const QuantArgs& a, int T, int K, hipStream_t s);
 hipError_t launch_stream8_token_down(const QuantArgs& a, int T, hipStream_t s);
 
+// The whole layer for few tokens (decode.hip): two launches.
+constexpr int kDecodeTokens = 64, kDecodeExperts = 1024;
+struct DecodeArgs {
+  const uint16_t* X; const uint16_t* Wr; const float* bias; const uint16_t* W1; const uint16_t* W2; const float* b1;
+  const float* b2; const uint16_t* R; uint16_t* O; int32_t* topk_idx; float* topk_w;
+  float* part;    // [slices][T][E] partial logits
+  int32_t* sync;  // decode_sync_words counters
+  uint16_t* A;    // [T K][n]
+  float* Y;       // [T K][d]
+  int T, d, n, E, K, slices;
+};
+int decode_slices(int T, int d, int E);
+size_t decode_sync_words(int T, int d, int E, int K);
+hipError_t launch_decode(const DecodeArgs& a, hipStream_t s);
+
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);
 hipError_t launch_agg_o_f32(const float* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);

@@ -227,6 +227,36 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   return off;
 }
 
+// moe_decode (and moe_decode_quant): the counters, partial logits, A and Y
+struct DecodeWs {
+  int32_t* sync;
+  float* part;
+  uint16_t* A;
+  float* Y;
+};
+size_t decode_layout(const moe_dims& m, char* base, DecodeWs* w) {
+  const size_t P = (size_t)m.T * m.K;
+  size_t off = 0;
+  off = carve(base, off, smoe::decode_sync_words(m.T, m.d, m.E, m.K) * 4, w ? (void**)&w->sync : nullptr);
+  off = carve(base, off, (size_t)smoe::decode_slices(m.T, m.d, m.E) * m.T * m.E * 4, w ? (void**)&w->part : nullptr);
+  off = carve(base, off, P * m.n * 2, w ? (void**)&w->A : nullptr);
+  off = carve(base, off, P * m.d * 4, w ? (void**)&w->Y : nullptr);
+  return off;
+}
+
+int check_decode(const moe_dims& m) {
+  int rc = check_dims(m);
+  if (rc) return rc;
+  if (m.T > smoe::kDecodeTokens)
+    return fail(MOE_ERR_UNSUPPORTED, "T must be at most %d (got %d): moe_route and moe_fwd take more", smoe::kDecodeTokens, m.T);
+  if (m.E > smoe::kDecodeExperts) return fail(MOE_ERR_UNSUPPORTED, "E must be at most %d (got %d)", smoe::kDecodeExperts, m.E);
+  // (32-bit byte offsets within an expert's weights, W_r and the rows)
+  const int64_t most = INT32_MAX;
+  if (4 * (int64_t)m.d * m.n > most || 2 * (int64_t)m.d * m.E > most || 2 * (int64_t)m.T * m.d > most || 4 * (int64_t)m.T * m.K * m.n > most)
+    return fail(MOE_ERR_UNSUPPORTED, "d = %d, n = %d: an expert's projection, W_r and the rows must be below 2^31 bytes each", m.d, m.n);
+  return MOE_OK;
+}
+
 size_t qexperts_layout(const moe_dims& m, char* base, moe_qexperts* q) {
   size_t off = 0;
   off = carve(base, off, m.E * smoe::w1q_bytes(m.d, m.n), q ? (void**)&q->W1 : nullptr);
@@ -444,6 +474,7 @@ size_t moe_workspace_bytes(moe_dims dims, int32_t capacity, int which) {
   if (which == MOE_WS_FWD_QUANT) return quant_layout(dims, capacity, nullptr, nullptr);
   if (which == MOE_WS_FWD_CKPT) return fwd_layout(dims, capacity, nullptr, nullptr);
   if (which == MOE_WS_BWD_CKPT) return bwd_ckpt_layout(dims, capacity, nullptr, nullptr, nullptr);
+  if (which == MOE_WS_DECODE) return check_decode(dims) == MOE_OK ? decode_layout(dims, nullptr, nullptr) : 0;
   return 0;
 }
 
@@ -980,6 +1011,36 @@ int moe_bwd_ckpt(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_ck
   return backward(m, dO, X, nullptr, c, W1, W2, eb, Wr, r, dX, dW1, dW2, dWr, dbias, dS, ws, ws_bytes, stream);
 }
 
+int moe_decode(moe_dims m, const moe_bf16* X, const moe_bf16* Wr, const float* bias, const moe_bf16* W1, const moe_bf16* W2,
+               const moe_expert_bias* eb, const moe_bf16* R, moe_bf16* O, int32_t* topk_idx, float* topk_w, void* ws,
+               size_t ws_bytes, void* stream_) {
+  int rc = check_decode(m);
+  if (rc) return rc;
+  CHECK_PTR(X, 16);
+  CHECK_PTR(Wr, 16);
+  CHECK_PTR(W1, 16);
+  CHECK_PTR(W2, 16);
+  CHECK_PTR(O, 16);
+  if (!aligned(R, 16)) return fail(MOE_ERR_INVALID_ARG, "R must be 16-byte aligned");
+  if (!aligned(bias, 4)) return fail(MOE_ERR_INVALID_ARG, "bias must be 4-byte aligned");
+  if (!aligned(topk_idx, 4)) return fail(MOE_ERR_INVALID_ARG, "topk_idx must be 4-byte aligned");
+  if (!aligned(topk_w, 4)) return fail(MOE_ERR_INVALID_ARG, "topk_w must be 4-byte aligned");
+  rc = check_expert_bias(eb);
+  if (rc) return rc;
+  const size_t need = decode_layout(m, nullptr, nullptr);
+  if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < required %zu", ws_bytes, need);
+  CHECK_PTR(ws, kAlign);
+  DecodeWs w;
+  decode_layout(m, (char*)ws, &w);
+  hipStream_t stream = (hipStream_t)stream_;
+  LAUNCH(MOE_KC_DECODE,
+         smoe::launch_decode({X, Wr, bias, W1, W2, eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, R, O, topk_idx, topk_w, w.part,
+                              w.sync, w.A, w.Y, m.T, m.d, m.n, m.E, m.K, smoe::decode_slices(m.T, m.d, m.E)},
+                             stream),
+         "layer of few tokens");
+  return MOE_OK;
+}
+
 int moe_prof_select(int kc) {
   if (kc < -1 || kc >= MOE_KC_COUNT) return fail(MOE_ERR_INVALID_ARG, "unknown kernel class %d", kc);
   std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -1011,7 +1072,7 @@ const char* moe_kernel_class_name(int kc) {
   static const char* names[MOE_KC_COUNT] = {"router_gemm", "topk", "routing_meta", "token_round", "up_proj",
                                             "down_proj", "aggregate_O", "dH", "dW2", "dXtilde",
                                             "dW1", "aggregate_dX", "dWr", "router_topk", "quantize",
-                                            "up_proj_quant", "down_proj_quant"};
+                                            "up_proj_quant", "down_proj_quant", "decode"};
   return (kc >= 0 && kc < MOE_KC_COUNT) ? names[kc] : "unknown";
 }
 
