@@ -15,14 +15,14 @@
 // ticket beyond the one it works on, and the lowest unfinished ticket waits for nothing
 // that is unfinished.  No co-residency of the grid is assumed.
 //
-// Selection is the routing kernels' (wave_topk on the softmax of the summed partials):
+// Selection is the routing kernels' (the K best of the softmax of the summed partials):
 // every workgroup forms it for itself from T x E logits in L2, which is cheaper than
 // another dependent step, and all get the same from the same sums.
 #include <algorithm>
 
 #include "launch.h"
 #include "stream_tile.h"
-#include "wave_topk.h"
+#include "topk_net.h"
 
 namespace smoe {
 
@@ -33,27 +33,30 @@ template <int KB, int MB>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode_router_kernel(const DecodeArgs a, int slice, int counters) {
   using Tile = RowTile<KB>;
   __shared__ typename Tile::Part part[kDecodeWaves];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)
-    for (int i = threadIdx.x; i < counters; i += kDecodeThreads) a.sync[i] = 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
+  for (int i = ((blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * kDecodeThreads + threadIdx.x; i < counters;
+       i += gridDim.x * gridDim.y * gridDim.z * kDecodeThreads)
+    a.sync[i] = 0;
   const int c0 = Tile::COLS * blockIdx.x, t0 = Tile::RT * MB * blockIdx.z;
   const int kbeg = blockIdx.y * slice, kend = min(a.d, kbeg + slice);
   const Rsrc w = buffer_of(a.Wr, (uint32_t)a.d * a.E * 2), x = buffer_of(a.X, (uint32_t)a.T * a.d * 2);
-  const int col = c0 + 8 * Tile::cg();
+  const int col = c0 + 8 * Tile::cg(lane);
   uint32_t xoff[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
-    const int t = t0 + Tile::RT * b + Tile::row();
+    const int t = t0 + Tile::RT * b + Tile::row(lane);
     xoff[b] = t < a.T ? (uint32_t)t * a.d * 2 : kBufferOut;
   }
   f32x4 acc[MB][8];
   zero_acc(acc);
-  stream_acc<KB, MB, 2, kDecodeWaves>(acc, w, a.E * 2, col < a.E ? col * 2 : kBufferOut, x, xoff, kbeg, kend, wave);
+  RowStream<KB, 2, kDecodeWaves> stream;
+  stream.prime(w, a.E * 2, col < a.E ? col * 2 : kBufferOut, kbeg, kend, wave, lane);
+  stream.template add<false>(acc, x, xoff);
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
     if (t0 + Tile::RT * b >= a.T) break;
     __syncthreads();
-    Tile::put(part[wave], acc[b]);
+    Tile::put(part[wave], acc[b], lane);
     __syncthreads();
     for (int i = threadIdx.x; i < Tile::RT * Tile::COLS / 4; i += kDecodeThreads) {
       const int row = i / (Tile::COLS / 4), c4 = i % (Tile::COLS / 4), t = t0 + Tile::RT * b + row, c = c0 + 4 * c4;
@@ -66,94 +69,232 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_router_kernel(const 
 // LDS of a workgroup behind the partial sums
 struct Picked {
   unsigned long long* word;  // [E] tokens of each expert, one bit each
+  int* first;                // [E] the first entry of a picked expert
   int* gexp;                 // [groups] the picked experts, ascending: a group each
   int* goff;                 // [groups + 1] their first entries in `rows`
-  int* rows;                 // [T K] entries t K + j by group, by token within
+  int* rows;                 // [T K] entries t K + j by group, by token within (one word more)
   int* sel;                  // [T K] expert of entry t K + j
-  int* group;                // [T K] its group
   float* w;                  // [T K] its weight
+  int* place;                // [T E] where waves share a token: the experts before each,
+  float* score;              // [T E] and the scores
 };
+// waves that can share a token
+__host__ __device__ inline int decode_share(int T, int E) { return E > 128 || T > 4 ? 1 : T == 1 ? 8 : T == 2 ? 4 : 2; }
 __host__ __device__ inline size_t picked_bytes(int T, int E, int K) {
   const int g = T * K < E ? T * K : E;
-  return 8 * (size_t)E + 4 * (size_t)(2 * g + 1) + 16 * (size_t)T * K;
+  const size_t shared = decode_share(T, E) > 1 ? 8 * (size_t)T * E : 0;
+  return (12 * (size_t)E + 4 * (size_t)(2 * g + 2) + 12 * (size_t)T * K + shared + 15) / 16 * 16;
 }
 __device__ __forceinline__ Picked picked_at(char* lds, int T, int E, int K) {
   const int g = min(T * K, E), n = T * K;
   Picked p;
   p.word = (unsigned long long*)lds;
-  p.gexp = (int*)(lds + 8 * (size_t)E);
+  p.first = (int*)(lds + 8 * (size_t)E);
+  p.gexp = p.first + E;
   p.goff = p.gexp + g;
   p.rows = p.goff + g + 1;
-  p.sel = p.rows + n;
-  p.group = p.sel + n;
-  p.w = (float*)(p.group + n);
+  p.sel = p.rows + n + 1;
+  p.w = (float*)(p.sel + n);
+  p.place = (int*)(p.w + n);
+  p.score = (float*)(p.place + T * E);
   return p;
 }
 
+// Where few experts are scored, an expert's place is the count of those before it, which the
+// `wpt` waves of a token share (a comparison with 64 of them costs about 50 clocks); else the
+// token's wave finds the winners one by one (450 clocks each).
+__device__ __forceinline__ bool by_count(const DecodeArgs& a, int epl, int wpt) { return a.E * epl <= 9 * a.K * wpt; }
+
+// selection of token t by waves 0 .. wpt - 1 of its `wpt` (wpt > 1: by count, place zeroed)
 template <int EPL>
-__device__ __forceinline__ void select_tokens(const DecodeArgs& a, const Picked& p) {
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
-  const size_t slab = (size_t)a.T * a.E;
-  for (int t = wave; t < a.T; t += kDecodeWaves) {
-    float v[EPL];
-    const float* in = a.part + (size_t)t * a.E;
-    for (int q0 = 0; q0 < a.slices; q0 += 4) {  // (four slabs' loads in flight, added in slice order)
-      float x[4][EPL];
+__device__ __forceinline__ void select_token(const DecodeArgs& a, const Picked& p, int t, int part, int wpt) {
+  const int lane = lane_id();
+  const uint32_t slab = (uint32_t)a.T * a.E;
+  const Rsrc in = buffer_of(a.part, a.slices * slab * 4);
+  float v[EPL];
+  for (int q0 = 0; q0 < a.slices; q0 += 4) {  // (four slabs' loads in flight, added in slice order; zero past the last)
+    float x[4][EPL];
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) {
-          const int e = lane + 64 * j;
-          x[q][j] = q0 + q < a.slices && e < a.E ? in[(q0 + q) * slab + e] : 0.f;
-        }
+      for (int j = 0; j < EPL; ++j) {
+        const int e = lane + 64 * j;
+        x[q][j] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+            in, e < a.E ? (int)(((q0 + q) * slab + t * a.E + e) * 4) : (int)kBufferOut, 0, 0));
+      }
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int j = 0; j < EPL; ++j) v[j] = q0 + q == 0 ? x[0][j] : v[j] + x[q][j];
-    }
-    float m = -INFINITY;
+      for (int j = 0; j < EPL; ++j) v[j] = q0 + q == 0 ? x[0][j] : v[j] + x[q][j];
+  }
+  float m = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < EPL; ++j) {
+    const int e = lane + 64 * j;
+    v[j] = e < a.E ? v[j] + (a.bias ? a.bias[e] : 0.f) : -INFINITY;
+    m = fmaxf(m, v[j]);
+  }
+  m = dpp_reduce(m, [](float x, float y) { return fmaxf(x, y); });
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < EPL; ++j) {
+    v[j] = lane + 64 * j < a.E ? expf(v[j] - m) : 0.f;
+    s += v[j];
+  }
+  s = dpp_reduce(s, [](float x, float y) { return x + y; });
+  // the order-preserving images of the scores (the routing kernels' order, NaN included)
+  uint32_t key[EPL];
+#pragma unroll
+  for (int j = 0; j < EPL; ++j) key[j] = lane + 64 * j < a.E ? topk_key(v[j] / s) : 0u;
+  if (EPL <= 2 && by_count(a, EPL, wpt)) {
+    int before[EPL];
+#pragma unroll
+    for (int j = 0; j < EPL; ++j) before[j] = 0;
+    const int per = kWave / wpt;
+#pragma unroll
+    for (int i = 0; i < (EPL <= 2 ? EPL : 1); ++i)
+#pragma unroll 8  // (per is a multiple of it)
+      for (int l = part * per; l < part * per + per; ++l) {
+        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key[i], l);
+        // (equal keys: the lower expert first; past E the keys are 0 and no expert is lower)
+#pragma unroll
+        for (int j = 0; j < EPL; ++j) before[j] += k > key[j] || (k == key[j] && 64 * i + l < lane + 64 * j);
+      }
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
       const int e = lane + 64 * j;
-      v[j] = e < a.E ? v[j] + (a.bias ? a.bias[e] : 0.f) : -INFINITY;
-      m = fmaxf(m, v[j]);
+      if (e >= a.E) continue;
+      if (wpt > 1) {
+        atomicAdd(&p.place[t * a.E + e], before[j]);
+        p.score[t * a.E + e] = topk_value(key[j]);  // (the same by every wave)
+      } else if (before[j] < a.K) {
+        p.sel[t * a.K + before[j]] = e;
+        p.w[t * a.K + before[j]] = topk_value(key[j]);
+      }
     }
-    m = dpp_reduce(m, [](float x, float y) { return fmaxf(x, y); });
-    float s = 0.f;
+    return;
+  }
+  // K rounds of an arg-max, in a loop that is not unrolled: its scalars would not fit
+  uint32_t taken = 0;
+#pragma unroll 1
+  for (int k = 0; k < a.K; ++k) {
+    uint32_t best = 0;
+    int at = INT32_MAX;  // the lane's best, the lowest expert among equals
 #pragma unroll
     for (int j = 0; j < EPL; ++j) {
-      v[j] = lane + 64 * j < a.E ? expf(v[j] - m) : 0.f;
-      s += v[j];
-    }
-    s = dpp_reduce(s, [](float x, float y) { return x + y; });
-#pragma unroll
-    for (int j = 0; j < EPL; ++j) v[j] = v[j] / s;
-    wave_topk<EPL>(v, a.E, a.K, [&](int k, int e, float w) {
-      p.sel[t * a.K + k] = e;
-      p.w[t * a.K + k] = w;
-      atomicOr(&p.word[e], 1ull << t);
-      if (blockIdx.x == 0) {
-        if (a.topk_idx) a.topk_idx[t * a.K + k] = e;
-        if (a.topk_w) a.topk_w[t * a.K + k] = w;
+      const int e = lane + 64 * j;
+      if (e < a.E && !((taken >> j) & 1u) && (at == INT32_MAX || key[j] > best)) {
+        best = key[j];
+        at = e;
       }
-    });
+    }
+    const uint32_t top = dpp_reduce(best, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    int e = INT32_MAX;
+    if constexpr (EPL <= 2) {
+#pragma unroll
+      for (int j = EPL - 1; j >= 0; --j) {
+        const uint64_t hit = __ballot(best == top && at >> 6 == j);
+        e = hit ? 64 * j + __ffsll((unsigned long long)hit) - 1 : e;
+      }
+    } else {
+      e = dpp_reduce(best == top ? at : INT32_MAX, [](int x, int y) { return x < y ? x : y; });
+    }
+    if (lane == (e & 63)) taken |= 1u << (e >> 6);
+    if (lane == 0) {
+      p.sel[t * a.K + k] = e;
+      p.w[t * a.K + k] = topk_value(top);
+    }
   }
 }
+__device__ __forceinline__ void select_token_of(const DecodeArgs& a, const Picked& p, int t, int part, int wpt) {
+  if (a.E <= 64)
+    select_token<1>(a, p, t, part, wpt);
+  else if (a.E <= 128)
+    select_token<2>(a, p, t, part, wpt);
+  else if (a.E <= 256)
+    select_token<4>(a, p, t, part, wpt);
+  else if (a.E <= 512)
+    select_token<8>(a, p, t, part, wpt);
+  else
+    select_token<16>(a, p, t, part, wpt);
+}
 
-// the selection and the groups; returns how many there are
-__device__ __forceinline__ int pick(const DecodeArgs& a, const Picked& p, int* scan_lds) {
+// a token's weights: its selected scores over their sum, in the order of the selection.  One
+// wave; `out`: to the caller's arrays; `all`: to every workgroup's too
+__device__ __forceinline__ void weigh_token(const DecodeArgs& a, const Picked& p, int t, bool out, bool all) {
+  const int lane = lane_id(), i = t * a.K + lane;
+  const float x = lane < a.K ? p.w[i] : 0.f;
+  float sum = 0.f;
+  for (int k = 0; k < a.K; ++k) sum += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), k));
+  if (lane >= a.K) return;
+  const int e = p.sel[i];
+  const float w = x / sum;
+  p.w[i] = w;
+  if (all) store8_shared(buffer_of(a.picked, (uint32_t)a.T * a.K * 8), i * 8, u32x2{(uint32_t)e, __float_as_uint(w)});
+  if (out && a.topk_idx) a.topk_idx[i] = e;
+  if (out && a.topk_w) a.topk_w[i] = w;
+}
+
+// the selection, by every workgroup for itself
+__device__ __forceinline__ void select_all(const DecodeArgs& a, const Picked& p) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool out = blockIdx.x == 0;
+  // waves of a token, where its experts' places are counted
+  const int share = decode_share(a.T, a.E), epl = a.E <= 64 ? 1 : 2;
+  const int wpt = share > 1 && by_count(a, epl, share) ? share : 1;
+  if (wpt > 1) {
+    for (int i = threadIdx.x; i < a.T * a.E; i += kDecodeThreads) p.place[i] = 0;
+    __syncthreads();
+    const int t = wave / wpt;
+    if (t < a.T) select_token_of(a, p, t, wave % wpt, wpt);
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.T * a.E; i += kDecodeThreads) {
+      const int k = p.place[i], u = i / a.E;
+      if (k < a.K) {
+        p.sel[u * a.K + k] = i - u * a.E;
+        p.w[u * a.K + k] = p.score[i];
+      }
+    }
+    __syncthreads();
+    if (wave < a.T) weigh_token(a, p, wave, out, false);
+  } else {
+    for (int t = wave; t < a.T; t += kDecodeWaves) {
+      select_token_of(a, p, t, 0, 1);
+      weigh_token(a, p, t, out, false);
+    }
+  }
+  __syncthreads();
+}
+// the same of one item's tokens, for all
+__device__ __forceinline__ void select_some(const DecodeArgs& a, const Picked& p, int item) {
+  const int t = item * kDecodeWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (t >= a.T) return;
+  select_token_of(a, p, t, 0, 1);
+  weigh_token(a, p, t, true, true);
+}
+__device__ __forceinline__ void read_selection(const DecodeArgs& a, const Picked& p) {
+  for (int i = threadIdx.x; i < a.T * a.K; i += kDecodeThreads) {
+    const uint64_t v = __hip_atomic_load((uint64_t*)a.picked + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    p.sel[i] = min((int)(uint32_t)v, a.E - 1);  // (in range even where a wait gave up)
+    p.w[i] = __uint_as_float((uint32_t)(v >> 32));
+  }
+  __syncthreads();
+}
+
+// the groups of a selection; returns how many there are
+__device__ __forceinline__ int form_groups(const DecodeArgs& a, const Picked& p, int* scan_lds) {
+  const int n = a.T * a.K;
+  if (a.T == 1) {  // each entry its own
+    for (int i = threadIdx.x; i <= n; i += kDecodeThreads) {
+      if (i < n) p.gexp[i] = p.sel[i];
+      p.goff[i] = p.rows[i] = i;
+    }
+    __syncthreads();
+    return n;
+  }
   for (int e = threadIdx.x; e < a.E; e += kDecodeThreads) p.word[e] = 0ull;
   __syncthreads();
-  if (a.E <= 64)
-    select_tokens<1>(a, p);
-  else if (a.E <= 128)
-    select_tokens<2>(a, p);
-  else if (a.E <= 256)
-    select_tokens<4>(a, p);
-  else if (a.E <= 512)
-    select_tokens<8>(a, p);
-  else
-    select_tokens<16>(a, p);
+  for (int i = threadIdx.x; i < n; i += kDecodeThreads) atomicOr(&p.word[p.sel[i]], 1ull << (i / a.K));
   __syncthreads();
   int groups = 0, entries = 0;
   for (int e0 = 0; e0 < a.E; e0 += kDecodeThreads) {
@@ -164,50 +305,63 @@ __device__ __forceinline__ int pick(const DecodeArgs& a, const Picked& p, int* s
     const int at = block_excl_scan<kDecodeThreads>(c ? c | 1 << 16 : 0, &total, scan_lds);
     if (c) {
       p.gexp[groups + (at >> 16)] = e;
-      p.goff[groups + (at >> 16)] = entries + (at & 0xffff);
+      p.goff[groups + (at >> 16)] = p.first[e] = entries + (at & 0xffff);
     }
     groups += total >> 16;
     entries += total & 0xffff;
   }
   if (threadIdx.x == 0) p.goff[groups] = entries;
   __syncthreads();
-  for (int i = threadIdx.x; i < a.T * a.K; i += kDecodeThreads) {
-    const int e = p.sel[i], t = i / a.K;
-    int lo = 0, hi = groups;  // gexp[lo] <= e < gexp[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (p.gexp[mid] <= e) lo = mid; else hi = mid;
-    }
-    p.group[i] = lo;
-    p.rows[p.goff[lo] + __popcll(p.word[e] & ((1ull << t) - 1))] = i;
+  for (int i = threadIdx.x; i < n; i += kDecodeThreads) {
+    const int e = p.sel[i];
+    p.rows[p.first[e] + __popcll(p.word[e] & ((1ull << (i / a.K)) - 1))] = i;
   }
   __syncthreads();
   return groups;
 }
 
 // ---------------------------------------------------------------- counters
-// sync: [0] the next ticket; from 32 on one word per group, of finished up-projection
-// items; then one per column tile, of finished down-projection items
-constexpr int kSyncUp = 32;
+// sync, in lines of 128 bytes of their own (the polls and counts of one line wait for each
+// other: eight counters in one line made a hop 3.5 us, apart they take 1): the ticket,
+// eight counters of all finished up-projection items, one of selection items, one per group,
+// one per column tile of finished down-projection items
+constexpr int kLine = 32;
+__device__ __forceinline__ int* ups_counter(const DecodeArgs& a, int i) { return a.sync + (1 + (i & 7)) * kLine; }
+__device__ __forceinline__ int* select_counter(const DecodeArgs& a) { return a.sync + 9 * kLine; }
+__device__ __forceinline__ int* group_counter(const DecodeArgs& a, int g) { return a.sync + (10 + g) * kLine; }
+__device__ __forceinline__ int* tile_counter(const DecodeArgs& a, int t) {
+  return a.sync + (10 + min(a.T * a.K, a.E) + t) * kLine;
+}
 __device__ __forceinline__ int take_ticket(const DecodeArgs& a) {
   return __hip_atomic_fetch_add(a.sync, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// An item's stores, by every thread of the workgroup, before its counter
+// An item's stores (shared ones), by every thread of the workgroup, before its counter.  LOADS:
+// so many loads of the wave's are younger than its stores and may be under way still.
+template <int LOADS>
 __device__ __forceinline__ void finish_item(int* counter) {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // each wave's own are in L2
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");  // each wave's own have arrived
   __syncthreads();
-  if (threadIdx.x == 0) __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
+  if (threadIdx.x == 0) __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// One lane waits until the counter has reached `want`.  A call that shares its workspace with
-// another one in flight, which is an error, may have lost counts: the wait is bounded
-// (seconds), and false makes the outputs NaN.
+// Wave 0 waits until the lanes' counters (lane i's where it has one) add up to `want`; then
+// the workgroup goes on.  A call that shares its workspace with another one in flight,
+// which is an error, may have lost counts: the wait is bounded (seconds), and false makes
+// the outputs NaN.
 constexpr int kMostPolls = 1 << 22;
-__device__ __forceinline__ bool wait_counter(int* counter, int want) {
-  for (int i = 0; i < kMostPolls; ++i) {
-    if (__hip_atomic_load(counter, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >= want) return true;
-    __builtin_amdgcn_s_sleep(2);
+template <class Counter>
+__device__ __forceinline__ bool await(Counter counter, int want, int* sh) {
+  if (threadIdx.x < kWave) {
+    int* c = counter(lane_id());
+    bool ok = false;
+    for (int i = 0; i < kMostPolls && !ok; ++i) {
+      if (i) __builtin_amdgcn_s_sleep(1);
+      const int n = c ? __hip_atomic_load(c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+      ok = dpp_reduce(n, [](int x, int y) { return x + y; }) >= want;
+    }
+    if (threadIdx.x == 0) *sh = ok;
   }
-  return false;
+  __syncthreads();  // (the loads behind it are shared ones, which no cache answers from before)
+  return *sh;
 }
 
 // ---------------------------------------------------------------- the layer
@@ -216,203 +370,396 @@ template <int KB, int MB>
 struct Decode {
   using Tile = RowTile<KB>;
   static constexpr int RT = Tile::RT, CG = Tile::CG, COLS = Tile::COLS, C4 = COLS / 4;
-  static constexpr int NBUF = MB == 1 ? 3 : MB == 2 ? 2 : 1;
+  // steps in flight of a wave, within the registers
+  static constexpr int NBUF = 2;
+  using Stream = RowStream<KB, NBUF, kDecodeWaves>;
 
-  // up-projection: COLS / 2 gate columns and the matching up columns of a group's rows
-  static __device__ void up(const DecodeArgs& a, const Picked& p, typename Tile::Part* part, int wave, int gi, int tile) {
-    const int e = __builtin_amdgcn_readfirstlane(p.gexp[gi]), r0 = p.goff[gi];
-    const int cnt = __builtin_amdgcn_readfirstlane(p.goff[gi + 1] - r0);
-    const int n = a.n, N = 2 * n;
-    const Rsrc w = buffer_of(a.W1 + (size_t)e * a.d * N, (uint32_t)a.d * N * 2), x = buffer_of(a.X, (uint32_t)a.T * a.d * 2);
-    const int c = tile * (COLS / 2) + 8 * (Tile::cg() & (CG / 2 - 1));
-    const uint32_t wcol = c < n ? 2 * (c + (Tile::cg() >= CG / 2 ? n : 0)) : kBufferOut;
-    auto run = [&](auto blocks) {
-      constexpr int B = decltype(blocks)::value;
-      uint32_t xoff[B];
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        const int r = RT * b + Tile::row();
-        xoff[b] = r < cnt ? (uint32_t)(p.rows[r0 + r] / a.K) * a.d * 2 : kBufferOut;
-      }
-      f32x4 acc[B][8];
-      zero_acc(acc);
-      stream_acc<KB, B, NBUF, kDecodeWaves>(acc, w, N * 2, wcol, x, xoff, 0, a.d, wave);
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        if (RT * b >= cnt) break;
-        __syncthreads();
-        Tile::put(part[wave], acc[b]);
-        __syncthreads();
-        for (int i = threadIdx.x; i < RT * C4 / 2; i += kDecodeThreads) {
-          const int row = i / (C4 / 2), c4 = i % (C4 / 2), col = tile * (COLS / 2) + 4 * c4;
-          if (RT * b + row >= cnt || col >= n) continue;
-          f32x4 hg = Tile::template sum<kDecodeWaves>(part, row, c4);
-          f32x4 hu = Tile::template sum<kDecodeWaves>(part, row, c4 + C4 / 2);
-          if (a.b1) {
-            const float* bias = a.b1 + (size_t)e * N + col;
-            const f32x4 bg = *(const f32x4*)bias, bu = *(const f32x4*)(bias + n);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              hg[q] += bg[q];
-              hu[q] += bu[q];
-            }
-          }
-          float v[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float sg;
-            v[q] = silu_sig(hg[q], &sg) * hu[q];
-          }
-          // (A to bf16, the type of the product that follows, as in the layer's forward)
-          *(u32x2*)(a.A + (size_t)p.rows[r0 + RT * b + row] * n + col) = pack_bf16x4(v[0], v[1], v[2], v[3]);
-        }
-      }
-    };
-    if constexpr (MB >= 4)
-      if (cnt > 2 * RT) return run(std::integral_constant<int, 4>{});
+  // f(B) with the row blocks that a group of cnt rows needs
+  template <class F>
+  static __device__ __forceinline__ void by_blocks(int cnt, F f) {
     if constexpr (MB >= 2)
-      if (cnt > RT) return run(std::integral_constant<int, 2>{});
-    run(std::integral_constant<int, 1>{});
+      if (cnt > RT) return f(std::integral_constant<int, 2>{});
+    f(std::integral_constant<int, 1>{});
   }
 
-  // down-projection of a group's rows: Y in fp32
-  static __device__ void down(const DecodeArgs& a, const Picked& p, typename Tile::Part* part, int wave, int gi, int tile) {
-    const int e = __builtin_amdgcn_readfirstlane(p.gexp[gi]), r0 = p.goff[gi];
-    const int cnt = __builtin_amdgcn_readfirstlane(p.goff[gi + 1] - r0);
-    const int n = a.n, d = a.d;
-    const Rsrc w = buffer_of(a.W2 + (size_t)e * n * d, (uint32_t)n * d * 2), x = buffer_of(a.A, (uint32_t)a.T * a.K * n * 2);
-    const uint32_t wcol = 2 * (tile * COLS + 8 * Tile::cg());
-    auto run = [&](auto blocks) {
+  // An item of a group: the up-projection of COLS / 2 gate columns and the matching up columns
+  // (a.ks > 1: of a slice of k), or the down-projection of COLS columns
+  struct Item {
+    bool up;
+    int gi, tile, slice, e, r0, cnt;  // (cnt: rows left, of which a pass takes RT MB)
+  };
+  static __device__ __forceinline__ Item item_of(const DecodeArgs& a, const Picked& p, bool up, int i, int tiles) {
+    Item t;
+    t.up = up;
+    t.slice = up ? i % a.ks : 0;
+    if (up) i /= a.ks;
+    t.gi = i / tiles;
+    t.tile = i % tiles;
+    t.e = __builtin_amdgcn_readfirstlane(p.gexp[t.gi]);
+    t.r0 = __builtin_amdgcn_readfirstlane(p.goff[t.gi]);
+    t.cnt = __builtin_amdgcn_readfirstlane(p.goff[t.gi + 1]) - t.r0;
+    return t;
+  }
+  static __device__ __forceinline__ void prime(const DecodeArgs& a, const Item& t, Stream& stream, int wave) {
+    const int n = a.n, d = a.d, lane = opaque_lane();
+    const uint32_t bytes = (uint32_t)n * d * 2;
+    if (t.up) {
+      const int c = t.tile * (COLS / 2) + 8 * (Tile::cg(lane) & (CG / 2 - 1));
+      stream.prime(buffer_of(a.W1 + (size_t)t.e * n * d * 2, 2 * bytes), n * 4,
+                   c < n ? 2 * (c + (Tile::cg(lane) >= CG / 2 ? n : 0)) : kBufferOut, t.slice * a.kslice,
+                   min(d, (t.slice + 1) * a.kslice), wave, lane);
+    } else {
+      stream.prime(buffer_of(a.W2 + (size_t)t.e * n * d, bytes), d * 2, 2 * (t.tile * COLS + 8 * Tile::cg(lane)), 0, n, wave, lane);
+    }
+  }
+  // the rest of the product of a primed item, into A (or the slices of H) or Y
+  static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& stream,
+                                             typename Tile::Part* part, int wave) {
+    const int n = a.n, d = a.d, N = 2 * n, P = a.T * a.K, lane = opaque_lane();
+    by_blocks(t.cnt, [&](auto blocks) __attribute__((always_inline)) {
       constexpr int B = decltype(blocks)::value;
       uint32_t xoff[B];
-#pragma unroll
-      for (int b = 0; b < B; ++b) {
-        const int r = RT * b + Tile::row();
-        xoff[b] = r < cnt ? (uint32_t)p.rows[r0 + r] * n * 2 : kBufferOut;
-      }
       f32x4 acc[B][8];
       zero_acc(acc);
-      stream_acc<KB, B, NBUF, kDecodeWaves>(acc, w, d * 2, wcol, x, xoff, 0, n, wave);
 #pragma unroll
       for (int b = 0; b < B; ++b) {
-        if (RT * b >= cnt) break;
-        __syncthreads();
-        Tile::put(part[wave], acc[b]);
-        __syncthreads();
-        for (int i = threadIdx.x; i < RT * C4; i += kDecodeThreads) {
-          const int row = i / C4, c4 = i % C4, col = tile * COLS + 4 * c4;
-          if (RT * b + row >= cnt) continue;
-          f32x4 y = Tile::template sum<kDecodeWaves>(part, row, c4);
-          if (a.b2) {
-            const f32x4 bias = *(const f32x4*)(a.b2 + (size_t)e * d + col);
+        const int r = RT * b + Tile::row(lane);
+        const int i = r < t.cnt ? p.rows[t.r0 + r] : -1;
+        xoff[b] = i < 0 ? kBufferOut : t.up ? (uint32_t)(i / a.K) * d * 2 : (uint32_t)i * n * 2;
+      }
+      // (X too by the access that A needs: one copy of the loop)
+      const Rsrc rows_in = t.up ? buffer_of(a.X, (uint32_t)a.T * d * 2) : buffer_of(a.A, (uint32_t)P * n * 2);
+      stream.template add<true>(acc, rows_in, xoff);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] += bias[q];
+      for (int b = 0; b < B; ++b) {
+        if (RT * b >= t.cnt) break;
+        if (b) __syncthreads();
+        Tile::put(part[wave], acc[b], lane);
+        __syncthreads();
+        const int rows = min(RT, t.cnt - RT * b);
+        if (t.up && a.ks == 1) {
+          for (int i = threadIdx.x; i < rows * (C4 / 2); i += kDecodeThreads) {
+            const int row = i / (C4 / 2), c4 = i % (C4 / 2), col = t.tile * (COLS / 2) + 4 * c4;
+            if (col >= n) continue;
+            f32x4 hg = Tile::template sum<kDecodeWaves>(part, row, c4);
+            f32x4 hu = Tile::template sum<kDecodeWaves>(part, row, c4 + C4 / 2);
+            if (a.b1) {
+              const float* bias = a.b1 + (size_t)t.e * N + col;
+              const f32x4 bg = *(const f32x4*)bias, bu = *(const f32x4*)(bias + n);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                hg[q] += bg[q];
+                hu[q] += bu[q];
+              }
+            }
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float sg;
+              v[q] = silu_sig(hg[q], &sg) * hu[q];
+            }
+            // (A to bf16, the type of the product that follows, as in the layer's forward)
+            store8_shared(buffer_of(a.A, (uint32_t)P * n * 2), (uint32_t)(p.rows[t.r0 + RT * b + row] * n + col) * 2,
+                          pack_bf16x4(v[0], v[1], v[2], v[3]));
           }
-          *(f32x4*)(a.Y + (size_t)p.rows[r0 + RT * b + row] * d + col) = y;
+          continue;
+        }
+        for (int i = threadIdx.x; i < rows * C4; i += kDecodeThreads) {
+          const int row = i / C4, c4 = i % C4, r = p.rows[t.r0 + RT * b + row];
+          f32x4 y = Tile::template sum<kDecodeWaves>(part, row, c4);
+          if (t.up) {
+            const int col = t.tile * (COLS / 2) + 4 * (c4 % (C4 / 2));
+            if (col < n)
+              store16_shared(buffer_of(a.H32, (uint32_t)a.ks * P * N * 4),
+                             (uint32_t)((t.slice * P + r) * N + col + (c4 < C4 / 2 ? 0 : n)) * 4, __builtin_bit_cast(u32x4, y));
+          } else {
+            const int col = t.tile * COLS + 4 * c4;
+            if (a.b2) {
+              const f32x4 bias = *(const f32x4*)(a.b2 + (size_t)t.e * d + col);
+#pragma unroll
+              for (int q = 0; q < 4; ++q) y[q] += bias[q];
+            }
+            store16_shared(buffer_of(a.Y, (uint32_t)P * d * 4), (uint32_t)(r * d + col) * 4, __builtin_bit_cast(u32x4, y));
+          }
         }
       }
-    };
-    if constexpr (MB >= 4)
-      if (cnt > 2 * RT) return run(std::integral_constant<int, 4>{});
-    if constexpr (MB >= 2)
-      if (cnt > RT) return run(std::integral_constant<int, 2>{});
-    run(std::integral_constant<int, 1>{});
+    });
+  }
+
+  static __device__ __forceinline__ void write_o(const DecodeArgs& a, int t, int col, f32x4 o, u32x2 r, bool ok) {
+    if (a.R) {
+      o[0] += bf_lo(r[0]);
+      o[1] += bf_hi(r[0]);
+      o[2] += bf_lo(r[1]);
+      o[3] += bf_hi(r[1]);
+    }
+    if (!ok) o = f32x4{NAN, NAN, NAN, NAN};
+    *(u32x2*)(a.O + (size_t)t * a.d + col) = pack_bf16x4(o[0], o[1], o[2], o[3]);
   }
 
   // O = R + sum of s Y over each token's entries, the columns of one down-projection tile
-  static __device__ void sum_tokens(const DecodeArgs& a, const Picked& p, int tile, int t0, int tokens, bool ok) {
+  static __device__ __forceinline__ void sum_tokens(const DecodeArgs& a, const Picked& p, int tile, int t0, int tokens, bool ok) {
+    const Rsrc y = buffer_of(a.Y, (uint32_t)a.T * a.K * a.d * 4);
     for (int i = threadIdx.x; i < tokens * C4; i += kDecodeThreads) {
       const int t = t0 + i / C4, col = tile * COLS + 4 * (i % C4);
       if (t >= a.T) break;
+      u32x2 res = {0, 0};
+      if (a.R) res = *(const u32x2*)(a.R + (size_t)t * a.d + col);
       f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
       for (int j = 0; j < a.K; ++j) {
-        const f32x4 y = *(const f32x4*)(a.Y + (size_t)(t * a.K + j) * a.d + col);
+        const f32x4 v = __builtin_bit_cast(f32x4, load16<true>(y, (uint32_t)((t * a.K + j) * a.d + col) * 4));
         const float w = p.w[t * a.K + j];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] += w * y[q];
+        for (int q = 0; q < 4; ++q) o[q] += w * v[q];
       }
-      if (a.R) {
-        const u32x2 r = *(const u32x2*)(a.R + (size_t)t * a.d + col);
-        o[0] += bf_lo(r[0]);
-        o[1] += bf_hi(r[0]);
-        o[2] += bf_lo(r[1]);
-        o[3] += bf_hi(r[1]);
+      write_o(a, t, col, o, res, ok);
+    }
+  }
+
+  // down-projection by token, with its sum: the token's K experts are one reduction of
+  // K n, a wave's step 32 KB k of one expert, whose product is weighted as it is added
+  template <class Wait>
+  static __device__ __forceinline__ void token_down(const DecodeArgs& a, const Picked& p, typename Tile::Part* part,
+                                                    uint16_t* rows, int wave, int t, int tile, Wait wait) {
+    constexpr int NB = 2;
+    const int n = a.n, d = a.d, spe = (n + Tile::KSTEP - 1) / Tile::KSTEP, steps = a.K * spe, lane = opaque_lane();
+    const uint32_t wcol = 2 * (tile * COLS + 8 * Tile::cg(lane));
+    u32x4 wv[NB][8];
+    bf16x8 xv[NB];
+    auto entry = [&](int s) { return t * a.K + min(wave + kDecodeWaves * s, steps - 1) / spe; };
+    auto first_k = [&](int s) { return min(wave + kDecodeWaves * s, steps - 1) % spe * Tile::KSTEP + Tile::k0(lane); };
+    auto load_w = [&](int buf, int s) {
+      const int e = __builtin_amdgcn_readfirstlane(p.sel[entry(s)]), k = first_k(s);
+      const Rsrc w = buffer_of(a.W2 + (size_t)e * n * d, (uint32_t)n * d * 2);
+      const uint32_t o = wave + kDecodeWaves * s < steps && k < n ? wcol + (uint32_t)k * d * 2 : kBufferOut;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) wv[buf][i] = load16(w, o + i * d * 2);
+    };
+    auto load_x = [&](int buf, int s) {
+      const int k = first_k(s);
+      if (a.ks > 1)
+        xv[buf] = __builtin_bit_cast(bf16x8, k < n ? *(const u32x4*)(rows + (entry(s) - t * a.K) * n + k) : u32x4{0, 0, 0, 0});
+      else
+        xv[buf] = __builtin_bit_cast(bf16x8, load16<true>(buffer_of(a.A, (uint32_t)a.T * a.K * n * 2),
+                                                          k < n ? (uint32_t)(entry(s) * n + k) * 2 : kBufferOut));
+    };
+#pragma unroll
+    for (int q = 0; q < NB; ++q) load_w(q, q);
+    // what else the end needs
+    const int col = tile * COLS + 4 * threadIdx.x;
+    u32x2 res = {0, 0};
+    f32x4 bias = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (threadIdx.x < C4) {
+      if (a.R) res = *(const u32x2*)(a.R + (size_t)t * d + col);
+      if (a.b2)
+        for (int j = 0; j < a.K; ++j) {
+          const f32x4 v = *(const f32x4*)(a.b2 + (size_t)p.sel[t * a.K + j] * d + col);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) bias[q] += p.w[t * a.K + j] * v[q];
+        }
+    }
+    wait();
+    if (a.ks > 1) {
+      // the token's A from the slices of H, added in slice order
+      const int P = a.T * a.K, N = 2 * n;
+      const Rsrc h = buffer_of(a.H32, (uint32_t)a.ks * P * N * 4);
+      for (int i = threadIdx.x; i < a.K * n / 4; i += kDecodeThreads) {
+        const int j = i / (n / 4), c = 4 * (i % (n / 4));
+        f32x4 hg = f32x4{0.f, 0.f, 0.f, 0.f}, hu = hg;
+        if (a.b1) {
+          const float* b1 = a.b1 + (size_t)p.sel[t * a.K + j] * N + c;
+          hg = *(const f32x4*)b1;
+          hu = *(const f32x4*)(b1 + n);
+        }
+#pragma unroll 4
+        for (int q = 0; q < a.ks; ++q) {
+          const uint32_t o = (uint32_t)((q * P + t * a.K + j) * N + c) * 4;
+          const f32x4 vg = __builtin_bit_cast(f32x4, load16<true>(h, o)), vu = __builtin_bit_cast(f32x4, load16<true>(h, o + 4 * n));
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            hg[r] += vg[r];
+            hu[r] += vu[r];
+          }
+        }
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float sg;
+          v[r] = silu_sig(hg[r], &sg) * hu[r];
+        }
+        *(u32x2*)(rows + j * n + c) = pack_bf16x4(v[0], v[1], v[2], v[3]);
       }
-      if (!ok) o = f32x4{NAN, NAN, NAN, NAN};
-      *(u32x2*)(a.O + (size_t)t * a.d + col) = pack_bf16x4(o[0], o[1], o[2], o[3]);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int q = 0; q < NB; ++q) load_x(q, q);
+    f32x4 acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int ns = (steps - wave + kDecodeWaves - 1) / kDecodeWaves;
+    auto run = [&]() __attribute__((always_inline)) {
+      if (ns <= 0) return;
+      for (int s = 0;; s += NB) {
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+          const float sw = p.w[entry(s + q)];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[q], column_of8(wv[q], j), f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[j][r] += sw * y[r];
+          }
+          if (s + q + 1 >= ns) return;
+          load_w(q, s + q + NB);
+          load_x(q, s + q + NB);
+        }
+      }
+    };
+    run();
+    // (every row of the product's k block is this token)
+    Tile::put(part[wave], acc, lane);
+    __syncthreads();
+    if (threadIdx.x < C4 * kDecodeWaves) {  // lanes of four columns, one for each wave's sums
+      static_assert(C4 * kDecodeWaves <= kWave);
+      const int c4 = threadIdx.x % C4, w = threadIdx.x / C4;
+      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        const f32x4 v = part[w][b][0][c4 & 1][c4 >> 1];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] += v[q];
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+#pragma unroll
+        for (int i = C4; i < C4 * kDecodeWaves; i *= 2) o[q] += __shfl_xor(o[q], i, kWave);
+        o[q] += bias[q];
+      }
+      if (threadIdx.x < C4) write_o(a, t, col, o, res, wait.ok());
     }
   }
 };
 
 constexpr int kSumTokens = 16;  // tokens of one item of the sums
 
-template <int KB, int MB>
+template <int KB, int MB, bool BY_TOKEN>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeArgs a) {
   using D = Decode<KB, MB>;
+  using TD = Decode<4, 1>;  // by token
   extern __shared__ __attribute__((aligned(16))) char dyn[];  // picked_bytes
   __shared__ typename D::Tile::Part part[kDecodeWaves];
   __shared__ int sh[2];
   __shared__ int scan_lds[kDecodeWaves];
   const Picked p = picked_at(dyn, a.T, a.E, a.K);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (threadIdx.x == 0) sh[0] = take_ticket(a);
-  const int groups = __builtin_amdgcn_readfirstlane(pick(a, p, scan_lds));
-  const int up_tiles = (a.n + D::COLS / 2 - 1) / (D::COLS / 2), down_tiles = a.d / D::COLS;
-  const int ups = groups * up_tiles, downs = groups * down_tiles;
-  const int sums = down_tiles * ((a.T + kSumTokens - 1) / kSumTokens);
-  int* up_done = a.sync + kSyncUp;
-  int* down_done = up_done + min(a.T * a.K, a.E);
-  bool ok = true;  // (of the waits so far)
-  for (;;) {
-    int item = __builtin_amdgcn_readfirstlane(sh[0]);
-    if (item >= ups + downs + sums) break;
-    int next = 0;
-    if (threadIdx.x == 0) next = take_ticket(a);
-    int* counter = nullptr;
-    int* awaited = nullptr;
-    int want = 0;
-    if (item >= ups + downs) {
-      awaited = down_done + (item - ups - downs) % down_tiles;
-      want = groups;
-    } else if (item >= ups) {
-      awaited = up_done + (item - ups) / down_tiles;
-      want = up_tiles;
-    }
-    if (awaited) {
-      if (threadIdx.x == 0) {
-        sh[1] = wait_counter(awaited, want);
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-      }
+  if (threadIdx.x == kDecodeThreads - 1) sh[0] = take_ticket(a);  // (not by a wave that selects)
+  // Up to 8 tokens every workgroup selects for itself.  More are the queue's first items, of 8
+  // tokens each (a wave takes 3.8 us for one, and 64 would take 30).
+  bool ok = true;  // (the waits so far)
+  const int selects = a.T <= kDecodeWaves ? 0 : (a.T + kDecodeWaves - 1) / kDecodeWaves;
+  int item;
+  if (selects == 0) {
+    select_all(a, p);
+    item = __builtin_amdgcn_readfirstlane(sh[0]);
+  } else {
+    __syncthreads();
+    for (;;) {
+      item = __builtin_amdgcn_readfirstlane(sh[0]);
+      if (item >= selects) break;
+      select_some(a, p, item);
+      finish_item<0>(select_counter(a));
+      if (threadIdx.x == 0) sh[0] = take_ticket(a);
       __syncthreads();
-      ok = ok && sh[1];
     }
-    if (item < ups) {
-      D::up(a, p, part, wave, item / up_tiles, item % up_tiles);
-      counter = up_done + item / up_tiles;
-    } else if (item < ups + downs) {
-      item -= ups;
-      D::down(a, p, part, wave, item / down_tiles, item % down_tiles);
-      counter = down_done + item % down_tiles;
+    item -= selects;
+    ok = await([&](int l) { return l == 0 ? select_counter(a) : nullptr; }, selects, sh + 1);
+    read_selection(a, p);
+  }
+  const int groups = __builtin_amdgcn_readfirstlane(form_groups(a, p, scan_lds));
+  const int up_tiles = (a.n + D::COLS / 2 - 1) / (D::COLS / 2), down_tiles = a.d / (BY_TOKEN ? TD::COLS : D::COLS);
+  const int per_group = up_tiles * a.ks, ups = groups * per_group, downs = (BY_TOKEN ? a.T : groups) * down_tiles;
+  const int sums = BY_TOKEN ? 0 : down_tiles * ((a.T + kSumTokens - 1) / kSumTokens);
+  const int total = ups + downs + sums;
+  // Where every item has a workgroup, no one asks for a second ticket (each costs 11 ns of all
+  // the others' time).  Else the next ticket is asked for before an item's work, and the next
+  // item's first weights between this one's stores and its count.
+  const bool more = selects || total > (int)gridDim.x;
+  typename D::Stream stream;
+  typename D::Item t;
+  const int last = BY_TOKEN ? ups : ups + downs;  // of the items of groups
+  auto start = [&]() __attribute__((always_inline)) {
+    if (item < last) {
+      t = D::item_of(a, p, item < ups, item < ups ? item : item - ups, item < ups ? up_tiles : down_tiles);
+      D::prime(a, t, stream, wave);
+    }
+  };
+  start();
+  while (item < last) {
+    int next = 0;
+    if (more && threadIdx.x == 0) next = take_ticket(a);
+    int* counter = BY_TOKEN ? ups_counter(a, item) : t.up ? group_counter(a, t.gi) : tile_counter(a, t.tile);
+    if (!t.up) ok = await([&](int l) { return l == 0 ? group_counter(a, t.gi) : nullptr; }, per_group, sh + 1) && ok;
+    if (more && threadIdx.x == 0) sh[0] = next;
+    while (MB > 1 && t.cnt > D::RT * MB) {  // (more rows than a pass takes: the weights again)
+      D::run(a, p, t, stream, part, wave);
+      t.r0 += D::RT * MB;
+      t.cnt -= D::RT * MB;
+      D::prime(a, t, stream, wave);
+      __syncthreads();
+    }
+    D::run(a, p, t, stream, part, wave);  // (has a barrier after which sh is read)
+    item = more ? __builtin_amdgcn_readfirstlane(sh[0]) - selects : total;
+    asm volatile("" ::: "memory");
+    if (!ok) counter = ups_counter(a, 8);  // (what gave up is not counted, so that nothing is summed from it)
+    if (item < last) {
+      start();
+      finish_item<8 * D::NBUF>(counter);
     } else {
-      item -= ups + downs;
-      D::sum_tokens(a, p, item % down_tiles, item / down_tiles * kSumTokens, kSumTokens, ok);
+      finish_item<0>(counter);
     }
-    if (counter && ok) finish_item(counter);  // (what gave up is not counted, so that nothing is summed from it)
+  }
+  while (item < total) {
+    const int i = item - last, tile = i % down_tiles;
+    if constexpr (BY_TOKEN) {
+      // (all up-projections: the token's own are seldom done much earlier)
+      struct {
+        const DecodeArgs& a; int ups; int* sh; bool* all;
+        __device__ __forceinline__ void operator()() const {
+          *all = await([&](int l) { return l < 8 ? ups_counter(a, l) : nullptr; }, ups, sh) && *all;
+        }
+        __device__ bool ok() const { return *all; }
+      } wait{a, ups, sh + 1, &ok};
+      TD::token_down(a, p, (typename TD::Tile::Part*)part, (uint16_t*)(dyn + picked_bytes(a.T, a.E, a.K)), wave, i / down_tiles,
+                     tile, wait);
+    } else {
+      ok = await([&](int l) { return l == 0 ? tile_counter(a, tile) : nullptr; }, groups, sh + 1) && ok;
+      D::sum_tokens(a, p, tile, i / down_tiles * kSumTokens, kSumTokens, ok);
+    }
+    if (!more) break;
+    if (threadIdx.x == 0) sh[0] = take_ticket(a);
     __syncthreads();
-    if (threadIdx.x == 0) sh[0] = next;
-    __syncthreads();
+    item = __builtin_amdgcn_readfirstlane(sh[0]) - selects;
+    __syncthreads();  // (sh and the partial sums are free again)
   }
 }
 
 // ---------------------------------------------------------------- host
 int decode_slices(int T, int d, int E) {
-  // about 64 workgroups, of two steps or more for each wave
+  // up to about 64 workgroups, of a step or more for each wave
   const int tiles = (E + 127) / 128 * ((T + 15) / 16);
-  const int want = std::max(1, std::min(64 / tiles, d / (2 * 32 * kDecodeWaves)));
+  const int want = std::max(1, std::min(64 / tiles, d / (32 * kDecodeWaves)));
   const int per = (d / 32 + want - 1) / want;
   return (d / 32 + per - 1) / per;
 }
-size_t decode_sync_words(int T, int d, int E, int K) { return kSyncUp + std::min(T * K, E) + d / 32; }
+size_t decode_sync_words(int T, int d, int E, int K) { return (size_t)kLine * (10 + std::min(T * K, E) + d / 32); }
+// whether the down-projection goes by token: where few entries repeat experts, whose weights are
+// then read again, and the items are one round; then the slices of k
+static bool decode_by_token(int T, int d, int E, int K) { return T == 1 || (2 * T * K <= E && T * (d / 32) <= 256); }
+int decode_ks(int T, int d, int n, int E, int K) {
+  if (!decode_by_token(T, d, E, K) || K * n > 8192) return 1;
+  return std::max(1, std::min({128 / (T * K * ((n + 63) / 64)), d / 256, 8}));
+}
 
 template <int KB, int MB>
 static hipError_t run_router(const DecodeArgs& a, hipStream_t s) {
@@ -423,22 +770,25 @@ static hipError_t run_router(const DecodeArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int KB, int MB>
+template <int KB, int MB, bool BY_TOKEN>
 static hipError_t run_decode(const DecodeArgs& a, hipStream_t s) {
   using D = Decode<KB, MB>;
-  const int64_t groups = std::min(a.T * a.K, a.E);
-  const int64_t items = groups * ((a.n + D::COLS / 2 - 1) / (D::COLS / 2) + a.d / D::COLS);
-  decode_kernel<KB, MB><<<(int)std::min<int64_t>(items, 256), kDecodeThreads, picked_bytes(a.T, a.E, a.K), s>>>(a);
+  const int64_t groups = std::min(a.T * a.K, a.E), down_tiles = a.d / (BY_TOKEN ? Decode<4, 1>::COLS : D::COLS);
+  int64_t items = groups * ((a.n + D::COLS / 2 - 1) / (D::COLS / 2)) * a.ks;
+  items += BY_TOKEN ? a.T * down_tiles : (groups + (a.T + kSumTokens - 1) / kSumTokens) * down_tiles;
+  const size_t lds = picked_bytes(a.T, a.E, a.K) + (a.ks > 1 ? 2 * (size_t)a.K * a.n : 0);
+  decode_kernel<KB, MB, BY_TOKEN><<<(int)std::min<int64_t>(items, 256), kDecodeThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_decode(const DecodeArgs& a, hipStream_t s) {
+hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
+  a.slices = decode_slices(a.T, a.d, a.E);
+  a.ks = decode_ks(a.T, a.d, a.n, a.E, a.K);
+  a.kslice = (a.d / 32 + a.ks - 1) / a.ks * 32;
   const hipError_t e = run_router<1, 1>(a, s);
   if (e != hipSuccess) return e;
-  if (a.T <= 4) return run_decode<2, 1>(a, s);
-  if (a.T <= 16) return run_decode<1, 1>(a, s);
-  if (a.T <= 32) return run_decode<1, 2>(a, s);
-  return run_decode<1, 4>(a, s);
+  if (decode_by_token(a.T, a.d, a.E, a.K)) return run_decode<1, 1, true>(a, s);
+  return a.T <= 16 ? run_decode<1, 1, false>(a, s) : run_decode<1, 2, false>(a, s);
 }
 
 }  // namespace smoe

@@ -264,13 +264,17 @@ struct DecodeArgs {
   const float* b2; const uint16_t* R; uint16_t* O; int32_t* topk_idx; float* topk_w;
   float* part;    // [slices][T][E] partial logits
   int32_t* sync;  // decode_sync_words counters
+  uint32_t* picked;  // [T K] expert and weight of each entry
   uint16_t* A;    // [T K][n]
   float* Y;       // [T K][d]
-  int T, d, n, E, K, slices;
+  float* H32;     // [ks][T K][2n], where k is sliced (ks > 1)
+  int T, d, n, E, K;
+  int slices = 0, ks = 0, kslice = 0;  // (set by launch_decode)
 };
 int decode_slices(int T, int d, int E);
+int decode_ks(int T, int d, int n, int E, int K);
 size_t decode_sync_words(int T, int d, int E, int K);
-hipError_t launch_decode(const DecodeArgs& a, hipStream_t s);
+hipError_t launch_decode(DecodeArgs a, hipStream_t s);
 
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);

@@ -231,16 +231,21 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
 struct DecodeWs {
   int32_t* sync;
   float* part;
+  uint32_t* picked;
   uint16_t* A;
   float* Y;
+  float* H32;
 };
 size_t decode_layout(const moe_dims& m, char* base, DecodeWs* w) {
   const size_t P = (size_t)m.T * m.K;
   size_t off = 0;
   off = carve(base, off, smoe::decode_sync_words(m.T, m.d, m.E, m.K) * 4, w ? (void**)&w->sync : nullptr);
   off = carve(base, off, (size_t)smoe::decode_slices(m.T, m.d, m.E) * m.T * m.E * 4, w ? (void**)&w->part : nullptr);
+  off = carve(base, off, P * 8, w ? (void**)&w->picked : nullptr);
   off = carve(base, off, P * m.n * 2, w ? (void**)&w->A : nullptr);
   off = carve(base, off, P * m.d * 4, w ? (void**)&w->Y : nullptr);
+  const int ks = smoe::decode_ks(m.T, m.d, m.n, m.E, m.K);
+  off = carve(base, off, ks > 1 ? ks * P * m.n * 8 : 0, w ? (void**)&w->H32 : nullptr);
   return off;
 }
 
@@ -1035,7 +1040,7 @@ int moe_decode(moe_dims m, const moe_bf16* X, const moe_bf16* Wr, const float* b
   hipStream_t stream = (hipStream_t)stream_;
   LAUNCH(MOE_KC_DECODE,
          smoe::launch_decode({X, Wr, bias, W1, W2, eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, R, O, topk_idx, topk_w, w.part,
-                              w.sync, w.A, w.Y, m.T, m.d, m.n, m.E, m.K, smoe::decode_slices(m.T, m.d, m.E)},
+                              w.sync, w.picked, w.A, w.Y, w.H32, m.T, m.d, m.n, m.E, m.K},
                              stream),
          "layer of few tokens");
   return MOE_OK;

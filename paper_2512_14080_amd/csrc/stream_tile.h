@@ -28,8 +28,22 @@ __device__ __forceinline__ Rsrc buffer_of(const void* p, uint32_t bytes) {
                                            0x00027000);
 }
 constexpr uint32_t kBufferOut = 0x80000000u;  // an offset past any of them, and so with up to 2^31 added
+// SHARED: what other workgroups of the same launch write (and read): such values go past
+// the caches that an XCD has to itself, loads and stores alike (the access of an
+// agent-scope atomic), so that no cache has to be written back or invalidated.  A write-back
+// of the L2 costs 3.2 us when every CU asks for it, an invalidation 1.8.
+constexpr int kSharedAccess = 16;  // sc1
+template <bool SHARED = false>
 __device__ __forceinline__ u32x4 load16(Rsrc r, uint32_t off) {
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, SHARED ? kSharedAccess : 0));
+}
+__device__ __forceinline__ void store16_shared(Rsrc r, uint32_t off, u32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(__attribute__((__vector_size__(16))) unsigned int, v), r, (int)off, 0,
+                                         kSharedAccess);
+}
+__device__ __forceinline__ void store8_shared(Rsrc r, uint32_t off, u32x2 v) {
+  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(__attribute__((__vector_size__(8))) unsigned int, v), r, (int)off, 0,
+                                        kSharedAccess);
 }
 
 // 8 rows (k) x 8 columns of bf16, one row per register quad -> per column the
@@ -42,37 +56,44 @@ __device__ __forceinline__ bf16x8 column_of8(const u32x4 (&w)[8], int j) {
   return __builtin_bit_cast(bf16x8, f);
 }
 
+// The lane index from a volatile asm: address arithmetic on it is done where it is used and
+// not hoisted out of a loop over items, where it would hold registers.
+__device__ __forceinline__ int opaque_lane() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
+
 template <int KB>
 struct RowTile {
   static_assert(KB == 1 || KB == 2 || KB == 4, "k blocks of a step");
   static constexpr int CG = 16 / KB, RT = 16 / KB, COLS = 8 * CG, KSTEP = 32 * KB;
-  // lane's column group, k block and row of the other operand
-  static __device__ __forceinline__ int cg() { return lane_id() & (CG - 1); }
-  static __device__ __forceinline__ int kk() { return (lane_id() & 15) / CG; }
-  static __device__ __forceinline__ int row() { return lane_id() & (RT - 1); }
+  // a lane's column group, k block and row of the other operand
+  static __device__ __forceinline__ int cg(int lane) { return lane & (CG - 1); }
+  static __device__ __forceinline__ int kk(int lane) { return (lane & 15) / CG; }
+  static __device__ __forceinline__ int row(int lane) { return lane & (RT - 1); }
   // the lane's first k within a step
-  static __device__ __forceinline__ int k0() { return 32 * kk() + 8 * (lane_id() >> 4); }
+  static __device__ __forceinline__ int k0(int lane) { return 32 * kk(lane) + 8 * (lane >> 4); }
   // one wave's partial sums: [k block][row][half of 8 columns][column group]
   typedef f32x4 Part[KB][RT][2][CG];
 
-  static __device__ __forceinline__ void put(Part& part, const f32x4 (&acc)[8]) {
-    const int g = lane_id() >> 4;
-    if (KB > 1 && g * KB / 4 != kk()) return;  // (another k block's rows)
+  static __device__ __forceinline__ void put(Part& part, const f32x4 (&acc)[8], int lane) {
+    const int g = lane >> 4;
+    if (KB > 1 && g * KB / 4 != kk(lane)) return;  // (another k block's rows)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        part[kk()][(4 * g + r) % RT][h][cg()] = f32x4{acc[4 * h][r], acc[4 * h + 1][r], acc[4 * h + 2][r], acc[4 * h + 3][r]};
+        part[kk(lane)][(4 * g + r) % RT][h][cg(lane)] = f32x4{acc[4 * h][r], acc[4 * h + 1][r], acc[4 * h + 2][r], acc[4 * h + 3][r]};
   }
   // the sum over the waves and k blocks of columns 4 c4 .. 4 c4 + 3, in a fixed order
   template <int KW>
   static __device__ __forceinline__ f32x4 sum(const Part* part, int row, int c4) {
-    f32x4 s = part[0][0][row][c4 & 1][c4 >> 1];
-#pragma unroll
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8 / KB  // (all the loads at once spilled)
     for (int w = 0; w < KW; ++w)
 #pragma unroll
       for (int b = 0; b < KB; ++b) {
-        if (w + b == 0) continue;
         const f32x4 v = part[w][b][row][c4 & 1][c4 >> 1];
 #pragma unroll
         for (int q = 0; q < 4; ++q) s[q] += v[q];
@@ -89,42 +110,65 @@ __device__ __forceinline__ void zero_acc(f32x4 (&acc)[MB][8]) {
     for (int j = 0; j < 8; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// acc += the wave's steps wave, wave + KW, ... of k in [kbeg, kend).  w: the matrix,
-// with ldw bytes from a k row to the next and the lane's column at byte wcol (kBufferOut:
-// none); x: the rows, xoff the byte of k = 0 of the lane's row (kBufferOut: none).
-template <int KB, int MB, int NBUF, int KW>
-__device__ __forceinline__ void stream_acc(f32x4 (&acc)[MB][8], Rsrc w, uint32_t ldw, uint32_t wcol, Rsrc x,
-                                           const uint32_t (&xoff)[MB], int kbeg, int kend, int wave) {
+// A wave's share of a reduction: steps wave, wave + KW, ... of k in [kbeg, kend), NBUF of
+// them in flight.  w: the matrix, with ldw bytes from a k row to the next and the lane's
+// column at byte wcol (kBufferOut: none); x: the rows, xoff the byte of k = 0 of the lane's
+// row (kBufferOut: none).  prime() requests the first steps' weights (8 NBUF loads, always),
+// add() the rest; SHARED: the rows are other workgroups' of this launch.
+template <int KB, int NBUF, int KW>
+struct RowStream {
   using Tile = RowTile<KB>;
-  const int ns = ((kend - kbeg + Tile::KSTEP - 1) / Tile::KSTEP - wave + KW - 1) / KW;  // this wave's steps
-  if (ns <= 0) return;
-  const int kl = kbeg + Tile::k0() + Tile::KSTEP * wave;
+  Rsrc w;
+  uint32_t ldw, wcol;
+  int kl, kend, ns;
   u32x4 wv[NBUF][8];
-  bf16x8 xv[NBUF][MB];
-  auto load = [&](int buf, int s) {
+
+  __device__ __forceinline__ void load_w(int buf, int s) {
     const int k = kl + Tile::KSTEP * KW * s;
     const uint32_t o = k < kend ? wcol + (uint32_t)k * ldw : kBufferOut;
 #pragma unroll
     for (int i = 0; i < 8; ++i) wv[buf][i] = load16(w, o + i * ldw);
+  }
+  __device__ __forceinline__ void prime(Rsrc w_, uint32_t ldw_, uint32_t wcol_, int kbeg, int kend_, int wave,
+                                        int lane) {
+    w = w_;
+    ldw = ldw_;
+    wcol = wcol_;
+    kend = kend_;
+    ns = ((kend - kbeg + Tile::KSTEP - 1) / Tile::KSTEP - wave + KW - 1) / KW;
+    kl = kbeg + Tile::k0(lane) + Tile::KSTEP * wave;
+    // (a wave without a step requests nothing: its k is past the end)
 #pragma unroll
-    for (int b = 0; b < MB; ++b)
-      xv[buf][b] = __builtin_bit_cast(bf16x8, load16(x, k < kend ? xoff[b] + 2 * (uint32_t)k : kBufferOut));
-  };
+    for (int q = 0; q < NBUF; ++q) load_w(q, q);
+  }
+  template <bool SHARED, int MB>
+  __device__ __forceinline__ void add(f32x4 (&acc)[MB][8], Rsrc x_, const uint32_t (&xoff)[MB]) {
+    if (ns <= 0) return;
+    bf16x8 xv[NBUF][MB];
+    auto load_x = [&](int buf, int s) {
+      const int k = kl + Tile::KSTEP * KW * s;
 #pragma unroll
-  for (int q = 0; q < NBUF; ++q) load(q, q);
-  for (int s = 0;; s += NBUF) {
+      for (int b = 0; b < MB; ++b)
+        xv[buf][b] = __builtin_bit_cast(bf16x8, load16<SHARED>(x_, k < kend ? xoff[b] + 2 * (uint32_t)k : kBufferOut));
+    };
 #pragma unroll
-    for (int q = 0; q < NBUF; ++q) {
+    for (int q = 0; q < NBUF; ++q) load_x(q, q);
+    for (int s = 0;; s += NBUF) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bf16x8 wf = column_of8(wv[q], j);
+      for (int q = 0; q < NBUF; ++q) {
 #pragma unroll
-        for (int b = 0; b < MB; ++b) acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[q][b], wf, acc[b][j], 0, 0, 0);
+        for (int j = 0; j < 8; ++j) {
+          const bf16x8 wf = column_of8(wv[q], j);
+#pragma unroll
+          for (int b = 0; b < MB; ++b)
+            acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[q][b], wf, acc[b][j], 0, 0, 0);
+        }
+        if (s + q + 1 >= ns) return;
+        load_w(q, s + q + NBUF);
+        load_x(q, s + q + NBUF);
       }
-      if (s + q + 1 >= ns) return;
-      load(q, s + q + NBUF);
     }
   }
-}
+};
 
 }  // namespace smoe
