@@ -482,6 +482,53 @@ int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float
                const moe_bf16 *W2, const moe_expert_bias *eb, const moe_bf16 *R, moe_bf16 *O, int32_t *topk_idx,
                float *topk_w, void *ws, size_t ws_bytes, void *stream);
 
+/*
+ * The dense matrix product with bias, activation and residual: what stands beside the
+ * routed experts (a shared expert's projections, a dense layer), so that O = R +
+ * shared(X) + experts(X) is three calls, the last adding to the one before.
+ *   H = X W + b;   Y = act(H) + R
+ * MOE_ACT_SWIGLU: W [k,2n], gate columns [0,n) and up columns [n,2n), as W1's, b and H
+ * as wide; act(H) = SiLU(H_gate) * H_up.  MOE_ACT_GELU is the form with erf.
+ */
+enum { MOE_ACT_NONE = 0, MOE_ACT_RELU = 1, MOE_ACT_SILU = 2, MOE_ACT_GELU = 3, MOE_ACT_SWIGLU = 4 };
+
+typedef struct {
+  int32_t T;   /* rows, >= 1                                                  */
+  int32_t k;   /* columns of X, a positive multiple of 8                      */
+  int32_t n;   /* columns of Y, a positive multiple of 8                      */
+  int32_t act; /* MOE_ACT_*                                                   */
+  /* elements from a row to the next of X (and dX), of R, and of Y (and dY): multiples
+   * of 8, at least the row's length, below 2^30; 0: the row's length */
+  int32_t ldx, ldr, ldy;
+} moe_linear;
+
+enum { MOE_WS_LINEAR_FWD = 1, MOE_WS_LINEAR_BWD = 2 };
+/* Workspace bytes of moe_linear_fwd or moe_linear_bwd, at least 256; 0 for an invalid l. */
+size_t moe_linear_workspace_bytes(moe_linear l, int which);
+
+/*
+ *   X [T,k] bf16;  W [k,n] bf16 ([k,2n]: swiglu), contiguous
+ *   b [n] fp32 ([2n]), nullable;  R [T,n] bf16, nullable; may be Y itself (with ldr = ldy)
+ *   H [T,n] ([T,2n]) bf16 out, contiguous, nullable: the pre-activation for the backward
+ *   Y [T,n] bf16 out: rounded once.  What lies between its rows is left as it was.
+ * X, W, R, H, Y are 16-byte aligned, b too; outputs overlap no input but R = Y.
+ */
+int moe_linear_fwd(moe_linear l, const moe_bf16 *X, const moe_bf16 *W, const float *b, const moe_bf16 *R, moe_bf16 *H,
+                   moe_bf16 *Y, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The gradients at the kept H (dR is dY itself):
+ *   dP = dY * act'(H);  dX = dP W^T + G;  dW = X^T dP;  db = column sums of dP
+ *   dY [T,n] bf16, with ldy between rows;  H as written by moe_linear_fwd, null and not
+ *      read with MOE_ACT_NONE
+ *   G  [T,k] bf16, nullable: what reaches X by its other ways, with ldx between rows;
+ *      may be dX itself
+ *   dX [T,k], dW as W, bf16, db as b, fp32: out, each nullable (X only for dW, W only for dX)
+ * dP is rounded to bf16 for the two products; db sums it before that, in a fixed order.
+ */
+int moe_linear_bwd(moe_linear l, const moe_bf16 *dY, const moe_bf16 *X, const moe_bf16 *W, const moe_bf16 *H,
+                   const moe_bf16 *G, moe_bf16 *dX, moe_bf16 *dW, float *db, void *ws, size_t ws_bytes, void *stream);
+
 /* Static description of an error code. */
 const char *moe_strerror(int code);
 /* Thread-local description of the last error returned on this thread. */
@@ -503,6 +550,7 @@ enum {
   MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT, /* (two launches over a long n, counted as one; for few
                                           tokens with the aggregation in it) */
   MOE_KC_DECODE, /* moe_decode: its two launches, counted as one */
+  MOE_KC_LINEAR, MOE_KC_LINEAR_BWD, /* moe_linear_fwd, moe_linear_bwd: all launches of a call */
   MOE_KC_COUNT
 };
 int moe_prof_select(int kernel_class);

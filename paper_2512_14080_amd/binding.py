@@ -46,6 +46,10 @@ MOE_WS_DECODE = 7
 
 MOE_DECODE_MAX_T = 64
 
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "swiglu": 4}
+MOE_WS_LINEAR_FWD = 1
+MOE_WS_LINEAR_BWD = 2
+
 MOE_HELD_EMPTY = 0
 MOE_HELD_WRITTEN = 1
 MOE_CKPT_X = 1
@@ -54,14 +58,15 @@ AGG_STRATEGIES = {"gather_sum": 0, "scatter_sum": 1, "atomic_f32": 2}
 
 KERNEL_CLASSES = ["router_gemm", "topk", "routing_meta", "token_round", "up_proj", "down_proj", "aggregate_O",
                   "dH", "dW2", "dXtilde", "dW1", "aggregate_dX", "dWr", "router_topk", "quantize", "up_proj_quant",
-                  "down_proj_quant", "decode"]
+                  "down_proj_quant", "decode", "linear", "linear_bwd"]
 
 EXPORTS = ["moe_routing_bytes", "moe_routing_init", "moe_round_capacity", "moe_route", "moe_round_tokens",
            "moe_workspace_bytes", "moe_fwd", "moe_bwd", "moe_strerror", "moe_last_error", "moe_prof_select",
            "moe_prof_read", "moe_kernel_class_name", "moe_fwd_aggregation_ablation", "moe_fwd_static",
            "moe_fwd_static_max_bytes", "moe_scale_stride", "moe_quantize_rows", "moe_dequantize_rows",
            "moe_qexperts_bytes", "moe_qexperts_init", "moe_quantize_experts", "moe_dequantize_experts",
-           "moe_ckpt_bytes", "moe_ckpt_init", "moe_fwd_quant", "moe_fwd_ckpt", "moe_bwd_ckpt", "moe_decode"]
+           "moe_ckpt_bytes", "moe_ckpt_init", "moe_fwd_quant", "moe_fwd_ckpt", "moe_bwd_ckpt", "moe_decode",
+           "moe_linear_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd"]
 
 
 class MoeDims(ctypes.Structure):
@@ -99,6 +104,10 @@ class MoeCkpt(ctypes.Structure):
                 ("state", ctypes.c_int32), ("reserved", ctypes.c_int32), ("H", _P), ("Hs", _P), ("X", _P), ("Xs", _P)]
 
 
+class MoeLinear(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("T", "k", "n", "act", "ldx", "ldr", "ldy")]
+
+
 class MoEError(RuntimeError):
     def __init__(self, fn, code, detail):
         super().__init__(f"{fn} failed with {code}: {detail}")
@@ -118,7 +127,7 @@ def lib():
     L = ctypes.CDLL(LIB_PATH)
     sz, i32, vp = ctypes.c_size_t, ctypes.c_int32, ctypes.c_void_p
     D, R, EB = MoeDims, ctypes.POINTER(MoeRouting), ctypes.POINTER(MoeExpertBias)
-    Q, C = ctypes.POINTER(MoeQExperts), ctypes.POINTER(MoeCkpt)
+    Q, C, L_ = ctypes.POINTER(MoeQExperts), ctypes.POINTER(MoeCkpt), MoeLinear
     sig = {
         "moe_routing_bytes": (sz, [D, i32, ctypes.c_int]),
         "moe_routing_init": (ctypes.c_int, [D, i32, ctypes.c_int, vp, sz, R]),
@@ -144,6 +153,9 @@ def lib():
         "moe_fwd_ckpt": (ctypes.c_int, [D, vp, vp, vp, EB, R, C, vp, vp, sz, vp]),
         "moe_bwd_ckpt": (ctypes.c_int, [D, vp, vp, C, vp, vp, EB, vp, R, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "moe_decode": (ctypes.c_int, [D, vp, vp, vp, vp, vp, EB, vp, vp, vp, vp, vp, sz, vp]),
+        "moe_linear_workspace_bytes": (sz, [L_, ctypes.c_int]),
+        "moe_linear_fwd": (ctypes.c_int, [L_, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "moe_linear_bwd": (ctypes.c_int, [L_, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "moe_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         "moe_last_error": (ctypes.c_char_p, []),
         "moe_prof_select": (ctypes.c_int, [ctypes.c_int]),
@@ -400,6 +412,28 @@ def moe_decode(D, X, Wr, bias, W1, W2, R, O, ws, topk_idx=None, topk_w=None, str
     _check("moe_decode", lib().moe_decode(D, _ptr(X), _ptr(Wr), _ptr(bias), _ptr(W1), _ptr(W2), _eb(eb), _ptr(R),
                                           _ptr(O), _ptr(topk_idx), _ptr(topk_w), _ptr(ws),
                                           ws.numel() * ws.element_size(), _stream(stream)))
+
+
+# ------------------------------------------------------------------ dense products
+def linear_dims(T, k, n, act="none", ldx=0, ldr=0, ldy=0) -> MoeLinear:
+    """Sizes, activation (a name of ACTIVATIONS) and row strides in elements (0: contiguous) of a dense product."""
+    return MoeLinear(T, k, n, ACTIVATIONS[act] if isinstance(act, str) else act, ldx, ldr, ldy)
+
+
+def moe_linear_workspace_bytes(L, which) -> int:
+    return lib().moe_linear_workspace_bytes(L, which)
+
+
+def moe_linear_fwd(L, X, W, b, R, H, Y, ws, stream=None):
+    """Y = act(X W + b) + R; b, R and H (the pre-activation, for moe_linear_bwd) may be None."""
+    _check("moe_linear_fwd", lib().moe_linear_fwd(L, _ptr(X), _ptr(W), _ptr(b), _ptr(R), _ptr(H), _ptr(Y), _ptr(ws),
+                                                  ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def moe_linear_bwd(L, dY, X, W, H, G, dX, dW, db, ws, stream=None):
+    """G (None: nothing) is added to dX; dX, dW and db may be None."""
+    _check("moe_linear_bwd", lib().moe_linear_bwd(L, _ptr(dY), _ptr(X), _ptr(W), _ptr(H), _ptr(G), _ptr(dX), _ptr(dW),
+                                                  _ptr(db), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)))
 
 
 def moe_prof_select(kernel_class):

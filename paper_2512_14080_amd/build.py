@@ -17,7 +17,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsonicmoe.so")
 SOURCES = ["moe_abi.cpp", "route_kernels.hip", "round_kernels.hip", "gemm_ops.hip", "stream_gemm.hip", "aggregate.hip",
-           "quant_kernels.hip", "decode.hip"]
+           "quant_kernels.hip", "decode.hip", "linear.hip"]
 ARCH = "gfx950"
 
 

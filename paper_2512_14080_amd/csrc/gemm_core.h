@@ -44,7 +44,7 @@ namespace smoe {
 
 constexpr int kBK = 64;  // default k depth of a stage
 
-enum SrcMode { ROWS = 0, KOUTER = 1 };
+enum SrcMode { ROWS = 0, KOUTER = 1, ROWS_TAIL = 2 };
 
 typedef short v4i16 __attribute__((ext_vector_type(4)));
 #define SMOE_LDS __attribute__((address_space(3)))
@@ -204,6 +204,25 @@ struct RowsSide {
   }
 };
 
+// ROWS whose reduction is no multiple of the stage depth (but of 8): the 16-byte chunks past
+// the end read the zero page.
+template <int R, int BK, int NW>
+struct RowsTailSide : RowsSide<R, BK, NW> {
+  using Base = RowsSide<R, BK, NW>;
+  int k_len;
+  __device__ __forceinline__ void issue(uint32_t lds_side, int k0, int part = 0, int parts = 1) const {
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < Base::Q; ++j) {
+      if (j % parts != part) continue;
+      const int logical = (lane % Base::C) ^ Base::swz(Base::RPI * (w + NW * j) + lane / Base::C);
+      const char* src = k0 + 8 * logical < k_len ? this->ptr[j] + k0 * 2 : (const char*)g_zero_page + lane * 16;
+      dma16(src, lds_side + (w + NW * j) * 1024);
+    }
+  }
+};
+
 // --------------------------------------------------------------- KOUTER side
 // LDS: [BK k][R] bf16 (2R bytes per k row, L = R/8 chunks), chunk c of row k
 // at k*2R + ((c ^ x(k)) << 4) with x(k) = 4*(k%4) for L >= 16 and
@@ -309,6 +328,10 @@ struct SideT;
 template <int R, int BK, int NW, bool AI>
 struct SideT<ROWS, R, BK, NW, AI> {
   using type = RowsSide<R, BK, NW, AI>;
+};
+template <int R, int BK, int NW, bool AI>
+struct SideT<ROWS_TAIL, R, BK, NW, AI> {
+  using type = RowsTailSide<R, BK, NW>;
 };
 template <int R, int BK, int NW, bool AI>
 struct SideT<KOUTER, R, BK, NW, AI> {

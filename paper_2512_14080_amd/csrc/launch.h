@@ -276,6 +276,31 @@ int decode_ks(int T, int d, int n, int E, int K);
 size_t decode_sync_words(int T, int d, int E, int K);
 hipError_t launch_decode(DecodeArgs a, hipStream_t s);
 
+// The dense product (linear.hip): Y [T,n] = act(X W + b) + R
+struct LinearArgs {
+  const uint16_t* X; const uint16_t* W; const float* b; const uint16_t* R;
+  uint16_t* H;  // [T][n or 2n] what is kept for the backward, or null
+  uint16_t* Y;
+  float* part;  // linear_fwd_part_bytes
+  int T, k, n, act;
+  int64_t ldx, ldr, ldy;  // elements from a row to the next
+};
+size_t linear_fwd_part_bytes(int T, int k, int n, int act, int64_t ldx);
+hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t s);
+struct LinearBwdArgs {
+  const uint16_t* dY; const uint16_t* X; const uint16_t* W; const uint16_t* H;
+  const uint16_t* G;  // [T,k] added to dX, or null
+  uint16_t* dX; uint16_t* dW; float* db;  // each may be null
+  uint16_t* dP;       // [T][N] workspace, null without an activation
+  float* db_part; float* dx_part; float* dw_part;
+  int T, k, n, act;
+  int64_t ldx, ldy;
+};
+size_t linear_dx_part_bytes(int T, int k, int64_t N);
+size_t linear_dw_part_bytes(int T, int k, int64_t N);
+size_t linear_db_part_bytes(int T, int64_t N);
+hipError_t launch_linear_bwd(const LinearBwdArgs& a, hipStream_t s);
+
 // aggregation and small kernels
 hipError_t launch_agg_o(const uint16_t* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);
 hipError_t launch_agg_o_f32(const float* Y, const moe_routing& r, uint16_t* O, int T, int d, hipStream_t s);

@@ -1046,6 +1046,98 @@ int moe_decode(moe_dims m, const moe_bf16* X, const moe_bf16* Wr, const float* b
   return MOE_OK;
 }
 
+// ---------------------------------------------------------------- dense products
+static int check_linear(moe_linear& l) {
+  if (l.T < 1) return fail(MOE_ERR_INVALID_ARG, "T must be >= 1 (got %d)", l.T);
+  if (l.k < 8 || l.k % 8) return fail(MOE_ERR_UNSUPPORTED, "k must be a positive multiple of 8 (got %d)", l.k);
+  if (l.n < 8 || l.n % 8) return fail(MOE_ERR_UNSUPPORTED, "n must be a positive multiple of 8 (got %d)", l.n);
+  if (l.act < MOE_ACT_NONE || l.act > MOE_ACT_SWIGLU) return fail(MOE_ERR_INVALID_ARG, "unknown activation %d", l.act);
+  if (l.k >= 1 << 24 || l.n >= 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "k = %d, n = %d: must be below 2^24", l.k, l.n);
+  int32_t* ld[] = {&l.ldx, &l.ldr, &l.ldy};
+  const char* name[] = {"ldx", "ldr", "ldy"};
+  const int len[] = {l.k, l.n, l.n};
+  for (int i = 0; i < 3; ++i) {
+    if (*ld[i] == 0) *ld[i] = len[i];
+    if (*ld[i] < len[i] || *ld[i] % 8 || *ld[i] >= 1 << 30)
+      return fail(MOE_ERR_INVALID_ARG, "%s must be a multiple of 8, at least %d and below 2^30 (got %d)", name[i], len[i], *ld[i]);
+  }
+  return MOE_OK;
+}
+static int64_t linear_columns(const moe_linear& l) { return l.act == MOE_ACT_SWIGLU ? 2 * (int64_t)l.n : l.n; }
+
+namespace {
+struct LinearBwdWs {
+  uint16_t* dP;
+  float* db;
+  float* dx;
+  float* dw;
+};
+size_t linear_bwd_layout(const moe_linear& l, char* base, LinearBwdWs* w) {
+  const int64_t N = linear_columns(l);
+  size_t off = 0;
+  off = carve(base, off, l.act == MOE_ACT_NONE ? 0 : (size_t)l.T * N * 2, w ? (void**)&w->dP : nullptr);
+  off = carve(base, off, smoe::linear_db_part_bytes(l.T, N), w ? (void**)&w->db : nullptr);
+  off = carve(base, off, smoe::linear_dx_part_bytes(l.T, l.k, N), w ? (void**)&w->dx : nullptr);
+  off = carve(base, off, smoe::linear_dw_part_bytes(l.T, l.k, N), w ? (void**)&w->dw : nullptr);
+  return off;
+}
+}  // namespace
+
+size_t moe_linear_workspace_bytes(moe_linear l, int which) {
+  if (check_linear(l) != MOE_OK) return 0;
+  if (which == MOE_WS_LINEAR_FWD)
+    return kAlign + align_up(smoe::linear_fwd_part_bytes(l.T, l.k, l.n, l.act, l.ldx));
+  if (which == MOE_WS_LINEAR_BWD) return kAlign + linear_bwd_layout(l, nullptr, nullptr);
+  return 0;
+}
+
+int moe_linear_fwd(moe_linear l, const moe_bf16* X, const moe_bf16* W, const float* b, const moe_bf16* R, moe_bf16* H,
+                   moe_bf16* Y, void* ws, size_t ws_bytes, void* stream_) {
+  int rc = check_linear(l);
+  if (rc) return rc;
+  CHECK_PTR(X, 16);
+  CHECK_PTR(W, 16);
+  CHECK_PTR(Y, 16);
+  if (!aligned(b, 16)) return fail(MOE_ERR_INVALID_ARG, "b must be 16-byte aligned");
+  if (!aligned(R, 16)) return fail(MOE_ERR_INVALID_ARG, "R must be 16-byte aligned");
+  if (!aligned(H, 16)) return fail(MOE_ERR_INVALID_ARG, "H must be 16-byte aligned");
+  const size_t need = moe_linear_workspace_bytes(l, MOE_WS_LINEAR_FWD);
+  if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < required %zu", ws_bytes, need);
+  CHECK_PTR(ws, kAlign);
+  hipStream_t stream = (hipStream_t)stream_;
+  LAUNCH(MOE_KC_LINEAR,
+         smoe::launch_linear_fwd({X, W, b, R, H, Y, (float*)ws, l.T, l.k, l.n, l.act, l.ldx, l.ldr, l.ldy}, stream),
+         "dense product");
+  return MOE_OK;
+}
+
+int moe_linear_bwd(moe_linear l, const moe_bf16* dY, const moe_bf16* X, const moe_bf16* W, const moe_bf16* H,
+                   const moe_bf16* G, moe_bf16* dX, moe_bf16* dW, float* db, void* ws, size_t ws_bytes, void* stream_) {
+  int rc = check_linear(l);
+  if (rc) return rc;
+  CHECK_PTR(dY, 16);
+  if (dW) CHECK_PTR(X, 16);
+  if (dX) CHECK_PTR(W, 16);
+  if (l.act != MOE_ACT_NONE) CHECK_PTR(H, 16);
+  if (!aligned(G, 16)) return fail(MOE_ERR_INVALID_ARG, "G must be 16-byte aligned");
+  if (!aligned(dX, 16)) return fail(MOE_ERR_INVALID_ARG, "dX must be 16-byte aligned");
+  if (!aligned(dW, 16)) return fail(MOE_ERR_INVALID_ARG, "dW must be 16-byte aligned");
+  if (!aligned(db, 16)) return fail(MOE_ERR_INVALID_ARG, "db must be 16-byte aligned");
+  if (!dX && !dW && !db) return fail(MOE_ERR_INVALID_ARG, "dX, dW and db must not all be null");
+  const size_t need = moe_linear_workspace_bytes(l, MOE_WS_LINEAR_BWD);
+  if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < required %zu", ws_bytes, need);
+  CHECK_PTR(ws, kAlign);
+  LinearBwdWs w;
+  linear_bwd_layout(l, (char*)ws, &w);
+  hipStream_t stream = (hipStream_t)stream_;
+  LAUNCH(MOE_KC_LINEAR_BWD,
+         smoe::launch_linear_bwd({dY, X, W, H, G, dX, dW, db, l.act == MOE_ACT_NONE ? nullptr : w.dP, w.db, w.dx, w.dw, l.T, l.k,
+                                  l.n, l.act, l.ldx, l.ldy},
+                                 stream),
+         "dense product's gradients");
+  return MOE_OK;
+}
+
 int moe_prof_select(int kc) {
   if (kc < -1 || kc >= MOE_KC_COUNT) return fail(MOE_ERR_INVALID_ARG, "unknown kernel class %d", kc);
   std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -1077,7 +1169,8 @@ const char* moe_kernel_class_name(int kc) {
   static const char* names[MOE_KC_COUNT] = {"router_gemm", "topk", "routing_meta", "token_round", "up_proj",
                                             "down_proj", "aggregate_O", "dH", "dW2", "dXtilde",
                                             "dW1", "aggregate_dX", "dWr", "router_topk", "quantize",
-                                            "up_proj_quant", "down_proj_quant", "decode"};
+                                            "up_proj_quant", "down_proj_quant", "decode", "linear",
+                                            "linear_bwd"};
   return (kc >= 0 && kc < MOE_KC_COUNT) ? names[kc] : "unknown";
 }
 
