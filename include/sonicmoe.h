@@ -231,12 +231,12 @@ typedef struct {
 
 /* Workspace bytes for moe_fwd (which = 1), moe_bwd (which = 2),
  * moe_fwd_aggregation_ablation (which = 3), moe_fwd_quant (which = 4),
- * moe_fwd_ckpt (which = 5), moe_bwd_ckpt (which = 6) and moe_decode (which = 7, whatever
- * the capacity). */
+ * moe_fwd_ckpt (which = 5), moe_bwd_ckpt (which = 6), moe_decode (which = 7) and
+ * moe_decode_quant (which = 8; these two whatever the capacity). */
 enum {
   MOE_WS_FWD = 1, MOE_WS_BWD = 2, MOE_WS_FWD_AGG_ABLATION = 3,
   MOE_WS_FWD_QUANT = 4, MOE_WS_FWD_CKPT = 5, MOE_WS_BWD_CKPT = 6,
-  MOE_WS_DECODE = 7
+  MOE_WS_DECODE = 7, MOE_WS_DECODE_QUANT = 8
 };
 size_t moe_workspace_bytes(moe_dims dims, int32_t capacity, int which);
 
@@ -483,6 +483,18 @@ int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float
                float *topk_w, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * The same with 8-bit expert products, as moe_fwd_quant's: H = q(X) q(W1_e) (+ b1_e), Y =
+ * q(A) q(W2_e) (+ b2_e), A quantised from fp32.  Up to 16 tokens the up-projection's codes
+ * are multiplied with fp32 sums (O's error to this definition in 64 bits is then that of
+ * its rounding, 1.7e-3), beyond by the block-scaled instruction.
+ *   q   weights in state MOE_HELD_WRITTEN, of the same d, n and E
+ *   ws  moe_workspace_bytes(dims, capacity, MOE_WS_DECODE_QUANT) bytes
+ */
+int moe_decode_quant(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float *bias, const moe_qexperts *q,
+                     const moe_expert_bias *eb, const moe_bf16 *R, moe_bf16 *O, int32_t *topk_idx, float *topk_w,
+                     void *ws, size_t ws_bytes, void *stream);
+
+/*
  * The dense matrix product with bias, activation and residual: what stands beside the
  * routed experts (a shared expert's projections, a dense layer), so that O = R +
  * shared(X) + experts(X) is three calls, the last adding to the one before.
@@ -549,7 +561,7 @@ enum {
   MOE_KC_QUANTIZE, /* rows and weights into or out of the 8-bit block format (moe_fwd_quant: and its m-tile lists) */
   MOE_KC_UP_QUANT, MOE_KC_DOWN_QUANT, /* (two launches over a long n, counted as one; for few
                                           tokens with the aggregation in it) */
-  MOE_KC_DECODE, /* moe_decode: its two launches, counted as one */
+  MOE_KC_DECODE, /* moe_decode, moe_decode_quant: the two launches, counted as one */
   MOE_KC_LINEAR, MOE_KC_LINEAR_BWD, /* moe_linear_fwd, moe_linear_bwd: all launches of a call */
   MOE_KC_COUNT
 };

@@ -43,6 +43,7 @@ MOE_WS_FWD_QUANT = 4
 MOE_WS_FWD_CKPT = 5
 MOE_WS_BWD_CKPT = 6
 MOE_WS_DECODE = 7
+MOE_WS_DECODE_QUANT = 8
 
 MOE_DECODE_MAX_T = 64
 
@@ -66,6 +67,7 @@ EXPORTS = ["moe_routing_bytes", "moe_routing_init", "moe_round_capacity", "moe_r
            "moe_fwd_static_max_bytes", "moe_scale_stride", "moe_quantize_rows", "moe_dequantize_rows",
            "moe_qexperts_bytes", "moe_qexperts_init", "moe_quantize_experts", "moe_dequantize_experts",
            "moe_ckpt_bytes", "moe_ckpt_init", "moe_fwd_quant", "moe_fwd_ckpt", "moe_bwd_ckpt", "moe_decode",
+           "moe_decode_quant",
            "moe_linear_workspace_bytes", "moe_linear_fwd", "moe_linear_bwd"]
 
 
@@ -153,6 +155,7 @@ def lib():
         "moe_fwd_ckpt": (ctypes.c_int, [D, vp, vp, vp, EB, R, C, vp, vp, sz, vp]),
         "moe_bwd_ckpt": (ctypes.c_int, [D, vp, vp, C, vp, vp, EB, vp, R, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "moe_decode": (ctypes.c_int, [D, vp, vp, vp, vp, vp, EB, vp, vp, vp, vp, vp, sz, vp]),
+        "moe_decode_quant": (ctypes.c_int, [D, vp, vp, vp, Q, EB, vp, vp, vp, vp, vp, sz, vp]),
         "moe_linear_workspace_bytes": (sz, [L_, ctypes.c_int]),
         "moe_linear_fwd": (ctypes.c_int, [L_, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
         "moe_linear_bwd": (ctypes.c_int, [L_, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
@@ -412,6 +415,12 @@ def moe_decode(D, X, Wr, bias, W1, W2, R, O, ws, topk_idx=None, topk_w=None, str
     _check("moe_decode", lib().moe_decode(D, _ptr(X), _ptr(Wr), _ptr(bias), _ptr(W1), _ptr(W2), _eb(eb), _ptr(R),
                                           _ptr(O), _ptr(topk_idx), _ptr(topk_w), _ptr(ws),
                                           ws.numel() * ws.element_size(), _stream(stream)))
+
+
+def moe_decode_quant(D, X, Wr, bias, q: QExperts, R, O, ws, topk_idx=None, topk_w=None, stream=None, eb=None):
+    _check("moe_decode_quant", lib().moe_decode_quant(D, _ptr(X), _ptr(Wr), _ptr(bias), _held(q), _eb(eb), _ptr(R),
+                                                      _ptr(O), _ptr(topk_idx), _ptr(topk_w), _ptr(ws),
+                                                      ws.numel() * ws.element_size(), _stream(stream)))
 
 
 # ------------------------------------------------------------------ dense products

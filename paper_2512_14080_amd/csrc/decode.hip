@@ -21,6 +21,7 @@
 #include <algorithm>
 
 #include "launch.h"
+#include "stream8_tile.h"
 #include "stream_tile.h"
 #include "topk_net.h"
 
@@ -49,8 +50,8 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_router_kernel(const 
   }
   f32x4 acc[MB][8];
   zero_acc(acc);
-  RowStream<KB, 2, kDecodeWaves> stream;
-  stream.prime(w, a.E * 2, col < a.E ? col * 2 : kBufferOut, kbeg, kend, wave, lane);
+  RowStream<KB, 2> stream;
+  stream.prime(w, a.E * 2, col < a.E ? col * 2 : kBufferOut, kbeg, kend, wave, kDecodeWaves, lane);
   stream.template add<false>(acc, x, xoff);
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
@@ -272,10 +273,10 @@ __device__ __forceinline__ void select_some(const DecodeArgs& a, const Picked& p
   select_token_of(a, p, t, 0, 1);
   weigh_token(a, p, t, true, true);
 }
-__device__ __forceinline__ void read_selection(const DecodeArgs& a, const Picked& p) {
+__device__ __forceinline__ void read_selection(const DecodeArgs& a, const Picked& p, bool ok) {
   for (int i = threadIdx.x; i < a.T * a.K; i += kDecodeThreads) {
     const uint64_t v = __hip_atomic_load((uint64_t*)a.picked + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    p.sel[i] = min((int)(uint32_t)v, a.E - 1);  // (in range even where a wait gave up)
+    p.sel[i] = ok ? (int)(uint32_t)v : i % a.K;  // (a selection even where the wait gave up)
     p.w[i] = __uint_as_float((uint32_t)(v >> 32));
   }
   __syncthreads();
@@ -365,6 +366,91 @@ __device__ __forceinline__ bool await(Counter counter, int want, int* sh) {
 }
 
 // ---------------------------------------------------------------- the layer
+__device__ __forceinline__ void write_o(const DecodeArgs& a, int t, int col, f32x4 o, u32x2 r, bool ok) {
+  if (a.R) {
+    o[0] += bf_lo(r[0]);
+    o[1] += bf_hi(r[0]);
+    o[2] += bf_lo(r[1]);
+    o[3] += bf_hi(r[1]);
+  }
+  if (!ok) o = f32x4{NAN, NAN, NAN, NAN};
+  *(u32x2*)(a.O + (size_t)t * a.d + col) = pack_bf16x4(o[0], o[1], o[2], o[3]);
+}
+
+// O = R + sum of s Y over each token's entries, the columns of one down-projection item
+__device__ __forceinline__ void sum_tokens(const DecodeArgs& a, const Picked& p, int cols, int tile, int t0, int tokens, bool ok) {
+  const int C4 = cols / 4;
+  const Rsrc y = buffer_of(a.Y, (uint32_t)a.T * a.K * a.d * 4);
+  for (int i = threadIdx.x; i < tokens * C4; i += kDecodeThreads) {
+    const int t = t0 + i / C4, col = tile * cols + 4 * (i % C4);
+    if (t >= a.T) break;
+    if (col >= a.d) continue;
+    u32x2 res = {0, 0};
+    if (a.R) res = *(const u32x2*)(a.R + (size_t)t * a.d + col);
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int j = 0; j < a.K; ++j) {
+      const f32x4 v = __builtin_bit_cast(f32x4, load16<true>(y, (uint32_t)((t * a.K + j) * a.d + col) * 4));
+      const float w = p.w[t * a.K + j];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) o[q] += w * v[q];
+    }
+    write_o(a, t, col, o, res, ok);
+  }
+}
+
+// a token's A from the slices of H, added in slice order: put(place in [K][n], four values)
+template <class Put>
+__device__ __forceinline__ void token_rows(const DecodeArgs& a, const Picked& p, int t, Put put) {
+  const int n = a.n, P = a.T * a.K, N = 2 * n;
+  const Rsrc h = buffer_of(a.H32, (uint32_t)a.ks * P * N * 4);
+  for (int i = threadIdx.x; i < a.K * n / 4; i += kDecodeThreads) {
+    const int j = i / (n / 4), c = 4 * (i % (n / 4));
+    f32x4 hg = f32x4{0.f, 0.f, 0.f, 0.f}, hu = hg;
+    if (a.b1) {
+      const float* b1 = a.b1 + (size_t)p.sel[t * a.K + j] * N + c;
+      hg = *(const f32x4*)b1;
+      hu = *(const f32x4*)(b1 + n);
+    }
+#pragma unroll 4
+    for (int q = 0; q < a.ks; ++q) {
+      const uint32_t o = (uint32_t)((q * P + t * a.K + j) * N + c) * 4;
+      const f32x4 vg = __builtin_bit_cast(f32x4, load16<true>(h, o)), vu = __builtin_bit_cast(f32x4, load16<true>(h, o + 4 * n));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        hg[r] += vg[r];
+        hu[r] += vu[r];
+      }
+    }
+    float v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float sg;
+      v[r] = silu_sig(hg[r], &sg) * hu[r];
+    }
+    put(j * n + c, v);
+  }
+}
+
+// Y of rows first .. first + rows of an item, from the column tiles (C4 times four columns) of
+// its waves' shares
+template <int C4, class Item, class Sum>
+__device__ __forceinline__ void store_y(const DecodeArgs& a, const Picked& p, const Item& t, int first, int rows, Sum sum) {
+  const int shares = kDecodeWaves / a.kw, per_row = C4 * shares;
+  for (int i = threadIdx.x; i < rows * per_row; i += kDecodeThreads) {
+    const int row = i / per_row, c = i % per_row, col = 4 * (t.tile * per_row + c);
+    if (col >= a.d) continue;
+    f32x4 y = sum(c / C4, row, c % C4);
+    if (a.b2) {
+      const f32x4 bias = *(const f32x4*)(a.b2 + (size_t)t.e * a.d + col);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] += bias[q];
+    }
+    store16_shared(buffer_of(a.Y, (uint32_t)a.T * a.K * a.d * 4), (uint32_t)(p.rows[t.r0 + first + row] * a.d + col) * 4,
+                   __builtin_bit_cast(u32x4, y));
+  }
+}
+
 // KB, MB: rows of a group in MB blocks of 16 / KB
 template <int KB, int MB>
 struct Decode {
@@ -372,27 +458,21 @@ struct Decode {
   static constexpr int RT = Tile::RT, CG = Tile::CG, COLS = Tile::COLS, C4 = COLS / 4;
   // steps in flight of a wave, within the registers
   static constexpr int NBUF = 2;
-  using Stream = RowStream<KB, NBUF, kDecodeWaves>;
+  using Stream = RowStream<KB, NBUF>;
+  using Part = typename Tile::Part;
+  static constexpr int UP_COLS = COLS / 2, DOWN_COLS = COLS, MAX_ROWS = RT * MB;
 
-  // f(B) with the row blocks that a group of cnt rows needs
-  template <class F>
-  static __device__ __forceinline__ void by_blocks(int cnt, F f) {
-    if constexpr (MB >= 2)
-      if (cnt > RT) return f(std::integral_constant<int, 2>{});
-    f(std::integral_constant<int, 1>{});
-  }
 
   // An item of a group: the up-projection of COLS / 2 gate columns and the matching up columns
-  // (a.ks > 1: of a slice of k), or the down-projection of COLS columns
+  // (a.ks > 1: of a slice of k), or the down-projection of COLS columns for every a.kw waves
   struct Item {
-    bool up;
     int gi, tile, slice, e, r0, cnt;  // (cnt: rows left, of which a pass takes RT MB)
   };
-  static __device__ __forceinline__ Item item_of(const DecodeArgs& a, const Picked& p, bool up, int i, int tiles) {
+  template <bool UP>
+  static __device__ __forceinline__ Item item_of(const DecodeArgs& a, const Picked& p, int i, int tiles) {
     Item t;
-    t.up = up;
-    t.slice = up ? i % a.ks : 0;
-    if (up) i /= a.ks;
+    t.slice = UP ? i % a.ks : 0;
+    if (UP) i /= a.ks;
     t.gi = i / tiles;
     t.tile = i % tiles;
     t.e = __builtin_amdgcn_readfirstlane(p.gexp[t.gi]);
@@ -400,24 +480,28 @@ struct Decode {
     t.cnt = __builtin_amdgcn_readfirstlane(p.goff[t.gi + 1]) - t.r0;
     return t;
   }
+  template <bool UP>
   static __device__ __forceinline__ void prime(const DecodeArgs& a, const Item& t, Stream& stream, int wave) {
     const int n = a.n, d = a.d, lane = opaque_lane();
     const uint32_t bytes = (uint32_t)n * d * 2;
-    if (t.up) {
+    if constexpr (UP) {
       const int c = t.tile * (COLS / 2) + 8 * (Tile::cg(lane) & (CG / 2 - 1));
       stream.prime(buffer_of(a.W1 + (size_t)t.e * n * d * 2, 2 * bytes), n * 4,
                    c < n ? 2 * (c + (Tile::cg(lane) >= CG / 2 ? n : 0)) : kBufferOut, t.slice * a.kslice,
-                   min(d, (t.slice + 1) * a.kslice), wave, lane);
+                   min(d, (t.slice + 1) * a.kslice), wave, kDecodeWaves, lane);
     } else {
-      stream.prime(buffer_of(a.W2 + (size_t)t.e * n * d, bytes), d * 2, 2 * (t.tile * COLS + 8 * Tile::cg(lane)), 0, n, wave, lane);
+      const int c = COLS * (t.tile * (kDecodeWaves / a.kw) + wave / a.kw) + 8 * Tile::cg(lane);
+      stream.prime(buffer_of(a.W2 + (size_t)t.e * n * d, bytes), d * 2, c < d ? 2 * c : kBufferOut, 0, n, wave % a.kw, a.kw, lane);
     }
   }
   // the rest of the product of a primed item, into A (or the slices of H) or Y
-  static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& stream,
-                                             typename Tile::Part* part, int wave) {
+  // (before(): called by every thread ahead of the first barrier)
+  template <bool UP, class Before>
+  static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& stream, Part* part,
+                                             int wave, Before before) {
     const int n = a.n, d = a.d, N = 2 * n, P = a.T * a.K, lane = opaque_lane();
-    by_blocks(t.cnt, [&](auto blocks) __attribute__((always_inline)) {
-      constexpr int B = decltype(blocks)::value;
+    {
+      constexpr int B = MB;  // (a path of its own for fewer rows spilled)
       uint32_t xoff[B];
       f32x4 acc[B][8];
       zero_acc(acc);
@@ -425,11 +509,10 @@ struct Decode {
       for (int b = 0; b < B; ++b) {
         const int r = RT * b + Tile::row(lane);
         const int i = r < t.cnt ? p.rows[t.r0 + r] : -1;
-        xoff[b] = i < 0 ? kBufferOut : t.up ? (uint32_t)(i / a.K) * d * 2 : (uint32_t)i * n * 2;
+        xoff[b] = i < 0 ? kBufferOut : UP ? (uint32_t)(i / a.K) * d * 2 : (uint32_t)i * n * 2;
       }
-      // (X too by the access that A needs: one copy of the loop)
-      const Rsrc rows_in = t.up ? buffer_of(a.X, (uint32_t)a.T * d * 2) : buffer_of(a.A, (uint32_t)P * n * 2);
-      stream.template add<true>(acc, rows_in, xoff);
+      stream.template add<!UP>(acc, UP ? buffer_of(a.X, (uint32_t)a.T * d * 2) : buffer_of(a.A, (uint32_t)P * n * 2), xoff);
+      before();
 #pragma unroll
       for (int b = 0; b < B; ++b) {
         if (RT * b >= t.cnt) break;
@@ -437,7 +520,7 @@ struct Decode {
         Tile::put(part[wave], acc[b], lane);
         __syncthreads();
         const int rows = min(RT, t.cnt - RT * b);
-        if (t.up && a.ks == 1) {
+        if (UP && a.ks == 1) {
           for (int i = threadIdx.x; i < rows * (C4 / 2); i += kDecodeThreads) {
             const int row = i / (C4 / 2), c4 = i % (C4 / 2), col = t.tile * (COLS / 2) + 4 * c4;
             if (col >= n) continue;
@@ -464,56 +547,19 @@ struct Decode {
           }
           continue;
         }
-        for (int i = threadIdx.x; i < rows * C4; i += kDecodeThreads) {
-          const int row = i / C4, c4 = i % C4, r = p.rows[t.r0 + RT * b + row];
-          f32x4 y = Tile::template sum<kDecodeWaves>(part, row, c4);
-          if (t.up) {
+        if constexpr (UP) {
+          for (int i = threadIdx.x; i < rows * C4; i += kDecodeThreads) {
+            const int row = i / C4, c4 = i % C4, r = p.rows[t.r0 + RT * b + row];
+            const f32x4 y = Tile::template sum<kDecodeWaves>(part, row, c4);
             const int col = t.tile * (COLS / 2) + 4 * (c4 % (C4 / 2));
             if (col < n)
               store16_shared(buffer_of(a.H32, (uint32_t)a.ks * P * N * 4),
                              (uint32_t)((t.slice * P + r) * N + col + (c4 < C4 / 2 ? 0 : n)) * 4, __builtin_bit_cast(u32x4, y));
-          } else {
-            const int col = t.tile * COLS + 4 * c4;
-            if (a.b2) {
-              const f32x4 bias = *(const f32x4*)(a.b2 + (size_t)t.e * d + col);
-#pragma unroll
-              for (int q = 0; q < 4; ++q) y[q] += bias[q];
-            }
-            store16_shared(buffer_of(a.Y, (uint32_t)P * d * 4), (uint32_t)(r * d + col) * 4, __builtin_bit_cast(u32x4, y));
           }
+          continue;
         }
+        store_y<C4>(a, p, t, RT * b, rows, [&](int sub, int row, int c4) { return Tile::sum_of(part + sub * a.kw, a.kw, row, c4); });
       }
-    });
-  }
-
-  static __device__ __forceinline__ void write_o(const DecodeArgs& a, int t, int col, f32x4 o, u32x2 r, bool ok) {
-    if (a.R) {
-      o[0] += bf_lo(r[0]);
-      o[1] += bf_hi(r[0]);
-      o[2] += bf_lo(r[1]);
-      o[3] += bf_hi(r[1]);
-    }
-    if (!ok) o = f32x4{NAN, NAN, NAN, NAN};
-    *(u32x2*)(a.O + (size_t)t * a.d + col) = pack_bf16x4(o[0], o[1], o[2], o[3]);
-  }
-
-  // O = R + sum of s Y over each token's entries, the columns of one down-projection tile
-  static __device__ __forceinline__ void sum_tokens(const DecodeArgs& a, const Picked& p, int tile, int t0, int tokens, bool ok) {
-    const Rsrc y = buffer_of(a.Y, (uint32_t)a.T * a.K * a.d * 4);
-    for (int i = threadIdx.x; i < tokens * C4; i += kDecodeThreads) {
-      const int t = t0 + i / C4, col = tile * COLS + 4 * (i % C4);
-      if (t >= a.T) break;
-      u32x2 res = {0, 0};
-      if (a.R) res = *(const u32x2*)(a.R + (size_t)t * a.d + col);
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-      for (int j = 0; j < a.K; ++j) {
-        const f32x4 v = __builtin_bit_cast(f32x4, load16<true>(y, (uint32_t)((t * a.K + j) * a.d + col) * 4));
-        const float w = p.w[t * a.K + j];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] += w * v[q];
-      }
-      write_o(a, t, col, o, res, ok);
     }
   }
 
@@ -521,8 +567,9 @@ struct Decode {
   // K n, a wave's step 32 KB k of one expert, whose product is weighted as it is added
   template <class Wait>
   static __device__ __forceinline__ void token_down(const DecodeArgs& a, const Picked& p, typename Tile::Part* part,
-                                                    uint16_t* rows, int wave, int t, int tile, Wait wait) {
+                                                    char* lds, int wave, int t, int tile, Wait wait) {
     constexpr int NB = 2;
+    uint16_t* rows = (uint16_t*)lds;  // [K][n] with slices of H
     const int n = a.n, d = a.d, spe = (n + Tile::KSTEP - 1) / Tile::KSTEP, steps = a.K * spe, lane = opaque_lane();
     const uint32_t wcol = 2 * (tile * COLS + 8 * Tile::cg(lane));
     u32x4 wv[NB][8];
@@ -561,35 +608,7 @@ struct Decode {
     }
     wait();
     if (a.ks > 1) {
-      // the token's A from the slices of H, added in slice order
-      const int P = a.T * a.K, N = 2 * n;
-      const Rsrc h = buffer_of(a.H32, (uint32_t)a.ks * P * N * 4);
-      for (int i = threadIdx.x; i < a.K * n / 4; i += kDecodeThreads) {
-        const int j = i / (n / 4), c = 4 * (i % (n / 4));
-        f32x4 hg = f32x4{0.f, 0.f, 0.f, 0.f}, hu = hg;
-        if (a.b1) {
-          const float* b1 = a.b1 + (size_t)p.sel[t * a.K + j] * N + c;
-          hg = *(const f32x4*)b1;
-          hu = *(const f32x4*)(b1 + n);
-        }
-#pragma unroll 4
-        for (int q = 0; q < a.ks; ++q) {
-          const uint32_t o = (uint32_t)((q * P + t * a.K + j) * N + c) * 4;
-          const f32x4 vg = __builtin_bit_cast(f32x4, load16<true>(h, o)), vu = __builtin_bit_cast(f32x4, load16<true>(h, o + 4 * n));
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            hg[r] += vg[r];
-            hu[r] += vu[r];
-          }
-        }
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float sg;
-          v[r] = silu_sig(hg[r], &sg) * hu[r];
-        }
-        *(u32x2*)(rows + j * n + c) = pack_bf16x4(v[0], v[1], v[2], v[3]);
-      }
+      token_rows(a, p, t, [&](int i, const float(&v)[4]) { *(u32x2*)(rows + i) = pack_bf16x4(v[0], v[1], v[2], v[3]); });
       __syncthreads();
     }
 #pragma unroll
@@ -641,14 +660,303 @@ struct Decode {
   }
 };
 
-constexpr int kSumTokens = 16;  // tokens of one item of the sums
+// The same with 8-bit weights (stream8_tile.h): a wave's step is one block of 128 k of 64 weight
+// columns, in the up-projection 32 gate columns and the matching up ones.  Rows are quantised
+// as they are loaded, X from bf16 and A from fp32.  EXACT: the up-projection's codes are
+// multiplied in bf16, with fp32 sums (as in the layer's 8-bit forward); the conversions bound it
+// where a workgroup has many items (32 tokens of a 30B-shaped layer: 206 us, 174 without).
+template <int MB, int NJ, bool EXACT>
+struct Decode8 {
+  static constexpr int NBUF = 1, UP_COLS = 8 * NJ, DOWN_COLS = 16 * NJ, MAX_ROWS = 16 * MB;
+  typedef Stream8Part<NJ> Part;
+  using Item = typename Decode<1, 1>::Item;
+  struct Stream {
+    Rsrc w;
+    const uint8_t* ws[2];
+    uint32_t row[NJ];
+    int kb, end, step;  // this wave's first block, the end, and from a block to the next
+    u32x4 wv[NBUF][NJ][2];
+    int sv[NBUF][2];
+    __device__ __forceinline__ void load(int buf, int s) {
+      const int b = min(kb + step * s, end - 1);  // (past the end: the last one again, unused)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        wv[buf][j][0] = load16(w, row[j] + kQBlock * b);
+        wv[buf][j][1] = load16(w, row[j] + kQBlock * b + 64);
+      }
+      sv[buf][0] = ws[0][b];
+      sv[buf][1] = ws[1][b];
+    }
+    __device__ __forceinline__ i32x8 frag(int buf, int j) const {
+      const u32x4 lo = wv[buf][j][0], hi = wv[buf][j][1];
+      return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    }
+  };
+  template <bool UP>
+  static __device__ __forceinline__ Item item_of(const DecodeArgs& a, const Picked& p, int i, int tiles) {
+    return Decode<1, 1>::template item_of<UP>(a, p, i, tiles);
+  }
+  template <bool UP>
+  static __device__ __forceinline__ void prime(const DecodeArgs& a, const Item& t, Stream& s, int wave) {
+    const int lane = opaque_lane(), g = lane >> 4, l = lane & 15, d = a.d, n = a.n;
+    int c0 = 0;
+    if constexpr (UP) {
+      s.w = buffer_of(a.W1q + (size_t)t.e * w1q_bytes(d, n), (uint32_t)w1q_bytes(d, n));
+      const uint8_t* ws = a.W1s + (size_t)t.e * w1s_bytes(d, n) + (size_t)(2 * (UP_COLS * t.tile / kQBlock)) * q_stride(d / kQBlock);
+      s.ws[0] = ws;
+      s.ws[1] = ws + q_stride(d / kQBlock);
+      s.kb = t.slice * (a.kslice / kQBlock) + wave;
+      s.end = min(d, (t.slice + 1) * a.kslice) / kQBlock;
+      s.step = kDecodeWaves;
+    } else {
+      s.w = buffer_of(a.W2q + (size_t)t.e * w2q_bytes(d, n), (uint32_t)w2q_bytes(d, n));
+      // (past the last column: the last tile's again, not stored)
+      c0 = min(DOWN_COLS * (t.tile * (kDecodeWaves / a.kw) + wave / a.kw), d - DOWN_COLS);
+      s.ws[0] = s.ws[1] = a.W2s + (size_t)t.e * w2s_bytes(d, n) + (size_t)(c0 / kQBlock) * q_stride(q_blocks(n));
+      s.kb = wave % a.kw;
+      s.step = a.kw;
+      s.end = q_blocks(n);
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = 16 * j + l, col = UP_COLS * t.tile + c % UP_COLS;
+      s.row[j] = 16 * g + (UP ? (uint32_t)(256 * (col / kQBlock) + w1q_row(col % kQBlock, c / UP_COLS)) * d
+                                : (uint32_t)(c0 + c) * q_pad(n));
+    }
+#pragma unroll
+    for (int q = 0; q < NBUF; ++q) s.load(q, q);
+  }
+  // the values of a row's block of 128 that a lane holds: 16 from k on and 16 from k + 64 on
+  template <bool F32>
+  static __device__ __forceinline__ void load_row(RowBlock8<F32>& x, Rsrc r, uint32_t off, int k, int len) {
+    constexpr int N = RowBlock8<F32>::N, ES = F32 ? 4 : 2;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int kk = k + (i >= N / 2 ? 64 : 0);
+      x.v[i] = load16<F32>(r, kk < len ? off + (uint32_t)kk * ES + 16 * (i % (N / 2)) : kBufferOut);
+    }
+  }
+  template <int B, bool F32>
+  static __device__ __forceinline__ void add(const DecodeArgs& a, Stream& s, f32x4 (&acc)[B][NJ], Rsrc r, const uint32_t (&xoff)[B],
+                                             int len, int lane) {
+    const int g = lane >> 4, ns = (s.end - s.kb + s.step - 1) / s.step;
+    if (ns <= 0) return;
+    RowBlock8<F32> xv[NBUF][B];
+    auto load_x = [&](int q, int i) {
+#pragma unroll
+      for (int b = 0; b < B; ++b) load_row(xv[q][b], r, xoff[b], kQBlock * (s.kb + s.step * i) + 16 * g, len);
+    };
+#pragma unroll
+    for (int q = 0; q < NBUF; ++q) load_x(q, q);
+    for (int i = 0;; i += NBUF) {
+#pragma unroll
+      for (int q = 0; q < NBUF; ++q) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+          int xs;
+          const i32x8 x = xv[q][b].codes(&xs);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const int ws = s.sv[q][2 * j / NJ];
+            if constexpr (EXACT && !F32) {
+              f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int h = 0; h < 4; ++h)
+                y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_bf16(s.frag(q, j), h, 1.f), codes_bf16(x, h, 1.f), y, 0, 0, 0);
+#pragma unroll
+              for (int h = 0; h < 4; ++h) acc[b][j][h] += ldexpf(y[h], ws + xs - 254);
+            } else {
+              acc[b][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(s.frag(q, j), x, acc[b][j], 0, 0, 0, ws, 0, xs);
+            }
+          }
+        }
+        if (i + q + 1 >= ns) return;
+        __builtin_amdgcn_sched_barrier(0);  // (not ahead of the products: it would take registers of their own)
+        s.load(q, i + q + NBUF);
+        load_x(q, i + q + NBUF);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  template <bool UP, class Before>
+  static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& s, Part* part, int wave,
+                                             Before before) {
+    const int cnt = min(t.cnt, MAX_ROWS);
+    auto go = [&](auto blocks) __attribute__((always_inline)) {
+      constexpr int B = decltype(blocks)::value;
+      const int n = a.n, d = a.d, N = 2 * n, P = a.T * a.K, lane = opaque_lane(), g = lane >> 4, l = lane & 15;
+      uint32_t xoff[B];
+      f32x4 acc[B][NJ];
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        // (a lane past the rows reads the last one's again)
+        const int i = p.rows[t.r0 + min(16 * b + l, cnt - 1)];
+        xoff[b] = UP ? (uint32_t)(i / a.K) * d * 2 : (uint32_t)i * n * 4;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      add<B, !UP>(a, s, acc, UP ? buffer_of(a.X, (uint32_t)a.T * d * 2) : buffer_of(a.A32, (uint32_t)P * n * 4), xoff, UP ? d : n, lane);
+      before();
+#pragma unroll
+      for (int b = 0; b < B; ++b) {
+        if (16 * b >= cnt) break;
+        if (b) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) part[wave][l][4 * j + g] = acc[b][j];
+        __syncthreads();
+        const int rows = min(16, cnt - 16 * b);
+        constexpr int C4 = 4 * NJ;
+        if (UP && a.ks == 1) {
+          for (int i = threadIdx.x; i < rows * (C4 / 2); i += kDecodeThreads) {
+            const int row = i / (C4 / 2), c4 = i % (C4 / 2), col = UP_COLS * t.tile + 4 * c4;
+            f32x4 hg = stream8_sum<kDecodeWaves, NJ>(part, row, c4), hu = stream8_sum<kDecodeWaves, NJ>(part, row, c4 + C4 / 2), v;
+            const float* b1 = a.b1 ? a.b1 + (size_t)t.e * N + col : nullptr;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (b1) {
+                hg[q] += b1[q];
+                hu[q] += b1[n + q];
+              }
+              float sg;
+              v[q] = silu_sig(hg[q], &sg) * hu[q];
+            }
+            store16_shared(buffer_of(a.A32, (uint32_t)P * n * 4), (uint32_t)(p.rows[t.r0 + 16 * b + row] * n + col) * 4,
+                           __builtin_bit_cast(u32x4, v));
+          }
+          continue;
+        }
+        if constexpr (UP) {
+          for (int i = threadIdx.x; i < rows * C4; i += kDecodeThreads) {
+            const int row = i / C4, c4 = i % C4, r = p.rows[t.r0 + 16 * b + row];
+            const f32x4 y = stream8_sum<kDecodeWaves, NJ>(part, row, c4);
+            const int col = UP_COLS * t.tile + 4 * (c4 % (C4 / 2));
+            store16_shared(buffer_of(a.H32, (uint32_t)a.ks * P * N * 4),
+                           (uint32_t)((t.slice * P + r) * N + col + (c4 < C4 / 2 ? 0 : n)) * 4, __builtin_bit_cast(u32x4, y));
+          }
+          continue;
+        }
+        store_y<C4>(a, p, t, 16 * b, rows, [&](int sub, int row, int c4) {
+          f32x4 y = part[sub * a.kw][row][c4];
+          for (int w = 1; w < a.kw; ++w)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] += part[sub * a.kw + w][row][c4][q];
+          return y;
+        });
+      }
+    };
+    go(std::integral_constant<int, MB>{});
+  }
 
-template <int KB, int MB, bool BY_TOKEN>
+  // by token: 32 columns, a wave's step one block of one entry, weighted as it is added
+  struct Token {
+    static constexpr int COLS = 32, C4 = COLS / 4;
+    typedef f32x4 Part[C4];
+    template <class Wait>
+    static __device__ __forceinline__ void token_down(const DecodeArgs& a, const Picked& p, Part* part, char* lds, int wave, int t,
+                                                      int tile, Wait wait) {
+      constexpr int NB = 2, J = 2;
+      const int n = a.n, d = a.d, blocks = q_blocks(n), steps = a.K * blocks, ns = (steps - wave + kDecodeWaves - 1) / kDecodeWaves;
+      const int lane = opaque_lane(), g = lane >> 4, l = lane & 15;
+      float* rows = (float*)lds;  // [K][n] with slices of H
+      u32x4 wv[NB][J][2];
+      int sv[NB];
+      auto at = [&](int s) { return min(wave + kDecodeWaves * s, steps - 1); };
+      auto load_w = [&](int q, int s) {
+        const int i = at(s), kb = i % blocks, e = __builtin_amdgcn_readfirstlane(p.sel[t * a.K + i / blocks]);
+        const uint8_t* w = a.W2q + (size_t)e * w2q_bytes(d, n) + 16 * g + kQBlock * kb;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const uint8_t* row = w + (size_t)(COLS * tile + 16 * j + l) * q_pad(n);
+          wv[q][j][0] = *(const u32x4*)row;
+          wv[q][j][1] = *(const u32x4*)(row + 64);
+        }
+        sv[q] = (a.W2s + (size_t)e * w2s_bytes(d, n) + (size_t)(COLS * tile / kQBlock) * q_stride(blocks))[kb];
+      };
+#pragma unroll
+      for (int q = 0; q < NB; ++q) load_w(q, q);
+      // what else the end needs
+      const int col = tile * COLS + 4 * threadIdx.x;
+      u32x2 res = {0, 0};
+      f32x4 bias = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (threadIdx.x < C4) {
+        if (a.R) res = *(const u32x2*)(a.R + (size_t)t * d + col);
+        if (a.b2)
+          for (int j = 0; j < a.K; ++j) {
+            const f32x4 v = *(const f32x4*)(a.b2 + (size_t)p.sel[t * a.K + j] * d + col);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) bias[q] += p.w[t * a.K + j] * v[q];
+          }
+      }
+      wait();
+      if (a.ks > 1) {
+        token_rows(a, p, t, [&](int i, const float(&v)[4]) { *(f32x4*)(rows + i) = f32x4{v[0], v[1], v[2], v[3]}; });
+        __syncthreads();
+      }
+      f32x4 acc[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const Rsrc x = buffer_of(a.A32, (uint32_t)a.T * a.K * n * 4);
+      auto run = [&]() __attribute__((always_inline)) {
+        if (ns <= 0) return;
+        for (int s = 0;; s += NB) {
+#pragma unroll
+          for (int q = 0; q < NB; ++q) {
+            const int i = at(s + q), kb = i % blocks, j0 = i / blocks, k = kQBlock * kb + 16 * g;
+            RowBlock8<true> xv;
+            if (a.ks > 1) {
+#pragma unroll
+              for (int h = 0; h < 8; ++h) {
+                const int kk = k + (h >= 4 ? 64 : 0);
+                xv.v[h] = kk < n ? *(const u32x4*)(rows + j0 * n + kk + 4 * (h % 4)) : u32x4{0, 0, 0, 0};
+              }
+            } else {
+              load_row(xv, x, (uint32_t)(t * a.K + j0) * n * 4, k, n);
+            }
+            int xs;
+            const i32x8 c = xv.codes(&xs);
+            const float sw = p.w[t * a.K + j0];
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+              const u32x4 lo = wv[q][j][0], hi = wv[q][j][1];
+              const i32x8 wf = {(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+              const f32x4 y = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, c, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, sv[q], 0, xs);
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[j][r] += sw * y[r];
+            }
+            if (s + q + 1 >= ns) return;
+            load_w(q, s + q + NB);
+          }
+        }
+      };
+      run();
+      if (l == 0)  // (all 16 rows of the product are this one)
+#pragma unroll
+        for (int j = 0; j < J; ++j) part[wave][4 * j + g] = acc[j];
+      __syncthreads();
+      if (threadIdx.x < C4 * kDecodeWaves) {
+        const int c4 = threadIdx.x % C4, w = threadIdx.x / C4;
+        f32x4 o = part[w][c4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+          for (int i = C4; i < C4 * kDecodeWaves; i *= 2) o[q] += __shfl_xor(o[q], i, kWave);
+          o[q] += bias[q];
+        }
+        if (threadIdx.x < C4) write_o(a, t, col, o, res, wait.ok());
+      }
+    }
+  };
+};
+
+// tokens of one item of the sums
+__host__ __device__ inline int sum_tokens_of(int cols) { return 4096 / cols; }
+
+// D: Decode or Decode8; TD: its down-projection by token
+template <class D, class TD, bool BY_TOKEN>
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeArgs a) {
-  using D = Decode<KB, MB>;
-  using TD = Decode<4, 1>;  // by token
-  extern __shared__ __attribute__((aligned(16))) char dyn[];  // picked_bytes
-  __shared__ typename D::Tile::Part part[kDecodeWaves];
+  extern __shared__ __attribute__((aligned(16))) char dyn[];  // picked_bytes, and a token's rows
+  __shared__ typename D::Part part[kDecodeWaves];
+  static_assert(sizeof(typename TD::Part) <= sizeof(typename D::Part), "the partial sums' area");
   __shared__ int sh[2];
   __shared__ int scan_lds[kDecodeWaves];
   const Picked p = picked_at(dyn, a.T, a.E, a.K);
@@ -674,51 +982,55 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
     }
     item -= selects;
     ok = await([&](int l) { return l == 0 ? select_counter(a) : nullptr; }, selects, sh + 1);
-    read_selection(a, p);
+    read_selection(a, p, ok);
   }
   const int groups = __builtin_amdgcn_readfirstlane(form_groups(a, p, scan_lds));
-  const int up_tiles = (a.n + D::COLS / 2 - 1) / (D::COLS / 2), down_tiles = a.d / (BY_TOKEN ? TD::COLS : D::COLS);
+  const int up_tiles = (a.n + D::UP_COLS - 1) / D::UP_COLS, down_cols = BY_TOKEN ? TD::COLS : D::DOWN_COLS * (kDecodeWaves / a.kw);
+  const int down_tiles = (a.d + down_cols - 1) / down_cols, sum_rows = sum_tokens_of(down_cols);
   const int per_group = up_tiles * a.ks, ups = groups * per_group, downs = (BY_TOKEN ? a.T : groups) * down_tiles;
-  const int sums = BY_TOKEN ? 0 : down_tiles * ((a.T + kSumTokens - 1) / kSumTokens);
+  const int sums = BY_TOKEN ? 0 : down_tiles * ((a.T + sum_rows - 1) / sum_rows);
   const int total = ups + downs + sums;
   // Where every item has a workgroup, no one asks for a second ticket (each costs 11 ns of all
   // the others' time).  Else the next ticket is asked for before an item's work, and the next
   // item's first weights between this one's stores and its count.
   const bool more = selects || total > (int)gridDim.x;
-  typename D::Stream stream;
-  typename D::Item t;
   const int last = BY_TOKEN ? ups : ups + downs;  // of the items of groups
-  auto start = [&]() __attribute__((always_inline)) {
-    if (item < last) {
-      t = D::item_of(a, p, item < ups, item < ups ? item : item - ups, item < ups ? up_tiles : down_tiles);
-      D::prime(a, t, stream, wave);
+  // the items [.., end) of one kind, from item - from on
+  auto kind = [&](auto up_c, int from, int end) __attribute__((always_inline)) {
+    constexpr bool UP = decltype(up_c)::value;
+    if (item >= end) return;
+    typename D::Stream stream;
+    typename D::Item t = D::template item_of<UP>(a, p, item - from, UP ? up_tiles : down_tiles);
+    D::template prime<UP>(a, t, stream, wave);
+    for (;;) {
+      int next = 0;
+      if (more && threadIdx.x == 0) next = take_ticket(a);
+      int* counter = !UP ? tile_counter(a, t.tile) : BY_TOKEN ? ups_counter(a, item) : group_counter(a, t.gi);
+      if constexpr (!UP) ok = await([&](int l) { return l == 0 ? group_counter(a, t.gi) : nullptr; }, per_group, sh + 1) && ok;
+      while (t.cnt > D::MAX_ROWS) {  // (more rows than a pass takes: the weights again)
+        D::template run<UP>(a, p, t, stream, part, wave, []() {});
+        t.r0 += D::MAX_ROWS;
+        t.cnt -= D::MAX_ROWS;
+        D::template prime<UP>(a, t, stream, wave);
+        __syncthreads();
+      }
+      D::template run<UP>(a, p, t, stream, part, wave, [&]() {
+        if (more && threadIdx.x == 0) sh[0] = next;
+      });
+      item = more ? __builtin_amdgcn_readfirstlane(sh[0]) - selects : total;
+      asm volatile("" ::: "memory");
+      if (!ok) counter = ups_counter(a, 8);  // (what gave up is not counted, so that nothing is summed from it)
+      if (item >= end) {
+        finish_item<0>(counter);
+        return;
+      }
+      t = D::template item_of<UP>(a, p, item - from, UP ? up_tiles : down_tiles);
+      D::template prime<UP>(a, t, stream, wave);
+      finish_item<8 * D::NBUF>(counter);
     }
   };
-  start();
-  while (item < last) {
-    int next = 0;
-    if (more && threadIdx.x == 0) next = take_ticket(a);
-    int* counter = BY_TOKEN ? ups_counter(a, item) : t.up ? group_counter(a, t.gi) : tile_counter(a, t.tile);
-    if (!t.up) ok = await([&](int l) { return l == 0 ? group_counter(a, t.gi) : nullptr; }, per_group, sh + 1) && ok;
-    if (more && threadIdx.x == 0) sh[0] = next;
-    while (MB > 1 && t.cnt > D::RT * MB) {  // (more rows than a pass takes: the weights again)
-      D::run(a, p, t, stream, part, wave);
-      t.r0 += D::RT * MB;
-      t.cnt -= D::RT * MB;
-      D::prime(a, t, stream, wave);
-      __syncthreads();
-    }
-    D::run(a, p, t, stream, part, wave);  // (has a barrier after which sh is read)
-    item = more ? __builtin_amdgcn_readfirstlane(sh[0]) - selects : total;
-    asm volatile("" ::: "memory");
-    if (!ok) counter = ups_counter(a, 8);  // (what gave up is not counted, so that nothing is summed from it)
-    if (item < last) {
-      start();
-      finish_item<8 * D::NBUF>(counter);
-    } else {
-      finish_item<0>(counter);
-    }
-  }
+  kind(std::true_type{}, 0, ups);
+  if constexpr (!BY_TOKEN) kind(std::false_type{}, ups, last);
   while (item < total) {
     const int i = item - last, tile = i % down_tiles;
     if constexpr (BY_TOKEN) {
@@ -730,11 +1042,10 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
         }
         __device__ bool ok() const { return *all; }
       } wait{a, ups, sh + 1, &ok};
-      TD::token_down(a, p, (typename TD::Tile::Part*)part, (uint16_t*)(dyn + picked_bytes(a.T, a.E, a.K)), wave, i / down_tiles,
-                     tile, wait);
+      TD::token_down(a, p, (typename TD::Part*)part, dyn + picked_bytes(a.T, a.E, a.K), wave, i / down_tiles, tile, wait);
     } else {
       ok = await([&](int l) { return l == 0 ? tile_counter(a, tile) : nullptr; }, groups, sh + 1) && ok;
-      D::sum_tokens(a, p, tile, i / down_tiles * kSumTokens, kSumTokens, ok);
+      sum_tokens(a, p, down_cols, tile, i / down_tiles * sum_rows, sum_rows, ok);
     }
     if (!more) break;
     if (threadIdx.x == 0) sh[0] = take_ticket(a);
@@ -756,9 +1067,10 @@ size_t decode_sync_words(int T, int d, int E, int K) { return (size_t)kLine * (1
 // whether the down-projection goes by token: where few entries repeat experts, whose weights are
 // then read again, and the items are one round; then the slices of k
 static bool decode_by_token(int T, int d, int E, int K) { return T == 1 || (2 * T * K <= E && T * (d / 32) <= 256); }
-int decode_ks(int T, int d, int n, int E, int K) {
+int decode_ks(int T, int d, int n, int E, int K, bool q8) {
   if (!decode_by_token(T, d, E, K) || K * n > 8192) return 1;
-  return std::max(1, std::min({128 / (T * K * ((n + 63) / 64)), d / 256, 8}));
+  const int items = T * K * ((n + 63) / 64) * (q8 ? 2 : 1);
+  return std::max(1, std::min({(q8 ? 256 : 128) / items, q8 ? (d + 1023) / 1024 : d / 256, 8}));
 }
 
 template <int KB, int MB>
@@ -770,25 +1082,41 @@ static hipError_t run_router(const DecodeArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int KB, int MB, bool BY_TOKEN>
+template <class D, class TD, bool BY_TOKEN>
 static hipError_t run_decode(const DecodeArgs& a, hipStream_t s) {
-  using D = Decode<KB, MB>;
-  const int64_t groups = std::min(a.T * a.K, a.E), down_tiles = a.d / (BY_TOKEN ? Decode<4, 1>::COLS : D::COLS);
-  int64_t items = groups * ((a.n + D::COLS / 2 - 1) / (D::COLS / 2)) * a.ks;
-  items += BY_TOKEN ? a.T * down_tiles : (groups + (a.T + kSumTokens - 1) / kSumTokens) * down_tiles;
-  const size_t lds = picked_bytes(a.T, a.E, a.K) + (a.ks > 1 ? 2 * (size_t)a.K * a.n : 0);
-  decode_kernel<KB, MB, BY_TOKEN><<<(int)std::min<int64_t>(items, 256), kDecodeThreads, lds, s>>>(a);
+  const int down_cols = BY_TOKEN ? TD::COLS : D::DOWN_COLS * (kDecodeWaves / a.kw), sum_rows = sum_tokens_of(down_cols);
+  const int64_t groups = std::min(a.T * a.K, a.E), down_tiles = (a.d + down_cols - 1) / down_cols;
+  int64_t items = groups * ((a.n + D::UP_COLS - 1) / D::UP_COLS) * a.ks;
+  items += BY_TOKEN ? a.T * down_tiles : (groups + (a.T + sum_rows - 1) / sum_rows) * down_tiles;
+  const size_t lds = picked_bytes(a.T, a.E, a.K) + (a.ks > 1 ? (a.W1q ? 4 : 2) * (size_t)a.K * a.n : 0);
+  decode_kernel<D, TD, BY_TOKEN><<<(int)std::min<int64_t>(items, 256), kDecodeThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
+  const bool q8 = a.W1q != nullptr, by_token = decode_by_token(a.T, a.d, a.E, a.K);
+  const int unit = q8 ? kQBlock : 32;  // of a slice
   a.slices = decode_slices(a.T, a.d, a.E);
-  a.ks = decode_ks(a.T, a.d, a.n, a.E, a.K);
-  a.kslice = (a.d / 32 + a.ks - 1) / a.ks * 32;
+  a.ks = decode_ks(a.T, a.d, a.n, a.E, a.K, q8);
+  a.kslice = (a.d / unit + a.ks - 1) / a.ks * unit;
+  // waves of a down-projection column tile: two steps each, where there are as many
+  const int steps = q8 ? q_blocks(a.n) : a.n / 32;
+  a.kw = 1;
+  while (2 * a.kw <= kDecodeWaves && 4 * a.kw <= steps) a.kw *= 2;
   const hipError_t e = run_router<1, 1>(a, s);
   if (e != hipSuccess) return e;
-  if (decode_by_token(a.T, a.d, a.E, a.K)) return run_decode<1, 1, true>(a, s);
-  return a.T <= 16 ? run_decode<1, 1, false>(a, s) : run_decode<1, 2, false>(a, s);
+  // one row block where a group seldom has more than its 16 rows
+  const bool one = a.T <= 16 || a.T * a.K <= 6 * a.E;
+  using Q1 = Decode8<1, 4, true>;
+  using B1 = Decode<1, 1>;
+  using BT = Decode<4, 1>;
+  if (q8) {
+    if (by_token) return run_decode<Q1, Q1::Token, true>(a, s);
+    if (a.T * a.K <= 16) return run_decode<Q1, Q1::Token, false>(a, s);
+    return one ? run_decode<Decode8<1, 8, false>, Q1::Token, false>(a, s) : run_decode<Decode8<2, 4, false>, Q1::Token, false>(a, s);
+  }
+  if (by_token) return run_decode<B1, BT, true>(a, s);
+  return one ? run_decode<B1, BT, false>(a, s) : run_decode<Decode<1, 2>, BT, false>(a, s);
 }
 
 }  // namespace smoe

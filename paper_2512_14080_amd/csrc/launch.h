@@ -269,10 +269,13 @@ struct DecodeArgs {
   float* Y;       // [T K][d]
   float* H32;     // [ks][T K][2n], where k is sliced (ks > 1)
   int T, d, n, E, K;
-  int slices = 0, ks = 0, kslice = 0;  // (set by launch_decode)
+  // 8-bit weights (then W1, W2 and A are null)
+  const uint8_t* W1q = nullptr; const uint8_t* W1s = nullptr; const uint8_t* W2q = nullptr; const uint8_t* W2s = nullptr;
+  float* A32 = nullptr;  // [T K][n]
+  int slices = 0, ks = 0, kslice = 0, kw = 0;  // (set by launch_decode)
 };
 int decode_slices(int T, int d, int E);
-int decode_ks(int T, int d, int n, int E, int K);
+int decode_ks(int T, int d, int n, int E, int K, bool q8);
 size_t decode_sync_words(int T, int d, int E, int K);
 hipError_t launch_decode(DecodeArgs a, hipStream_t s);
 

@@ -92,8 +92,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void linear_few_kernel(const Linear
   const int kbeg = blockIdx.y * slice, kend = min(a.k, kbeg + slice);
   const int c = GATED ? c0 + 8 * (Tile::cg(lane) & (CG / 2 - 1)) : c0 + 8 * Tile::cg(lane);
   const uint32_t wcol = c < n ? 2 * (c + (GATED && Tile::cg(lane) >= CG / 2 ? n : 0)) : kBufferOut;
-  RowStream<KB, MB == 4 ? 1 : 2, kFewWaves8> stream;
-  stream.prime(buffer_of(a.W, (uint32_t)a.k * N * 2), N * 2, wcol, kbeg, kend, wave, lane);
+  RowStream<KB, MB == 4 ? 1 : 2> stream;
+  stream.prime(buffer_of(a.W, (uint32_t)a.k * N * 2), N * 2, wcol, kbeg, kend, wave, kFewWaves8, lane);
   uint32_t xoff[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) {

@@ -227,24 +227,25 @@ size_t quant_layout(const moe_dims& m, int64_t cap, char* base, QuantWs* w) {
   return off;
 }
 
-// moe_decode (and moe_decode_quant): the counters, partial logits, A and Y
+// moe_decode and moe_decode_quant: the counters, partial logits, the selection, A (in fp32 for
+// the 8-bit one), Y and the slices of H
 struct DecodeWs {
   int32_t* sync;
   float* part;
   uint32_t* picked;
-  uint16_t* A;
+  void* A;
   float* Y;
   float* H32;
 };
-size_t decode_layout(const moe_dims& m, char* base, DecodeWs* w) {
+size_t decode_layout(const moe_dims& m, bool q8, char* base, DecodeWs* w) {
   const size_t P = (size_t)m.T * m.K;
   size_t off = 0;
   off = carve(base, off, smoe::decode_sync_words(m.T, m.d, m.E, m.K) * 4, w ? (void**)&w->sync : nullptr);
   off = carve(base, off, (size_t)smoe::decode_slices(m.T, m.d, m.E) * m.T * m.E * 4, w ? (void**)&w->part : nullptr);
   off = carve(base, off, P * 8, w ? (void**)&w->picked : nullptr);
-  off = carve(base, off, P * m.n * 2, w ? (void**)&w->A : nullptr);
+  off = carve(base, off, P * m.n * (q8 ? 4 : 2), w ? &w->A : nullptr);
   off = carve(base, off, P * m.d * 4, w ? (void**)&w->Y : nullptr);
-  const int ks = smoe::decode_ks(m.T, m.d, m.n, m.E, m.K);
+  const int ks = smoe::decode_ks(m.T, m.d, m.n, m.E, m.K, q8);
   off = carve(base, off, ks > 1 ? ks * P * m.n * 8 : 0, w ? (void**)&w->H32 : nullptr);
   return off;
 }
@@ -257,7 +258,7 @@ int check_decode(const moe_dims& m) {
   if (m.E > smoe::kDecodeExperts) return fail(MOE_ERR_UNSUPPORTED, "E must be at most %d (got %d)", smoe::kDecodeExperts, m.E);
   // (32-bit byte offsets within an expert's weights, W_r and the rows)
   const int64_t most = INT32_MAX;
-  if (4 * (int64_t)m.d * m.n > most || 2 * (int64_t)m.d * m.E > most || 2 * (int64_t)m.T * m.d > most || 4 * (int64_t)m.T * m.K * m.n > most)
+  if (4 * (int64_t)m.d * m.n > most || 2 * (int64_t)m.d * m.E > most || 2 * (int64_t)m.T * m.d > most || 8 * (int64_t)m.T * m.K * m.n > most || 4 * (int64_t)m.T * m.K * m.d > most)
     return fail(MOE_ERR_UNSUPPORTED, "d = %d, n = %d: an expert's projection, W_r and the rows must be below 2^31 bytes each", m.d, m.n);
   return MOE_OK;
 }
@@ -479,7 +480,8 @@ size_t moe_workspace_bytes(moe_dims dims, int32_t capacity, int which) {
   if (which == MOE_WS_FWD_QUANT) return quant_layout(dims, capacity, nullptr, nullptr);
   if (which == MOE_WS_FWD_CKPT) return fwd_layout(dims, capacity, nullptr, nullptr);
   if (which == MOE_WS_BWD_CKPT) return bwd_ckpt_layout(dims, capacity, nullptr, nullptr, nullptr);
-  if (which == MOE_WS_DECODE) return check_decode(dims) == MOE_OK ? decode_layout(dims, nullptr, nullptr) : 0;
+  if (which == MOE_WS_DECODE) return check_decode(dims) == MOE_OK ? decode_layout(dims, false, nullptr, nullptr) : 0;
+  if (which == MOE_WS_DECODE_QUANT) return check_decode(dims) == MOE_OK ? decode_layout(dims, true, nullptr, nullptr) : 0;
   return 0;
 }
 
@@ -1016,34 +1018,66 @@ int moe_bwd_ckpt(moe_dims m, const moe_bf16* dO, const moe_bf16* X, const moe_ck
   return backward(m, dO, X, nullptr, c, W1, W2, eb, Wr, r, dX, dW1, dW2, dWr, dbias, dS, ws, ws_bytes, stream);
 }
 
-int moe_decode(moe_dims m, const moe_bf16* X, const moe_bf16* Wr, const float* bias, const moe_bf16* W1, const moe_bf16* W2,
-               const moe_expert_bias* eb, const moe_bf16* R, moe_bf16* O, int32_t* topk_idx, float* topk_w, void* ws,
-               size_t ws_bytes, void* stream_) {
-  int rc = check_decode(m);
-  if (rc) return rc;
+// whether [p, p + n) and [q, q + m) share a byte
+static bool overlap(const void* p, size_t n, const void* q, size_t m) {
+  const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+  return p && q && a < b + m && b < a + n;
+}
+
+// moe_decode and moe_decode_quant: what they check alike, and the launches
+static int decode(const moe_dims& m, const moe_bf16* X, const moe_bf16* Wr, const float* bias, const moe_bf16* W1,
+                  const moe_bf16* W2, const moe_qexperts* q, const moe_expert_bias* eb, const moe_bf16* R, moe_bf16* O,
+                  int32_t* topk_idx, float* topk_w, void* ws, size_t ws_bytes, hipStream_t stream) {
   CHECK_PTR(X, 16);
   CHECK_PTR(Wr, 16);
-  CHECK_PTR(W1, 16);
-  CHECK_PTR(W2, 16);
+  if (!q) {
+    CHECK_PTR(W1, 16);
+    CHECK_PTR(W2, 16);
+  }
   CHECK_PTR(O, 16);
   if (!aligned(R, 16)) return fail(MOE_ERR_INVALID_ARG, "R must be 16-byte aligned");
   if (!aligned(bias, 4)) return fail(MOE_ERR_INVALID_ARG, "bias must be 4-byte aligned");
   if (!aligned(topk_idx, 4)) return fail(MOE_ERR_INVALID_ARG, "topk_idx must be 4-byte aligned");
   if (!aligned(topk_w, 4)) return fail(MOE_ERR_INVALID_ARG, "topk_w must be 4-byte aligned");
-  rc = check_expert_bias(eb);
+  const size_t rows = (size_t)m.T * m.d * 2;
+  if (overlap(O, rows, X, rows)) return fail(MOE_ERR_INVALID_ARG, "O must not overlap X, which is read until the end");
+  if (R != O && overlap(O, rows, R, rows)) return fail(MOE_ERR_INVALID_ARG, "R must be O itself or not overlap it");
+  int rc = check_expert_bias(eb);
   if (rc) return rc;
-  const size_t need = decode_layout(m, nullptr, nullptr);
+  const size_t need = decode_layout(m, q, nullptr, nullptr);
   if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < required %zu", ws_bytes, need);
   CHECK_PTR(ws, kAlign);
   DecodeWs w;
-  decode_layout(m, (char*)ws, &w);
-  hipStream_t stream = (hipStream_t)stream_;
-  LAUNCH(MOE_KC_DECODE,
-         smoe::launch_decode({X, Wr, bias, W1, W2, eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, R, O, topk_idx, topk_w, w.part,
-                              w.sync, w.picked, w.A, w.Y, w.H32, m.T, m.d, m.n, m.E, m.K},
-                             stream),
-         "layer of few tokens");
+  decode_layout(m, q, (char*)ws, &w);
+  smoe::DecodeArgs a{X, Wr, bias, W1, W2, eb ? eb->b1 : nullptr, eb ? eb->b2 : nullptr, R, O, topk_idx, topk_w, w.part,
+                     w.sync, w.picked, q ? nullptr : (uint16_t*)w.A, w.Y, w.H32, m.T, m.d, m.n, m.E, m.K};
+  if (q) {
+    a.W1q = q->W1;
+    a.W1s = q->W1s;
+    a.W2q = q->W2;
+    a.W2s = q->W2s;
+    a.A32 = (float*)w.A;
+  }
+  LAUNCH(MOE_KC_DECODE, smoe::launch_decode(a, stream), "layer of few tokens");
   return MOE_OK;
+}
+
+int moe_decode(moe_dims m, const moe_bf16* X, const moe_bf16* Wr, const float* bias, const moe_bf16* W1, const moe_bf16* W2,
+               const moe_expert_bias* eb, const moe_bf16* R, moe_bf16* O, int32_t* topk_idx, float* topk_w, void* ws,
+               size_t ws_bytes, void* stream) {
+  int rc = check_decode(m);
+  if (rc) return rc;
+  return decode(m, X, Wr, bias, W1, W2, nullptr, eb, R, O, topk_idx, topk_w, ws, ws_bytes, (hipStream_t)stream);
+}
+
+int moe_decode_quant(moe_dims m, const moe_bf16* X, const moe_bf16* Wr, const float* bias, const moe_qexperts* q,
+                     const moe_expert_bias* eb, const moe_bf16* R, moe_bf16* O, int32_t* topk_idx, float* topk_w, void* ws,
+                     size_t ws_bytes, void* stream) {
+  int rc = check_decode(m);
+  if (rc) return rc;
+  rc = check_qexperts(m, q, true);
+  if (rc) return rc;
+  return decode(m, X, Wr, bias, nullptr, nullptr, q, eb, R, O, topk_idx, topk_w, ws, ws_bytes, (hipStream_t)stream);
 }
 
 // ---------------------------------------------------------------- dense products

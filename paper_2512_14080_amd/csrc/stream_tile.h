@@ -86,7 +86,18 @@ struct RowTile {
       for (int h = 0; h < 2; ++h)
         part[kk(lane)][(4 * g + r) % RT][h][cg(lane)] = f32x4{acc[4 * h][r], acc[4 * h + 1][r], acc[4 * h + 2][r], acc[4 * h + 3][r]};
   }
-  // the sum over the waves and k blocks of columns 4 c4 .. 4 c4 + 3, in a fixed order
+  // the sum over kw waves and the k blocks of columns 4 c4 .. 4 c4 + 3, in a fixed order
+  static __device__ __forceinline__ f32x4 sum_of(const Part* part, int kw, int row, int c4) {
+    f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < kw; ++w)
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        const f32x4 v = part[w][b][row][c4 & 1][c4 >> 1];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) s[q] += v[q];
+      }
+    return s;
+  }
   template <int KW>
   static __device__ __forceinline__ f32x4 sum(const Part* part, int row, int c4) {
     f32x4 s = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -110,32 +121,33 @@ __device__ __forceinline__ void zero_acc(f32x4 (&acc)[MB][8]) {
     for (int j = 0; j < 8; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 }
 
-// A wave's share of a reduction: steps wave, wave + KW, ... of k in [kbeg, kend), NBUF of
+// A wave's share of a reduction: steps wave, wave + kw, ... of k in [kbeg, kend), NBUF of
 // them in flight.  w: the matrix, with ldw bytes from a k row to the next and the lane's
 // column at byte wcol (kBufferOut: none); x: the rows, xoff the byte of k = 0 of the lane's
 // row (kBufferOut: none).  prime() requests the first steps' weights (8 NBUF loads, always),
 // add() the rest; SHARED: the rows are other workgroups' of this launch.
-template <int KB, int NBUF, int KW>
+template <int KB, int NBUF>
 struct RowStream {
   using Tile = RowTile<KB>;
   Rsrc w;
   uint32_t ldw, wcol;
-  int kl, kend, ns;
+  int kl, kend, ns, step;
   u32x4 wv[NBUF][8];
 
   __device__ __forceinline__ void load_w(int buf, int s) {
-    const int k = kl + Tile::KSTEP * KW * s;
+    const int k = kl + step * s;
     const uint32_t o = k < kend ? wcol + (uint32_t)k * ldw : kBufferOut;
 #pragma unroll
     for (int i = 0; i < 8; ++i) wv[buf][i] = load16(w, o + i * ldw);
   }
   __device__ __forceinline__ void prime(Rsrc w_, uint32_t ldw_, uint32_t wcol_, int kbeg, int kend_, int wave,
-                                        int lane) {
+                                        int kw, int lane) {
     w = w_;
     ldw = ldw_;
     wcol = wcol_;
     kend = kend_;
-    ns = ((kend - kbeg + Tile::KSTEP - 1) / Tile::KSTEP - wave + KW - 1) / KW;
+    step = Tile::KSTEP * kw;
+    ns = (kend - kbeg - Tile::KSTEP * wave + step - 1) / step;
     kl = kbeg + Tile::k0(lane) + Tile::KSTEP * wave;
     // (a wave without a step requests nothing: its k is past the end)
 #pragma unroll
@@ -146,7 +158,7 @@ struct RowStream {
     if (ns <= 0) return;
     bf16x8 xv[NBUF][MB];
     auto load_x = [&](int buf, int s) {
-      const int k = kl + Tile::KSTEP * KW * s;
+      const int k = kl + step * s;
 #pragma unroll
       for (int b = 0; b < MB; ++b)
         xv[buf][b] = __builtin_bit_cast(bf16x8, load16<SHARED>(x_, k < kend ? xoff[b] + 2 * (uint32_t)k : kBufferOut));
@@ -164,8 +176,10 @@ struct RowStream {
             acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[q][b], wf, acc[b][j], 0, 0, 0);
         }
         if (s + q + 1 >= ns) return;
+        __builtin_amdgcn_sched_barrier(0);  // (not ahead of the products: it would take registers of their own)
         load_w(q, s + q + NBUF);
         load_x(q, s + q + NBUF);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
