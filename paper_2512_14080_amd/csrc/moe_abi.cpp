@@ -5,6 +5,7 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -1097,6 +1098,18 @@ static int check_linear(moe_linear& l) {
   }
   return MOE_OK;
 }
+// bytes of T rows of `cols` bf16 that are `ld` apart
+static size_t rows_bytes(int64_t T, int64_t cols, int64_t ld) { return 2 * (size_t)((T - 1) * ld + cols); }
+struct Region {
+  const char* name;
+  const void* p;
+  size_t bytes;
+};
+static int check_overlap(const Region& out, std::initializer_list<Region> others) {
+  for (const Region& r : others)
+    if (overlap(out.p, out.bytes, r.p, r.bytes)) return fail(MOE_ERR_INVALID_ARG, "%s must not overlap %s", out.name, r.name);
+  return MOE_OK;
+}
 static int64_t linear_columns(const moe_linear& l) { return l.act == MOE_ACT_SWIGLU ? 2 * (int64_t)l.n : l.n; }
 
 namespace {
@@ -1135,6 +1148,15 @@ int moe_linear_fwd(moe_linear l, const moe_bf16* X, const moe_bf16* W, const flo
   if (!aligned(b, 16)) return fail(MOE_ERR_INVALID_ARG, "b must be 16-byte aligned");
   if (!aligned(R, 16)) return fail(MOE_ERR_INVALID_ARG, "R must be 16-byte aligned");
   if (!aligned(H, 16)) return fail(MOE_ERR_INVALID_ARG, "H must be 16-byte aligned");
+  const int64_t N = linear_columns(l);
+  const Region x{"X", X, rows_bytes(l.T, l.k, l.ldx)}, wr{"W", W, 2 * (size_t)l.k * N}, bb{"b", b, 4 * (size_t)N};
+  const Region h{"H", H, 2 * (size_t)l.T * N}, y{"Y", Y, rows_bytes(l.T, l.n, l.ldy)};
+  const bool in_place = R == Y && l.ldr == l.ldy;
+  const Region r{"R (unless it is Y, with ldr = ldy)", in_place ? nullptr : R, rows_bytes(l.T, l.n, l.ldr)};
+  rc = check_overlap(y, {x, wr, bb, h, r});
+  if (rc) return rc;
+  rc = check_overlap(h, {x, wr, bb, r});
+  if (rc) return rc;
   const size_t need = moe_linear_workspace_bytes(l, MOE_WS_LINEAR_FWD);
   if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < required %zu", ws_bytes, need);
   CHECK_PTR(ws, kAlign);
@@ -1158,6 +1180,16 @@ int moe_linear_bwd(moe_linear l, const moe_bf16* dY, const moe_bf16* X, const mo
   if (!aligned(dW, 16)) return fail(MOE_ERR_INVALID_ARG, "dW must be 16-byte aligned");
   if (!aligned(db, 16)) return fail(MOE_ERR_INVALID_ARG, "db must be 16-byte aligned");
   if (!dX && !dW && !db) return fail(MOE_ERR_INVALID_ARG, "dX, dW and db must not all be null");
+  const int64_t N = linear_columns(l);
+  const Region dy{"dY", dY, rows_bytes(l.T, l.n, l.ldy)}, x{"X", X, rows_bytes(l.T, l.k, l.ldx)}, wr{"W", W, 2 * (size_t)l.k * N};
+  const Region h{"H", H, 2 * (size_t)l.T * N}, g{"G (unless it is dX)", G == dX ? nullptr : G, rows_bytes(l.T, l.k, l.ldx)};
+  const Region dx{"dX", dX, rows_bytes(l.T, l.k, l.ldx)}, dw{"dW", dW, 2 * (size_t)l.k * N}, b{"db", db, 4 * (size_t)N};
+  rc = check_overlap(dx, {dy, x, wr, h, g, dw, b});
+  if (rc) return rc;
+  rc = check_overlap(dw, {dy, x, wr, h, g, b});
+  if (rc) return rc;
+  rc = check_overlap(b, {dy, x, wr, h, g});
+  if (rc) return rc;
   const size_t need = moe_linear_workspace_bytes(l, MOE_WS_LINEAR_BWD);
   if (ws_bytes < need) return fail(MOE_ERR_WORKSPACE, "workspace %zu < required %zu", ws_bytes, need);
   CHECK_PTR(ws, kAlign);

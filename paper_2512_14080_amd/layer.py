@@ -1,4 +1,5 @@
-"""Device buffers for one MoE layer and the call sequence route -> round -> fwd -> bwd.
+"""Device buffers for one MoE layer and the call sequence route -> round -> fwd -> bwd (or decode), and for a shared
+expert beside it.
 
 Allocation (torch) and argument marshalling only; the work happens in the
 library's kernels through the C ABI.
@@ -102,6 +103,7 @@ class DeviceLayer:
         self.db1 = torch.empty((E, 2 * n), dtype=f32, device=device) if b1 is not None else None
         self.db2 = torch.empty((E, d), dtype=f32, device=device) if b2 is not None else None
         self.eb = B.expert_bias(self.b1, self.b2, self.db1, self.db2)
+        self.ws_d = None  # of decode, at its first call
 
     @property
     def routing(self):
@@ -141,3 +143,61 @@ class DeviceLayer:
     def rows(self) -> int:
         """P, the number of routed rows (reads the device offsets)."""
         return int(self.routing.arrays()["offsets"][-1].item())
+
+    def decode(self, R=None, stream=None, topk_idx=None, topk_w=None):
+        """The forward of a few tokens (T <= MOE_DECODE_MAX_T) in one call, routing included: O = R + the layer's output.
+        Token choice only, on the 8-bit weights with held8="quant" (quantise them first: quantize_experts)."""
+        if self.round_mode:
+            raise ValueError("decode routes by token choice: round_mode must be None")
+        if self.ws_d is None:
+            which = B.MOE_WS_DECODE_QUANT if self.qw is not None else B.MOE_WS_DECODE
+            nbytes = B.moe_workspace_bytes(self.D, self.T * self.K, which)
+            self.ws_d = _aligned_empty(nbytes, self.X.device)
+        if self.qw is not None:
+            B.moe_decode_quant(self.D, self.X, self.Wr, self.bias, self.qw, R, self.O, self.ws_d, topk_idx, topk_w,
+                               stream, eb=self.eb)
+        else:
+            B.moe_decode(self.D, self.X, self.Wr, self.bias, self.W1, self.W2, R, self.O, self.ws_d, topk_idx, topk_w,
+                         stream, eb=self.eb)
+
+    def quantize_experts(self, stream=None):
+        B.moe_quantize_experts(self.D, self.W1, self.W2, self.qw, stream)
+
+
+class SharedExpert:
+    """A dense SwiGLU expert that every token passes through, beside the routed ones:
+    Y = R + (SiLU(X Wu_gate) * X Wu_up) Wd, with Wu [d,2m] (gate columns first) and Wd [m,d] in bf16 and optional fp32
+    biases [2m] and [d].  ``train`` keeps what the backward reads."""
+
+    def __init__(self, T, Wu, Wd, bu=None, bd=None, train=False):
+        import torch
+        d, m = Wu.shape[0], Wd.shape[0]
+        if Wu.shape != (d, 2 * m) or Wd.shape != (m, d):
+            raise ValueError(f"Wu must be [d, 2m] and Wd [m, d] (got {tuple(Wu.shape)}, {tuple(Wd.shape)})")
+        self.Wu, self.Wd, self.bu, self.bd = Wu, Wd, bu, bd
+        self.up, self.down = B.linear_dims(T, d, m, "swiglu"), B.linear_dims(T, m, d)
+        dev, bf16, f32 = Wu.device, torch.bfloat16, torch.float32
+
+        def workspace(which):
+            sizes = (B.moe_linear_workspace_bytes(L, which) for L in (self.up, self.down))
+            return _aligned_empty(max(sizes), dev)
+
+        def like(t):
+            return None if t is None else torch.empty_like(t)
+
+        self.A = torch.empty((T, m), dtype=bf16, device=dev)
+        self.ws_f = workspace(B.MOE_WS_LINEAR_FWD)
+        self.H = None
+        if train:
+            self.H = torch.empty((T, 2 * m), dtype=bf16, device=dev)
+            self.dA, self.ws_b = torch.empty_like(self.A), workspace(B.MOE_WS_LINEAR_BWD)
+            self.dWu, self.dWd, self.dbu, self.dbd = like(Wu), like(Wd), like(bu), like(bd)
+
+    def forward(self, X, Y, R=None, stream=None):
+        B.moe_linear_fwd(self.up, X, self.Wu, self.bu, None, self.H, self.A, self.ws_f, stream)
+        B.moe_linear_fwd(self.down, self.A, self.Wd, self.bd, R, None, Y, self.ws_f, stream)
+
+    def backward(self, dY, X, dX, G=None, stream=None):
+        """dX = the gradient through this expert + G (which may be dX itself), and dWu, dWd, dbu, dbd."""
+        B.moe_linear_bwd(self.down, dY, self.A, self.Wd, None, None, self.dA, self.dWd, self.dbd, self.ws_b, stream)
+        B.moe_linear_bwd(self.up, self.dA, X, self.Wu, self.H, G, dX, self.dWu, self.dbu, self.ws_b, stream)
