@@ -287,6 +287,7 @@ struct LinearArgs {
   float* part;  // linear_fwd_part_bytes
   int T, k, n, act;
   int64_t ldx, ldr, ldy;  // elements from a row to the next
+  int col0 = 0, cols = 0;  // (tiles: the output columns of a launch)
 };
 size_t linear_fwd_part_bytes(int T, int k, int n, int act, int64_t ldx);
 hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t s);

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void linear_few_kernel(const Linear
   const int kbeg = blockIdx.y * slice, kend = min(a.k, kbeg + slice);
   const int c = GATED ? c0 + 8 * (Tile::cg(lane) & (CG / 2 - 1)) : c0 + 8 * Tile::cg(lane);
   const uint32_t wcol = c < n ? 2 * (c + (GATED && Tile::cg(lane) >= CG / 2 ? n : 0)) : kBufferOut;
-  RowStream<KB, MB == 4 ? 1 : 2> stream;
+  RowStream<KB, 2> stream;
   stream.prime(buffer_of(a.W, (uint32_t)a.k * N * 2), N * 2, wcol, kbeg, kend, wave, kFewWaves8, lane);
   uint32_t xoff[MB];
 #pragma unroll
@@ -211,7 +211,8 @@ __device__ __forceinline__ bool dense_tile(int M, int N, int K, int splits, int 
   return true;
 }
 
-// PART: fp32 partial sums of a k chunk to a.part, else the epilogue
+// The output columns [col0, col0 + cols).  PART: fp32 partial sums of a k chunk to a.part, else
+// the epilogue
 // (the activation is a constant: a choice among them in the unrolled epilogue kept the
 // accumulators out of the registers)
 template <class Cfg_, int ACT, bool TAIL, bool PART>
@@ -233,33 +234,33 @@ struct OpLinear {
       return q < Wn / 2 ? c0 + w * (Wn / 2) + q : n + c0 + w * (Wn / 2) + (q - Wn / 2);
     }
   };
-  static __device__ int columns(const Params& p) { return GATED ? 2 * p.a.n : p.a.n; }
+  static __device__ int columns(const Params& p) { return GATED ? 2 * p.a.n : p.a.n; }  // of W
   // (GATED: tiles of BN / 2 gate columns, counted as BN of twice the columns of whole tiles)
   static __device__ int tile_columns(const Params& p) {
-    return GATED ? (p.a.n + Cfg::BN / 2 - 1) / (Cfg::BN / 2) * Cfg::BN : p.a.n;
+    return GATED ? (p.a.cols + Cfg::BN / 2 - 1) / (Cfg::BN / 2) * Cfg::BN : p.a.cols;
   }
   static __device__ int count(const Params& p, int*) {
     return p.splits * ((p.a.T + Cfg::BM - 1) / Cfg::BM) * ((tile_columns(p) + Cfg::BN - 1) / Cfg::BN);
   }
   static __device__ bool tile(const Params& p, int id, TileInfo& ti, int*) {
     const bool ok = dense_tile<Cfg>(p.a.T, tile_columns(p), p.a.k, p.splits, p.chunk, id, ti);
-    if (GATED && (ti.n0 + Cfg::BN) / 2 > p.a.n) ti.ncols = 0;  // (not a full tile)
+    if (GATED && (ti.n0 + Cfg::BN) / 2 > p.a.cols) ti.ncols = 0;  // (not a full tile)
     return ok;
   }
-  static __device__ int first_col(const TileInfo& ti) { return GATED ? ti.n0 / 2 : ti.n0; }
+  static __device__ int first_col(const Params& p, const TileInfo& ti) { return p.a.col0 + (GATED ? ti.n0 / 2 : ti.n0); }
   template <class Side>
   static __device__ void init_m(const Params& p, const TileInfo& ti, Side& s) {
     s.init(p.a.X + ti.k_begin, p.a.ldx, nullptr, ti.row_base, ti.mrows);
     if constexpr (TAIL) s.k_len = ti.k_len;
   }
   static __device__ void init_n(const Params& p, const TileInfo& ti, KOuterSide<Cfg::BN, Cfg::BK, Cfg::NW>& s) {
-    s.init(p.a.W, columns(p), nullptr, ti.k_begin, ti.k_len, columns(p), ColMap{first_col(ti), p.a.n});
+    s.init(p.a.W, columns(p), nullptr, ti.k_begin, ti.k_len, columns(p), ColMap{first_col(p, ti), p.a.n});
   }
   static __device__ void epilogue(const Params& p, const TileInfo& ti, Acc<Cfg>& t, char* epi) {
     const LinearArgs& a = p.a;
-    const int n = a.n, N = columns(p), wn = t.wave_n(), lane = epilogue_lane();
+    const int n = a.n, end = a.col0 + a.cols, N = columns(p), wn = t.wave_n(), lane = epilogue_lane();
     const int wm0 = Cfg::wave_m(threadIdx.x >> 6) * (Cfg::BM / Cfg::WM);
-    const int c0 = first_col(ti) + wn * (GATED ? Wn / 2 : Wn);  // this wave's first output column
+    const int c0 = first_col(p, ti) + wn * (GATED ? Wn / 2 : Wn);  // this wave's first output column
     if constexpr (PART) {
 #pragma unroll
       for (int i = 0; i < Cfg::RM; ++i) {
@@ -271,7 +272,7 @@ struct OpLinear {
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int c = c0 + 32 * (j % RC) + 8 * g + 4 * (lane >> 5);
-            if (c >= n) continue;
+            if (c >= end) continue;
             f32x4 v;
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] = t.acc[i][j][4 * g + q];
@@ -286,7 +287,7 @@ struct OpLinear {
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int c = c0 + 32 * (j % RC) + 8 * g + 4 * (lane >> 5);
-          if (c >= n) continue;
+          if (c >= end) continue;
           const f32x4 b = *(const f32x4*)(a.b + c + (j >= RC ? n : 0));
 #pragma unroll
           for (int i = 0; i < Cfg::RM; ++i)
@@ -311,7 +312,7 @@ struct OpLinear {
       auto values = [&](int jj, u32x2(&v)[4]) {
         u32x2 r[4] = {};
         const int col = c0 + 32 * jj;
-        if (a.R) load_cols(a.R + row * a.ldr, col, n, r);
+        if (a.R) load_cols(a.R + row * a.ldr, col, end, r);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           float y[4];
@@ -336,7 +337,7 @@ struct OpLinear {
 #pragma unroll
         for (int jj = 0; jj < RC; jj += 2) {
           const int col = c0 + 32 * jj;
-          if (col >= n) continue;
+          if (col >= end) continue;
           u32x2 v[4];
           if (a.H) {
 #pragma unroll
@@ -345,31 +346,31 @@ struct OpLinear {
               stage_block32(st, 0, v);
               pack(jj + 1 + half * RC, v);
               stage_block32(st, 1, v);
-              store_staged_cols(st, a.H + r0 * N + half * n, N, ti.mrows - m0, col, n);
+              store_staged_cols(st, a.H + r0 * N + half * n, N, ti.mrows - m0, col, end);
             }
           }
           values(jj, v);
           stage_block32(st, 0, v);
           values(jj + 1, v);
           stage_block32(st, 1, v);
-          store_staged_cols(st, a.Y + r0 * a.ldy, a.ldy, ti.mrows - m0, col, n);
+          store_staged_cols(st, a.Y + r0 * a.ldy, a.ldy, ti.mrows - m0, col, end);
         }
       } else {
 #pragma unroll
         for (int jj = 0; jj < RC; ++jj) {
           const int col = c0 + 32 * jj;
-          if (col >= n) continue;
+          if (col >= end) continue;
           u32x2 v[4];
           if (a.H) {
             pack(jj, v);
-            if (m < ti.mrows) store_cols(a.H + row * N, col, n, v);
+            if (m < ti.mrows) store_cols(a.H + row * N, col, end, v);
             if constexpr (GATED) {
               pack(jj + RC, v);
-              if (m < ti.mrows) store_cols(a.H + row * N + n, col, n, v);
+              if (m < ti.mrows) store_cols(a.H + row * N + n, col, end, v);
             }
           }
           values(jj, v);
-          if (m < ti.mrows) store_cols(a.Y + row * a.ldy, col, n, v);
+          if (m < ti.mrows) store_cols(a.Y + row * a.ldy, col, end, v);
         }
       }
     }
@@ -391,7 +392,7 @@ struct OpLinearDX {
   static __device__ void init_m(const Params& p, const TileInfo& ti, Side& s) { Fwd::init_m(p, ti, s); }
   template <class Side>
   static __device__ void init_n(const Params& p, const TileInfo& ti, Side& s) {
-    s.init(p.a.W + ti.k_begin, p.a.k, nullptr, ti.n0, ti.ncols);
+    s.init(p.a.W + ti.k_begin, p.a.k, nullptr, p.a.col0 + ti.n0, ti.ncols);
     if constexpr (TAIL) s.k_len = ti.k_len;
   }
   static __device__ void epilogue(const Params& p, const TileInfo& ti, Acc<Cfg>& t, char* epi) {
@@ -462,18 +463,19 @@ struct OpLinearDW {
 };
 
 // ---------------------------------------------------------------- dP and db
-// A workgroup takes 256 columns (32 threads of 8) of kDpRows rows; dP is formed where the
+// A workgroup takes 256 columns (32 threads of 8) of `rows` rows; dP is formed where the
 // product has an activation, and the column sums of the rows in fp32, from the values before
-// their rounding.  grid: column blocks of the (gate's) columns x, row chunks y
-constexpr int kDpRows = 64;
+// their rounding.  grid: `blocks` column blocks of the (gate's) columns for each row chunk
 template <bool GATED>
-__global__ __launch_bounds__(256) void linear_dp_kernel(const LinearBwdArgs a, float* __restrict__ sums) {
-  const int c = threadIdx.x & 31, rl = threadIdx.x >> 5, col = 256 * blockIdx.x + 8 * c;
+__global__ __launch_bounds__(256) void linear_dp_kernel(const LinearBwdArgs a, int blocks, int rows, float* __restrict__ sums) {
+  const int chunk = blockIdx.x / blocks, first = 256 * (blockIdx.x - chunk * blocks);
+  const int c = threadIdx.x & 31, rl = threadIdx.x >> 5, col = first + 8 * c;
   const int n = a.n, N = GATED ? 2 * n : n;
-  const int64_t t0 = (int64_t)blockIdx.y * kDpRows;
+  const int64_t t0 = (int64_t)chunk * rows;
   float s[GATED ? 2 : 1][8] = {};
   if (col < n)
-    for (int r = rl; r < kDpRows && t0 + r < a.T; r += 8) {
+#pragma unroll 2
+    for (int r = rl; r < rows && t0 + r < a.T; r += 8) {
       const size_t t = t0 + r;
       const u32x4 y = *(const u32x4*)(a.dY + t * a.ldy + col);
       float d[8], e[8];
@@ -520,14 +522,14 @@ __global__ __launch_bounds__(256) void linear_dp_kernel(const LinearBwdArgs a, f
 #pragma unroll
     for (int q = 0; q < 8; ++q) lds[rl][h][8 * c + q] = s[h][q];
   __syncthreads();
-  const int out = 256 * blockIdx.x + threadIdx.x;
+  const int out = first + threadIdx.x;
   if (out >= n) return;
 #pragma unroll
   for (int h = 0; h < (GATED ? 2 : 1); ++h) {
     float v = 0.f;
 #pragma unroll
     for (int r = 0; r < 8; ++r) v += lds[r][h][threadIdx.x];
-    sums[(size_t)blockIdx.y * N + h * n + out] = v;
+    sums[(size_t)chunk * N + h * n + out] = v;
   }
 }
 
@@ -569,48 +571,66 @@ __global__ __launch_bounds__(256) void linear_sums_kernel(const float* __restric
 using L256x256 = GemmCfg<256, 256, 4, 2, 2>;           // 64 x 128 a wave
 using L256x128 = GemmCfg<256, 128, 4, 2, 3>;
 using L128x128 = GemmCfg<128, 128, 4, 2, 2, kBK, 2>;   // two workgroups to a CU
+using L128x128d = GemmCfg<128, 128, 4, 2, 4>;          // one, three stages ahead
 using D256x256 = GemmCfg<256, 256, 2, 4, 2>;
 using D128x128 = GemmCfg<128, 128, 4, 2, 2, kBK, 2>;
+using D128x128d = GemmCfg<128, 128, 4, 2, 4>;
 
 constexpr int kLinearMaxSlices = 16;
 constexpr size_t kSlabBytes = (size_t)256 << 20;
-
-// Forward (and dX): M x N outputs over K.  few: streaming, with kb k blocks of a step and mb
-// row blocks; else tiles of bm x bn.  slices: of K, whose partial sums are joined.
-struct LinearPlan { bool few; int kb, mb, bm, bn, slices, chunk; };
+constexpr int kCus = 256;  // (a size of workspaces: not the device's own count)
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// rows of a workgroup of linear_dp_kernel: 64, fewer where that leaves CUs idle
+static int dp_rows(int T, int64_t N) {
+  int rows = 64;
+  while (rows > 8 && ceil_div(T, rows) * ceil_div(N, 256) < 4 * kCus) rows /= 2;
+  return rows;
+}
 
-static LinearPlan tiled_plan(int64_t M, int64_t N, int64_t K) {
-  // rounds over the CUs times a tile's time for a k step (relative), and what the join
-  // of slices reads
-  struct Shape { int bm, bn, occ, step; };
-  static const Shape shapes[] = {{256, 256, 1, 100}, {256, 128, 1, 60}, {128, 128, 2, 72}};
-  LinearPlan best{false, 0, 0, 256, 256, 1, (int)K};
-  double least = 0;
-  const int64_t cus = 256;
+// Forward (and dX): M x N outputs over K.  few: streaming, with kb k blocks of a step and mb
+// row blocks; else tiles of bm x bn.  slices: of K, whose partial sums are joined.  deep: three
+// stages of loads ahead of the products, where a workgroup has its CU to itself.
+struct LinearPlan { bool few; int kb, mb, bm, bn; bool deep; int slices, chunk; double cost; };
+
+// Rounds over the CUs times a tile's time for a k step, in 17 ns (a 256 x 256 tile: 100), and what
+// the join of slices costs: a launch, and its reading.
+static LinearPlan tiled_plan(int64_t M, int64_t N, int64_t K, int most_slices = kLinearMaxSlices) {
+  struct Shape { int bm, bn; bool deep; int slots, step; };
+  static const Shape shapes[] = {{256, 256, false, kCus, 100}, {256, 128, false, kCus, 60}, {128, 128, false, 2 * kCus, 72},
+                                 {128, 128, true, kCus, 36}};
+  LinearPlan best{};
   for (const Shape& t : shapes) {
     const int64_t tiles = ceil_div(M, t.bm) * ceil_div(N, t.bn);
-    for (int slices = 1; slices <= kLinearMaxSlices; slices *= 2) {
+    for (int slices = 1; slices <= most_slices; slices *= 2) {
       if (slices > 1 && (K < 512 * slices || (int64_t)slices * M * N * 4 > (int64_t)kSlabBytes)) break;
-      const int64_t wgs = tiles * slices, steps = ceil_div(ceil_div(K, slices), kBK);
-      // (a workgroup that has its CU to itself is faster than one of two, not twice)
-      const double round = t.occ == 2 && wgs <= cus ? 0.6 * t.step : t.step;
-      double cost = ceil_div(wgs, cus * t.occ) * (double)round * (steps + 4);
-      if (slices > 1) cost += 700 + slices * M * N * 4 / 40e3;  // (a launch; 4 TB/s)
-      if (least == 0 || cost < 0.97 * least) {
-        best = {false, 0, 0, t.bm, t.bn, slices, (int)(ceil_div(steps, 1) * kBK)};
-        least = cost;
-      }
+      const int64_t steps = ceil_div(ceil_div(K, slices), kBK);
+      double cost = ceil_div(tiles * slices, t.slots) * (double)t.step * (steps + 4);
+      if (slices > 1) cost += 250 + slices * M * N * 4 / 70e3;
+      if (best.cost == 0 || cost < 0.97 * best.cost)
+        best = {false, 0, 0, t.bm, t.bn, t.deep, slices, slices == 1 ? (int)K : (int)(steps * kBK), cost};
     }
   }
-  if (best.slices == 1) best.chunk = (int)K;
+  best.slices = (int)ceil_div(K, best.chunk);
   return best;
+}
+// The columns that whole rounds of 256 x 256 tiles take, where the others are better off in a
+// launch of their own (T = 1777, k = 4096, n = 14336 gated: 784 tiles are 3 rounds and 16 more);
+// 0: all in one.
+static int64_t whole_rounds(int64_t M, int64_t N, int64_t K, const LinearPlan& all) {
+  if (all.bn != 256 || all.slices > 1) return 0;
+  const int64_t mt = ceil_div(M, 256), nt = ceil_div(N, 256), rounds = mt * nt / kCus;
+  if (rounds == 0 || mt * nt % kCus == 0) return 0;
+  const int64_t cols = rounds * kCus / mt * 256;
+  if (cols == 0 || cols >= N) return 0;
+  const LinearPlan rest = tiled_plan(M, N - cols, K, 1);  // (no partial sums for a part of the columns)
+  return rounds * 100. * (ceil_div(K, kBK) + 4) + rest.cost + 200 < 0.97 * all.cost ? cols : 0;
 }
 
 static LinearPlan forward_plan(int T, int k, int n, int act, int64_t ldx) {
   const int64_t N = act == MOE_ACT_SWIGLU ? 2 * (int64_t)n : n;
-  if (T > 64 || (int64_t)k * N * 2 > INT32_MAX || (T * ldx + k) * 2 > INT32_MAX) return tiled_plan(T, N, k);
+  // (four row blocks cost registers: T = 64, k = 4096, n = 14336 33 us, in tiles 29; k = 3328, n = 3840 15.3, 13.2)
+  if (T > 32 || (int64_t)k * N * 2 > INT32_MAX || (T * ldx + k) * 2 > INT32_MAX) return tiled_plan(T, N, k);
   // narrower tiles for fewer rows, while that gives up to a workgroup to two CUs
   int kb = 1;
   while (kb < 4 && 16 / (2 * kb) >= T && ceil_div(N, 128 / kb) < 128) kb *= 2;
@@ -620,28 +640,29 @@ static LinearPlan forward_plan(int T, int k, int n, int act, int64_t ldx) {
   while (2 * slices * tiles <= 256 && 2 * slices <= kLinearMaxSlices && k / slices * (256 / kb) > 256 * 1024) slices *= 2;
   const int chunk = (int)ceil_div(ceil_div(k, slices), 128) * 128;
   slices = (int)ceil_div(k, chunk);
-  return {true, kb, T <= 16 ? 1 : T <= 32 ? 2 : 4, 0, 0, slices, chunk};
+  return {true, kb, T <= 16 ? 1 : 2, 0, 0, false, slices, chunk, 0};
 }
 
 static LinearPlan dx_plan(int T, int k, int64_t N) { return tiled_plan(T, k, N); }
-struct DwPlan { int bm, splits, chunk; };
+struct DwPlan { int bm; bool deep; int splits, chunk; };
 static DwPlan dw_plan(int T, int64_t k, int64_t N) {
-  DwPlan best{256, 1, T};
+  struct Shape { int bm; bool deep; int slots, step; };
+  static const Shape shapes[] = {{256, false, kCus, 100}, {128, false, 2 * kCus, 72}, {128, true, kCus, 38}};
+  DwPlan best{};
   double least = 0;
-  for (const int bm : {256, 128}) {
-    const int64_t tiles = ceil_div(k, bm) * ceil_div(N, bm), slots = bm == 256 ? 256 : 512;
-    for (int splits = 1; splits <= kLinearMaxSlices; splits *= 2) {
-      if (splits > 1 && (T < 512 * splits || splits * k * N * 4 > (int64_t)kSlabBytes)) break;
+  for (const Shape& t : shapes) {
+    const int64_t tiles = ceil_div(k, t.bm) * ceil_div(N, t.bm);
+    for (int splits = 1; splits <= 2 * kLinearMaxSlices; ++splits) {
+      if (splits > 1 && (T < 256 * splits || splits * k * N * 4 > (int64_t)kSlabBytes)) break;
       const int64_t steps = ceil_div(ceil_div(T, splits), kBK);
-      double cost = ceil_div(tiles * splits, slots) * (bm == 256 ? 100. : tiles * splits <= 256 ? 40. : 72.) * (steps + 5);
-      if (splits > 1) cost += 700 + splits * k * N * 4 / 40e3;
+      double cost = ceil_div(tiles * splits, t.slots) * (double)t.step * (steps + 5);
+      if (splits > 1) cost += 250 + splits * k * N * 4 / 70e3;
       if (least == 0 || cost < 0.97 * least) {
-        best = {bm, splits, (int)(steps * kBK)};
+        best = {t.bm, t.deep, splits, splits == 1 ? T : (int)(steps * kBK)};
         least = cost;
       }
     }
   }
-  if (best.splits == 1) best.chunk = T;
   best.splits = (int)ceil_div(T, best.chunk);
   return best;
 }
@@ -658,7 +679,7 @@ size_t linear_dw_part_bytes(int T, int k, int64_t N) {
   const DwPlan p = dw_plan(T, k, N);
   return p.splits > 1 ? (size_t)p.splits * k * N * 4 : 0;
 }
-size_t linear_db_part_bytes(int T, int64_t N) { return (size_t)ceil_div(T, kDpRows) * N * 4; }
+size_t linear_db_part_bytes(int T, int64_t N) { return (size_t)ceil_div(T, dp_rows(T, N)) * N * 4; }
 
 template <bool GATED>
 static hipError_t join(const LinearArgs& a, int slices, hipStream_t s) {
@@ -681,10 +702,8 @@ static hipError_t few_rows(const LinearArgs& a, const LinearPlan& p, hipStream_t
     e = run_few<GATED, 2, 1>(a, p, s);
   else if (p.mb == 1)
     e = run_few<GATED, 1, 1>(a, p, s);
-  else if (p.mb == 2)
-    e = run_few<GATED, 1, 2>(a, p, s);
   else
-    e = run_few<GATED, 1, 4>(a, p, s);
+    e = run_few<GATED, 1, 2>(a, p, s);
   return e == hipSuccess && p.slices > 1 ? join<GATED>(a, p.slices, s) : e;
 }
 
@@ -699,7 +718,25 @@ static hipError_t run_tiles(const LinearArgs& a, const LinearPlan& p, int64_t N,
     return tail ? run<Op<C, true, false>>({a, 1, p.chunk}, tiles, s) : run<Op<C, false, false>>({a, 1, p.chunk}, tiles, s);
   };
   if (p.bn == 256) return go(L256x256{});
-  return p.bm == 256 ? go(L256x128{}) : go(L128x128{});
+  if (p.bm == 256) return go(L256x128{});
+  return p.deep ? go(L128x128d{}) : go(L128x128{});
+}
+// all columns, or those of whole rounds and the others
+template <template <class, bool, bool> class Op>
+static hipError_t run_columns(LinearArgs a, int64_t N, int per_col, bool tail, hipStream_t s) {
+  a.col0 = 0;
+  a.cols = (int)(N / per_col);
+  const LinearPlan all = tiled_plan(a.T, N, a.k);
+  const int64_t cols = whole_rounds(a.T, N, a.k, all);
+  if (cols == 0) return run_tiles<Op>(a, all, per_col * ceil_div(a.cols, all.bn / per_col) * (all.bn / per_col), tail, s);
+  const int n = a.cols;
+  a.cols = (int)(cols / per_col);
+  const hipError_t e = run_tiles<Op>(a, all, cols, tail, s);
+  if (e != hipSuccess) return e;
+  a.col0 = a.cols;
+  a.cols = n - a.col0;
+  const LinearPlan rest = tiled_plan(a.T, N - cols, a.k, 1);
+  return run_tiles<Op>(a, rest, per_col * ceil_div(a.cols, rest.bn / per_col) * (rest.bn / per_col), tail, s);
 }
 template <int ACT>
 struct LinearOf {
@@ -712,14 +749,15 @@ hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t s) {
   const LinearPlan p = forward_plan(a.T, a.k, a.n, a.act, a.ldx);
   if (p.few) return gated ? few_rows<true>(a, p, s) : few_rows<false>(a, p, s);
   const bool tail = a.k % kBK != 0;
-  const int64_t N = gated ? 2 * ceil_div(a.n, p.bn / 2) * (p.bn / 2) : a.n;
+  const int per_col = gated ? 2 : 1;  // columns of W to an output column
+  const int64_t N = (int64_t)per_col * a.n;
   hipError_t e;
   switch (a.act) {
-    case MOE_ACT_RELU: e = run_tiles<LinearOf<MOE_ACT_RELU>::Op>(a, p, N, tail, s); break;
-    case MOE_ACT_SILU: e = run_tiles<LinearOf<MOE_ACT_SILU>::Op>(a, p, N, tail, s); break;
-    case MOE_ACT_GELU: e = run_tiles<LinearOf<MOE_ACT_GELU>::Op>(a, p, N, tail, s); break;
-    case MOE_ACT_SWIGLU: e = run_tiles<LinearOf<MOE_ACT_SWIGLU>::Op>(a, p, N, tail, s); break;
-    default: e = run_tiles<LinearOf<MOE_ACT_NONE>::Op>(a, p, N, tail, s);
+    case MOE_ACT_RELU: e = run_columns<LinearOf<MOE_ACT_RELU>::Op>(a, N, per_col, tail, s); break;
+    case MOE_ACT_SILU: e = run_columns<LinearOf<MOE_ACT_SILU>::Op>(a, N, per_col, tail, s); break;
+    case MOE_ACT_GELU: e = run_columns<LinearOf<MOE_ACT_GELU>::Op>(a, N, per_col, tail, s); break;
+    case MOE_ACT_SWIGLU: e = run_columns<LinearOf<MOE_ACT_SWIGLU>::Op>(a, N, per_col, tail, s); break;
+    default: e = run_columns<LinearOf<MOE_ACT_NONE>::Op>(a, N, per_col, tail, s);
   }
   if (e != hipSuccess || p.slices == 1) return e;
   return gated ? join<true>(a, p.slices, s) : join<false>(a, p.slices, s);
@@ -728,14 +766,14 @@ hipError_t launch_linear_fwd(const LinearArgs& a, hipStream_t s) {
 hipError_t launch_linear_bwd(const LinearBwdArgs& a, hipStream_t s) {
   const bool gated = a.act == MOE_ACT_SWIGLU;
   const int64_t N = gated ? 2 * (int64_t)a.n : a.n;
-  const int chunks = (int)ceil_div(a.T, kDpRows);
+  const int rows = dp_rows(a.T, N), chunks = (int)ceil_div(a.T, rows);
   if (a.dP || a.db) {
-    const dim3 grid((unsigned)ceil_div(a.n, 256), chunks);
+    const int blocks = (int)ceil_div(a.n, 256);
     float* sums = a.db ? a.db_part : nullptr;
     if (gated)
-      linear_dp_kernel<true><<<grid, 256, 0, s>>>(a, sums);
+      linear_dp_kernel<true><<<chunks * blocks, 256, 0, s>>>(a, blocks, rows, sums);
     else
-      linear_dp_kernel<false><<<grid, 256, 0, s>>>(a, sums);
+      linear_dp_kernel<false><<<chunks * blocks, 256, 0, s>>>(a, blocks, rows, sums);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -744,7 +782,7 @@ hipError_t launch_linear_bwd(const LinearBwdArgs& a, hipStream_t s) {
   if (a.dX) {
     const LinearPlan p = dx_plan(a.T, a.k, N);
     const LinearArgs x{dP, a.W, nullptr, a.G, nullptr, a.dX, a.dx_part, a.T, (int)N, a.k, MOE_ACT_NONE, ldp, a.ldx, a.ldx};
-    hipError_t e = run_tiles<OpLinearDX>(x, p, a.k, N % kBK != 0, s);
+    hipError_t e = run_columns<OpLinearDX>(x, a.k, 1, N % kBK != 0, s);
     if (e == hipSuccess && p.slices > 1) e = join<false>(x, p.slices, s);
     if (e != hipSuccess) return e;
   }
@@ -759,7 +797,7 @@ hipError_t launch_linear_bwd(const LinearBwdArgs& a, hipStream_t s) {
       return splits > 1 ? run<OpLinearDW<C, true>>({x, dP, ldp, a.dW, (int)N, splits, p.chunk}, tiles, s)
                         : run<OpLinearDW<C, false>>({x, dP, ldp, a.dW, (int)N, 1, p.chunk}, tiles, s);
     };
-    const hipError_t e = p.bm == 256 ? go(D256x256{}) : go(D128x128{});
+    const hipError_t e = p.bm == 256 ? go(D256x256{}) : p.deep ? go(D128x128d{}) : go(D128x128{});
     if (e != hipSuccess) return e;
   }
   if (splits > 1 || a.db) {
