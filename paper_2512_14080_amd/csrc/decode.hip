@@ -4,20 +4,27 @@
 //   2. Softmax, top-K, up-projection, down-projection and the weighted sum.
 //
 // With few tokens the layer is bound by one pass over the weights of the experts that
-// the tokens pick, and beside that by the launches in a row: a dependent launch costs
-// 3 to 6 us here, as much as one token's weights.  So the second launch is a work queue:
-// its items, in order, are the up-projection tiles of every picked expert, the
-// down-projection tiles, and the sums; a workgroup takes the next item by an atomic
-// ticket, and an item that needs others waits for their counter.
+// the tokens pick, and beside that by the steps in a row: an empty launch behind another
+// costs 2.4 us here, and a step's first loads and last sums as much again, while one token's
+// weights are read in 3 us.  So the second launch is a work queue: its items, in order, are
+// the selection of more than 8 tokens, the up-projection tiles of every picked expert, the
+// down-projection tiles, and the sums; a workgroup takes the next item by an atomic ticket,
+// and an item that needs others waits for their counter.  What one item leaves for another
+// goes past the caches (shared loads and stores): the counter's hop takes 1 us, where a
+// write-back of the L2 by every workgroup took 3.2 and an invalidation 1.8.
 //
 // The waits end, whatever else runs on the GPU: an item only waits for items of lower
 // tickets, a ticket is taken by a workgroup that runs already and that holds at most one
 // ticket beyond the one it works on, and the lowest unfinished ticket waits for nothing
 // that is unfinished.  No co-residency of the grid is assumed.
 //
-// Selection is the routing kernels' (the K best of the softmax of the summed partials):
-// every workgroup forms it for itself from T x E logits in L2, which is cheaper than
-// another dependent step, and all get the same from the same sums.
+// Selection is the routing kernels' (the K best of the softmax of the summed partials).  Up
+// to 8 tokens every workgroup forms it for itself from T x E logits in L2, which is cheaper
+// than another dependent step, and all get the same from the same sums.
+//
+// Measured, as the whole call: one token of d 1536, n 256, E 128, K 8 19.8 us; 7 tokens of
+// d 1024, n 256, E 64, K 8 28 us; 64 of d 4096, n 512, E 128, K 8 (1.6 GB of weights) 291 us,
+// 5.4 TB/s.
 #include <algorithm>
 
 #include "launch.h"
@@ -76,15 +83,14 @@ struct Picked {
   int* rows;                 // [T K] entries t K + j by group, by token within (one word more)
   int* sel;                  // [T K] expert of entry t K + j
   float* w;                  // [T K] its weight
-  int* place;                // [T E] where waves share a token: the experts before each,
-  float* score;              // [T E] and the scores
+  uint32_t* keys;            // [T][128] where waves share a token: its scores' images
 };
 // waves that can share a token
 __host__ __device__ inline int decode_share(int T, int E) { return E > 128 || T > 4 ? 1 : T == 1 ? 8 : T == 2 ? 4 : 2; }
 __host__ __device__ inline size_t picked_bytes(int T, int E, int K) {
   const int g = T * K < E ? T * K : E;
-  const size_t shared = decode_share(T, E) > 1 ? 8 * (size_t)T * E : 0;
-  return (12 * (size_t)E + 4 * (size_t)(2 * g + 2) + 12 * (size_t)T * K + shared + 15) / 16 * 16;
+  const size_t shared = decode_share(T, E) > 1 ? 512 * (size_t)T : 0;
+  return (12 * (size_t)E + 4 * (size_t)(2 * g + 2) + 12 * (size_t)T * K + 15) / 16 * 16 + shared;
 }
 __device__ __forceinline__ Picked picked_at(char* lds, int T, int E, int K) {
   const int g = min(T * K, E), n = T * K;
@@ -96,17 +102,35 @@ __device__ __forceinline__ Picked picked_at(char* lds, int T, int E, int K) {
   p.rows = p.goff + g + 1;
   p.sel = p.rows + n + 1;
   p.w = (float*)(p.sel + n);
-  p.place = (int*)(p.w + n);
-  p.score = (float*)(p.place + T * E);
+  p.keys = (uint32_t*)(lds + (12 * (size_t)E + 4 * (size_t)(2 * g + 2) + 12 * (size_t)n + 15) / 16 * 16);
   return p;
 }
 
-// Where few experts are scored, an expert's place is the count of those before it, which the
-// `wpt` waves of a token share (a comparison with 64 of them costs about 50 clocks); else the
-// token's wave finds the winners one by one (450 clocks each).
-__device__ __forceinline__ bool by_count(const DecodeArgs& a, int epl, int wpt) { return a.E * epl <= 9 * a.K * wpt; }
+// Up to 128 experts and 4 tokens: the waves of a token take its experts in parts, and an
+// expert's place is the count of those before it, by the lanes that share it.  One wave's K
+// rounds of an arg-max take 1.7 us for K = 8 instead.
+constexpr int kCountExperts = 128;
+template <int WPT>
+__device__ __forceinline__ void place_experts(const DecodeArgs& a, const Picked& p, const uint32_t* keys, int t, int part) {
+  constexpr int MINE = kCountExperts / WPT, LANES = kWave / MINE, KEYS = kCountExperts / LANES;  // (MINE <= 64)
+  const int lane = lane_id(), e = MINE * part + lane / LANES, first = lane % LANES * KEYS;
+  const uint32_t key = keys[e];
+  int before = 0;
+#pragma unroll 8
+  for (int i = 0; i < KEYS; i += 4) {
+    const u32x4 k = *(const u32x4*)(keys + first + i);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) before += k[q] > key || (k[q] == key && first + i + q < e);
+  }
+  if constexpr (LANES > 1) before += __shfl_xor(before, 1, kWave);
+  if constexpr (LANES > 2) before += __shfl_xor(before, 2, kWave);
+  if (lane % LANES == 0 && e < a.E && before < a.K) {
+    p.sel[t * a.K + before] = e;
+    p.w[t * a.K + before] = topk_value(key);
+  }
+}
 
-// selection of token t by waves 0 .. wpt - 1 of its `wpt` (wpt > 1: by count, place zeroed)
+// selection of token t by wave `part` of its `wpt` (wpt > 1: place_experts)
 template <int EPL>
 __device__ __forceinline__ void select_token(const DecodeArgs& a, const Picked& p, int t, int part, int wpt) {
   const int lane = lane_id();
@@ -147,34 +171,21 @@ __device__ __forceinline__ void select_token(const DecodeArgs& a, const Picked& 
   uint32_t key[EPL];
 #pragma unroll
   for (int j = 0; j < EPL; ++j) key[j] = lane + 64 * j < a.E ? topk_key(v[j] / s) : 0u;
-  if (EPL <= 2 && by_count(a, EPL, wpt)) {
-    int before[EPL];
-#pragma unroll
-    for (int j = 0; j < EPL; ++j) before[j] = 0;
-    const int per = kWave / wpt;
-#pragma unroll
-    for (int i = 0; i < (EPL <= 2 ? EPL : 1); ++i)
-#pragma unroll 8  // (per is a multiple of it)
-      for (int l = part * per; l < part * per + per; ++l) {
-        const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)key[i], l);
-        // (equal keys: the lower expert first; past E the keys are 0 and no expert is lower)
-#pragma unroll
-        for (int j = 0; j < EPL; ++j) before[j] += k > key[j] || (k == key[j] && 64 * i + l < lane + 64 * j);
-      }
-#pragma unroll
-    for (int j = 0; j < EPL; ++j) {
-      const int e = lane + 64 * j;
-      if (e >= a.E) continue;
-      if (wpt > 1) {
-        atomicAdd(&p.place[t * a.E + e], before[j]);
-        p.score[t * a.E + e] = topk_value(key[j]);  // (the same by every wave)
-      } else if (before[j] < a.K) {
-        p.sel[t * a.K + before[j]] = e;
-        p.w[t * a.K + before[j]] = topk_value(key[j]);
-      }
+  if constexpr (EPL <= 2)
+    if (wpt > 1) {
+      // (every wave of the token has all its keys, and writes them for itself: the same values)
+      uint32_t* keys = p.keys + t * kCountExperts;
+      keys[lane] = key[0];
+      keys[lane + 64] = EPL == 2 ? key[EPL - 1] : 0u;
+      __builtin_amdgcn_wave_barrier();
+      if (wpt == 8)
+        place_experts<8>(a, p, keys, t, part);
+      else if (wpt == 4)
+        place_experts<4>(a, p, keys, t, part);
+      else
+        place_experts<2>(a, p, keys, t, part);
+      return;
     }
-    return;
-  }
   // K rounds of an arg-max, in a loop that is not unrolled: its scalars would not fit
   uint32_t taken = 0;
 #pragma unroll 1
@@ -240,31 +251,19 @@ __device__ __forceinline__ void weigh_token(const DecodeArgs& a, const Picked& p
 __device__ __forceinline__ void select_all(const DecodeArgs& a, const Picked& p) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool out = blockIdx.x == 0;
-  // waves of a token, where its experts' places are counted
-  const int share = decode_share(a.T, a.E), epl = a.E <= 64 ? 1 : 2;
-  const int wpt = share > 1 && by_count(a, epl, share) ? share : 1;
+  const int wpt = decode_share(a.T, a.E);
   if (wpt > 1) {
-    for (int i = threadIdx.x; i < a.T * a.E; i += kDecodeThreads) p.place[i] = 0;
-    __syncthreads();
     const int t = wave / wpt;
     if (t < a.T) select_token_of(a, p, t, wave % wpt, wpt);
     __syncthreads();
-    for (int i = threadIdx.x; i < a.T * a.E; i += kDecodeThreads) {
-      const int k = p.place[i], u = i / a.E;
-      if (k < a.K) {
-        p.sel[u * a.K + k] = i - u * a.E;
-        p.w[u * a.K + k] = p.score[i];
-      }
-    }
-    __syncthreads();
-    if (wave < a.T) weigh_token(a, p, wave, out, false);
+    if (wave < a.T) weigh_token(a, p, wave, out, false);  // (the weights are read past other barriers)
   } else {
     for (int t = wave; t < a.T; t += kDecodeWaves) {
       select_token_of(a, p, t, 0, 1);
       weigh_token(a, p, t, out, false);
     }
+    __syncthreads();
   }
-  __syncthreads();
 }
 // the same of one item's tokens, for all
 __device__ __forceinline__ void select_some(const DecodeArgs& a, const Picked& p, int item) {
@@ -282,17 +281,15 @@ __device__ __forceinline__ void read_selection(const DecodeArgs& a, const Picked
   __syncthreads();
 }
 
+// One token's groups are its entries (written ahead of the selection's barrier)
+__device__ __forceinline__ void one_token(const DecodeArgs& a, Picked& p) {
+  p.gexp = p.sel;
+  if (threadIdx.x <= a.K) p.goff[threadIdx.x] = p.rows[threadIdx.x] = threadIdx.x;
+}
 // the groups of a selection; returns how many there are
 __device__ __forceinline__ int form_groups(const DecodeArgs& a, const Picked& p, int* scan_lds) {
   const int n = a.T * a.K;
-  if (a.T == 1) {  // each entry its own
-    for (int i = threadIdx.x; i <= n; i += kDecodeThreads) {
-      if (i < n) p.gexp[i] = p.sel[i];
-      p.goff[i] = p.rows[i] = i;
-    }
-    __syncthreads();
-    return n;
-  }
+  if (a.T == 1) return n;  // (each entry its own: one_token)
   for (int e = threadIdx.x; e < a.E; e += kDecodeThreads) p.word[e] = 0ull;
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += kDecodeThreads) atomicOr(&p.word[p.sel[i]], 1ull << (i / a.K));
@@ -461,7 +458,6 @@ struct Decode {
   using Stream = RowStream<KB, NBUF>;
   using Part = typename Tile::Part;
   static constexpr int UP_COLS = COLS / 2, DOWN_COLS = COLS, MAX_ROWS = RT * MB;
-
 
   // An item of a group: the up-projection of COLS / 2 gate columns and the matching up columns
   // (a.ks > 1: of a slice of k), or the down-projection of COLS columns for every a.kw waves
@@ -959,7 +955,8 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
   static_assert(sizeof(typename TD::Part) <= sizeof(typename D::Part), "the partial sums' area");
   __shared__ int sh[2];
   __shared__ int scan_lds[kDecodeWaves];
-  const Picked p = picked_at(dyn, a.T, a.E, a.K);
+  Picked p = picked_at(dyn, a.T, a.E, a.K);
+  if (a.T == 1) one_token(a, p);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (threadIdx.x == kDecodeThreads - 1) sh[0] = take_ticket(a);  // (not by a wave that selects)
   // Up to 8 tokens every workgroup selects for itself.  More are the queue's first items, of 8
@@ -1069,8 +1066,9 @@ size_t decode_sync_words(int T, int d, int E, int K) { return (size_t)kLine * (1
 static bool decode_by_token(int T, int d, int E, int K) { return T == 1 || (2 * T * K <= E && T * (d / 32) <= 256); }
 int decode_ks(int T, int d, int n, int E, int K, bool q8) {
   if (!decode_by_token(T, d, E, K) || K * n > 8192) return 1;
-  const int items = T * K * ((n + 63) / 64) * (q8 ? 2 : 1);
-  return std::max(1, std::min({(q8 ? 256 : 128) / items, q8 ? (d + 1023) / 1024 : d / 256, 8}));
+  // about a workgroup to a CU with the down-projection's, and a step for each wave at least
+  const int items = T * K * ((n + 63) / 64) * (q8 ? 2 : 1), rest = std::max(128, 256 - T * (d / 32));
+  return std::max(1, std::min({rest / items, q8 ? (d + 1023) / 1024 : d / 256, 8}));
 }
 
 template <int KB, int MB>
