@@ -484,9 +484,10 @@ int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float
 
 /*
  * The same with 8-bit expert products, as moe_fwd_quant's: H = q(X) q(W1_e) (+ b1_e), Y =
- * q(A) q(W2_e) (+ b2_e), A quantised from fp32.  Up to 16 tokens the up-projection's codes
- * are multiplied with fp32 sums (O's error to this definition in 64 bits is then that of
- * its rounding, 1.7e-3), beyond by the block-scaled instruction.
+ * q(A) q(W2_e) (+ b2_e), A quantised from fp32.  For one token, and where T K is at most 16
+ * or E / 2 (with T d / 32 at most 256), the up-projection's codes are multiplied with fp32
+ * sums, else by the block-scaled instruction, whose sums are 1.3e-5 of the result off: a
+ * value of A next to the middle of two codes may then take the other one.
  *   q   weights in state MOE_HELD_WRITTEN, of the same d, n and E
  *   ws  moe_workspace_bytes(dims, capacity, MOE_WS_DECODE_QUANT) bytes
  */
@@ -505,9 +506,9 @@ int moe_decode_quant(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const
 enum { MOE_ACT_NONE = 0, MOE_ACT_RELU = 1, MOE_ACT_SILU = 2, MOE_ACT_GELU = 3, MOE_ACT_SWIGLU = 4 };
 
 typedef struct {
-  int32_t T;   /* rows, >= 1                                                  */
-  int32_t k;   /* columns of X, a positive multiple of 8                      */
-  int32_t n;   /* columns of Y, a positive multiple of 8                      */
+  int32_t T;   /* rows, 1 to 2^28; no matrix has more than 2^37 elements      */
+  int32_t k;   /* columns of X, a positive multiple of 8 below 2^24           */
+  int32_t n;   /* columns of Y, a positive multiple of 8 below 2^24           */
   int32_t act; /* MOE_ACT_*                                                   */
   /* elements from a row to the next of X (and dX), of R, and of Y (and dY): multiples
    * of 8, at least the row's length, below 2^30; 0: the row's length */

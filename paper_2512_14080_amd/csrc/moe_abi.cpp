@@ -1088,6 +1088,11 @@ static int check_linear(moe_linear& l) {
   if (l.n < 8 || l.n % 8) return fail(MOE_ERR_UNSUPPORTED, "n must be a positive multiple of 8 (got %d)", l.n);
   if (l.act < MOE_ACT_NONE || l.act > MOE_ACT_SWIGLU) return fail(MOE_ERR_INVALID_ARG, "unknown activation %d", l.act);
   if (l.k >= 1 << 24 || l.n >= 1 << 24) return fail(MOE_ERR_UNSUPPORTED, "k = %d, n = %d: must be below 2^24", l.k, l.n);
+  // (counts of tiles, row chunks and threads of a launch are 32-bit)
+  if (l.T > 1 << 28) return fail(MOE_ERR_UNSUPPORTED, "T must be at most 2^28 (got %d)", l.T);
+  const int64_t most = (int64_t)1 << 37, N = l.act == MOE_ACT_SWIGLU ? 2 * (int64_t)l.n : l.n;
+  if (l.T * N > most || (int64_t)l.T * l.k > most || l.k * N > most)
+    return fail(MOE_ERR_UNSUPPORTED, "T = %d, k = %d, n = %d: no matrix may have more than 2^37 elements", l.T, l.k, l.n);
   int32_t* ld[] = {&l.ldx, &l.ldr, &l.ldy};
   const char* name[] = {"ldx", "ldr", "ldy"};
   const int len[] = {l.k, l.n, l.n};

@@ -99,6 +99,10 @@ BAD_LINEAR = [
     ((4, 64, 64, 5), {}, B.MOE_ERR_INVALID_ARG),
     ((4, 64, 64, -1), {}, B.MOE_ERR_INVALID_ARG),
     ((4, 1 << 24, 64, "none"), {}, B.MOE_ERR_UNSUPPORTED),
+    (((1 << 28) + 1, 8, 8, "none"), {}, B.MOE_ERR_UNSUPPORTED),  # beyond the grids' 32-bit counts
+    ((1 << 28, 520, 8, "none"), {}, B.MOE_ERR_UNSUPPORTED),
+    ((1 << 28, 8, 264, "swiglu"), {}, B.MOE_ERR_UNSUPPORTED),
+    ((4, (1 << 24) - 8, 1 << 15, "none"), {}, B.MOE_ERR_UNSUPPORTED),
     ((4, 64, 64, "none"), {"ldx": 56}, B.MOE_ERR_INVALID_ARG),
     ((4, 64, 64, "none"), {"ldx": 68}, B.MOE_ERR_INVALID_ARG),
     ((4, 64, 64, "none"), {"ldy": 1 << 30}, B.MOE_ERR_INVALID_ARG),
