@@ -458,6 +458,7 @@ struct Decode {
   using Stream = RowStream<KB, NBUF>;
   using Part = typename Tile::Part;
   static constexpr int UP_COLS = COLS / 2, DOWN_COLS = COLS, MAX_ROWS = RT * MB;
+  static size_t stage_bytes(int) { return 0; }
 
   // An item of a group: the up-projection of COLS / 2 gate columns and the matching up columns
   // (a.ks > 1: of a slice of k), or the down-projection of COLS columns for every a.kw waves
@@ -494,7 +495,7 @@ struct Decode {
   // (before(): called by every thread ahead of the first barrier)
   template <bool UP, class Before>
   static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& stream, Part* part,
-                                             int wave, Before before) {
+                                             char*, int wave, Before before) {
     const int n = a.n, d = a.d, N = 2 * n, P = a.T * a.K, lane = opaque_lane();
     {
       constexpr int B = MB;  // (a path of its own for fewer rows spilled)
@@ -660,21 +661,35 @@ struct Decode {
 // columns, in the up-projection 32 gate columns and the matching up ones.  Rows are quantised
 // as they are loaded, X from bf16 and A from fp32.  EXACT: the up-projection's codes are
 // multiplied in bf16, with fp32 sums (as in the layer's 8-bit forward); the conversions bound it
-// where a workgroup has many items (32 tokens of a 30B-shaped layer: 206 us, 174 without).
+// where a workgroup has many items (32 tokens of a 30B-shaped layer: 206 us, 174 without, at
+// an earlier step).  MB = 2 is for groups of more than 16 rows.
 template <int MB, int NJ, bool EXACT>
 struct Decode8 {
   static constexpr int NBUF = 1, UP_COLS = 8 * NJ, DOWN_COLS = 16 * NJ, MAX_ROWS = 16 * MB;
+  static size_t stage_bytes(int n) { return (size_t)q_blocks(n) * MB * kStageBlock; }
   typedef Stream8Part<NJ> Part;
   using Item = typename Decode<1, 1>::Item;
   struct Stream {
     Rsrc w;
     const uint8_t* ws[2];
     uint32_t row[NJ];
-    int kb, end, step;  // this wave's first block, the end, and from a block to the next
+    // This wave's first block, the end, from a block to the next, and its steps, which begin
+    // at step `rot`: where rows are 4 KB apart, one block of them all lies in few memory channels,
+    // and items that all began there would ask the same ones (32 tokens of a 30B-shaped layer:
+    // 161 us, 148 so; 64: 184, 167)
+    int kb, end, step, ns, rot;
+    __device__ __forceinline__ void turn(int by) {
+      ns = max((end - kb + step - 1) / step, 1);
+      rot = by % ns;
+    }
+    __device__ __forceinline__ int block(int s) const {  // (past the end: the last one again, unused)
+      const int i = min(s, ns - 1) + rot;
+      return min(kb + step * (i >= ns ? i - ns : i), end - 1);
+    }
     u32x4 wv[NBUF][NJ][2];
     int sv[NBUF][2];
     __device__ __forceinline__ void load(int buf, int s) {
-      const int b = min(kb + step * s, end - 1);  // (past the end: the last one again, unused)
+      const int b = block(s);
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         wv[buf][j][0] = load16(w, row[j] + kQBlock * b);
@@ -704,6 +719,7 @@ struct Decode8 {
       s.kb = t.slice * (a.kslice / kQBlock) + wave;
       s.end = min(d, (t.slice + 1) * a.kslice) / kQBlock;
       s.step = kDecodeWaves;
+      s.turn(t.tile);
     } else {
       s.w = buffer_of(a.W2q + (size_t)t.e * w2q_bytes(d, n), (uint32_t)w2q_bytes(d, n));
       // (past the last column: the last tile's again, not stored)
@@ -712,6 +728,7 @@ struct Decode8 {
       s.kb = wave % a.kw;
       s.step = a.kw;
       s.end = q_blocks(n);
+      s.turn(t.tile);
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
@@ -732,15 +749,18 @@ struct Decode8 {
       x.v[i] = load16<F32>(r, kk < len ? off + (uint32_t)kk * ES + 16 * (i % (N / 2)) : kBufferOut);
     }
   }
-  template <int B, bool F32>
-  static __device__ __forceinline__ void add(const DecodeArgs& a, Stream& s, f32x4 (&acc)[B][NJ], Rsrc r, const uint32_t (&xoff)[B],
-                                             int len, int lane) {
-    const int g = lane >> 4, ns = (s.end - s.kb + s.step - 1) / s.step;
-    if (ns <= 0) return;
-    RowBlock8<F32> xv[NBUF][B];
+  // The rows of a step: quantised from what was loaded for it, or (F32, where column tiles share
+  // them) codes in LDS, a kStageBlock for each block and row block.
+  static constexpr int kStageBlock = kWave * 36;
+  template <bool F32, bool STAGED, class Row>
+  static __device__ __forceinline__ void add(Stream& s, f32x4 (&acc)[MB][NJ], const char* stage, int lane, Row row) {
+    const int ns = s.ns;
+    if (s.kb >= s.end) return;
+    RowBlock8<F32> xv[STAGED ? 1 : NBUF][MB];
     auto load_x = [&](int q, int i) {
+      if constexpr (!STAGED)
 #pragma unroll
-      for (int b = 0; b < B; ++b) load_row(xv[q][b], r, xoff[b], kQBlock * (s.kb + s.step * i) + 16 * g, len);
+        for (int b = 0; b < MB; ++b) row(xv[q][b], b, s.block(i));
     };
 #pragma unroll
     for (int q = 0; q < NBUF; ++q) load_x(q, q);
@@ -748,9 +768,17 @@ struct Decode8 {
 #pragma unroll
       for (int q = 0; q < NBUF; ++q) {
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
+        for (int b = 0; b < MB; ++b) {
           int xs;
-          const i32x8 x = xv[q][b].codes(&xs);
+          i32x8 x;
+          if constexpr (STAGED) {
+            const char* at = stage + (s.block(i + q) * MB + b) * kStageBlock;
+            const u32x4 lo = *(const u32x4*)(at + 16 * lane), hi = *(const u32x4*)(at + 16 * (kWave + lane));
+            x = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+            xs = *(const int*)(at + 32 * kWave + 4 * lane);
+          } else {
+            x = xv[q][b].codes(&xs);
+          }
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
             const int ws = s.sv[q][2 * j / NJ];
@@ -775,72 +803,90 @@ struct Decode8 {
     }
   }
   template <bool UP, class Before>
-  static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& s, Part* part, int wave,
-                                             Before before) {
+  static __device__ __forceinline__ void run(const DecodeArgs& a, const Picked& p, const Item& t, Stream& s, Part* part,
+                                             char* stage, int wave, Before before) {
     const int cnt = min(t.cnt, MAX_ROWS);
-    auto go = [&](auto blocks) __attribute__((always_inline)) {
-      constexpr int B = decltype(blocks)::value;
-      const int n = a.n, d = a.d, N = 2 * n, P = a.T * a.K, lane = opaque_lane(), g = lane >> 4, l = lane & 15;
-      uint32_t xoff[B];
-      f32x4 acc[B][NJ];
+    const int n = a.n, d = a.d, N = 2 * n, P = a.T * a.K, lane = opaque_lane(), g = lane >> 4, l = lane & 15;
+    uint32_t xoff[MB];
+    f32x4 acc[MB][NJ];
 #pragma unroll
-      for (int b = 0; b < B; ++b) {
-        // (a lane past the rows reads the last one's again)
-        const int i = p.rows[t.r0 + min(16 * b + l, cnt - 1)];
-        xoff[b] = UP ? (uint32_t)(i / a.K) * d * 2 : (uint32_t)i * n * 4;
+    for (int b = 0; b < MB; ++b) {
+      // (a lane past the rows reads the last one's again)
+      const int i = p.rows[t.r0 + min(16 * b + l, cnt - 1)];
+      xoff[b] = UP ? (uint32_t)(i / a.K) * d * 2 : (uint32_t)i * n * 4;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      }
-      add<B, !UP>(a, s, acc, UP ? buffer_of(a.X, (uint32_t)a.T * d * 2) : buffer_of(a.A32, (uint32_t)P * n * 4), xoff, UP ? d : n, lane);
-      before();
+      for (int j = 0; j < NJ; ++j) acc[b][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const Rsrc r = UP ? buffer_of(a.X, (uint32_t)a.T * d * 2) : buffer_of(a.A32, (uint32_t)P * n * 4);
+    auto row = [&](RowBlock8<!UP>& x, int b, int kb) { load_row(x, r, xoff[b], kQBlock * kb + 16 * g, UP ? d : n); };
+    if constexpr (UP) {
+      add<false, false>(s, acc, nullptr, lane, row);
+    } else if (a.kw == kDecodeWaves) {
+      add<true, false>(s, acc, nullptr, lane, row);
+    } else {
+      // (a wave for each block; 64 tokens of d 1536, n 256, E 128, K 8: 59.1 us without, 57.4 so)
+      for (int kb = wave; kb < q_blocks(n); kb += kDecodeWaves)
 #pragma unroll
-      for (int b = 0; b < B; ++b) {
-        if (16 * b >= cnt) break;
-        if (b) __syncthreads();
+        for (int b = 0; b < MB; ++b) {
+          RowBlock8<true> x;
+          row(x, b, kb);
+          int xs;
+          const i32x8 c = x.codes(&xs);
+          char* at = stage + (kb * MB + b) * kStageBlock;
+          *(u32x4*)(at + 16 * lane) = u32x4{(uint32_t)c[0], (uint32_t)c[1], (uint32_t)c[2], (uint32_t)c[3]};
+          *(u32x4*)(at + 16 * (kWave + lane)) = u32x4{(uint32_t)c[4], (uint32_t)c[5], (uint32_t)c[6], (uint32_t)c[7]};
+          *(int*)(at + 32 * kWave + 4 * lane) = xs;
+        }
+      __syncthreads();
+      add<true, true>(s, acc, stage, lane, row);
+    }
+    before();
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) part[wave][l][4 * j + g] = acc[b][j];
-        __syncthreads();
-        const int rows = min(16, cnt - 16 * b);
-        constexpr int C4 = 4 * NJ;
-        if (UP && a.ks == 1) {
-          for (int i = threadIdx.x; i < rows * (C4 / 2); i += kDecodeThreads) {
-            const int row = i / (C4 / 2), c4 = i % (C4 / 2), col = UP_COLS * t.tile + 4 * c4;
-            f32x4 hg = stream8_sum<kDecodeWaves, NJ>(part, row, c4), hu = stream8_sum<kDecodeWaves, NJ>(part, row, c4 + C4 / 2), v;
-            const float* b1 = a.b1 ? a.b1 + (size_t)t.e * N + col : nullptr;
+    for (int b = 0; b < MB; ++b) {
+      if (16 * b >= cnt) break;
+      if (b) __syncthreads();
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if (b1) {
-                hg[q] += b1[q];
-                hu[q] += b1[n + q];
-              }
-              float sg;
-              v[q] = silu_sig(hg[q], &sg) * hu[q];
+      for (int j = 0; j < NJ; ++j) part[wave][l][4 * j + g] = acc[b][j];
+      __syncthreads();
+      const int rows = min(16, cnt - 16 * b);
+      constexpr int C4 = 4 * NJ;
+      if (UP && a.ks == 1) {
+        for (int i = threadIdx.x; i < rows * (C4 / 2); i += kDecodeThreads) {
+          const int row = i / (C4 / 2), c4 = i % (C4 / 2), col = UP_COLS * t.tile + 4 * c4;
+          f32x4 hg = stream8_sum<kDecodeWaves, NJ>(part, row, c4), hu = stream8_sum<kDecodeWaves, NJ>(part, row, c4 + C4 / 2), v;
+          const float* b1 = a.b1 ? a.b1 + (size_t)t.e * N + col : nullptr;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (b1) {
+              hg[q] += b1[q];
+              hu[q] += b1[n + q];
             }
-            store16_shared(buffer_of(a.A32, (uint32_t)P * n * 4), (uint32_t)(p.rows[t.r0 + 16 * b + row] * n + col) * 4,
-                           __builtin_bit_cast(u32x4, v));
+            float sg;
+            v[q] = silu_sig(hg[q], &sg) * hu[q];
           }
-          continue;
+          store16_shared(buffer_of(a.A32, (uint32_t)P * n * 4), (uint32_t)(p.rows[t.r0 + 16 * b + row] * n + col) * 4,
+                         __builtin_bit_cast(u32x4, v));
         }
-        if constexpr (UP) {
-          for (int i = threadIdx.x; i < rows * C4; i += kDecodeThreads) {
-            const int row = i / C4, c4 = i % C4, r = p.rows[t.r0 + 16 * b + row];
-            const f32x4 y = stream8_sum<kDecodeWaves, NJ>(part, row, c4);
-            const int col = UP_COLS * t.tile + 4 * (c4 % (C4 / 2));
-            store16_shared(buffer_of(a.H32, (uint32_t)a.ks * P * N * 4),
-                           (uint32_t)((t.slice * P + r) * N + col + (c4 < C4 / 2 ? 0 : n)) * 4, __builtin_bit_cast(u32x4, y));
-          }
-          continue;
-        }
-        store_y<C4>(a, p, t, 16 * b, rows, [&](int sub, int row, int c4) {
-          f32x4 y = part[sub * a.kw][row][c4];
-          for (int w = 1; w < a.kw; ++w)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] += part[sub * a.kw + w][row][c4][q];
-          return y;
-        });
+        continue;
       }
-    };
-    go(std::integral_constant<int, MB>{});
+      if constexpr (UP) {
+        for (int i = threadIdx.x; i < rows * C4; i += kDecodeThreads) {
+          const int row = i / C4, c4 = i % C4, r = p.rows[t.r0 + 16 * b + row];
+          const f32x4 y = stream8_sum<kDecodeWaves, NJ>(part, row, c4);
+          const int col = UP_COLS * t.tile + 4 * (c4 % (C4 / 2));
+          store16_shared(buffer_of(a.H32, (uint32_t)a.ks * P * N * 4),
+                         (uint32_t)((t.slice * P + r) * N + col + (c4 < C4 / 2 ? 0 : n)) * 4, __builtin_bit_cast(u32x4, y));
+        }
+        continue;
+      }
+      store_y<C4>(a, p, t, 16 * b, rows, [&](int sub, int row, int c4) {
+        f32x4 y = part[sub * a.kw][row][c4];
+        for (int w = 1; w < a.kw; ++w)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) y[q] += part[sub * a.kw + w][row][c4][q];
+        return y;
+      });
+    }
   }
 
   // by token: 32 columns, a wave's step one block of one entry, weighted as it is added
@@ -1005,13 +1051,13 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
       int* counter = !UP ? tile_counter(a, t.tile) : BY_TOKEN ? ups_counter(a, item) : group_counter(a, t.gi);
       if constexpr (!UP) ok = await([&](int l) { return l == 0 ? group_counter(a, t.gi) : nullptr; }, per_group, sh + 1) && ok;
       while (t.cnt > D::MAX_ROWS) {  // (more rows than a pass takes: the weights again)
-        D::template run<UP>(a, p, t, stream, part, wave, []() {});
+        D::template run<UP>(a, p, t, stream, part, dyn + picked_bytes(a.T, a.E, a.K), wave, []() {});
         t.r0 += D::MAX_ROWS;
         t.cnt -= D::MAX_ROWS;
         D::template prime<UP>(a, t, stream, wave);
         __syncthreads();
       }
-      D::template run<UP>(a, p, t, stream, part, wave, [&]() {
+      D::template run<UP>(a, p, t, stream, part, dyn + picked_bytes(a.T, a.E, a.K), wave, [&]() {
         if (more && threadIdx.x == 0) sh[0] = next;
       });
       item = more ? __builtin_amdgcn_readfirstlane(sh[0]) - selects : total;
@@ -1086,7 +1132,11 @@ static hipError_t run_decode(const DecodeArgs& a, hipStream_t s) {
   const int64_t groups = std::min(a.T * a.K, a.E), down_tiles = (a.d + down_cols - 1) / down_cols;
   int64_t items = groups * ((a.n + D::UP_COLS - 1) / D::UP_COLS) * a.ks;
   items += BY_TOKEN ? a.T * down_tiles : (groups + (a.T + sum_rows - 1) / sum_rows) * down_tiles;
-  const size_t lds = picked_bytes(a.T, a.E, a.K) + (a.ks > 1 ? (a.W1q ? 4 : 2) * (size_t)a.K * a.n : 0);
+  size_t lds = picked_bytes(a.T, a.E, a.K);  // and a token's rows, or the codes of an item's
+  if (a.ks > 1)
+    lds += (a.W1q ? 4 : 2) * (size_t)a.K * a.n;
+  else if (!BY_TOKEN && a.kw < kDecodeWaves)
+    lds += D::stage_bytes(a.n);
   decode_kernel<D, TD, BY_TOKEN><<<(int)std::min<int64_t>(items, 256), kDecodeThreads, lds, s>>>(a);
   return hipGetLastError();
 }
@@ -1100,7 +1150,12 @@ hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
   // waves of a down-projection column tile: two steps each, where there are as many
   const int steps = q8 ? q_blocks(a.n) : a.n / 32;
   a.kw = 1;
-  while (2 * a.kw <= kDecodeWaves && 4 * a.kw <= steps) a.kw *= 2;
+  // (8-bit: one step each, while the items are fewer than two to a CU: 9 tokens of d 1536, n 256,
+  // E 128, K 8 46.1 us, 38.5 so; in 16 bits 46.9 and 47.5, and 7 tokens of the 1B layer 27.2 and 29.2)
+  const int64_t groups = std::min(a.T * a.K, a.E);
+  while (2 * a.kw <= kDecodeWaves &&
+         (4 * a.kw <= steps || (q8 && 2 * a.kw <= steps && groups * a.d * a.kw < 512 * 64 * kDecodeWaves)))
+    a.kw *= 2;
   const hipError_t e = run_router<1, 1>(a, s);
   if (e != hipSuccess) return e;
   // one row block where a group seldom has more than its 16 rows
