@@ -83,14 +83,14 @@ struct Picked {
   int* rows;                 // [T K] entries t K + j by group, by token within (one word more)
   int* sel;                  // [T K] expert of entry t K + j
   float* w;                  // [T K] its weight
-  uint32_t* keys;            // [T][128] where waves share a token: its scores' images
+  uint32_t* keys;            // [T][64 or 128] where waves share a token: its scores' images
 };
-// waves that can share a token
+// waves that share a token, whose experts are then placed by counting (place_experts)
 __host__ __device__ inline int decode_share(int T, int E) { return E > 128 || T > 4 ? 1 : T == 1 ? 8 : T == 2 ? 4 : 2; }
 __host__ __device__ inline size_t picked_bytes(int T, int E, int K) {
   const int g = T * K < E ? T * K : E;
-  const size_t shared = decode_share(T, E) > 1 ? 512 * (size_t)T : 0;
-  return (12 * (size_t)E + 4 * (size_t)(2 * g + 2) + 12 * (size_t)T * K + 15) / 16 * 16 + shared;
+  const size_t keys = decode_share(T, E) > 1 ? (E <= 64 ? 256 : 512) * (size_t)T : 0;
+  return (12 * (size_t)E + 4 * (size_t)(2 * g + 2) + 12 * (size_t)T * K + 15) / 16 * 16 + keys;
 }
 __device__ __forceinline__ Picked picked_at(char* lds, int T, int E, int K) {
   const int g = min(T * K, E), n = T * K;
@@ -106,13 +106,14 @@ __device__ __forceinline__ Picked picked_at(char* lds, int T, int E, int K) {
   return p;
 }
 
-// Up to 128 experts and 4 tokens: the waves of a token take its experts in parts, and an
-// expert's place is the count of those before it, by the lanes that share it.  One wave's K
-// rounds of an arg-max take 1.7 us for K = 8 instead.
-constexpr int kCountExperts = 128;
-template <int WPT>
+// An expert's place is the count of those before it, of N: the waves of a token take N / WPT
+// experts each, and the lanes of an expert a part of the keys each.  (4 tokens of d 1024, n 256,
+// E 64, K 8 24.3 us, 26 with K rounds of an arg-max in one wave; by one wave for a token it loses:
+// 16 tokens 36.0, with the arg-max 35.0.)
+template <int N, int WPT>
 __device__ __forceinline__ void place_experts(const DecodeArgs& a, const Picked& p, const uint32_t* keys, int t, int part) {
-  constexpr int MINE = kCountExperts / WPT, LANES = kWave / MINE, KEYS = kCountExperts / LANES;  // (MINE <= 64)
+  constexpr int MINE = N / WPT, LANES = kWave / MINE, KEYS = N / LANES;
+  static_assert(MINE <= kWave && KEYS >= 4);
   const int lane = lane_id(), e = MINE * part + lane / LANES, first = lane % LANES * KEYS;
   const uint32_t key = keys[e];
   int before = 0;
@@ -122,15 +123,16 @@ __device__ __forceinline__ void place_experts(const DecodeArgs& a, const Picked&
 #pragma unroll
     for (int q = 0; q < 4; ++q) before += k[q] > key || (k[q] == key && first + i + q < e);
   }
-  if constexpr (LANES > 1) before += __shfl_xor(before, 1, kWave);
-  if constexpr (LANES > 2) before += __shfl_xor(before, 2, kWave);
+#pragma unroll
+  for (int i = 1; i < LANES; i *= 2) before += __shfl_xor(before, i, kWave);
+  // (past E the keys are 0, and behind every expert's)
   if (lane % LANES == 0 && e < a.E && before < a.K) {
     p.sel[t * a.K + before] = e;
     p.w[t * a.K + before] = topk_value(key);
   }
 }
 
-// selection of token t by wave `part` of its `wpt` (wpt > 1: place_experts)
+// selection of token t by wave `part` of its `wpt`
 template <int EPL>
 __device__ __forceinline__ void select_token(const DecodeArgs& a, const Picked& p, int t, int part, int wpt) {
   const int lane = lane_id();
@@ -174,16 +176,16 @@ __device__ __forceinline__ void select_token(const DecodeArgs& a, const Picked& 
   if constexpr (EPL <= 2)
     if (wpt > 1) {
       // (every wave of the token has all its keys, and writes them for itself: the same values)
-      uint32_t* keys = p.keys + t * kCountExperts;
-      keys[lane] = key[0];
-      keys[lane + 64] = EPL == 2 ? key[EPL - 1] : 0u;
+      constexpr int N = 64 * EPL;
+      uint32_t* keys = p.keys + t * N;
+      for (int j = 0; j < EPL; ++j) keys[lane + 64 * j] = key[j];
       __builtin_amdgcn_wave_barrier();
       if (wpt == 8)
-        place_experts<8>(a, p, keys, t, part);
+        place_experts<N, 8>(a, p, keys, t, part);
       else if (wpt == 4)
-        place_experts<4>(a, p, keys, t, part);
+        place_experts<N, 4>(a, p, keys, t, part);
       else
-        place_experts<2>(a, p, keys, t, part);
+        place_experts<N, 2>(a, p, keys, t, part);
       return;
     }
   // K rounds of an arg-max, in a loop that is not unrolled: its scalars would not fit
@@ -1108,8 +1110,9 @@ int decode_slices(int T, int d, int E) {
 }
 size_t decode_sync_words(int T, int d, int E, int K) { return (size_t)kLine * (10 + std::min(T * K, E) + d / 32); }
 // whether the down-projection goes by token: where few entries repeat experts, whose weights are
-// then read again, and the items are one round; then the slices of k
-static bool decode_by_token(int T, int d, int E, int K) { return T == 1 || (2 * T * K <= E && T * (d / 32) <= 256); }
+// then read again, and the items leave CUs for the up-projection's (two tokens of d 1536, n 256,
+// E 128, K 8 25.2 us, by group 27.0; four 35.8, 34.0).  decode_ks: the slices of k
+static bool decode_by_token(int T, int d, int E, int K) { return T == 1 || (2 * T * K <= E && T * (d / 32) <= 160); }
 int decode_ks(int T, int d, int n, int E, int K, bool q8) {
   if (!decode_by_token(T, d, E, K) || K * n > 8192) return 1;
   // about a workgroup to a CU with the down-projection's, and a step for each wave at least
