@@ -81,7 +81,7 @@ __device__ __forceinline__ void finish4(const LinearArgs& a, size_t t, int col, 
 
 // ---------------------------------------------------------------- few rows
 constexpr int kFewWaves8 = 8, kFewThreads = 64 * kFewWaves8;
-// grid: column tiles, k slices.  KB, MB: rows in MB blocks of 16 / KB
+// grid: column tiles, k slices, groups of MB blocks of 16 / KB rows
 template <bool GATED, int KB, int MB>
 __global__ __launch_bounds__(kFewThreads, 2) void linear_few_kernel(const LinearArgs a, int slice) {
   using Tile = RowTile<KB>;
@@ -92,12 +92,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void linear_few_kernel(const Linear
   const int kbeg = blockIdx.y * slice, kend = min(a.k, kbeg + slice);
   const int c = GATED ? c0 + 8 * (Tile::cg(lane) & (CG / 2 - 1)) : c0 + 8 * Tile::cg(lane);
   const uint32_t wcol = c < n ? 2 * (c + (GATED && Tile::cg(lane) >= CG / 2 ? n : 0)) : kBufferOut;
+  const int t0 = Tile::RT * MB * blockIdx.z;
   RowStream<KB, 2> stream;
   stream.prime(buffer_of(a.W, (uint32_t)a.k * N * 2), N * 2, wcol, kbeg, kend, wave, kFewWaves8, lane);
   uint32_t xoff[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
-    const int t = Tile::RT * b + Tile::row(lane);
+    const int t = t0 + Tile::RT * b + Tile::row(lane);
     xoff[b] = t < a.T ? (uint32_t)t * a.ldx * 2 : kBufferOut;
   }
   f32x4 acc[MB][8];
@@ -105,17 +106,18 @@ __global__ __launch_bounds__(kFewThreads, 2) void linear_few_kernel(const Linear
   stream.template add<false>(acc, buffer_of(a.X, ((uint32_t)(a.T - 1) * a.ldx + a.k) * 2), xoff);
 #pragma unroll
   for (int b = 0; b < MB; ++b) {
-    if (Tile::RT * b >= a.T) break;
+    const int first = t0 + Tile::RT * b;
+    if (first >= a.T) break;
     if (b) __syncthreads();
     Tile::put(part[wave], acc[b], lane);
     __syncthreads();
-    const int rows = min(Tile::RT, a.T - Tile::RT * b);
+    const int rows = min(Tile::RT, a.T - first);
     if (gridDim.y > 1) {
       for (int i = threadIdx.x; i < rows * C4; i += kFewThreads) {
         const int row = i / C4, c4 = i % C4;
         const int col = GATED ? c0 + 4 * (c4 % (C4 / 2)) : c0 + 4 * c4;
         if (col >= n) continue;
-        float* out = a.part + ((size_t)blockIdx.y * a.T + Tile::RT * b + row) * N + col + (GATED && c4 >= C4 / 2 ? n : 0);
+        float* out = a.part + ((size_t)blockIdx.y * a.T + first + row) * N + col + (GATED && c4 >= C4 / 2 ? n : 0);
         *(f32x4*)out = Tile::template sum<kFewWaves8>(part, row, c4);
       }
       continue;
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void linear_few_kernel(const Linear
       if (col >= n) continue;
       const f32x4 v = Tile::template sum<kFewWaves8>(part, row, c4);
       const f32x4 u = GATED ? Tile::template sum<kFewWaves8>(part, row, c4 + C4 / 2) : v;
-      finish4<GATED>(a, Tile::RT * b + row, col, v, u);
+      finish4<GATED>(a, first + row, col, v, u);
     }
   }
 }
@@ -581,8 +583,11 @@ constexpr size_t kSlabBytes = (size_t)256 << 20;
 constexpr int kCus = 256;  // (a size of workspaces: not the device's own count)
 
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-// rows of a workgroup of linear_dp_kernel: 64, fewer where that leaves CUs idle
+// rows of a workgroup of linear_dp_kernel: 64, fewer where that leaves CUs idle; but all of up to
+// 16 rows, whose sums are then db itself (a step of one row, k = 1024, n = 1536, silu, with bias:
+// 30.0 us, 26.7 so; 56 rows of k = 832, n = 1024 would take 36.7, not 29.2)
 static int dp_rows(int T, int64_t N) {
+  if (T <= 16) return 16;
   int rows = 64;
   while (rows > 8 && ceil_div(T, rows) * ceil_div(N, 256) < 4 * kCus) rows /= 2;
   return rows;
@@ -627,20 +632,50 @@ static int64_t whole_rounds(int64_t M, int64_t N, int64_t K, const LinearPlan& a
   return rounds * 100. * (ceil_div(K, kBK) + 4) + rest.cost + 200 < 0.97 * all.cost ? cols : 0;
 }
 
+// More than 16 rows streamed, in groups of 16 or 32 that each read the weights.  In us, fitted: a
+// start; the larger of a workgroup's reading of its columns (a CU: 60 GB/s, 50 with two row
+// blocks; 1.7 us at least), in rounds, and all reads (5.5 TB/s; a group's after the first are found nearer, at
+// four times that); and the join.
+static double join_us(int slices, int64_t T, int64_t N) { return slices > 1 ? 2.5 + 0.12 * slices + slices * T * N * 4 / 4e6 : 0; }
+static void stream_plan(int T, int64_t k, int64_t N, LinearPlan& best) {
+  for (int mb = 1; mb <= 2; ++mb) {
+    const int64_t groups = ceil_div(T, 16 * mb), tiles = ceil_div(N, 128) * groups;
+    const double reads = (1 + (groups - 1) / 4.) * k * N * 2 / 5.5e6;
+    for (int slices = 1; slices <= kLinearMaxSlices; slices *= 2) {
+      if (slices > 1 && k < 256 * slices) break;
+      const int64_t chunk = ceil_div(ceil_div(k, slices), 128) * 128;
+      const double rounds = ceil_div(tiles * slices, kCus) * std::max(1.7, chunk * (mb == 1 ? 4.3 : 5.3) / 1024);
+      const double us = (mb == 1 ? 3.1 : 4.4) + std::max(rounds, reads) + join_us(slices, T, N);
+      if (us < 0.97 * best.cost) best = {true, 1, mb, 0, 0, false, (int)ceil_div(k, chunk), (int)chunk, us};
+    }
+  }
+}
+// the same of a tiled plan, whose own cost compares tiles only
+static double tiled_us(const LinearPlan& p, int64_t T, int64_t N) {
+  const double join = p.slices > 1 ? 250 + p.slices * T * N * 4 / 70e3 : 0;
+  return 2.4 + 0.0146 * (p.cost - join) + join_us(p.slices, T, N);
+}
 static LinearPlan forward_plan(int T, int k, int n, int act, int64_t ldx) {
   const int64_t N = act == MOE_ACT_SWIGLU ? 2 * (int64_t)n : n;
-  // (four row blocks cost registers: T = 64, k = 4096, n = 14336 33 us, in tiles 29; k = 3328, n = 3840 15.3, 13.2)
-  if (T > 32 || (int64_t)k * N * 2 > INT32_MAX || (T * ldx + k) * 2 > INT32_MAX) return tiled_plan(T, N, k);
+  const bool fits = (int64_t)k * N * 2 <= INT32_MAX && (T * ldx + k) * 2 <= INT32_MAX;
+  if (T > 16 || !fits) {
+    LinearPlan best = tiled_plan(T, N, k);
+    // T = 45, k = 1000, n = 2824: 8.5 us, 13.0 in tiles; 256 rows 12.7 and 16.2, 512 22.5 and
+    // 16.3; T = 512, k = 512, n = 512 5.4 and 10.6; T = 40, k = 4096, n = 14336 41 and 27
+    best.cost = tiled_us(best, T, N);
+    if (fits && T <= 1 << 14) stream_plan(T, k, N, best);
+    return best;
+  }
   // narrower tiles for fewer rows, while that gives up to a workgroup to two CUs
   int kb = 1;
   while (kb < 4 && 16 / (2 * kb) >= T && ceil_div(N, 128 / kb) < 128) kb *= 2;
   const int64_t tiles = ceil_div(N, 128 / kb);
   int slices = 1;
   // k slices where a workgroup would read more than 256 KB on its own
-  while (2 * slices * tiles <= 256 && 2 * slices <= kLinearMaxSlices && k / slices * (256 / kb) > 256 * 1024) slices *= 2;
+  while (2 * slices * tiles <= kCus && 2 * slices <= kLinearMaxSlices && k / slices * (256 / kb) > 256 * 1024) slices *= 2;
   const int chunk = (int)ceil_div(ceil_div(k, slices), 128) * 128;
   slices = (int)ceil_div(k, chunk);
-  return {true, kb, T <= 16 ? 1 : 2, 0, 0, false, slices, chunk, 0};
+  return {true, kb, 1, 0, 0, false, slices, chunk, 0};
 }
 
 static LinearPlan dx_plan(int T, int k, int64_t N) { return tiled_plan(T, k, N); }
@@ -690,7 +725,8 @@ static hipError_t join(const LinearArgs& a, int slices, hipStream_t s) {
 template <bool GATED, int KB, int MB>
 static hipError_t run_few(const LinearArgs& a, const LinearPlan& p, hipStream_t s) {
   constexpr int out = RowTile<KB>::COLS / (GATED ? 2 : 1);
-  linear_few_kernel<GATED, KB, MB><<<dim3((unsigned)ceil_div(a.n, out), p.slices), kFewThreads, 0, s>>>(a, p.chunk);
+  linear_few_kernel<GATED, KB, MB><<<dim3((unsigned)ceil_div(a.n, out), p.slices, (unsigned)ceil_div(a.T, RowTile<KB>::RT * MB)), kFewThreads, 0, s>>>(a,
+                                                                                                           p.chunk);
   return hipGetLastError();
 }
 template <bool GATED>
@@ -769,7 +805,7 @@ hipError_t launch_linear_bwd(const LinearBwdArgs& a, hipStream_t s) {
   const int rows = dp_rows(a.T, N), chunks = (int)ceil_div(a.T, rows);
   if (a.dP || a.db) {
     const int blocks = (int)ceil_div(a.n, 256);
-    float* sums = a.db ? a.db_part : nullptr;
+    float* sums = chunks == 1 ? a.db : a.db ? a.db_part : nullptr;
     if (gated)
       linear_dp_kernel<true><<<chunks * blocks, 256, 0, s>>>(a, blocks, rows, sums);
     else
@@ -800,10 +836,11 @@ hipError_t launch_linear_bwd(const LinearBwdArgs& a, hipStream_t s) {
     const hipError_t e = p.bm == 256 ? go(D256x256{}) : p.deep ? go(D128x128d{}) : go(D128x128{});
     if (e != hipSuccess) return e;
   }
-  if (splits > 1 || a.db) {
+  const bool join_db = a.db && chunks > 1;
+  if (splits > 1 || join_db) {
     const int64_t MN = (int64_t)a.k * N;
     const int wgs = splits > 1 ? (int)std::min<int64_t>(ceil_div(MN / 4, 256), 2048) : 0;
-    const int cols = a.db ? (int)ceil_div(N, 32) : 0;
+    const int cols = join_db ? (int)ceil_div(N, 32) : 0;
     linear_sums_kernel<<<wgs + cols, 256, 0, s>>>(a.dw_part, splits, MN, a.dW, wgs, a.db_part, chunks, (int)N, a.db);
     return hipGetLastError();
   }

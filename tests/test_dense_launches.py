@@ -72,9 +72,12 @@ def test_decode_is_two_launches(kind, tmp_path):
         assert got[1][1] <= 256
 
 
-def test_linear_few_rows_stream(tmp_path):
-    few, many = launches([["fwd", 32, 1000, 2824, "gelu"], ["fwd", 33, 1000, 2824, "gelu"]], tmp_path)
-    assert "linear_few" in few[0][0] and not any("linear_few" in g[0] for g in many)
+def test_linear_streams_or_tiles(tmp_path):
+    """Streamed in groups of rows while the workgroups are about one round, in tiles beyond."""
+    sizes = [(1, 1024, 1536), (45, 1000, 2824), (512, 512, 512), (512, 1000, 2824), (40, 4096, 14336)]
+    got = launches([["fwd", *s, "gelu"] for s in sizes], tmp_path)
+    assert ["linear_few" in g[0][0] for g in got] == [True, True, True, False, False]
+    assert got[1][0][1:] == [23, 1, 3]
 
 
 def test_linear_whole_rounds(tmp_path):

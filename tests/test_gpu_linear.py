@@ -124,6 +124,18 @@ def test_large(T, k, n, act):
     print("shares of the bounds:", c.check_fwd(), c.check_bwd(), flush=True)
 
 
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T,k,n", [(17, 520, 136), (33, 264, 264), (100, 1032, 520), (257, 512, 512), (500, 2056, 72),
+                                   (1024, 64, 64), (130, 72, 4104), (2049, 72, 40)])
+def test_row_groups(T, k, n, act):
+    """Streamed products whose rows go to several groups, the last one short, with and without slices of k."""
+    c = Case(T, k, n, act, 8, bias=T % 2 == 0, residual=T % 3 != 0)
+    c.fwd()
+    c.bwd()
+    c.guards()
+    print("shares of the bounds:", c.check_fwd(), c.check_bwd(), flush=True)
+
+
 @pytest.mark.parametrize("T", [3, 50, 300])
 def test_parts(T):
     """Each output alone, without H, without bias and residual, R in place, on another stream."""
