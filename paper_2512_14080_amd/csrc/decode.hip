@@ -346,14 +346,14 @@ __device__ __forceinline__ void finish_item(int* counter) {
 // Wave 0 waits until the lanes' counters (lane i's where it has one) add up to `want`; then
 // the workgroup goes on.  A call that shares its workspace with another one in flight,
 // which is an error, may have lost counts: the wait is bounded (seconds), and false makes
-// the outputs NaN.
+// the outputs NaN.  `ok`: no wait before gave up (then this one does not wait either).
 constexpr int kMostPolls = 1 << 22;
 template <class Counter>
-__device__ __forceinline__ bool await(Counter counter, int want, int* sh) {
+__device__ __forceinline__ bool await(Counter counter, int want, int* sh, bool so_far = true) {
   if (threadIdx.x < kWave) {
     int* c = counter(lane_id());
     bool ok = false;
-    for (int i = 0; i < kMostPolls && !ok; ++i) {
+    for (int i = 0; i < (so_far ? kMostPolls : 1) && !ok; ++i) {
       if (i) __builtin_amdgcn_s_sleep(1);
       const int n = c ? __hip_atomic_load(c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
       ok = dpp_reduce(n, [](int x, int y) { return x + y; }) >= want;
@@ -361,7 +361,7 @@ __device__ __forceinline__ bool await(Counter counter, int want, int* sh) {
     if (threadIdx.x == 0) *sh = ok;
   }
   __syncthreads();  // (the loads behind it are shared ones, which no cache answers from before)
-  return *sh;
+  return so_far && *sh;
 }
 
 // ---------------------------------------------------------------- the layer
@@ -1051,7 +1051,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
       int next = 0;
       if (more && threadIdx.x == 0) next = take_ticket(a);
       int* counter = !UP ? tile_counter(a, t.tile) : BY_TOKEN ? ups_counter(a, item) : group_counter(a, t.gi);
-      if constexpr (!UP) ok = await([&](int l) { return l == 0 ? group_counter(a, t.gi) : nullptr; }, per_group, sh + 1) && ok;
+      if constexpr (!UP) ok = await([&](int l) { return l == 0 ? group_counter(a, t.gi) : nullptr; }, per_group, sh + 1, ok);
       while (t.cnt > D::MAX_ROWS) {  // (more rows than a pass takes: the weights again)
         D::template run<UP>(a, p, t, stream, part, dyn + picked_bytes(a.T, a.E, a.K), wave, []() {});
         t.r0 += D::MAX_ROWS;
@@ -1064,7 +1064,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
       });
       item = more ? __builtin_amdgcn_readfirstlane(sh[0]) - selects : total;
       asm volatile("" ::: "memory");
-      if (!ok) counter = ups_counter(a, 8);  // (what gave up is not counted, so that nothing is summed from it)
+      if (!ok) counter = a.sync + 1;  // (no one's: what gave up is not counted, so that nothing is summed from it)
       if (item >= end) {
         finish_item<0>(counter);
         return;
@@ -1083,13 +1083,13 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
       struct {
         const DecodeArgs& a; int ups; int* sh; bool* all;
         __device__ __forceinline__ void operator()() const {
-          *all = await([&](int l) { return l < 8 ? ups_counter(a, l) : nullptr; }, ups, sh) && *all;
+          *all = await([&](int l) { return l < 8 ? ups_counter(a, l) : nullptr; }, ups, sh, *all);
         }
         __device__ bool ok() const { return *all; }
       } wait{a, ups, sh + 1, &ok};
       TD::token_down(a, p, (typename TD::Part*)part, dyn + picked_bytes(a.T, a.E, a.K), wave, i / down_tiles, tile, wait);
     } else {
-      ok = await([&](int l) { return l == 0 ? tile_counter(a, tile) : nullptr; }, groups, sh + 1) && ok;
+      ok = await([&](int l) { return l == 0 ? tile_counter(a, tile) : nullptr; }, groups, sh + 1, ok);
       sum_tokens(a, p, down_cols, tile, i / down_tiles * sum_rows, sum_rows, ok);
     }
     if (!more) break;

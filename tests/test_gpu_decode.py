@@ -249,7 +249,7 @@ def test_graphs_that_share_a_workspace(quant):
 
 QUANT = [(1, 1536, 256, 128, 8, False), (1, 128, 64, 8, 2, True), (2, 256, 1088, 16, 16, True), (3, 512, 192, 16, 4, True),
          (9, 896, 192, 40, 3, True), (16, 256, 128, 8, 4, False), (20, 1280, 64, 128, 2, True), (33, 384, 320, 8, 8, False),
-         (64, 256, 128, 64, 8, True), (64, 256, 192, 512, 4, True)]
+         (64, 256, 128, 64, 8, True), (64, 256, 192, 512, 4, True), (48, 128, 960, 8, 6, False), (24, 512, 576, 16, 4, True)]
 
 
 @pytest.mark.parametrize("T,d,n,E,K,biases", QUANT)

@@ -114,9 +114,10 @@ def test_linear(T, k, n, pad, act):
 
 
 @pytest.mark.parametrize("T,k,n,act", [(20000, 512, 256, "swiglu"), (4100, 1544, 2056, "gelu"), (70, 8192, 512, "silu"),
-                                       (48, 8192, 2048, "none"), (9000, 256, 64, "relu"), (3, 16384, 1024, "swiglu")])
+                                       (48, 8192, 2048, "none"), (9000, 256, 64, "relu"), (3, 16384, 1024, "swiglu"),
+                                       (1777, 72, 14336, "swiglu"), (1777, 28672, 72, "relu")])
 def test_large(T, k, n, act):
-    """Many tiles and rounds, sliced reductions, split gradients."""
+    """Many tiles and rounds, sliced reductions, split gradients, whole rounds of columns apart (the last two)."""
     c = Case(T, k, n, act, 8)
     c.fwd()
     c.bwd()
