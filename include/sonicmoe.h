@@ -484,10 +484,8 @@ int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float
 
 /*
  * The same with 8-bit expert products, as moe_fwd_quant's: H = q(X) q(W1_e) (+ b1_e), Y =
- * q(A) q(W2_e) (+ b2_e), A quantised from fp32.  For one token, and where T K is at most 16
- * or E / 2 (with T d / 32 at most 160), the up-projection's codes are multiplied with fp32
- * sums, else by the block-scaled instruction, whose sums are 1.3e-5 of the result off: a
- * value of A next to the middle of two codes may then take the other one.
+ * q(A) q(W2_e) (+ b2_e), A quantised from fp32.  The up-projection's codes are multiplied
+ * with fp32 sums, so that A's codes are an fp32 form's but where a sum's order moves one.
  *   q   weights in state MOE_HELD_WRITTEN, of the same d, n and E
  *   ws  moe_workspace_bytes(dims, capacity, MOE_WS_DECODE_QUANT) bytes
  */

@@ -661,11 +661,13 @@ struct Decode {
 
 // The same with 8-bit weights (stream8_tile.h): a wave's step is one block of 128 k of 64 weight
 // columns, in the up-projection 32 gate columns and the matching up ones.  Rows are quantised
-// as they are loaded, X from bf16 and A from fp32.  EXACT: the up-projection's codes are
-// multiplied in bf16, with fp32 sums (as in the layer's 8-bit forward); the conversions bound it
-// where a workgroup has many items (32 tokens of a 30B-shaped layer: 206 us, 174 without, at
-// an earlier step).  MB = 2 is for groups of more than 16 rows.
-template <int MB, int NJ, bool EXACT>
+// as they are loaded, X from bf16 and A from fp32.  The up-projection's codes are multiplied
+// in bf16 (exact products), with fp32 sums: the 8-bit instruction's are 1.3e-5 of the result
+// off, which moves A's codes, and now and then a whole block's scale, to the other side of a
+// step (6 tokens of d 1536, n 256, E 128, K 8: one token's O 7e-3 off, so 1.7e-3).  It costs
+// 1%, since the weights bound it (32 tokens of a 30B-shaped layer: 150 us, 152 so).  MB = 2 is
+// for groups of more than 16 rows.
+template <int MB, int NJ>
 struct Decode8 {
   static constexpr int NBUF = 1, UP_COLS = 8 * NJ, DOWN_COLS = 16 * NJ, MAX_ROWS = 16 * MB;
   static size_t stage_bytes(int n) { return (size_t)q_blocks(n) * MB * kStageBlock; }
@@ -678,7 +680,7 @@ struct Decode8 {
     // This wave's first block, the end, from a block to the next, and its steps, which begin
     // at step `rot`: where rows are 4 KB apart, one block of them all lies in few memory channels,
     // and items that all began there would ask the same ones (32 tokens of a 30B-shaped layer:
-    // 161 us, 148 so; 64: 184, 167)
+    // 161 us, 148 so; 64 184 and 167)
     int kb, end, step, ns, rot;
     __device__ __forceinline__ void turn(int by) {
       ns = max((end - kb + step - 1) / step, 1);
@@ -784,7 +786,7 @@ struct Decode8 {
 #pragma unroll
           for (int j = 0; j < NJ; ++j) {
             const int ws = s.sv[q][2 * j / NJ];
-            if constexpr (EXACT && !F32) {
+            if constexpr (!F32) {
               f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
               for (int h = 0; h < 4; ++h)
@@ -1163,13 +1165,15 @@ hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
   if (e != hipSuccess) return e;
   // one row block where a group seldom has more than its 16 rows
   const bool one = a.T <= 16 || a.T * a.K <= 6 * a.E;
-  using Q1 = Decode8<1, 4, true>;
+  using Q1 = Decode8<1, 4>;
   using B1 = Decode<1, 1>;
   using BT = Decode<4, 1>;
   if (q8) {
     if (by_token) return run_decode<Q1, Q1::Token, true>(a, s);
-    if (a.T * a.K <= 16) return run_decode<Q1, Q1::Token, false>(a, s);
-    return one ? run_decode<Decode8<1, 8, false>, Q1::Token, false>(a, s) : run_decode<Decode8<2, 4, false>, Q1::Token, false>(a, s);
+    // smaller tiles for few items (8 tokens of d 1024, n 256, E 64, K 8 26.1 us, 26.8 in the
+    // larger; 16 of d 1536, n 256, E 128, K 8 47.1 and 43.3)
+    if (a.T * a.K <= 64) return run_decode<Q1, Q1::Token, false>(a, s);
+    return one ? run_decode<Decode8<1, 8>, Q1::Token, false>(a, s) : run_decode<Decode8<2, 4>, Q1::Token, false>(a, s);
   }
   if (by_token) return run_decode<B1, BT, true>(a, s);
   return one ? run_decode<B1, BT, false>(a, s) : run_decode<Decode<1, 2>, BT, false>(a, s);
