@@ -161,6 +161,8 @@ class DeviceLayer:
                          stream, eb=self.eb)
 
     def quantize_experts(self, stream=None):
+        if self.qw is None:
+            raise ValueError('quantize_experts needs held8="quant"')
         B.moe_quantize_experts(self.D, self.W1, self.W2, self.qw, stream)
 
 
@@ -174,6 +176,8 @@ class SharedExpert:
         d, m = Wu.shape[0], Wd.shape[0]
         if Wu.shape != (d, 2 * m) or Wd.shape != (m, d):
             raise ValueError(f"Wu must be [d, 2m] and Wd [m, d] (got {tuple(Wu.shape)}, {tuple(Wd.shape)})")
+        if not (Wu.is_contiguous() and Wd.is_contiguous()):
+            raise ValueError("Wu and Wd must be contiguous")
         self.Wu, self.Wd, self.bu, self.bd = Wu, Wd, bu, bd
         self.up, self.down = B.linear_dims(T, d, m, "swiglu"), B.linear_dims(T, m, d)
         dev, bf16, f32 = Wu.device, torch.bfloat16, torch.float32

@@ -151,3 +151,12 @@ def test_linear_refuses_arguments():
         assert bwd(**{k: v}) == inv, (k, B.moe_last_error())
         assert "overlap" in B.moe_last_error()
     assert bwd(dw=O) == inv  # dX and dW in one place
+
+
+def test_shared_expert_refuses():
+    import torch
+    from paper_2512_14080_amd.layer import SharedExpert
+    Wu, Wd = torch.zeros(64, 48, dtype=torch.bfloat16), torch.zeros(24, 64, dtype=torch.bfloat16)
+    for wu, wd in ((Wu, Wd[:, :32]), (Wu[:, :40], Wd), (Wu.t().contiguous().t(), Wd), (Wu, Wd.t().contiguous().t())):
+        with pytest.raises(ValueError):
+            SharedExpert(4, wu, wd)
