@@ -247,6 +247,33 @@ def test_graphs_that_share_a_workspace(quant):
             assert torch.equal(c.results()[0], o), rep
 
 
+def test_calls_at_once_on_streams_of_their_own():
+    """Calls under way together, each with its workspace: as alone."""
+    torch = _t()
+    from paper_2512_14080_amd import binding as B
+    work = []
+    for T, d, n, E, K, quant in ((1, 1536, 256, 128, 8, False), (7, 1024, 256, 64, 8, False), (40, 512, 192, 32, 4, False),
+                                 (16, 1536, 256, 128, 8, True)):
+        x = _inputs(T, d, n, E, K, 400 + T)
+        call, q = Call(T, d, n, E, K, quant), None
+        if quant:
+            q = B.QExperts(call.D)
+            B.moe_quantize_experts(call.D, x[3], x[4], q)
+        call(*x, q=q)
+        alone = call.results()
+        work.append((call, x, q, alone, torch.cuda.Stream()))
+    for rep in range(3):
+        for call, *_ in work:
+            call.O[:call.T * call.d].fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for call, x, q, _, side in work:
+                call(*x, q=q, stream=side)
+        torch.cuda.synchronize()
+        for call, _, _, alone, _ in work:
+            assert all(torch.equal(a, b) for a, b in zip(call.results(), alone)), (rep, call.T)
+
+
 QUANT = [(1, 1536, 256, 128, 8, False), (1, 128, 64, 8, 2, True), (2, 256, 1088, 16, 16, True), (3, 512, 192, 16, 4, True),
          (9, 896, 192, 40, 3, True), (16, 256, 128, 8, 4, False), (20, 1280, 64, 128, 2, True), (33, 384, 320, 8, 8, False),
          (64, 256, 128, 64, 8, True), (64, 256, 192, 512, 4, True), (48, 128, 960, 8, 6, False), (24, 512, 576, 16, 4, True)]
