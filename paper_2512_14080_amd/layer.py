@@ -35,6 +35,26 @@ def bf16_to_f32(t) -> np.ndarray:
     return t.detach().float().cpu().numpy()
 
 
+def _row_stride(name, t, rows, cols, device):
+    """The elements from a row to the next of t, bf16 [rows, cols] on the device with whole rows that do not overlap, as the
+    dense products take them (0: one after the other)."""
+    import torch
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols) or t.device != device:
+        raise ValueError(f"{name} must be bfloat16 [{rows}, {cols}] on {device} (got {t.dtype} {tuple(t.shape)} on {t.device})")
+    if t.stride(1) != 1 or (rows > 1 and not cols <= t.stride(0) < 1 << 30):
+        raise ValueError(f"the rows of {name} must be whole and apart (got strides {t.stride()})")
+    return t.stride(0) if rows > 1 else 0
+
+
+def _check_device(device, stream):
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"the tensors must be on a GPU (they are on {device})")
+    for at in [torch.device("cuda", torch.cuda.current_device())] + ([] if stream is None else [stream.device]):
+        if at != device:
+            raise ValueError(f"the tensors are on {device}, the current device or the stream is {at}")
+
+
 class DeviceLayer:
     """All device tensors of one layer invocation.
 
@@ -169,7 +189,10 @@ class DeviceLayer:
 class SharedExpert:
     """A dense SwiGLU expert that every token passes through, beside the routed ones:
     Y = R + (SiLU(X Wu_gate) * X Wu_up) Wd, with Wu [d,2m] (gate columns first) and Wd [m,d] in bf16 and optional fp32
-    biases [2m] and [d].  ``train`` keeps what the backward reads."""
+    biases [2m] and [d].  ``train`` keeps what the backward reads.
+
+    X, Y, R and the gradients are bf16 [T,d] of exactly T rows; rows may be further apart than they are long (by a
+    multiple of 8 elements), and what lies between them is neither read nor written."""
 
     def __init__(self, T, Wu, Wd, bu=None, bd=None, train=False):
         import torch
@@ -178,13 +201,14 @@ class SharedExpert:
             raise ValueError(f"Wu must be [d, 2m] and Wd [m, d] (got {tuple(Wu.shape)}, {tuple(Wd.shape)})")
         if not (Wu.is_contiguous() and Wd.is_contiguous()):
             raise ValueError("Wu and Wd must be contiguous")
+        self.T, self.d, self.m = T, d, m
         self.Wu, self.Wd, self.bu, self.bd = Wu, Wd, bu, bd
-        self.up, self.down = B.linear_dims(T, d, m, "swiglu"), B.linear_dims(T, m, d)
         dev, bf16, f32 = Wu.device, torch.bfloat16, torch.float32
 
         def workspace(which):
-            sizes = (B.moe_linear_workspace_bytes(L, which) for L in (self.up, self.down))
-            return _aligned_empty(max(sizes), dev)
+            # (of any stride: rows that pass 32-bit offsets go another way, whose workspace may be the larger)
+            forms = (self._up(0), self._up((1 << 30) - 8), self._down(0, 0))
+            return _aligned_empty(max(B.moe_linear_workspace_bytes(L, which) for L in forms), dev)
 
         def like(t):
             return None if t is None else torch.empty_like(t)
@@ -197,11 +221,28 @@ class SharedExpert:
             self.dA, self.ws_b = torch.empty_like(self.A), workspace(B.MOE_WS_LINEAR_BWD)
             self.dWu, self.dWd, self.dbu, self.dbd = like(Wu), like(Wd), like(bu), like(bd)
 
+    def _up(self, ldx):
+        return B.linear_dims(self.T, self.d, self.m, "swiglu", ldx=ldx)
+
+    def _down(self, ldr, ldy):
+        return B.linear_dims(self.T, self.m, self.d, ldr=ldr, ldy=ldy)
+
+    def _stride(self, name, t):
+        return 0 if t is None else _row_stride(name, t, self.T, self.d, self.Wu.device)
+
     def forward(self, X, Y, R=None, stream=None):
-        B.moe_linear_fwd(self.up, X, self.Wu, self.bu, None, self.H, self.A, self.ws_f, stream)
-        B.moe_linear_fwd(self.down, self.A, self.Wd, self.bd, R, None, Y, self.ws_f, stream)
+        up, down = self._up(self._stride("X", X)), self._down(self._stride("R", R), self._stride("Y", Y))
+        _check_device(self.Wu.device, stream)
+        B.moe_linear_fwd(up, X, self.Wu, self.bu, None, self.H, self.A, self.ws_f, stream)
+        B.moe_linear_fwd(down, self.A, self.Wd, self.bd, R, None, Y, self.ws_f, stream)
 
     def backward(self, dY, X, dX, G=None, stream=None):
-        """dX = the gradient through this expert + G (which may be dX itself), and dWu, dWd, dbu, dbd."""
-        B.moe_linear_bwd(self.down, dY, self.A, self.Wd, None, None, self.dA, self.dWd, self.dbd, self.ws_b, stream)
-        B.moe_linear_bwd(self.up, self.dA, X, self.Wu, self.H, G, dX, self.dWu, self.dbu, self.ws_b, stream)
+        """dX = the gradient through this expert + G (which may be dX itself), and dWu, dWd, dbu, dbd.  X, dX and G have
+        their rows equally far apart."""
+        down, ldx = self._down(0, self._stride("dY", dY)), self._stride("X", X)
+        for name, t in (("dX", dX), ("G", G)):
+            if t is not None and self._stride(name, t) != ldx:
+                raise ValueError(f"the rows of X and {name} must be equally far apart (got {X.stride()}, {t.stride()})")
+        _check_device(self.Wu.device, stream)
+        B.moe_linear_bwd(down, dY, self.A, self.Wd, None, None, self.dA, self.dWd, self.dbd, self.ws_b, stream)
+        B.moe_linear_bwd(self._up(ldx), self.dA, X, self.Wu, self.H, G, dX, self.dWu, self.dbu, self.ws_b, stream)

@@ -1,0 +1,76 @@
+"""What layer.SharedExpert and DeviceLayer.decode refuse of their tensors, before any call of the library (no GPU needed)."""
+import os
+
+import pytest
+import torch
+
+from paper_2512_14080_amd import binding as B
+from paper_2512_14080_amd.layer import SharedExpert
+
+pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="libsonicmoe.so not built")
+T, D, M = 6, 64, 24
+
+
+def _bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def _shared(T=T, **kw):
+    return SharedExpert(T, _bf16(D, 2 * M), _bf16(M, D), **kw)
+
+
+BAD_ROWS = {
+    "fewer rows": lambda: _bf16(T - 1, D),
+    "more rows": lambda: _bf16(T + 1, D),
+    "other columns": lambda: _bf16(T, D + 8),
+    "fp32": lambda: torch.zeros(T, D),
+    "fp16": lambda: torch.zeros(T, D, dtype=torch.float16),
+    "a vector": lambda: _bf16(T * D),
+    "transposed": lambda: _bf16(D, T).t(),
+    "every other column": lambda: _bf16(T, 2 * D)[:, ::2],
+    "one row for all": lambda: _bf16(1, D).expand(T, D),
+    "rows that overlap": lambda: _bf16(T * D).as_strided((T, D), (D - 8, 1)),
+    "another device": lambda: torch.empty((T, D), dtype=torch.bfloat16, device="meta"),
+}
+
+
+@pytest.mark.parametrize("bad", BAD_ROWS)
+def test_shared_expert_refuses_rows(bad):
+    s, good, t = _shared(train=True), _bf16(T, D), BAD_ROWS[bad]()
+    for args in ((t, good), (good, t), (good, good, t)):
+        with pytest.raises(ValueError, match="^(X|Y|R) must be|^the rows of (X|Y|R) must"):
+            s.forward(*args)
+    for args in ((t, good, good), (good, t, good), (good, good, t), (good, good, good, t)):
+        with pytest.raises(ValueError, match="^(dY|X|dX|G) must be|^the rows of (dY|X|dX|G) must"):
+            s.backward(*args)
+
+
+def test_shared_expert_refuses_unlike_strides_of_x():
+    """X, dX and G have one stride in the library's call."""
+    s, good, wide = _shared(train=True), _bf16(T, D), _bf16(T, D + 8)[:, :D]
+    for args in ((good, good, wide), (good, wide, good), (good, good, good, wide)):
+        with pytest.raises(ValueError, match="equally far apart"):
+            s.backward(*args)
+
+
+def test_shared_expert_needs_a_gpu():
+    s, good, wide = _shared(train=True), _bf16(T, D), _bf16(T, D + 8)[:, :D]
+    for x in (good, wide):
+        with pytest.raises(ValueError, match="must be on a GPU"):
+            s.forward(x, good, wide)
+        with pytest.raises(ValueError, match="must be on a GPU"):
+            s.backward(wide, x, x, x)
+    one = _shared(1)  # (one row: its stride means nothing)
+    with pytest.raises(ValueError, match="must be on a GPU"):
+        one.forward(_bf16(D, 1).t(), _bf16(1, D))
+
+
+def test_shared_expert_workspace_holds_any_stride():
+    for t, d, m in ((1, 64, 24), (16, 8192, 256), (64, 4096, 512), (300, 16384, 64)):
+        s = SharedExpert(t, _bf16(d, 2 * m), _bf16(m, d), train=True)
+        for ld in (0, d + 8, (1 << 30) - 8):
+            assert s.ws_f.numel() >= B.moe_linear_workspace_bytes(B.linear_dims(t, d, m, "swiglu", ldx=ld), B.MOE_WS_LINEAR_FWD)
+            assert s.ws_b.numel() >= B.moe_linear_workspace_bytes(B.linear_dims(t, d, m, "swiglu", ldx=ld), B.MOE_WS_LINEAR_BWD)
+            down = B.linear_dims(t, m, d, ldr=ld, ldy=ld)
+            assert s.ws_f.numel() >= B.moe_linear_workspace_bytes(down, B.MOE_WS_LINEAR_FWD)
+            assert s.ws_b.numel() >= B.moe_linear_workspace_bytes(down, B.MOE_WS_LINEAR_BWD)
