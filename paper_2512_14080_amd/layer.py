@@ -35,6 +35,12 @@ def bf16_to_f32(t) -> np.ndarray:
     return t.detach().float().cpu().numpy()
 
 
+def _check_tensor(name, t, dtype, shape, device):
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on {device} (got {t.dtype} {list(t.shape)}, strides "
+                         f"{t.stride()}, on {t.device})")
+
+
 def _row_stride(name, t, rows, cols, device):
     """The elements from a row to the next of t, bf16 [rows, cols] on the device with whole rows that do not overlap, as the
     dense products take them (0: one after the other)."""
@@ -201,6 +207,11 @@ class SharedExpert:
             raise ValueError(f"Wu must be [d, 2m] and Wd [m, d] (got {tuple(Wu.shape)}, {tuple(Wd.shape)})")
         if not (Wu.is_contiguous() and Wd.is_contiguous()):
             raise ValueError("Wu and Wd must be contiguous")
+        if Wu.dtype != torch.bfloat16 or Wd.dtype != torch.bfloat16 or Wd.device != Wu.device:
+            raise ValueError(f"Wu and Wd must be bfloat16 on one device (got {Wu.dtype} on {Wu.device}, {Wd.dtype} on {Wd.device})")
+        for name, b, size in (("bu", bu, 2 * m), ("bd", bd, d)):
+            if b is not None:
+                _check_tensor(name, b, torch.float32, (size,), Wu.device)
         self.T, self.d, self.m = T, d, m
         self.Wu, self.Wd, self.bu, self.bd = Wu, Wd, bu, bd
         dev, bf16, f32 = Wu.device, torch.bfloat16, torch.float32

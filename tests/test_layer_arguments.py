@@ -74,3 +74,17 @@ def test_shared_expert_workspace_holds_any_stride():
             down = B.linear_dims(t, m, d, ldr=ld, ldy=ld)
             assert s.ws_f.numel() >= B.moe_linear_workspace_bytes(down, B.MOE_WS_LINEAR_FWD)
             assert s.ws_b.numel() >= B.moe_linear_workspace_bytes(down, B.MOE_WS_LINEAR_BWD)
+
+
+@pytest.mark.parametrize("name,bad", [
+    ("bu", lambda: _bf16(2 * M)), ("bu", lambda: torch.zeros(M)), ("bu", lambda: torch.zeros(2 * M, dtype=torch.float64)),
+    ("bu", lambda: torch.zeros(4 * M)[::2]), ("bu", lambda: torch.zeros(1).expand(2 * M)), ("bu", lambda: torch.zeros(1, 2 * M)),
+    ("bd", lambda: _bf16(D)), ("bd", lambda: torch.zeros(D - 8)), ("bd", lambda: torch.zeros(D, device="meta")),
+    ("Wu", lambda: torch.zeros(D, 2 * M)), ("Wd", lambda: torch.zeros(M, D, dtype=torch.float16)),
+    ("Wd", lambda: torch.empty((M, D), dtype=torch.bfloat16, device="meta")),
+])
+def test_shared_expert_refuses_weights_and_biases(name, bad):
+    args = {"Wu": _bf16(D, 2 * M), "Wd": _bf16(M, D), "bu": torch.zeros(2 * M), "bd": torch.zeros(D)}
+    SharedExpert(T, **args)
+    with pytest.raises(ValueError, match=name):
+        SharedExpert(T, **{**args, name: bad()})
