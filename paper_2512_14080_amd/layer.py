@@ -250,6 +250,8 @@ class SharedExpert:
     def backward(self, dY, X, dX, G=None, stream=None):
         """dX = the gradient through this expert + G (which may be dX itself), and dWu, dWd, dbu, dbd.  X, dX and G have
         their rows equally far apart."""
+        if self.H is None:
+            raise ValueError("backward needs train=True")
         down, ldx = self._down(0, self._stride("dY", dY)), self._stride("X", X)
         for name, t in (("dX", dX), ("G", G)):
             if t is not None and self._stride(name, t) != ldx:

@@ -88,3 +88,8 @@ def test_shared_expert_refuses_weights_and_biases(name, bad):
     SharedExpert(T, **args)
     with pytest.raises(ValueError, match=name):
         SharedExpert(T, **{**args, name: bad()})
+
+
+def test_shared_expert_backward_needs_train():
+    with pytest.raises(ValueError, match="train=True"):
+        _shared().backward(_bf16(T, D), _bf16(T, D), _bf16(T, D))
