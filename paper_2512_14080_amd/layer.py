@@ -35,21 +35,29 @@ def bf16_to_f32(t) -> np.ndarray:
     return t.detach().float().cpu().numpy()
 
 
-def _check_tensor(name, t, dtype, shape, device):
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)} on {device} (got {t.dtype} {list(t.shape)}, strides "
-                         f"{t.stride()}, on {t.device})")
+def _whole(t, rows, cols):
+    """Whether t is contiguous and holds rows of cols elements, under any leading shape ([b,s,cols]) or none."""
+    return t.is_contiguous() and t.numel() == rows * cols and (t.dim() == 1 or t.shape[-1] == cols)
+
+
+def _check_tensor(name, t, dtype, rows, cols, device):
+    if t.dtype != dtype or t.device != device or not _whole(t, rows, cols):
+        raise ValueError(f"{name} must be contiguous {dtype} [{rows}, {cols}] on {device} (got {t.dtype} {list(t.shape)}, "
+                         f"strides {t.stride()}, on {t.device})")
 
 
 def _row_stride(name, t, rows, cols, device):
     """The elements from a row to the next of t, bf16 [rows, cols] on the device with whole rows that do not overlap, as the
     dense products take them (0: one after the other)."""
     import torch
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, cols) or t.device != device:
-        raise ValueError(f"{name} must be bfloat16 [{rows}, {cols}] on {device} (got {t.dtype} {tuple(t.shape)} on {t.device})")
-    if t.stride(1) != 1 or (rows > 1 and not cols <= t.stride(0) < 1 << 30):
+    whole = _whole(t, rows, cols)
+    if t.dtype != torch.bfloat16 or t.device != device or not (whole or tuple(t.shape) == (rows, cols)):
+        raise ValueError(f"{name} must be bfloat16 [{rows}, {cols}] on {device} (got {t.dtype} {list(t.shape)} on {t.device})")
+    if whole or (rows == 1 and t.stride(1) == 1):
+        return 0
+    if t.stride(1) != 1 or not cols <= t.stride(0) < 1 << 30:
         raise ValueError(f"the rows of {name} must be whole and apart (got strides {t.stride()})")
-    return t.stride(0) if rows > 1 else 0
+    return t.stride(0)
 
 
 def _check_device(device, stream):
@@ -197,7 +205,7 @@ class SharedExpert:
     Y = R + (SiLU(X Wu_gate) * X Wu_up) Wd, with Wu [d,2m] (gate columns first) and Wd [m,d] in bf16 and optional fp32
     biases [2m] and [d].  ``train`` keeps what the backward reads.
 
-    X, Y, R and the gradients are bf16 [T,d] of exactly T rows; rows may be further apart than they are long (by a
+    X, Y, R and the gradients are bf16 [T,d] of exactly T rows (contiguous ones under any leading shape); rows may be further apart than they are long (by a
     multiple of 8 elements), and what lies between them is neither read nor written."""
 
     def __init__(self, T, Wu, Wd, bu=None, bd=None, train=False):
@@ -211,7 +219,7 @@ class SharedExpert:
             raise ValueError(f"Wu and Wd must be bfloat16 on one device (got {Wu.dtype} on {Wu.device}, {Wd.dtype} on {Wd.device})")
         for name, b, size in (("bu", bu, 2 * m), ("bd", bd, d)):
             if b is not None:
-                _check_tensor(name, b, torch.float32, (size,), Wu.device)
+                _check_tensor(name, b, torch.float32, 1, size, Wu.device)
         self.T, self.d, self.m = T, d, m
         self.Wu, self.Wd, self.bu, self.bd = Wu, Wd, bu, bd
         dev, bf16, f32 = Wu.device, torch.bfloat16, torch.float32

@@ -25,8 +25,9 @@ BAD_ROWS = {
     "other columns": lambda: _bf16(T, D + 8),
     "fp32": lambda: torch.zeros(T, D),
     "fp16": lambda: torch.zeros(T, D, dtype=torch.float16),
-    "a vector": lambda: _bf16(T * D),
+    "columns for rows": lambda: _bf16(D, T),
     "transposed": lambda: _bf16(D, T).t(),
+    "rows apart in three dimensions": lambda: _bf16(2, T // 2, D + 8)[..., :D],
     "every other column": lambda: _bf16(T, 2 * D)[:, ::2],
     "one row for all": lambda: _bf16(1, D).expand(T, D),
     "rows that overlap": lambda: _bf16(T * D).as_strided((T, D), (D - 8, 1)),
@@ -55,7 +56,7 @@ def test_shared_expert_refuses_unlike_strides_of_x():
 
 def test_shared_expert_needs_a_gpu():
     s, good, wide = _shared(train=True), _bf16(T, D), _bf16(T, D + 8)[:, :D]
-    for x in (good, wide):
+    for x in (good, wide, good.view(2, -1, D), good.view(-1)):
         with pytest.raises(ValueError, match="must be on a GPU"):
             s.forward(x, good, wide)
         with pytest.raises(ValueError, match="must be on a GPU"):
@@ -78,7 +79,7 @@ def test_shared_expert_workspace_holds_any_stride():
 
 @pytest.mark.parametrize("name,bad", [
     ("bu", lambda: _bf16(2 * M)), ("bu", lambda: torch.zeros(M)), ("bu", lambda: torch.zeros(2 * M, dtype=torch.float64)),
-    ("bu", lambda: torch.zeros(4 * M)[::2]), ("bu", lambda: torch.zeros(1).expand(2 * M)), ("bu", lambda: torch.zeros(1, 2 * M)),
+    ("bu", lambda: torch.zeros(4 * M)[::2]), ("bu", lambda: torch.zeros(1).expand(2 * M)), ("bu", lambda: torch.zeros(M, 2)),
     ("bd", lambda: _bf16(D)), ("bd", lambda: torch.zeros(D - 8)), ("bd", lambda: torch.zeros(D, device="meta")),
     ("Wu", lambda: torch.zeros(D, 2 * M)), ("Wd", lambda: torch.zeros(M, D, dtype=torch.float16)),
     ("Wd", lambda: torch.empty((M, D), dtype=torch.bfloat16, device="meta")),
