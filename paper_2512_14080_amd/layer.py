@@ -180,9 +180,16 @@ class DeviceLayer:
 
     def decode(self, R=None, stream=None, topk_idx=None, topk_w=None):
         """The forward of a few tokens (T <= MOE_DECODE_MAX_T) in one call, routing included: O = R + the layer's output.
+        R is bf16 [T,d]; topk_idx (int32) and topk_w (fp32), [T,K], take the selection.
         Token choice only, on the 8-bit weights with held8="quant" (quantise them first: quantize_experts)."""
         if self.round_mode:
             raise ValueError("decode routes by token choice: round_mode must be None")
+        import torch
+        for name, t, dtype, cols in (("R", R, torch.bfloat16, self.d), ("topk_idx", topk_idx, torch.int32, self.K),
+                                     ("topk_w", topk_w, torch.float32, self.K)):
+            if t is not None:
+                _check_tensor(name, t, dtype, self.T, cols, self.X.device)
+        _check_device(self.X.device, stream)
         if self.ws_d is None:
             which = B.MOE_WS_DECODE_QUANT if self.qw is not None else B.MOE_WS_DECODE
             nbytes = B.moe_workspace_bytes(self.D, self.T * self.K, which)

@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2512_14080_amd import binding as B
-from paper_2512_14080_amd.layer import SharedExpert
+from paper_2512_14080_amd import workloads as W
+from paper_2512_14080_amd.layer import DeviceLayer, SharedExpert
 
 pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="libsonicmoe.so not built")
 T, D, M = 6, 64, 24
@@ -94,3 +95,38 @@ def test_shared_expert_refuses_weights_and_biases(name, bad):
 def test_shared_expert_backward_needs_train():
     with pytest.raises(ValueError, match="train=True"):
         _shared().backward(_bf16(T, D), _bf16(T, D), _bf16(T, D))
+
+
+# ------------------------------------------------------------------ decode
+CFG = W.MoEConfig("decode", T=5, d=128, n=64, E=8, K=2, m_tile=64)
+
+
+def _layer(**kw):
+    return DeviceLayer(W.make_inputs(CFG, 3), device="cpu", **kw)
+
+
+BAD_DECODE = {
+    "R of fewer rows": lambda: {"R": _bf16(4, 128)},
+    "R of other columns": lambda: {"R": _bf16(5, 64)},
+    "R in fp32": lambda: {"R": torch.zeros(5, 128)},
+    "R with rows apart": lambda: {"R": _bf16(5, 136)[:, :128]},
+    "one row of R for all": lambda: {"R": _bf16(1, 128).expand(5, 128)},
+    "R elsewhere": lambda: {"R": torch.empty((5, 128), dtype=torch.bfloat16, device="meta")},
+    "topk_idx in 64 bits": lambda: {"topk_idx": torch.zeros((5, 2), dtype=torch.int64)},
+    "topk_idx of fewer rows": lambda: {"topk_idx": torch.zeros((4, 2), dtype=torch.int32)},
+    "topk_idx of one column": lambda: {"topk_idx": torch.zeros((5, 1), dtype=torch.int32)},
+    "topk_w in bf16": lambda: {"topk_w": _bf16(5, 2)},
+    "topk_w transposed": lambda: {"topk_w": torch.zeros((2, 5)).t()},
+}
+
+
+@pytest.mark.parametrize("bad", BAD_DECODE)
+def test_decode_refuses_tensors(bad):
+    kw = BAD_DECODE[bad]()
+    with pytest.raises(ValueError, match=f"{next(iter(kw))} must be"):
+        _layer().decode(**kw)
+
+
+def test_decode_needs_a_gpu():
+    with pytest.raises(ValueError, match="must be on a GPU"):
+        _layer().decode(_bf16(5, 128), topk_idx=torch.zeros((5, 2), dtype=torch.int32), topk_w=torch.zeros((5, 2)))
