@@ -184,6 +184,8 @@ class DeviceLayer:
         Token choice only, on the 8-bit weights with held8="quant" (quantise them first: quantize_experts)."""
         if self.round_mode:
             raise ValueError("decode routes by token choice: round_mode must be None")
+        if self.route_flags & B.MOE_ROUTE_SCORES_IN:
+            raise ValueError("decode routes by softmax(X Wr + bias): scores_in must be None")
         import torch
         for name, t, dtype, cols in (("R", R, torch.bfloat16, self.d), ("topk_idx", topk_idx, torch.int32, self.K),
                                      ("topk_w", topk_w, torch.float32, self.K)):

@@ -130,3 +130,11 @@ def test_decode_refuses_tensors(bad):
 def test_decode_needs_a_gpu():
     with pytest.raises(ValueError, match="must be on a GPU"):
         _layer().decode(_bf16(5, 128), topk_idx=torch.zeros((5, 2), dtype=torch.int32), topk_w=torch.zeros((5, 2)))
+
+
+def test_decode_refuses_given_scores():
+    """route and step go by the scores given to the layer, which the call cannot take."""
+    import numpy as np
+    scores = np.random.default_rng(0).random((5, 8), np.float32)
+    with pytest.raises(ValueError, match="scores_in"):
+        _layer(scores_in=scores).decode()
