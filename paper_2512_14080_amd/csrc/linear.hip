@@ -679,7 +679,7 @@ static LinearPlan forward_plan(int T, int k, int n, int act, int64_t ldx) {
   const int64_t tiles = ceil_div(N, 128 / kb);
   int slices = 1;
   // k slices where a workgroup would read more than 256 KB on its own
-  while (2 * slices * tiles <= kCus && 2 * slices <= kLinearMaxSlices && k / slices * (256 / kb) > 256 * 1024) slices *= 2;
+  while (2 * slices * tiles <= kCus && 2 * slices <= kLinearMaxSlices && (int64_t)(k / slices) * (256 / kb) > 256 * 1024) slices *= 2;
   const int chunk = (int)ceil_div(ceil_div(k, slices), 128) * 128;
   slices = (int)ceil_div(k, chunk);
   return {true, kb, 1, 0, 0, false, slices, chunk, 0};
