@@ -530,6 +530,7 @@ int moe_linear_fwd(moe_linear l, const moe_bf16 *X, const moe_bf16 *W, const flo
 /*
  * The gradients at the kept H (dR is dY itself):
  *   dP = dY * act'(H);  dX = dP W^T + G;  dW = X^T dP;  db = column sums of dP
+ * MOE_ACT_RELU: dP is dY where H > 0 and 0 elsewhere, whatever dY is there.
  *   dY [T,n] bf16, with ldy between rows;  H as written by moe_linear_fwd, null and not
  *      read with MOE_ACT_NONE
  *   G  [T,k] bf16, nullable: what reaches X by its other ways, with ldx between rows;

@@ -33,17 +33,17 @@ __device__ __forceinline__ float act_value(int act, float h) {
     default: return h;
   }
 }
-// act'(h)
-__device__ __forceinline__ float act_slope(int act, float h) {
+// d act'(h); ReLU lets d through or not, so that an infinite d of a unit that is off is none
+__device__ __forceinline__ float act_grad(int act, float h, float d) {
   switch (act) {
-    case MOE_ACT_RELU: return h > 0.f ? 1.f : 0.f;
+    case MOE_ACT_RELU: return h > 0.f ? d : 0.f;
     case MOE_ACT_SILU: {
       const float s = fast_sigmoid(h);
-      return s * (1.f + h * (1.f - s));
+      return d * (s * (1.f + h * (1.f - s)));
     }
     case MOE_ACT_GELU:
-      return 0.5f * (1.f + erff(h * 0.70710678118654752f)) + h * 0.39894228040143268f * __expf(-0.5f * h * h);
-    default: return 1.f;
+      return d * (0.5f * (1.f + erff(h * 0.70710678118654752f)) + h * 0.39894228040143268f * __expf(-0.5f * h * h));
+    default: return d;
   }
 }
 
@@ -511,7 +511,7 @@ __global__ __launch_bounds__(256) void linear_dp_kernel(const LinearBwdArgs a, i
           *(u32x4*)(a.dP + t * N + n + col) = o2;
         } else {
 #pragma unroll
-          for (int q = 0; q < 8; ++q) d[q] *= act_slope(a.act, q & 1 ? bf_hi(h[q / 2]) : bf_lo(h[q / 2]));
+          for (int q = 0; q < 8; ++q) d[q] = act_grad(a.act, q & 1 ? bf_hi(h[q / 2]) : bf_lo(h[q / 2]), d[q]);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) o[q] = pack_bf2(d[2 * q], d[2 * q + 1]);
