@@ -474,8 +474,9 @@ int moe_bwd_ckpt(moe_dims dims, const moe_bf16 *dO, const moe_bf16 *X, const moe
  *   topk_idx, topk_w   [T,K] out, nullable: the selection by (score descending, expert
  *         ascending) and its weights, as moe_route writes them
  *   ws    moe_workspace_bytes(dims, capacity, MOE_WS_DECODE) bytes.  Calls that share
- *         one must be ordered, like those of moe_fwd: of two at once either waits
- *         (for seconds at most) for counts that the other took, and then writes NaN.
+ *         one must be ordered, like those of moe_fwd: of two at once the results are
+ *         undefined (NaN where a wait for counts that the other took gave up), and either
+ *         may take seconds; both end, and touch nothing but their operands.
  */
 enum { MOE_DECODE_MAX_T = 64 };
 int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float *bias, const moe_bf16 *W1,

@@ -27,6 +27,7 @@
 // 5.4 TB/s.
 #include <algorithm>
 
+#include "decode_queue.h"
 #include "launch.h"
 #include "stream8_tile.h"
 #include "stream_tile.h"
@@ -241,8 +242,9 @@ __device__ __forceinline__ void weigh_token(const DecodeArgs& a, const Picked& p
   float sum = 0.f;
   for (int k = 0; k < a.K; ++k) sum += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), k));
   if (lane >= a.K) return;
-  const int e = p.sel[i];
+  const int e = expert_within((uint32_t)p.sel[i], a.E);
   const float w = x / sum;
+  p.sel[i] = e;
   p.w[i] = w;
   if (all) store8_shared(buffer_of(a.picked, (uint32_t)a.T * a.K * 8), i * 8, u32x2{(uint32_t)e, __float_as_uint(w)});
   if (out && a.topk_idx) a.topk_idx[i] = e;
@@ -277,7 +279,7 @@ __device__ __forceinline__ void select_some(const DecodeArgs& a, const Picked& p
 __device__ __forceinline__ void read_selection(const DecodeArgs& a, const Picked& p, bool ok) {
   for (int i = threadIdx.x; i < a.T * a.K; i += kDecodeThreads) {
     const uint64_t v = __hip_atomic_load((uint64_t*)a.picked + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    p.sel[i] = ok ? (int)(uint32_t)v : i % a.K;  // (a selection even where the wait gave up)
+    p.sel[i] = ok ? expert_within((uint32_t)v, a.E) : i % a.K;  // (a selection even where the wait gave up)
     p.w[i] = __uint_as_float((uint32_t)(v >> 32));
   }
   __syncthreads();
@@ -345,8 +347,9 @@ __device__ __forceinline__ void finish_item(int* counter) {
 }
 // Wave 0 waits until the lanes' counters (lane i's where it has one) add up to `want`; then
 // the workgroup goes on.  A call that shares its workspace with another one in flight,
-// which is an error, may have lost counts: the wait is bounded (seconds), and false makes
-// the outputs NaN.  `ok`: no wait before gave up (then this one does not wait either).
+// which is an error, may have lost counts, or take the other's for its own: the wait is bounded
+// (seconds), and false makes what the workgroup writes of O NaN.  `so_far`: no wait before
+// gave up (then this one does not wait either).
 constexpr int kMostPolls = 1 << 22;
 template <class Counter>
 __device__ __forceinline__ bool await(Counter counter, int want, int* sh, bool so_far = true) {
@@ -474,7 +477,7 @@ struct Decode {
     if (UP) i /= a.ks;
     t.gi = i / tiles;
     t.tile = i % tiles;
-    t.e = __builtin_amdgcn_readfirstlane(p.gexp[t.gi]);
+    t.e = expert_within(__builtin_amdgcn_readfirstlane(p.gexp[t.gi]), a.E);  // (of one token: ahead of weigh_token's)
     t.r0 = __builtin_amdgcn_readfirstlane(p.goff[t.gi]);
     t.cnt = __builtin_amdgcn_readfirstlane(p.goff[t.gi + 1]) - t.r0;
     return t;
@@ -576,7 +579,7 @@ struct Decode {
     auto entry = [&](int s) { return t * a.K + min(wave + kDecodeWaves * s, steps - 1) / spe; };
     auto first_k = [&](int s) { return min(wave + kDecodeWaves * s, steps - 1) % spe * Tile::KSTEP + Tile::k0(lane); };
     auto load_w = [&](int buf, int s) {
-      const int e = __builtin_amdgcn_readfirstlane(p.sel[entry(s)]), k = first_k(s);
+      const int e = expert_within(__builtin_amdgcn_readfirstlane(p.sel[entry(s)]), a.E), k = first_k(s);
       const Rsrc w = buffer_of(a.W2 + (size_t)e * n * d, (uint32_t)n * d * 2);
       const uint32_t o = wave + kDecodeWaves * s < steps && k < n ? wcol + (uint32_t)k * d * 2 : kBufferOut;
 #pragma unroll
@@ -908,7 +911,7 @@ struct Decode8 {
       int sv[NB];
       auto at = [&](int s) { return min(wave + kDecodeWaves * s, steps - 1); };
       auto load_w = [&](int q, int s) {
-        const int i = at(s), kb = i % blocks, e = __builtin_amdgcn_readfirstlane(p.sel[t * a.K + i / blocks]);
+        const int i = at(s), kb = i % blocks, e = expert_within(__builtin_amdgcn_readfirstlane(p.sel[t * a.K + i / blocks]), a.E);
         const uint8_t* w = a.W2q + (size_t)e * w2q_bytes(d, n) + 16 * g + kQBlock * kb;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
@@ -1016,11 +1019,11 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
   int item;
   if (selects == 0) {
     select_all(a, p);
-    item = __builtin_amdgcn_readfirstlane(sh[0]);
+    item = next_item(-1, __builtin_amdgcn_readfirstlane(sh[0]));
   } else {
     __syncthreads();
-    for (;;) {
-      item = __builtin_amdgcn_readfirstlane(sh[0]);
+    for (item = -1;;) {
+      item = next_item(item, __builtin_amdgcn_readfirstlane(sh[0]));
       if (item >= selects) break;
       select_some(a, p, item);
       finish_item<0>(select_counter(a));
@@ -1064,7 +1067,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
       D::template run<UP>(a, p, t, stream, part, dyn + picked_bytes(a.T, a.E, a.K), wave, [&]() {
         if (more && threadIdx.x == 0) sh[0] = next;
       });
-      item = more ? __builtin_amdgcn_readfirstlane(sh[0]) - selects : total;
+      item = more ? next_item(item + selects, __builtin_amdgcn_readfirstlane(sh[0])) - selects : total;
       asm volatile("" ::: "memory");
       if (!ok) counter = a.sync + 1;  // (no one's: what gave up is not counted, so that nothing is summed from it)
       if (item >= end) {
@@ -1097,7 +1100,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
     if (!more) break;
     if (threadIdx.x == 0) sh[0] = take_ticket(a);
     __syncthreads();
-    item = __builtin_amdgcn_readfirstlane(sh[0]) - selects;
+    item = next_item(item + selects, __builtin_amdgcn_readfirstlane(sh[0])) - selects;
     __syncthreads();  // (sh and the partial sums are free again)
   }
 }
