@@ -38,39 +38,29 @@ namespace smoe {
 constexpr int kDecodeWaves = 8, kDecodeThreads = 64 * kDecodeWaves;
 
 // ---------------------------------------------------------------- router
-template <int KB, int MB>
+// grid: column tiles, k slices, groups of 16 rows
 __global__ __launch_bounds__(kDecodeThreads, 2) void decode_router_kernel(const DecodeArgs a, int slice, int counters) {
-  using Tile = RowTile<KB>;
+  using Tile = RowTile<1>;
   __shared__ typename Tile::Part part[kDecodeWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
   for (int i = ((blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * kDecodeThreads + threadIdx.x; i < counters;
        i += gridDim.x * gridDim.y * gridDim.z * kDecodeThreads)
     a.sync[i] = 0;
-  const int c0 = Tile::COLS * blockIdx.x, t0 = Tile::RT * MB * blockIdx.z;
+  const int c0 = Tile::COLS * blockIdx.x, t0 = Tile::RT * blockIdx.z;
   const int kbeg = blockIdx.y * slice, kend = min(a.d, kbeg + slice);
   const Rsrc w = buffer_of(a.Wr, (uint32_t)a.d * a.E * 2), x = buffer_of(a.X, (uint32_t)a.T * a.d * 2);
-  const int col = c0 + 8 * Tile::cg(lane);
-  uint32_t xoff[MB];
-#pragma unroll
-  for (int b = 0; b < MB; ++b) {
-    const int t = t0 + Tile::RT * b + Tile::row(lane);
-    xoff[b] = t < a.T ? (uint32_t)t * a.d * 2 : kBufferOut;
-  }
-  f32x4 acc[MB][8];
+  const int col = c0 + 8 * Tile::cg(lane), r = t0 + Tile::row(lane);
+  const uint32_t xoff[1] = {r < a.T ? (uint32_t)r * a.d * 2 : kBufferOut};
+  f32x4 acc[1][8];
   zero_acc(acc);
-  RowStream<KB, 2> stream;
+  RowStream<1, 2> stream;
   stream.prime(w, a.E * 2, col < a.E ? col * 2 : kBufferOut, kbeg, kend, wave, kDecodeWaves, lane);
   stream.template add<false>(acc, x, xoff);
-#pragma unroll
-  for (int b = 0; b < MB; ++b) {
-    if (t0 + Tile::RT * b >= a.T) break;
-    __syncthreads();
-    Tile::put(part[wave], acc[b], lane);
-    __syncthreads();
-    for (int i = threadIdx.x; i < Tile::RT * Tile::COLS / 4; i += kDecodeThreads) {
-      const int row = i / (Tile::COLS / 4), c4 = i % (Tile::COLS / 4), t = t0 + Tile::RT * b + row, c = c0 + 4 * c4;
-      if (t < a.T && c < a.E) *(f32x4*)(a.part + ((size_t)blockIdx.y * a.T + t) * a.E + c) = Tile::template sum<kDecodeWaves>(part, row, c4);
-    }
+  Tile::put(part[wave], acc[0], lane);
+  __syncthreads();
+  for (int i = threadIdx.x; i < Tile::RT * Tile::COLS / 4; i += kDecodeThreads) {
+    const int row = i / (Tile::COLS / 4), c4 = i % (Tile::COLS / 4), t = t0 + row, c = c0 + 4 * c4;
+    if (t < a.T && c < a.E) *(f32x4*)(a.part + ((size_t)blockIdx.y * a.T + t) * a.E + c) = Tile::template sum<kDecodeWaves>(part, row, c4);
   }
 }
 
@@ -1125,12 +1115,11 @@ int decode_ks(int T, int d, int n, int E, int K, bool q8) {
   return std::max(1, std::min({rest / items, q8 ? (d + 1023) / 1024 : d / 256, 8}));
 }
 
-template <int KB, int MB>
 static hipError_t run_router(const DecodeArgs& a, hipStream_t s) {
-  using Tile = RowTile<KB>;
+  using Tile = RowTile<1>;
   const int per = (a.d / 32 + a.slices - 1) / a.slices;
-  const dim3 grid((a.E + Tile::COLS - 1) / Tile::COLS, a.slices, (a.T + Tile::RT * MB - 1) / (Tile::RT * MB));
-  decode_router_kernel<KB, MB><<<grid, kDecodeThreads, 0, s>>>(a, 32 * per, (int)decode_sync_words(a.T, a.d, a.E, a.K));
+  const dim3 grid((a.E + Tile::COLS - 1) / Tile::COLS, a.slices, (a.T + Tile::RT - 1) / Tile::RT);
+  decode_router_kernel<<<grid, kDecodeThreads, 0, s>>>(a, 32 * per, (int)decode_sync_words(a.T, a.d, a.E, a.K));
   return hipGetLastError();
 }
 
@@ -1164,7 +1153,7 @@ hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
   while (2 * a.kw <= kDecodeWaves &&
          (4 * a.kw <= steps || (q8 && 2 * a.kw <= steps && groups * a.d * a.kw < 512 * 64 * kDecodeWaves)))
     a.kw *= 2;
-  const hipError_t e = run_router<1, 1>(a, s);
+  const hipError_t e = run_router(a, s);
   if (e != hipSuccess) return e;
   // one row block where a group seldom has more than its 16 rows
   const bool one = a.T <= 16 || a.T * a.K <= 6 * a.E;

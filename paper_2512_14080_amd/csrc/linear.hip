@@ -413,7 +413,7 @@ template <class Cfg_, bool PART>
 struct OpLinearDW {
   using Cfg = Cfg_;
   static constexpr int M_MODE = KOUTER, N_MODE = KOUTER, EPI_LDS = 0;
-  static constexpr bool LINES = kWholeLines<Cfg> && Cfg::RN % 2 == 0;
+  static_assert(kWholeLines<Cfg> && Cfg::RN % 2 == 0, "stored in whole lines");
   struct Params { LinearArgs a; const uint16_t* dP; int64_t ldp; uint16_t* dW; int N, splits, chunk; };
   static __device__ int count(const Params& p, int*) {
     return p.splits * ((p.a.k + Cfg::BM - 1) / Cfg::BM) * ((p.N + Cfg::BN - 1) / Cfg::BN);
@@ -434,9 +434,9 @@ struct OpLinearDW {
       store_part_f32<Cfg>(p.a.part + (size_t)ti.e * p.a.k * p.N, p.N, ti.m0, ti.n0, mrows, ncols, t);
       return;
     }
-    const int lane = epilogue_lane(), wm0 = Cfg::wave_m(threadIdx.x >> 6) * (Cfg::BM / Cfg::WM);
+    const int wm0 = Cfg::wave_m(threadIdx.x >> 6) * (Cfg::BM / Cfg::WM);
     const int c0 = ti.n0 + t.wave_n() * (Cfg::BN / Cfg::WN);
-    char* st = LINES ? epi - Cfg::STAGE_BYTES + (threadIdx.x >> 6) * 4096 : nullptr;
+    char* st = epi - Cfg::STAGE_BYTES + (threadIdx.x >> 6) * 4096;
 #pragma unroll
     for (int i = 0; i < Cfg::RM; ++i) {
       const int m0 = wm0 + 32 * i;
@@ -451,20 +451,11 @@ struct OpLinearDW {
         const int col = c0 + 32 * j;
         if (col >= p.N) continue;
         u32x2 v[4];
-        if constexpr (LINES) {
-          pack(j, v);
-          stage_block32(st, 0, v);
-          pack(j + 1, v);
-          stage_block32(st, 1, v);
-          store_staged_cols(st, p.dW + (size_t)(ti.m0 + m0) * p.N, p.N, mrows - m0, col, p.N);
-        } else {
-          uint16_t* row = p.dW + (size_t)(ti.m0 + m0 + (lane & 31)) * p.N;
-          const bool live = m0 + (lane & 31) < mrows;
-          pack(j, v);
-          if (live) store_cols(row, col, p.N, v);
-          pack(j + 1, v);
-          if (live) store_cols(row, col + 32, p.N, v);
-        }
+        pack(j, v);
+        stage_block32(st, 0, v);
+        pack(j + 1, v);
+        stage_block32(st, 1, v);
+        store_staged_cols(st, p.dW + (size_t)(ti.m0 + m0) * p.N, p.N, mrows - m0, col, p.N);
       }
     }
   }

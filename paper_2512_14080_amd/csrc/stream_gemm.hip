@@ -25,18 +25,9 @@
 
 #include "launch.h"
 #include "stream8_tile.h"
+#include "stream_tile.h"
 
 namespace smoe {
-
-// 8 rows (k) x 8 columns of bf16, one row per register quad -> per column the
-// 8 k values (an MFMA operand)
-__device__ __forceinline__ bf16x8 column_of(const u32x4 (&w)[8], int j) {
-  const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
-  u32x4 f;
-#pragma unroll
-  for (int p = 0; p < 4; ++p) f[p] = __builtin_amdgcn_perm(w[2 * p + 1][j >> 1], w[2 * p][j >> 1], sel);
-  return __builtin_bit_cast(bf16x8, f);
-}
 
 constexpr int kStreamCols = 128;  // columns of a workgroup
 typedef f32x4 StreamPart[16][2][16];  // one wave's 16 x 128 partial: [row][half of 8 columns][lane column]
@@ -159,7 +150,7 @@ __global__ __launch_bounds__(64 * KW, OCC) void stream_gemm_kernel(const typenam
       for (int q = 0; q < NBUF; ++q) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bf16x8 wf = column_of(wv[q], j);
+          const bf16x8 wf = column_of8(wv[q], j);
 #pragma unroll
           for (int b = 0; b < MB; ++b)
             acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv[q][b], wf, acc[b][j], 0, 0, 0);
