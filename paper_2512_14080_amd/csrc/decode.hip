@@ -22,8 +22,8 @@
 // to 8 tokens every workgroup forms it for itself from T x E logits in L2, which is cheaper
 // than another dependent step, and all get the same from the same sums.
 //
-// Measured, as the whole call: one token of d 1536, n 256, E 128, K 8 19.8 us; 7 tokens of
-// d 1024, n 256, E 64, K 8 28 us; 64 of d 4096, n 512, E 128, K 8 (1.6 GB of weights) 291 us,
+// Measured, as the whole call: one token of d 1536, n 256, E 128, K 8 19 us; 7 tokens of
+// d 1024, n 256, E 64, K 8 27.5 us; 64 of d 4096, n 512, E 128, K 8 (1.6 GB of weights) 291 us,
 // 5.4 TB/s.
 #include <algorithm>
 
@@ -533,7 +533,9 @@ struct Decode {
               float sg;
               v[q] = silu_sig(hg[q], &sg) * hu[q];
             }
-            // (A to bf16, the type of the product that follows, as in the layer's forward)
+            // (A to bf16, the type of the product that follows, as in the layer's forward: its
+            // instruction takes no fp32, and A in two bf16 parts would double the products.  O is
+            // then 2.3e-3 off, 1.7e-3 without: 16 tokens of d 4096, n 14336, E 8, K 2)
             store8_shared(buffer_of(a.A, (uint32_t)P * n * 2), (uint32_t)(p.rows[t.r0 + RT * b + row] * n + col) * 2,
                           pack_bf16x4(v[0], v[1], v[2], v[3]));
           }
@@ -600,6 +602,7 @@ struct Decode {
     }
     wait();
     if (a.ks > 1) {
+      // (A to bf16, as in run)
       token_rows(a, p, t, [&](int i, const float(&v)[4]) { *(u32x2*)(rows + i) = pack_bf16x4(v[0], v[1], v[2], v[3]); });
       __syncthreads();
     }
@@ -658,8 +661,10 @@ struct Decode {
 // in bf16 (exact products), with fp32 sums: the 8-bit instruction's are 1.3e-5 of the result
 // off, which moves A's codes, and now and then a whole block's scale, to the other side of a
 // step (6 tokens of d 1536, n 256, E 128, K 8: one token's O 7e-3 off, so 1.7e-3).  It costs
-// 1%, since the weights bound it (32 tokens of a 30B-shaped layer: 150 us, 152 so).  MB = 2 is
-// for groups of more than 16 rows.
+// 2%, since the weights bound it (32 tokens of a 30B-shaped layer: 148 us, 151 so).  The
+// down-projection's sums are the 8-bit instruction's, as moe_fwd_quant's: no code follows
+// that they could move, and 1.3e-5 is far below O's own rounding.  MB = 2 is for groups of
+// more than 16 rows.
 template <int MB, int NJ>
 struct Decode8 {
   static constexpr int NBUF = 1, UP_COLS = 8 * NJ, DOWN_COLS = 16 * NJ, MAX_ROWS = 16 * MB;
@@ -673,7 +678,7 @@ struct Decode8 {
     // This wave's first block, the end, from a block to the next, and its steps, which begin
     // at step `rot`: where rows are 4 KB apart, one block of them all lies in few memory channels,
     // and items that all began there would ask the same ones (32 tokens of a 30B-shaped layer:
-    // 161 us, 148 so; 64 184 and 167)
+    // 162 us, 151 so; 64 184 and 170)
     int kb, end, step, ns, rot;
     __device__ __forceinline__ void turn(int by) {
       ns = max((end - kb + step - 1) / step, 1);
@@ -821,7 +826,8 @@ struct Decode8 {
     } else if (a.kw == kDecodeWaves) {
       add<true, false>(s, acc, nullptr, lane, row);
     } else {
-      // (a wave for each block; 64 tokens of d 1536, n 256, E 128, K 8: 59.1 us without, 57.4 so)
+      // (a wave for each block; 64 tokens of d 4096, n 1792, E 16, K 2 114 us without, 105 so; of
+      // n 512, E 128, K 8 172.6 and 170.1)
       for (int kb = wave; kb < q_blocks(n); kb += kDecodeWaves)
 #pragma unroll
         for (int b = 0; b < MB; ++b) {
@@ -1001,7 +1007,7 @@ __global__ __launch_bounds__(kDecodeThreads, 2) void decode_kernel(const DecodeA
   Picked p = picked_at(dyn, a.T, a.E, a.K);
   if (a.T == 1) one_token(a, p);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (threadIdx.x == kDecodeThreads - 1) sh[0] = take_ticket(a);  // (not by a wave that selects)
+  if (threadIdx.x == kDecodeThreads - 1) sh[0] = take_ticket(a);  // (asked for ahead of the selection)
   // Up to 8 tokens every workgroup selects for itself.  More are the queue's first items, of 8
   // tokens each (a wave takes 3.8 us for one, and 64 would take 30).
   bool ok = true;  // (the waits so far)
@@ -1106,7 +1112,7 @@ int decode_slices(int T, int d, int E) {
 size_t decode_sync_words(int T, int d, int E, int K) { return (size_t)kLine * (10 + std::min(T * K, E) + d / 32); }
 // whether the down-projection goes by token: where few entries repeat experts, whose weights are
 // then read again, and the items leave CUs for the up-projection's (two tokens of d 1536, n 256,
-// E 128, K 8 25.2 us, by group 27.0; four 35.8, 34.0).  decode_ks: the slices of k
+// E 128, K 8 25.4 us, by group 27.1; four 35.4, 33.0).  decode_ks: the slices of k
 static bool decode_by_token(int T, int d, int E, int K) { return T == 1 || (2 * T * K <= E && T * (d / 32) <= 160); }
 int decode_ks(int T, int d, int n, int E, int K, bool q8) {
   if (!decode_by_token(T, d, E, K) || K * n > 8192) return 1;
@@ -1148,7 +1154,7 @@ hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
   const int steps = q8 ? q_blocks(a.n) : a.n / 32;
   a.kw = 1;
   // (8-bit: one step each, while the items are fewer than two to a CU: 9 tokens of d 1536, n 256,
-  // E 128, K 8 46.1 us, 38.5 so; in 16 bits 46.9 and 47.5, and 7 tokens of the 1B layer 27.2 and 29.2)
+  // E 128, K 8 46.3 us, 38.8 so; in 16 bits 46.9 and 47.5, and 7 tokens of the 1B layer 27.2 and 29.2)
   const int64_t groups = std::min(a.T * a.K, a.E);
   while (2 * a.kw <= kDecodeWaves &&
          (4 * a.kw <= steps || (q8 && 2 * a.kw <= steps && groups * a.d * a.kw < 512 * 64 * kDecodeWaves)))
@@ -1162,8 +1168,8 @@ hipError_t launch_decode(DecodeArgs a, hipStream_t s) {
   using BT = Decode<4, 1>;
   if (q8) {
     if (by_token) return run_decode<Q1, Q1::Token, true>(a, s);
-    // smaller tiles for few items (8 tokens of d 1024, n 256, E 64, K 8 26.1 us, 26.8 in the
-    // larger; 16 of d 1536, n 256, E 128, K 8 47.1 and 43.3)
+    // smaller tiles for few items (8 tokens of d 1024, n 256, E 64, K 8 27.2 us, 27.7 in the
+    // larger; 16 of d 1536, n 256, E 128, K 8 45.5 and 42.5)
     if (a.T * a.K <= 64) return run_decode<Q1, Q1::Token, false>(a, s);
     return one ? run_decode<Decode8<1, 8>, Q1::Token, false>(a, s) : run_decode<Decode8<2, 4>, Q1::Token, false>(a, s);
   }

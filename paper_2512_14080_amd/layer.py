@@ -181,7 +181,9 @@ class DeviceLayer:
     def decode(self, R=None, stream=None, topk_idx=None, topk_w=None):
         """The forward of a few tokens (T <= MOE_DECODE_MAX_T) in one call, routing included: O = R + the layer's output.
         R is bf16 [T,d]; topk_idx (int32) and topk_w (fp32), [T,K], take the selection.
-        Token choice only, on the 8-bit weights with held8="quant" (quantise them first: quantize_experts)."""
+        Token choice only, on the 8-bit weights with held8="quant" (quantise them first: quantize_experts), where route
+        and forward on weights that are quantised already are mostly as fast or faster from two tokens on (moe_decode_quant
+        in the header)."""
         if self.round_mode:
             raise ValueError("decode routes by token choice: round_mode must be None")
         if self.route_flags & B.MOE_ROUTE_SCORES_IN:
