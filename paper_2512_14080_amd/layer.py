@@ -41,18 +41,22 @@ def _whole(t, rows, cols):
 
 
 def _check_tensor(name, t, dtype, rows, cols, device):
+    if t is None or (t.shape == (rows, cols) and t.is_contiguous() and t.dtype == dtype and t.device == device):
+        return
     if t.dtype != dtype or t.device != device or not _whole(t, rows, cols):
         raise ValueError(f"{name} must be contiguous {dtype} [{rows}, {cols}] on {device} (got {t.dtype} {list(t.shape)}, "
                          f"strides {t.stride()}, on {t.device})")
 
 
-def _row_stride(name, t, rows, cols, device):
-    """The elements from a row to the next of t, bf16 [rows, cols] on the device with whole rows that do not overlap, as the
-    dense products take them (0: one after the other)."""
-    import torch
+def _row_stride(name, t, rows, cols, like):
+    """The elements from a row to the next of t, [rows, cols] of like's type and device with whole rows that do not overlap,
+    as the dense products take them (0: one after the other)."""
+    if t.shape == (rows, cols) and t.is_contiguous() and t.dtype == like.dtype and t.device == like.device:
+        return 0
     whole = _whole(t, rows, cols)
-    if t.dtype != torch.bfloat16 or t.device != device or not (whole or tuple(t.shape) == (rows, cols)):
-        raise ValueError(f"{name} must be bfloat16 [{rows}, {cols}] on {device} (got {t.dtype} {list(t.shape)} on {t.device})")
+    if t.dtype != like.dtype or t.device != like.device or not (whole or t.shape == (rows, cols)):
+        raise ValueError(f"{name} must be {like.dtype} [{rows}, {cols}] on {like.device} (got {t.dtype} {list(t.shape)} on "
+                         f"{t.device})")
     if whole or (rows == 1 and t.stride(1) == 1):
         return 0
     if t.stride(1) != 1 or not cols <= t.stride(0) < 1 << 30:
@@ -61,12 +65,12 @@ def _row_stride(name, t, rows, cols, device):
 
 
 def _check_device(device, stream):
-    import torch
     if device.type != "cuda":
         raise ValueError(f"the tensors must be on a GPU (they are on {device})")
-    for at in [torch.device("cuda", torch.cuda.current_device())] + ([] if stream is None else [stream.device]):
-        if at != device:
-            raise ValueError(f"the tensors are on {device}, the current device or the stream is {at}")
+    import torch
+    at = torch.cuda.current_device()
+    if at != device.index or (stream is not None and getattr(stream, "device", device) != device):
+        raise ValueError(f"the tensors are on {device}, the current device is {at}, the stream {stream}")
 
 
 class DeviceLayer:
@@ -189,11 +193,11 @@ class DeviceLayer:
         if self.route_flags & B.MOE_ROUTE_SCORES_IN:
             raise ValueError("decode routes by softmax(X Wr + bias): scores_in must be None")
         import torch
-        for name, t, dtype, cols in (("R", R, torch.bfloat16, self.d), ("topk_idx", topk_idx, torch.int32, self.K),
-                                     ("topk_w", topk_w, torch.float32, self.K)):
-            if t is not None:
-                _check_tensor(name, t, dtype, self.T, cols, self.X.device)
-        _check_device(self.X.device, stream)
+        device = self.X.device
+        _check_tensor("R", R, torch.bfloat16, self.T, self.d, device)
+        _check_tensor("topk_idx", topk_idx, torch.int32, self.T, self.K, device)
+        _check_tensor("topk_w", topk_w, torch.float32, self.T, self.K, device)
+        _check_device(device, stream)
         if self.ws_d is None:
             which = B.MOE_WS_DECODE_QUANT if self.qw is not None else B.MOE_WS_DECODE
             nbytes = B.moe_workspace_bytes(self.D, self.T * self.K, which)
@@ -229,9 +233,8 @@ class SharedExpert:
         if Wu.dtype != torch.bfloat16 or Wd.dtype != torch.bfloat16 or Wd.device != Wu.device:
             raise ValueError(f"Wu and Wd must be bfloat16 on one device (got {Wu.dtype} on {Wu.device}, {Wd.dtype} on {Wd.device})")
         for name, b, size in (("bu", bu, 2 * m), ("bd", bd, d)):
-            if b is not None:
-                _check_tensor(name, b, torch.float32, 1, size, Wu.device)
-        self.T, self.d, self.m = T, d, m
+            _check_tensor(name, b, torch.float32, 1, size, Wu.device)
+        self.T, self.d, self.m, self._sizes = T, d, m, {}
         self.Wu, self.Wd, self.bu, self.bd = Wu, Wd, bu, bd
         dev, bf16, f32 = Wu.device, torch.bfloat16, torch.float32
 
@@ -251,14 +254,21 @@ class SharedExpert:
             self.dA, self.ws_b = torch.empty_like(self.A), workspace(B.MOE_WS_LINEAR_BWD)
             self.dWu, self.dWd, self.dbu, self.dbd = like(Wu), like(Wd), like(bu), like(bd)
 
+    # (the sizes of the two products for given strides, formed once)
     def _up(self, ldx):
-        return B.linear_dims(self.T, self.d, self.m, "swiglu", ldx=ldx)
+        L = self._sizes.get(ldx)
+        if L is None:
+            L = self._sizes[ldx] = B.linear_dims(self.T, self.d, self.m, "swiglu", ldx=ldx)
+        return L
 
     def _down(self, ldr, ldy):
-        return B.linear_dims(self.T, self.m, self.d, ldr=ldr, ldy=ldy)
+        L = self._sizes.get((ldr, ldy))
+        if L is None:
+            L = self._sizes[ldr, ldy] = B.linear_dims(self.T, self.m, self.d, ldr=ldr, ldy=ldy)
+        return L
 
     def _stride(self, name, t):
-        return 0 if t is None else _row_stride(name, t, self.T, self.d, self.Wu.device)
+        return 0 if t is None else _row_stride(name, t, self.T, self.d, self.Wu)
 
     def forward(self, X, Y, R=None, stream=None):
         up, down = self._up(self._stride("X", X)), self._down(self._stride("R", R), self._stride("Y", Y))
