@@ -141,7 +141,11 @@ class DeviceLayer:
         self.db1 = torch.empty((E, 2 * n), dtype=f32, device=device) if b1 is not None else None
         self.db2 = torch.empty((E, d), dtype=f32, device=device) if b2 is not None else None
         self.eb = B.expert_bias(self.b1, self.b2, self.db1, self.db2)
-        self.ws_d = None  # of decode, at its first call
+        # of decode (made here: memory taken in a call belongs to the current stream, not to the call's)
+        self.ws_d = None
+        if not self.round_mode and scores_in is None:
+            which = B.MOE_WS_DECODE if self.qw is None else B.MOE_WS_DECODE_QUANT
+            self.ws_d = _aligned_empty(B.moe_workspace_bytes(self.D, T * K, which), device)
 
     @property
     def routing(self):
@@ -187,7 +191,7 @@ class DeviceLayer:
         R is bf16 [T,d]; topk_idx (int32) and topk_w (fp32), [T,K], take the selection.
         Token choice only, on the 8-bit weights with held8="quant" (quantise them first: quantize_experts), where route
         and forward on weights that are quantised already are mostly as fast or faster from two tokens on (moe_decode_quant
-        in the header)."""
+        in the header).  Calls share the layer's buffers and must be ordered."""
         if self.round_mode:
             raise ValueError("decode routes by token choice: round_mode must be None")
         if self.route_flags & B.MOE_ROUTE_SCORES_IN:
@@ -198,10 +202,6 @@ class DeviceLayer:
         _check_tensor("topk_idx", topk_idx, torch.int32, self.T, self.K, device)
         _check_tensor("topk_w", topk_w, torch.float32, self.T, self.K, device)
         _check_device(device, stream)
-        if self.ws_d is None:
-            which = B.MOE_WS_DECODE_QUANT if self.qw is not None else B.MOE_WS_DECODE
-            nbytes = B.moe_workspace_bytes(self.D, self.T * self.K, which)
-            self.ws_d = _aligned_empty(nbytes, self.X.device)
         if self.qw is not None:
             B.moe_decode_quant(self.D, self.X, self.Wr, self.bias, self.qw, R, self.O, self.ws_d, topk_idx, topk_w,
                                stream, eb=self.eb)
@@ -221,7 +221,8 @@ class SharedExpert:
     biases [2m] and [d].  ``train`` keeps what the backward reads.
 
     X, Y, R and the gradients are bf16 [T,d] of exactly T rows (contiguous ones under any leading shape); rows may be further apart than they are long (by a
-    multiple of 8 elements), and what lies between them is neither read nor written."""
+    multiple of 8 elements), and what lies between them is neither read nor written.  Calls share the object's buffers and
+    must be ordered; backward is that of the forward before it."""
 
     def __init__(self, T, Wu, Wd, bu=None, bd=None, train=False):
         import torch

@@ -60,3 +60,18 @@ def test_rows_apart(T, d, m):
     s.backward(dy, x, gg, gg)
     torch.cuda.synchronize()
     assert torch.equal(r, Y) and torch.equal(gg, dX)
+
+
+def test_decode_of_a_layer_too_long():
+    """More tokens than the call takes: the library's error, with nothing launched."""
+    torch = _t()
+    from paper_2512_14080_amd import binding as B
+    from paper_2512_14080_amd import workloads as W
+    from paper_2512_14080_amd.layer import DeviceLayer
+    cfg = W.MoEConfig("decode", T=65, d=128, n=64, E=8, K=2, m_tile=64)
+    layer = DeviceLayer(W.make_inputs(cfg, 3))
+    layer.O.fill_(7.0)
+    with pytest.raises(B.MoEError, match="at most 64"):
+        layer.decode()
+    torch.cuda.synchronize()
+    assert bool((layer.O == 7.0).all())

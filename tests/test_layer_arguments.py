@@ -138,3 +138,14 @@ def test_decode_refuses_given_scores():
     scores = np.random.default_rng(0).random((5, 8), np.float32)
     with pytest.raises(ValueError, match="scores_in"):
         _layer(scores_in=scores).decode()
+
+
+def test_decode_takes_no_memory_in_a_call():
+    """A workspace made in a call on another stream than the current one would be memory that the current one may still be
+    writing for someone else."""
+    D = B.dims(5, 128, 64, 8, 2)
+    assert _layer().ws_d.numel() == B.moe_workspace_bytes(D, 10, B.MOE_WS_DECODE)
+    assert _layer(held8="quant").ws_d.numel() == B.moe_workspace_bytes(D, 10, B.MOE_WS_DECODE_QUANT)
+    assert _layer(round_mode="nearest").ws_d is None
+    long = W.MoEConfig("decode", T=65, d=128, n=64, E=8, K=2, m_tile=64)
+    assert DeviceLayer(W.make_inputs(long, 3), device="cpu").ws_d.numel() == 0  # (the call refuses T)
