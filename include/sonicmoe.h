@@ -478,8 +478,8 @@ int moe_bwd_ckpt(moe_dims dims, const moe_bf16 *dO, const moe_bf16 *X, const moe
  *         undefined (NaN where a wait for counts that the other took gave up), and either
  *         may take seconds; both end, and touch nothing but their operands.
  * moe_route and moe_fwd compute the same but for R.  Measured beside them, moe_decode takes up
- * to a quarter less time at n <= 3584 (a few sizes of 2 to 8 tokens: up to 8% more); at
- * n = 14336 one token, or 32 and more, take 8% more.
+ * to a quarter less time at n <= 3584 (at some sizes, mostly of 2 to 4 tokens, up to 8% more);
+ * at n = 14336 one token, or 32 and more, take 9% more.
  */
 enum { MOE_DECODE_MAX_T = 64 };
 int moe_decode(moe_dims dims, const moe_bf16 *X, const moe_bf16 *Wr, const float *bias, const moe_bf16 *W1,
